@@ -1,0 +1,485 @@
+"""Performance cases of the operators around a model's DQT linears: attention
+over packed sequences, the SwiGLU product fused with the 8-bit quantisation of
+its output, and the log probabilities of a step's targets.
+
+Operators, each in its forms (kind):
+  attn     softmax attention, causal, grouped heads, packed sequences of
+           different lengths (dqt_attn_fwd, dqt_attn_bwd).  "fwd": a prompt, or
+           one new token per sequence over its earlier keys; "train": forward
+           and backward.
+  swiglu   silu(gate) * up quantised per token for the down projection
+           (dqt_swiglu_act_quant).  "fwd": alone; "train": gate and up also
+           kept as 8-bit checkpoints, and the backward from those
+           (dqt_swiglu_backward).
+  logprob  log probability of each row's given token, entropy, and the most
+           probable alternatives (dqt_logprob_fwd).  "score": without a
+           gradient; "train": forward and the logits' gradient
+           (dqt_logprob_bwd).
+
+With own = False, run() computes the same from elementary torch operations in
+fp32, rounding once at the end.
+
+Values: activations N(0, 1) and upstream gradients N(0, 0.01) as in
+paper_2412_04787_amd/workloads.py; logits N(0, 2) with some columns masked to
+-inf as a tokenizer's unused ids are.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+GROUP = 128            # consecutive elements of a checkpoint that share a scale
+
+
+def listed():
+    return [
+        # attention: the smallest call, one short prompt through the small test model's heads
+        dict(name="attn_fwd_37_d64", op="attn", kind="fwd", heads=4, kv_heads=4, d=64, n_seq=1, q_lo=37, q_hi=37,
+             ctx_lo=0, ctx_hi=0),
+        # serving at hidden 4096: one new token for each of 32 sequences, 1 to 8192 earlier keys
+        dict(name="attn_fwd_decode_h4096", op="attn", kind="fwd", heads=32, kv_heads=8, d=128, n_seq=32, q_lo=1, q_hi=1,
+             ctx_lo=0, ctx_hi=8191),
+        # prompts of odd lengths packed together, hidden 4096 with grouped heads
+        dict(name="attn_fwd_packed_h4096", op="attn", kind="fwd", heads=32, kv_heads=8, d=128, n_seq=5, q_lo=301,
+             q_hi=3001, ctx_lo=0, ctx_hi=0),
+        # a training batch of the smallest LLaMA block: documents of different lengths, 12 heads of 64
+        dict(name="attn_train_packed_h768", op="attn", kind="train", heads=12, kv_heads=12, d=64, n_seq=13, q_lo=1,
+             q_hi=1300, ctx_lo=0, ctx_hi=0),
+        # the 24-layer model's training batch, 8 x 2048 tokens, 16 heads of 128: the largest
+        dict(name="attn_train_h2048", op="attn", kind="train", heads=16, kv_heads=16, d=128, n_seq=8, q_lo=2048,
+             q_hi=2048, ctx_lo=0, ctx_hi=0),
+        # decoding 8 sequences through the hidden-4096 block's feed-forward
+        dict(name="swiglu_fwd_h4096_m8", op="swiglu", kind="fwd", m=8, k=11008, dt="bf16", act="e4m3"),
+        # a ragged batch of the fp32 environment
+        dict(name="swiglu_fwd_h768_m333_f32", op="swiglu", kind="fwd", m=333, k=2048, dt="f32", act="int8"),
+        # the 24-layer model's feed-forward in training, int8 activations
+        dict(name="swiglu_train_h2048", op="swiglu", kind="train", m=16384, k=5632, dt="bf16", act="int8"),
+        # the hidden-4096 block's feed-forward in training, e4m3 activations
+        dict(name="swiglu_train_h4096", op="swiglu", kind="train", m=8192, k=11008, dt="bf16", act="e4m3"),
+        # decoding 8 sequences: the sampled tokens' log probabilities and 20 alternatives, a large vocabulary
+        dict(name="logprob_score_m8_v128000", op="logprob", kind="score", m=8, v=128000, dt="f32", top=20, ent=True),
+        # scoring a ragged batch of continuations: 5 alternatives each, odd vocabulary
+        dict(name="logprob_score_m777_v50001", op="logprob", kind="score", m=777, v=50001, dt="bf16", top=5, ent=True),
+        # the loss of the 24-layer model's training batch
+        dict(name="logprob_train_m16384_v32000", op="logprob", kind="train", m=16384, v=32000, dt="bf16", top=0,
+             ent=False),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    op = rng.choice(("attn", "attn", "swiglu", "logprob"))
+    if op == "attn":
+        d = rng.choice((64, 128))
+        kv = rng.choice((1, 2, 3, 4, 8, 12, 16))
+        g = rng.choice([x for x in (1, 2, 3, 4, 8) if kv * x <= 32])
+        form = rng.choice(("decode", "prompt", "chunk", "train", "train"))
+        if form == "decode":
+            n, q, c = _log_int(rng, 1, 32), 1, _log_int(rng, 1, 8191)
+            lim = dict(q_lo=1, q_hi=1, ctx_lo=rng.randint(0, c), ctx_hi=c)
+        elif form == "chunk":
+            n, q, c = _log_int(rng, 1, 8), _log_int(rng, 2, 512), _log_int(rng, 1, 2048)
+            lim = dict(q_lo=rng.randint(1, q), q_hi=q, ctx_lo=rng.randint(0, c), ctx_hi=c)
+        else:
+            n, q, c = _log_int(rng, 1, 16), _log_int(rng, 1, 2600), 0
+            lim = dict(q_lo=rng.randint(1, q), q_hi=q, ctx_lo=0, ctx_hi=0)
+        # no more score entries than the largest listed case
+        while n > 1 and n * kv * g * lim["q_hi"] * (lim["q_hi"] + lim["ctx_hi"]) > 8 * 16 * 2048 * 2048:
+            n -= 1
+        return dict(op=op, kind="train" if form == "train" else "fwd", heads=kv * g, kv_heads=kv, d=d, n_seq=n, **lim)
+    if op == "swiglu":
+        k = _log_int(rng, 16, 11008) // 16 * 16
+        return dict(op=op, kind=rng.choice(("fwd", "train")), m=_log_int(rng, 1, 8192), k=k,
+                    dt=rng.choice(("bf16", "f32")), act=rng.choice(("int8", "e4m3")))
+    kind = rng.choice(("score", "train"))
+    m = _log_int(rng, 1, 4096)
+    v = _log_int(rng, 100, min(128000, 16384 * 32000 // m))
+    top = rng.choice((0, 1, 5, 20)) if kind == "score" else 0
+    while top and m * v > 2 ** 27:       # (the plain form sorts whole rows)
+        m = m // 2
+    return dict(op=op, kind=kind, m=m, v=v, dt=rng.choice(("bf16", "f32")), top=top, ent=rng.choice((True, False)))
+
+
+# ------------------------------------------------------------------ inputs
+
+def _lengths(case):
+    """Query and key lengths of each sequence: spread over the case's ranges,
+    the largest first, so that they follow from the case alone."""
+    n = case["n_seq"]
+    f = [1.0 if n == 1 else 1.0 - i / (n - 1) for i in range(n)]
+    lq = [case["q_lo"] + round((case["q_hi"] - case["q_lo"]) * x) for x in f]
+    # (contexts in another order than the query lengths)
+    lc = [case["ctx_lo"] + round((case["ctx_hi"] - case["ctx_lo"]) * f[(i * 5 + 2) % n]) for i in range(n)]
+    return lq, [a + b for a, b in zip(lq, lc)]
+
+
+def _dtype(case):
+    return torch.bfloat16 if case.get("dt", "bf16") == "bf16" else torch.float32
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(int(seed))
+
+    def normal(shape, std, dtype):
+        return (torch.randn(shape, generator=g, device=DEV, dtype=torch.float32) * std).to(dtype)
+
+    s = dict(case=dict(case))
+    if case["op"] == "attn":
+        lq, lk = _lengths(case)
+        s["lq"], s["lk"] = max(lq), max(lk)
+        starts = torch.zeros((2, len(lq) + 1), dtype=torch.int64)
+        starts[0, 1:] = torch.tensor(lq).cumsum(0)
+        starts[1, 1:] = torch.tensor(lk).cumsum(0)
+        s["tq"], s["tk"] = int(starts[0, -1]), int(starts[1, -1])
+        starts = starts.to(device=DEV, dtype=torch.int32)
+        s["q_start"], s["k_start"] = starts[0].clone(), starts[1].clone()
+        h, kv, d = case["heads"], case["kv_heads"], case["d"]
+        s["Q"] = normal((s["tq"], h, d), 1.0, torch.bfloat16)
+        s["K"] = normal((s["tk"], kv, d), 1.0, torch.bfloat16)
+        s["V"] = normal((s["tk"], kv, d), 1.0, torch.bfloat16)
+        if case["kind"] == "train":
+            s["dO"] = normal((s["tq"], h, d), 1e-2, torch.bfloat16)
+    elif case["op"] == "swiglu":
+        shape = (case["m"], case["k"])
+        s["G"] = normal(shape, 1.0, _dtype(case))
+        s["U"] = normal(shape, 1.0, _dtype(case))
+        if case["kind"] == "train":
+            s["dH"] = normal(shape, 1e-2, _dtype(case))
+    else:
+        m, v = case["m"], case["v"]
+        x = normal((m, v), 2.0, _dtype(case))
+        x[:, v - v // 64:] = -math.inf           # unused ids at the vocabulary's end
+        s["logits"] = x
+        s["targets"] = torch.randint(0, v - v // 64, (m,), generator=g, device=DEV)
+        if m > 3:
+            s["targets"][m // 2] = -1            # a row without a target (padding)
+        if case["kind"] == "train":
+            s["dlogp"] = torch.full((m,), -1.0 / m, dtype=torch.float32, device=DEV)
+            s["dent"] = torch.full((m,), 1e-3 / m, dtype=torch.float32, device=DEV) if case["ent"] else None
+    return s
+
+
+# ------------------------------------------------------------------ plain form
+
+def _plain_attn(s):
+    c = s["case"]
+    h, kv, d = c["heads"], c["kv_heads"], c["d"]
+    grp, n, Lq, Lk = h // kv, c["n_seq"], s["lq"], s["lk"]
+    qs, ks = s["q_start"].long(), s["k_start"].long()
+    lq, lk = qs[1:] - qs[:-1], ks[1:] - ks[:-1]
+    iq, ik = torch.arange(Lq, device=DEV), torch.arange(Lk, device=DEV)
+    at_q = (qs[:-1, None] + iq).clamp(max=s["tq"] - 1)
+    at_k = (ks[:-1, None] + ik).clamp(max=s["tk"] - 1)
+    # query i of a sequence sees its keys up to i + lk - lq
+    see = (ik < lk[:, None])[:, None, :] & (iq < lq[:, None])[:, :, None]
+    see = (see & (ik <= iq[:, None] + (lk - lq)[:, None, None]))[:, None, None]     # [n, 1, 1, Lq, Lk]
+
+    def rows_q(x):       # [tokens, heads, d] -> [n, kv, group, Lq, d]
+        return x.float()[at_q].view(n, Lq, kv, grp, d).permute(0, 2, 3, 1, 4)
+
+    def rows_k(x):       # -> [n, kv, 1, Lk, d]
+        return x.float()[at_k].permute(0, 2, 1, 3).unsqueeze(2)
+
+    tok = torch.arange(s["tq"], device=DEV)
+    sq = torch.searchsorted(qs[1:], tok, right=True)
+    pq = tok - qs[sq]
+    tok = torch.arange(s["tk"], device=DEV)
+    sk = torch.searchsorted(ks[1:], tok, right=True)
+    pk = tok - ks[sk]
+
+    def back_q(x):       # [n, kv, group, Lq, d] -> [tokens, heads, d]
+        return x.permute(0, 3, 1, 2, 4)[sq, pq].reshape(s["tq"], h, -1)
+
+    def back_k(x):       # [n, kv, Lk, d] -> [tokens, kv, d]
+        return x.permute(0, 2, 1, 3)[sk, pk]
+
+    scale = 1.0 / math.sqrt(d)
+    q, k, v = rows_q(s["Q"]), rows_k(s["K"]), rows_k(s["V"])
+    z = (q @ k.transpose(-1, -2)) * scale
+    z = z.masked_fill(~see, -math.inf)
+    top = z.amax(-1, keepdim=True)
+    top = torch.where(top == -math.inf, torch.zeros_like(top), top)
+    p = torch.exp(z - top)
+    tot = p.sum(-1, keepdim=True)
+    p = torch.where(tot > 0, p / tot, torch.zeros_like(p))
+    o = p @ v
+    out = dict(O=back_q(o).to(torch.bfloat16), lse=back_q(top + torch.log(tot)).squeeze(-1).t().contiguous())
+    if c["kind"] == "train":
+        do = rows_q(s["dO"])
+        dz = p * (do @ v.transpose(-1, -2) - (do * o).sum(-1, keepdim=True)) * scale
+        out["dQ"] = back_q(dz @ k).to(torch.bfloat16)
+        out["dK"] = back_k((dz.transpose(-1, -2) @ q).sum(2)).to(torch.bfloat16)
+        # (rows behind a sequence's end hold another one's dO; p is zero there)
+        out["dV"] = back_k((p.transpose(-1, -2) @ do).sum(2)).to(torch.bfloat16)
+    return out
+
+
+def _plain_codes(x, act):
+    """Per-token 8-bit codes and scales of fp32 rows."""
+    top = 127.0 if act == "int8" else 448.0
+    mx = x.abs().amax(-1, keepdim=True).clamp(min=1e-5)
+    y = x * (torch.full_like(mx, top) / mx)
+    if act == "int8":
+        y = torch.round(y).clamp(-128, 127).to(torch.int8)
+    else:
+        y = y.clamp(-448, 448).to(torch.float8_e4m3fn)
+    return y, (mx / torch.full_like(mx, top)).squeeze(-1)
+
+
+def _plain_checkpoint(x):
+    """x through its 8-bit checkpoint: int8 codes, one scale for GROUP elements."""
+    m, k = x.shape
+    pad = -k % GROUP
+    y = torch.nn.functional.pad(x, (0, pad)).view(m, -1, GROUP)
+    mx = y.abs().amax(-1, keepdim=True).clamp(min=1e-5)
+    q = torch.round(y * (torch.full_like(mx, 127.0) / mx)).clamp(-128, 127)
+    return (q * (mx / torch.full_like(mx, 127.0))).view(m, -1)[:, :k]
+
+
+def _plain_swiglu(s):
+    c = s["case"]
+    g, u = s["G"].float(), s["U"].float()
+    h = g / (1 + torch.exp(-g)) * u
+    codes, scale = _plain_codes(h, c["act"])
+    out = dict(Xq=codes, xdq=scale)
+    if c["kind"] == "train":
+        g, u, dh = _plain_checkpoint(g), _plain_checkpoint(u), s["dH"].float()
+        sg = 1 / (1 + torch.exp(-g))
+        out["dU"] = (dh * (g * sg)).to(s["dH"].dtype)
+        out["dG"] = (dh * u * (sg * (1 + g * (1 - sg)))).to(s["dH"].dtype)
+    return out
+
+
+def _plain_logprob(s):
+    c = s["case"]
+    x = s["logits"].float()
+    mx = x.amax(-1, keepdim=True)
+    e = torch.exp(x - mx)
+    tot = e.sum(-1, keepdim=True)
+    lse = mx + torch.log(tot)
+    t = s["targets"]
+    has = t >= 0
+    lp = torch.where(has, x.gather(1, t.clamp(min=0)[:, None]).squeeze(1) - lse.squeeze(1), torch.zeros_like(lse[:, 0]))
+    out = dict(logp=lp, lse=lse.squeeze(1))
+    p = e / tot
+    if c["ent"]:
+        plogp = torch.where(p > 0, p * (x - lse), torch.zeros_like(p))
+        out["entropy"] = -plogp.sum(-1)
+    if c["top"]:
+        val, idx = torch.sort(x, dim=-1, descending=True, stable=True)
+        out["top_ids"], out["top_logp"] = idx[:, :c["top"]], val[:, :c["top"]] - lse
+    if c["kind"] == "train":
+        gl = torch.where(has, s["dlogp"], torch.zeros_like(s["dlogp"]))[:, None]
+        dx = -p * gl
+        if c["ent"]:
+            dx = dx - s["dent"][:, None] * (plogp + p * out["entropy"][:, None])
+        dx.scatter_add_(1, t.clamp(min=0)[:, None], gl)
+        out["dlogits"] = dx.to(s["logits"].dtype)
+    return out
+
+
+# ------------------------------------------------------------------ the library's calls
+
+def _own_attn(s):
+    from paper_2412_04787_amd import dqt
+    c = s["case"]
+    b = s.get("own")
+    if b is None:        # descriptor, outputs and workspace, as a program keeps them
+        a = dqt.attn(s["tq"], s["tk"], c["heads"], c["kv_heads"], c["d"], s["q_start"], s["k_start"])
+        b = dict(a=a, O=torch.empty_like(s["Q"]), lse=torch.empty((c["heads"], s["tq"]), dtype=torch.float32, device=DEV),
+                 ws=dqt.workspace(dqt.dqt_attn_fwd_workspace(a), DEV))
+        if c["kind"] == "train":
+            b.update(dQ=torch.empty_like(s["Q"]), dK=torch.empty_like(s["K"]), dV=torch.empty_like(s["V"]),
+                     bws=dqt.workspace(dqt.dqt_attn_bwd_workspace(a), DEV))
+        s["own"] = b
+    dqt.dqt_attn_fwd(b["a"], s["Q"], s["K"], s["V"], b["O"], b["lse"], b["ws"])
+    out = dict(O=b["O"], lse=b["lse"])
+    if c["kind"] == "train":
+        dqt.dqt_attn_bwd(b["a"], s["Q"], s["K"], s["V"], b["O"], b["lse"], s["dO"], b["dQ"], b["dK"], b["dV"], b["bws"])
+        out.update(dQ=b["dQ"], dK=b["dK"], dV=b["dV"])
+    return out
+
+
+def _own_swiglu(s):
+    from paper_2412_04787_amd import dqt
+    c = s["case"]
+    m, k = c["m"], c["k"]
+    b = s.get("own")
+    if b is None:
+        e4m3 = c["act"] == "e4m3"
+        b = dict(act=dqt.DQT_FP8E4M3 if e4m3 else dqt.DQT_I8, xdq=torch.empty((m,), dtype=torch.float32, device=DEV),
+                 Xq=torch.empty((m, k), dtype=torch.float8_e4m3fn if e4m3 else torch.int8, device=DEV), ckpt=None)
+        if c["kind"] == "train":
+            b["ckpt"] = dqt.swiglu_ckpt(m, k, DEV)
+            b.update(dG=torch.empty_like(s["G"]), dU=torch.empty_like(s["U"]))
+        s["own"] = b
+    dqt.dqt_swiglu_act_quant(s["G"], s["U"], b["act"], b["Xq"], b["xdq"], b["ckpt"])
+    out = dict(Xq=b["Xq"], xdq=b["xdq"])
+    if c["kind"] == "train":
+        dqt.dqt_swiglu_backward_ckpt(s["dH"], b["ckpt"], b["dG"], b["dU"])
+        out.update(dG=b["dG"], dU=b["dU"])
+    return out
+
+
+def _own_logprob(s):
+    from paper_2412_04787_amd import dqt
+    c = s["case"]
+    m, v, top = c["m"], c["v"], c["top"]
+    b = s.get("own")
+    if b is None:
+        def vec(*shape, dtype=torch.float32):
+            return torch.empty(shape, dtype=dtype, device=DEV)
+        b = dict(logp=vec(m), lse=vec(m), ent=vec(m) if c["ent"] else None,
+                 ids=vec(m, top, dtype=torch.int64) if top else None, tlp=vec(m, top) if top else None,
+                 ws=dqt.workspace(dqt.dqt_logprob_workspace(m, v, top), DEV))
+        if c["kind"] == "train":
+            b["dx"] = torch.empty_like(s["logits"])
+        s["own"] = b
+    dqt.dqt_logprob_fwd(s["logits"], s["targets"], b["logp"], b["lse"], b["ent"], b["ids"], b["tlp"], b["ws"])
+    out = dict(logp=b["logp"], lse=b["lse"])
+    if c["ent"]:
+        out["entropy"] = b["ent"]
+    if top:
+        out.update(top_ids=b["ids"], top_logp=b["tlp"])
+    if c["kind"] == "train":
+        dqt.dqt_logprob_bwd(s["logits"], s["targets"], b["lse"], s["dlogp"], b["dx"], b["ent"], s["dent"])
+        out["dlogits"] = b["dx"]
+    return out
+
+
+def run(state):
+    op = state["case"]["op"]
+    if own:
+        return _own_attn(state) if op == "attn" else _own_swiglu(state) if op == "swiglu" else _own_logprob(state)
+    return _plain_attn(state) if op == "attn" else _plain_swiglu(state) if op == "swiglu" else _plain_logprob(state)
+
+
+# ------------------------------------------------------------------ work and exact values
+
+def work(case):
+    if case["op"] == "attn":
+        h, kv, d = case["heads"], case["kv_heads"], case["d"]
+        lq, lk = _lengths(case)
+        # pairs that the causal mask leaves: query i sees i + 1 + lk - lq keys
+        pairs = sum(a * (b - a) + a * (a + 1) // 2 for a, b in zip(lq, lk))
+        tq, tk = sum(lq), sum(lk)
+        by = 2 * d * (2 * tq * h + 2 * tk * kv) + 4 * tq * h
+        fl = 4 * d * h * pairs
+        if case["kind"] == "train":      # also dO read; dQ, dK, dV written; five products for two
+            by += 2 * d * (2 * tq * h + 2 * tk * kv)
+            fl += 10 * d * h * pairs
+        return {"bytes": by, "flops": fl}
+    eb = 2 if case["dt"] == "bf16" else 4
+    if case["op"] == "swiglu":
+        n = case["m"] * case["k"]
+        by, fl = n * (2 * eb + 1) + 4 * case["m"], 8 * n
+        if case["kind"] == "train":      # checkpoints written, then read with dH; dG and dU written
+            by += n * 4 + n * 3 * eb
+            fl += 20 * n
+        return {"bytes": by, "flops": fl}
+    n = case["m"] * case["v"]
+    by, fl = n * eb + case["m"] * (16 + 12 * case["top"]), 4 * n
+    if case["kind"] == "train":          # logits read again, their gradient written
+        by += 2 * n * eb
+        fl += 4 * n
+    return {"bytes": by, "flops": fl}
+
+
+def _exact_attn(case, s):
+    h, kv, d = case["heads"], case["kv_heads"], case["d"]
+    grp = h // kv
+    qs, ks = s["q_start"].tolist(), s["k_start"].tolist()
+    train = case["kind"] == "train"
+    O = torch.empty((s["tq"], h, d), dtype=torch.float64, device=DEV)
+    lse = torch.empty((h, s["tq"]), dtype=torch.float64, device=DEV)
+    dQ = torch.empty_like(O)
+    dK = torch.empty((s["tk"], kv, d), dtype=torch.float64, device=DEV)
+    dV = torch.empty_like(dK)
+    for i in range(len(qs) - 1):
+        a, b, e, f = qs[i], qs[i + 1], ks[i], ks[i + 1]
+        far = torch.ones((b - a, f - e), dtype=torch.bool, device=DEV).triu(1 + (f - e) - (b - a))
+        for j in range(kv):
+            k = s["K"][e:f, j].double().requires_grad_(train)
+            v = s["V"][e:f, j].double().requires_grad_(train)
+            for x in range(j * grp, (j + 1) * grp):
+                q = s["Q"][a:b, x].double().requires_grad_(train)
+                z = torch.mm(q, k.t()) / math.sqrt(d)
+                z = z.masked_fill(far, -math.inf)
+                lse[x, a:b] = torch.logsumexp(z.detach(), -1)
+                o = torch.mm(torch.softmax(z, -1), v)
+                O[a:b, x] = o.detach()
+                if train:
+                    o.backward(s["dO"][a:b, x].double())
+                    dQ[a:b, x] = q.grad
+            if train:
+                dK[e:f, j], dV[e:f, j] = k.grad, v.grad
+    return dict(O=O, lse=lse, dQ=dQ, dK=dK, dV=dV) if train else dict(O=O, lse=lse)
+
+
+def _exact_swiglu(case, s):
+    g, u = s["G"].double(), s["U"].double()
+    h = torch.nn.functional.silu(g) * u
+    r = 127.0 if case["act"] == "int8" else 448.0
+    mx = h.abs().amax(-1).clamp(min=float(torch.tensor(1e-5)))
+    # (int8 codes are whole numbers; those of e4m3 are h on the row's scale, before its rounding to 8 bits)
+    out = dict(Xq=None if case["act"] == "int8" else h * (r / mx)[:, None], xdq=mx / r)
+    if case["kind"] == "train":
+        def stored(x):
+            m, k = x.shape
+            y = torch.cat([x, x.new_zeros((m, -k % GROUP))], 1).reshape(m, -1, GROUP)
+            t = y.abs().amax(-1, keepdim=True).clamp(min=float(torch.tensor(1e-5)))
+            return ((y * 127.0 / t).round() * t / 127.0).reshape(m, -1)[:, :k]
+        g, u = stored(g).requires_grad_(True), stored(u).requires_grad_(True)
+        (torch.nn.functional.silu(g) * u).backward(s["dH"].double())
+        out.update(dG=g.grad, dU=u.grad)
+    return out
+
+
+def _exact_logprob(case, s):
+    train = case["kind"] == "train"
+    m, v = case["m"], case["v"]
+    out = dict(logp=torch.empty(m, dtype=torch.float64, device=DEV), lse=torch.empty(m, dtype=torch.float64, device=DEV))
+    if case["ent"]:
+        out["entropy"] = torch.empty(m, dtype=torch.float64, device=DEV)
+    if case["top"]:
+        out["top_ids"] = None
+        out["top_logp"] = torch.empty((m, case["top"]), dtype=torch.float64, device=DEV)
+    if train:
+        out["dlogits"] = torch.empty((m, v), dtype=torch.float64, device=DEV)
+    rows = max(1, 2 ** 27 // v)
+    for a in range(0, m, rows):
+        b = min(m, a + rows)
+        x = s["logits"][a:b].double()
+        t = s["targets"][a:b]
+        y = torch.log_softmax(x, -1)
+        p = y.exp()
+        ent = -torch.special.xlogy(p, p).sum(-1)
+        pick = torch.nn.functional.one_hot(t.clamp(min=0), v).double() * (t >= 0)[:, None]
+        out["lse"][a:b] = torch.logsumexp(x, -1)
+        out["logp"][a:b] = torch.where(pick > 0, y, torch.zeros_like(y)).sum(-1)
+        if case["ent"]:
+            out["entropy"][a:b] = ent
+        if case["top"]:
+            out["top_logp"][a:b] = torch.topk(y, case["top"], -1).values
+        if train:
+            gl = s["dlogp"][a:b, None].double() * (t >= 0)[:, None]
+            d = gl * (pick - p)
+            if case["ent"]:
+                d -= s["dent"][a:b, None].double() * (torch.special.xlogy(p, p) + p * ent[:, None])
+            out["dlogits"][a:b] = d
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] == "attn":
+        return _exact_attn(case, s)
+    return _exact_swiglu(case, s) if case["op"] == "swiglu" else _exact_logprob(case, s)
