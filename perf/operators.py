@@ -341,16 +341,16 @@ def _own_logprob(s):
                  ids=vec(m, top, dtype=torch.int64) if top else None, tlp=vec(m, top) if top else None,
                  ws=dqt.workspace(dqt.dqt_logprob_workspace(m, v, top), DEV))
         if c["kind"] == "train":
-            b["dx"] = torch.empty_like(s["logits"])
+            b["dx"], b["stat"] = torch.empty_like(s["logits"]), vec(m, 2)
         s["own"] = b
-    dqt.dqt_logprob_fwd(s["logits"], s["targets"], b["logp"], b["lse"], b["ent"], b["ids"], b["tlp"], b["ws"])
+    dqt.dqt_logprob_fwd(s["logits"], s["targets"], b["logp"], b["lse"], b["ent"], b.get("stat"), b["ids"], b["tlp"], b["ws"])
     out = dict(logp=b["logp"], lse=b["lse"])
     if c["ent"]:
         out["entropy"] = b["ent"]
     if top:
         out.update(top_ids=b["ids"], top_logp=b["tlp"])
     if c["kind"] == "train":
-        dqt.dqt_logprob_bwd(s["logits"], s["targets"], b["lse"], s["dlogp"], b["dx"], b["ent"], s["dent"])
+        dqt.dqt_logprob_bwd(s["logits"], s["targets"], b["stat"], s["dlogp"], b["dx"], b["ent"], s["dent"])
         out["dlogits"] = b["dx"]
     return out
 
