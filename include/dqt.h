@@ -32,7 +32,7 @@
  *    the caller's next synchronisation.  Nothing throws or aborts.
  *  - Shapes: d_in and d_out are multiples of 16 and at least 16; M >= 0 (any
  *    value, M = 0 is a no-op except that dW is then written as zeros).
- *    Base pointers must be 16-byte aligned.
+ *    Base pointers must be 16-byte aligned; per-row fp32 outputs 4-byte.
  *  - Non-finite values in X or dY are not checked.
  *  - Workspaces (dqt_linear_fwd / dqt_linear_bwd and their batches) are
  *    caller-owned device buffers of at least the size the matching
@@ -179,6 +179,162 @@ dqt_status dqt_rmsnorm_act_quant(const void* X, int32_t x_t, const float* gamma,
 dqt_status dqt_rmsnorm_backward(int32_t n_dy, const void* const* dY, const void* X, int32_t x_t,
                                 const float* gamma, const float* rinv, int64_t M, int32_t K,
                                 void* dX, float* gpart, int32_t blocks, void* stream);
+
+/*
+ * The SwiGLU product of a LLaMA block's feed-forward and its per-token
+ * quantisation (the input of the down projection; Sec. 4.1 trains LLaMA
+ * blocks, Sec. 3.2 quantises the linears' inputs to 8 bits), in one launch:
+ * the product never reaches memory.  For each row of G and U [M, K], every
+ * operation one correctly rounded fp32 operation and exp the device library's
+ * expf:
+ *   h = (g / (1 + exp(-g))) u,  then dqt_act_quant of the row of h.
+ * With a checkpoint, G and U are also kept in 8 bits for the backward, so
+ * that a training step need not hold them in 16: for each group of
+ * DQT_CKPT_GROUP consecutive elements of a row (the last one shorter when K
+ * is not a multiple),
+ *   a = max(max |x|, 1e-5), code = clamp(rint(x fl(127 / a)), -128, 127),
+ *   scale = fl(a / 127).
+ *   G, U: [M, K], x_t = DQT_F32 or DQT_BF16.  Xq: [M, K] codes; xdq: [M].
+ *   ckpt: NULL, or all four buffers.  K a multiple of 16; M at most 2^28 and
+ *   M K < 2^35.  Non-finite values are not checked.
+ */
+#define DQT_CKPT_GROUP 128
+typedef struct {
+  int8_t* Gq;           /* [M, K] codes of G (device)                          */
+  int8_t* Uq;           /* [M, K] codes of U                                   */
+  float* gs;            /* [M, ceil(K / DQT_CKPT_GROUP)] scales of Gq          */
+  float* us;            /* ... of Uq                                           */
+} dqt_ckpt_io;
+
+dqt_status dqt_swiglu_act_quant(const void* G, const void* U, int32_t x_t, int64_t M,
+                                int32_t K, int32_t act_q, void* Xq, float* xdq,
+                                const dqt_ckpt_io* ckpt, void* stream);
+
+/*
+ * Backward of the SwiGLU product (the quantiser passes the gradient through,
+ * as everywhere).  With s = 1 / (1 + exp(-g)), in fp32, rounded once:
+ *   dU = dH (g s),   dG = dH u s (1 + g (1 - s))
+ *   dH, dG, dU: [M, K], h_t = DQT_F32 or DQT_BF16; dG or dU may be dH's buffer.
+ *   g, u: from the checkpoint of the forward (code times scale; G and U NULL),
+ *   or, with ckpt NULL, from G and U [M, K] of type h_t.
+ *   Both given: DQT_ERR_UNSUPPORTED.  Sizes as for dqt_swiglu_act_quant.
+ */
+dqt_status dqt_swiglu_backward(const void* dH, int32_t h_t, const void* G, const void* U,
+                               const dqt_ckpt_io* ckpt, int64_t M, int32_t K,
+                               void* dG, void* dU, void* stream);
+
+/*
+ * Log probabilities of given tokens (the training loss is the mean of -logp;
+ * a continuation's score, and from it perplexity and multiple-choice accuracy,
+ * the sum of its logp).  For each row of logits X [M, V], in fp32:
+ *   lse = log sum_j exp(x_j),  logp = x_t - lse,
+ *   entropy = -sum_j p_j log p_j  with p_j = exp(x_j - lse)
+ *   top_ids, top_logp: the top_k most probable tokens in descending order, the
+ *   lower id first among equals, and their log probabilities.
+ * A logit of -inf (a masked token) has p = 0 and adds nothing to the entropy;
+ * a row of nothing else has lse = logp = -inf and entropy 0.  A row with a
+ * +inf or a NaN gives NaN for all three (its top_ids are distinct tokens).
+ *   X: x_t = DQT_F32 or DQT_BF16; `stride` elements from row to row (>= V),
+ *      any alignment of rows; the base pointer 16-byte aligned.
+ *   targets: [M] int64, or NULL when logp is NULL.  A target outside 0 .. V-1
+ *      (padding) gives logp = 0 and no gradient.
+ *   logp, lse, entropy: [M] fp32, each may be NULL (not written).
+ *   stat: NULL, or [M, 2] fp32, 8-byte aligned, for the backward: the row's
+ *      largest logit and log sum_j exp(x_j - it).
+ *   top_k: 0 .. DQT_MAX_TOP, at most V; top_ids [M, top_k] int64, top_logp
+ *      [M, top_k] fp32 (NULL allowed when top_k is 0).
+ *   ws: dqt_logprob_workspace(M, V, top_k) bytes (0 for many rows; rows are
+ *      split over blocks when there are few).
+ *   M at most 2^23, V at most 2^28.
+ */
+#define DQT_MAX_TOP 32
+size_t dqt_logprob_workspace(int64_t M, int32_t V, int32_t top_k);
+dqt_status dqt_logprob_fwd(const void* X, int32_t x_t, int64_t M, int32_t V, int64_t stride,
+                           const int64_t* targets, float* logp, float* lse, float* entropy,
+                           float* stat, int32_t top_k, int64_t* top_ids, float* top_logp,
+                           void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gradient of dqt_logprob_fwd's logp and entropy with respect to the logits:
+ *   dX_j = g [j = t] - p_j (g + e (x_j - lse + entropy))
+ * with g = dlogp of the row (0 for a row without a target) and e = dent; rounded
+ * once to x_t.  A masked logit, and a row of nothing else, get 0.
+ *   stat, entropy: the forward's (entropy may be NULL when dent is).
+ *   dlogp, dent: [M] fp32 upstream gradients, NULL for zero.
+ *   dX: [M, V] of type x_t with stride dx_stride >= V; may be X itself (same
+ *      stride), otherwise the two do not overlap.  Elements between rows are
+ *      left as they are.
+ */
+dqt_status dqt_logprob_bwd(const void* X, int32_t x_t, int64_t M, int32_t V, int64_t stride,
+                           const int64_t* targets, const float* stat, const float* entropy,
+                           const float* dlogp, const float* dent, void* dX, int64_t dx_stride,
+                           void* stream);
+
+/*
+ * Softmax attention over packed sequences (the block's attention; Sec. 4.1
+ * trains LLaMA blocks).  Sequence s owns the query tokens q_start[s] ..
+ * q_start[s + 1] - 1 and the key tokens k_start[s] .. k_start[s + 1] - 1, lq
+ * and lk of them.  Its query i sees its key j when causal = 0, or when
+ * j <= i + lk - lq: the queries are the last lq of the lk positions, so
+ * lq = lk is a whole prompt, lq = 1 a new token over its lk - 1 predecessors,
+ * and anything between a chunk.  Query head h reads key head h / (heads /
+ * kv_heads).  Per query and head:
+ *   z_j = scale q.k_j,  lse = log sum exp(z_j),  O = sum_j exp(z_j - lse) v_j
+ * over the keys it sees; O = 0 and lse = -inf when it sees none.  Operands and
+ * results are bf16; scores, softmax and sums fp32; probabilities are rounded
+ * to bf16 for the matrix cores.
+ *   q_start, k_start: device int32 [n_seq + 1], ascending, 0 <= start <=
+ *      tokens; either may be NULL when n_seq = 1 (one sequence of all tokens).
+ *      Empty sequences are allowed.  Values that break these rules give wrong
+ *      results but no access outside the tensors.  Tokens outside every
+ *      sequence are neither read into another's result nor written.
+ *   d: 64 or 128.  heads a multiple of kv_heads, at most 1024.
+ *   q_tokens * heads < 2^28; k_tokens and q_tokens * (heads / kv_heads) < 2^31.
+ *   scale: 2^-20 .. 2^20.
+ * Tensors are strided: token t's head h is the d consecutive values from
+ * p + t * token + h * head (elements; both strides multiples of 8, at most
+ * 2^31; 0 allowed for inputs).  Outputs alias neither an input nor each other,
+ * and their rows do not overlap (DQT_ERR_SHAPE).  A non-finite value in K or V
+ * may reach any query of its own sequence and head, masked or not, and one in
+ * Q or dO any gradient of its sequence; none reaches another sequence.
+ */
+typedef struct {
+  const int32_t* q_start;
+  const int32_t* k_start;
+  int64_t q_tokens;
+  int64_t k_tokens;
+  int32_t n_seq;
+  int32_t heads;
+  int32_t kv_heads;
+  int32_t d;
+  float scale;
+  int32_t causal;       /* 0 or 1                                              */
+  int64_t reserved;     /* must be 0                                           */
+} dqt_attn;
+
+typedef struct {
+  void* p;              /* device, bf16, 16-byte aligned                       */
+  int64_t token;        /* elements from token to token                        */
+  int64_t head;         /* elements from head to head                          */
+} dqt_rows;
+
+/* Forward.  lse: NULL, or [heads, q_tokens] fp32 (for the backward).  ws:
+ * dqt_attn_fwd_workspace() bytes, which depend on the descriptor's sizes alone
+ * (0 unless few rows leave the keys to be split over blocks). */
+size_t dqt_attn_fwd_workspace(const dqt_attn* a);
+dqt_status dqt_attn_fwd(const dqt_attn* a, const dqt_rows* Q, const dqt_rows* K,
+                        const dqt_rows* V, const dqt_rows* O, float* lse,
+                        void* ws, size_t ws_bytes, void* stream);
+
+/* Backward: dQ, dK, dV of the forward's O for the upstream gradient dO, from
+ * the forward's O and lse.  Gradients of a key head are summed over the query
+ * heads that share it, in fp32 and a fixed order (bit-reproducible).  Keys
+ * that no query sees get 0. */
+size_t dqt_attn_bwd_workspace(const dqt_attn* a);
+dqt_status dqt_attn_bwd(const dqt_attn* a, const dqt_rows* Q, const dqt_rows* K,
+                        const dqt_rows* V, const dqt_rows* O, const float* lse,
+                        const dqt_rows* dO, const dqt_rows* dQ, const dqt_rows* dK,
+                        const dqt_rows* dV, void* ws, size_t ws_bytes, void* stream);
 
 /* Bytes of device workspace for the fastest form of dqt_linear_fwd on this
  * weight: the 256 counter bytes, plus, for ternary, 3-bit and 4-bit codes,

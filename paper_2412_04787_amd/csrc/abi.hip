@@ -111,6 +111,261 @@ dqt_status dqt_rmsnorm_backward(int32_t n_dy, const void* const* dY, const void*
                                                static_cast<hipStream_t>(stream)));
 }
 
+namespace {
+
+bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// A checkpoint is given as a whole or not at all.
+dqt_status check_ckpt(const dqt_ckpt_io* c, dqt::Ckpt* out) {
+  *out = dqt::Ckpt{};
+  if (c == nullptr) return DQT_OK;
+  if (c->Gq == nullptr || c->Uq == nullptr || c->gs == nullptr || c->us == nullptr) return DQT_ERR_NULL;
+  if (!aligned16(c->Gq) || !aligned16(c->Uq) || !aligned16(c->gs) || !aligned16(c->us)) return DQT_ERR_ALIGN;
+  *out = dqt::Ckpt{c->Gq, c->Uq, c->gs, c->us};
+  return DQT_OK;
+}
+dqt_status check_swiglu(int64_t M, int32_t K) {
+  if (M < 0 || M > (int64_t(1) << 28) || K < 16 || (K % 16) != 0) return DQT_ERR_SHAPE;
+  if (M * (K / 8) >= (int64_t(1) << 32)) return DQT_ERR_SHAPE;
+  return DQT_OK;
+}
+
+}  // namespace
+
+dqt_status dqt_swiglu_act_quant(const void* G, const void* U, int32_t x_t, int64_t M, int32_t K, int32_t act_q,
+                                void* Xq, float* xdq, const dqt_ckpt_io* ckpt, void* stream) {
+  dqt_status st = check_swiglu(M, K);
+  if (st != DQT_OK) return st;
+  if (!is_float_type(x_t) || (act_q != DQT_I8 && act_q != DQT_FP8E4M3)) return DQT_ERR_DTYPE;
+  if (M == 0) return DQT_OK;
+  dqt::Ckpt c;
+  st = check_ckpt(ckpt, &c);
+  if (st != DQT_OK) return st;
+  if (G == nullptr || U == nullptr || Xq == nullptr || xdq == nullptr) return DQT_ERR_NULL;
+  if (!aligned16(G) || !aligned16(U) || !aligned16(Xq) || !aligned16(xdq)) return DQT_ERR_ALIGN;
+  return from_hip(dqt::launch_swiglu_act_quant(G, U, x_t == DQT_BF16, M, K, act_q == DQT_FP8E4M3, Xq, xdq, c,
+                                               static_cast<hipStream_t>(stream)));
+}
+
+dqt_status dqt_swiglu_backward(const void* dH, int32_t h_t, const void* G, const void* U, const dqt_ckpt_io* ckpt,
+                               int64_t M, int32_t K, void* dG, void* dU, void* stream) {
+  dqt_status st = check_swiglu(M, K);
+  if (st != DQT_OK) return st;
+  if (!is_float_type(h_t)) return DQT_ERR_DTYPE;
+  if (M == 0) return DQT_OK;
+  dqt::Ckpt c;
+  st = check_ckpt(ckpt, &c);
+  if (st != DQT_OK) return st;
+  if (dH == nullptr || dG == nullptr || dU == nullptr) return DQT_ERR_NULL;
+  if (ckpt == nullptr && (G == nullptr || U == nullptr)) return DQT_ERR_NULL;
+  if (ckpt != nullptr && (G != nullptr || U != nullptr)) return DQT_ERR_UNSUPPORTED;
+  if (!aligned16(dH) || !aligned16(G) || !aligned16(U) || !aligned16(dG) || !aligned16(dU)) return DQT_ERR_ALIGN;
+  return from_hip(dqt::launch_swiglu_backward(dH, h_t == DQT_BF16, G, U, c, M, K, dG, dU,
+                                              static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+dqt_status check_logprob(int64_t M, int32_t V, int32_t x_t, int64_t stride) {
+  if (M < 0 || M > (int64_t(1) << 23) || V < 1 || V > (1 << 28) || stride < V) return DQT_ERR_SHAPE;
+  if (!is_float_type(x_t)) return DQT_ERR_DTYPE;
+  return DQT_OK;
+}
+// workspace of a forward whose rows are split: partial sums, then keys
+size_t logprob_part_bytes(int64_t M, int splits) { return ((size_t)M * splits * 16 + 15) / 16 * 16; }
+
+}  // namespace
+
+size_t dqt_logprob_workspace(int64_t M, int32_t V, int32_t top_k) {
+  if (M < 1 || M > (int64_t(1) << 23) || V < 1 || V > (1 << 28) || top_k < 0 || top_k > DQT_MAX_TOP) return 0;
+  const int s = dqt::logprob_splits(M, V);
+  return s == 1 ? 0 : logprob_part_bytes(M, s) + (size_t)M * s * top_k * 8;
+}
+
+dqt_status dqt_logprob_fwd(const void* X, int32_t x_t, int64_t M, int32_t V, int64_t stride, const int64_t* targets,
+                           float* logp, float* lse, float* entropy, float* stat, int32_t top_k, int64_t* top_ids,
+                           float* top_logp, void* ws, size_t ws_bytes, void* stream) {
+  const dqt_status st = check_logprob(M, V, x_t, stride);
+  if (st != DQT_OK) return st;
+  if (top_k < 0 || top_k > DQT_MAX_TOP || top_k > V) return DQT_ERR_SHAPE;
+  if (M == 0) return DQT_OK;
+  if (X == nullptr || (logp != nullptr && targets == nullptr)) return DQT_ERR_NULL;
+  if (top_k > 0 && (top_ids == nullptr || top_logp == nullptr)) return DQT_ERR_NULL;
+  if (!aligned16(X) || !aligned8(targets) || !aligned4(logp) || !aligned4(lse) || !aligned4(entropy) ||
+      !aligned8(stat) || !aligned8(top_ids) || !aligned4(top_logp) || !aligned16(ws))
+    return DQT_ERR_ALIGN;
+  const size_t need = dqt_logprob_workspace(M, V, top_k);
+  if (need > 0 && (ws == nullptr || ws_bytes < need)) return DQT_ERR_WORKSPACE;
+  dqt::LogprobArgs a{};
+  a.x = X; a.stride = stride; a.M = M; a.V = V; a.targets = targets;
+  a.logp = logp; a.lse = lse; a.entropy = entropy; a.stat = stat;
+  a.top = top_k; a.top_ids = top_ids; a.top_logp = top_logp;
+  a.splits = dqt::logprob_splits(M, V);
+  if (a.splits > 1) {
+    a.part = static_cast<float*>(ws);
+    a.part_top = reinterpret_cast<uint64_t*>(static_cast<uint8_t*>(ws) + logprob_part_bytes(M, a.splits));
+  }
+  return from_hip(dqt::launch_logprob_fwd(a, x_t == DQT_BF16, static_cast<hipStream_t>(stream)));
+}
+
+dqt_status dqt_logprob_bwd(const void* X, int32_t x_t, int64_t M, int32_t V, int64_t stride, const int64_t* targets,
+                           const float* stat, const float* entropy, const float* dlogp, const float* dent, void* dX,
+                           int64_t dx_stride, void* stream) {
+  const dqt_status st = check_logprob(M, V, x_t, stride);
+  if (st != DQT_OK) return st;
+  if (dx_stride < V) return DQT_ERR_SHAPE;
+  if (M == 0) return DQT_OK;
+  if (X == nullptr || stat == nullptr || dX == nullptr) return DQT_ERR_NULL;
+  if (dlogp != nullptr && targets == nullptr) return DQT_ERR_NULL;
+  if (dent != nullptr && entropy == nullptr) return DQT_ERR_NULL;
+  if (!aligned16(X) || !aligned16(dX) || !aligned8(targets) || !aligned8(stat) || !aligned4(entropy) || !aligned4(dlogp) ||
+      !aligned4(dent))
+    return DQT_ERR_ALIGN;
+  if (dX == X && dx_stride != stride) return DQT_ERR_SHAPE;
+  dqt::LogprobArgs a{};
+  a.x = X; a.stride = stride; a.M = M; a.V = V; a.targets = targets;
+  a.stat = const_cast<float*>(stat); a.entropy = const_cast<float*>(entropy);
+  a.dlogp = dlogp; a.dent = dent; a.dx = dX; a.dx_stride = dx_stride; a.splits = 1;
+  return from_hip(dqt::launch_logprob_bwd(a, x_t == DQT_BF16, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+constexpr int64_t kMaxBlocks = int64_t(1) << 24;      // of 256 threads: the runtime's grids end at 2^32 threads
+
+// Checks the descriptor and fills the sizes of the launch arguments.
+dqt_status check_attn(const dqt_attn* d, dqt::AttnArgs* a) {
+  if (d == nullptr) return DQT_ERR_NULL;
+  if (d->d != 64 && d->d != 128) return DQT_ERR_SHAPE;
+  if (d->heads < 1 || d->kv_heads < 1 || d->heads > 1024 || d->heads % d->kv_heads != 0) return DQT_ERR_SHAPE;
+  if (d->n_seq < 1 || d->q_tokens < 0 || d->k_tokens < 0) return DQT_ERR_SHAPE;
+  const int64_t g = d->heads / d->kv_heads, most = (int64_t(1) << 31) - 1;
+  if (d->q_tokens > most || d->k_tokens > most || d->q_tokens * g > most) return DQT_ERR_SHAPE;
+  // (the delta pass has 16 rows per block)
+  if (d->q_tokens * d->heads / 16 >= kMaxBlocks) return DQT_ERR_SHAPE;
+  const int64_t rt = dqt::attn_row_tiles(d->q_tokens, g, d->n_seq), kt = dqt::attn_row_tiles(d->k_tokens, 1, d->n_seq);
+  if (rt * d->kv_heads >= kMaxBlocks || kt * d->kv_heads >= kMaxBlocks) return DQT_ERR_SHAPE;
+  if ((d->q_start == nullptr || d->k_start == nullptr) && d->n_seq != 1) return DQT_ERR_NULL;
+  if (!aligned4(d->q_start) || !aligned4(d->k_start)) return DQT_ERR_ALIGN;
+  if (!(d->scale >= 0x1p-20f && d->scale <= 0x1p20f)) return DQT_ERR_RANGE;
+  if (d->causal != 0 && d->causal != 1) return DQT_ERR_RANGE;
+  if (d->reserved != 0) return DQT_ERR_RANGE;
+  *a = dqt::AttnArgs{};
+  a->q_start = d->q_start;
+  a->k_start = d->k_start;
+  a->tq = (int)d->q_tokens;
+  a->tk = (int)d->k_tokens;
+  a->n_seq = d->n_seq;
+  a->heads = d->heads;
+  a->kv_heads = d->kv_heads;
+  a->group = (int)g;
+  if (g > 1) {      // r / g = umulhi(r, m) >> (b - 1) with m = ceil(2^(31 + b) / g), b = ceil(log2 g), for r < 2^31
+    int b = 1;
+    while ((int64_t(1) << b) < g) ++b;
+    a->gmul = (uint32_t)(((uint64_t(1) << (31 + b)) + g - 1) / g);
+    a->gshift = b - 1;
+  }
+  a->scale = d->scale;
+  a->causal = d->causal;
+  a->row_tiles = (int)rt;
+  a->key_tiles = (int)kt;
+  a->splits = dqt::attn_splits(d->q_tokens, d->k_tokens, d->n_seq, d->heads, d->kv_heads);
+  return DQT_OK;
+}
+
+size_t attn_part_bytes(const dqt::AttnArgs& a, int d) {
+  return a.splits == 1 ? 0 : (size_t)a.splits * a.heads * a.tq * (d + 1) * 4;
+}
+
+// A strided tensor [tokens, heads, d] of bf16: non-negative strides that keep
+// 16-byte alignment; an output's rows must not overlap.
+dqt_status check_rows(const dqt_rows* t, int64_t tokens, int32_t heads, int32_t d, bool output) {
+  if (t == nullptr) return DQT_ERR_NULL;
+  if (tokens > 0 && t->p == nullptr) return DQT_ERR_NULL;
+  if (!aligned16(t->p) || (t->token & 7) != 0 || (t->head & 7) != 0) return DQT_ERR_ALIGN;
+  const int64_t most = int64_t(1) << 31;
+  if (t->token < 0 || t->head < 0 || t->token > most || t->head > most) return DQT_ERR_SHAPE;
+  if (tokens > 0 && (tokens - 1) * t->token + (heads - 1) * t->head > (int64_t(1) << 48)) return DQT_ERR_SHAPE;
+  if (output && tokens > 0) {
+    const bool by_token = (heads == 1 || t->head >= d) && (tokens == 1 || t->token >= (heads - 1) * t->head + d);
+    const bool by_head = (tokens == 1 || t->token >= d) && (heads == 1 || t->head >= (tokens - 1) * t->token + d);
+    if (!by_token && !by_head) return DQT_ERR_SHAPE;
+  }
+  return DQT_OK;
+}
+
+}  // namespace
+
+size_t dqt_attn_fwd_workspace(const dqt_attn* d) {
+  dqt::AttnArgs a;
+  if (check_attn(d, &a) != DQT_OK) return 0;
+  return attn_part_bytes(a, d->d);
+}
+
+size_t dqt_attn_bwd_workspace(const dqt_attn* d) {
+  dqt::AttnArgs a;
+  if (check_attn(d, &a) != DQT_OK) return 0;
+  return (size_t)a.heads * a.tq * 8;
+}
+
+dqt_status dqt_attn_fwd(const dqt_attn* d, const dqt_rows* Q, const dqt_rows* K, const dqt_rows* V, const dqt_rows* O,
+                        float* lse, void* ws, size_t ws_bytes, void* stream) {
+  dqt::AttnArgs a;
+  dqt_status st = check_attn(d, &a);
+  if (st != DQT_OK) return st;
+  if ((st = check_rows(Q, a.tq, a.heads, d->d, false)) != DQT_OK) return st;
+  if ((st = check_rows(K, a.tk, a.kv_heads, d->d, false)) != DQT_OK) return st;
+  if ((st = check_rows(V, a.tk, a.kv_heads, d->d, false)) != DQT_OK) return st;
+  if ((st = check_rows(O, a.tq, a.heads, d->d, true)) != DQT_OK) return st;
+  if (!aligned4(lse) || !aligned16(ws)) return DQT_ERR_ALIGN;
+  if (a.tq == 0) return DQT_OK;
+  const size_t need = attn_part_bytes(a, d->d);
+  if (need > 0 && (ws == nullptr || ws_bytes < need)) return DQT_ERR_WORKSPACE;
+  a.Q = static_cast<const uint8_t*>(Q->p); a.q_tok = Q->token * 2; a.q_head = Q->head * 2;
+  a.K = static_cast<const uint8_t*>(K->p); a.k_tok = K->token * 2; a.k_head = K->head * 2;
+  a.V = static_cast<const uint8_t*>(V->p); a.v_tok = V->token * 2; a.v_head = V->head * 2;
+  a.O = static_cast<uint8_t*>(O->p); a.o_tok = O->token * 2; a.o_head = O->head * 2;
+  a.lse = lse;
+  if (a.splits > 1) {
+    a.part = static_cast<float*>(ws);
+    a.part_lse = a.part + (size_t)a.splits * a.heads * a.tq * d->d;
+  }
+  return from_hip(dqt::launch_attn_fwd(d->d, a, static_cast<hipStream_t>(stream)));
+}
+
+dqt_status dqt_attn_bwd(const dqt_attn* d, const dqt_rows* Q, const dqt_rows* K, const dqt_rows* V, const dqt_rows* O,
+                        const float* lse, const dqt_rows* dO, const dqt_rows* dQ, const dqt_rows* dK, const dqt_rows* dV,
+                        void* ws, size_t ws_bytes, void* stream) {
+  dqt::AttnArgs a;
+  dqt_status st = check_attn(d, &a);
+  if (st != DQT_OK) return st;
+  if ((st = check_rows(Q, a.tq, a.heads, d->d, false)) != DQT_OK) return st;
+  if ((st = check_rows(K, a.tk, a.kv_heads, d->d, false)) != DQT_OK) return st;
+  if ((st = check_rows(V, a.tk, a.kv_heads, d->d, false)) != DQT_OK) return st;
+  if ((st = check_rows(O, a.tq, a.heads, d->d, false)) != DQT_OK) return st;
+  if ((st = check_rows(dO, a.tq, a.heads, d->d, false)) != DQT_OK) return st;
+  if ((st = check_rows(dQ, a.tq, a.heads, d->d, true)) != DQT_OK) return st;
+  if ((st = check_rows(dK, a.tk, a.kv_heads, d->d, true)) != DQT_OK) return st;
+  if ((st = check_rows(dV, a.tk, a.kv_heads, d->d, true)) != DQT_OK) return st;
+  if (a.tq > 0 && lse == nullptr) return DQT_ERR_NULL;
+  if (!aligned4(lse) || !aligned16(ws)) return DQT_ERR_ALIGN;
+  const size_t need = (size_t)a.heads * a.tq * 8;
+  if (need > 0 && (ws == nullptr || ws_bytes < need)) return DQT_ERR_WORKSPACE;
+  a.Q = static_cast<const uint8_t*>(Q->p); a.q_tok = Q->token * 2; a.q_head = Q->head * 2;
+  a.K = static_cast<const uint8_t*>(K->p); a.k_tok = K->token * 2; a.k_head = K->head * 2;
+  a.V = static_cast<const uint8_t*>(V->p); a.v_tok = V->token * 2; a.v_head = V->head * 2;
+  a.O = static_cast<uint8_t*>(O->p); a.o_tok = O->token * 2; a.o_head = O->head * 2;
+  a.dO = static_cast<const uint8_t*>(dO->p); a.do_tok = dO->token * 2; a.do_head = dO->head * 2;
+  a.dQ = static_cast<uint8_t*>(dQ->p); a.dq_tok = dQ->token * 2; a.dq_head = dQ->head * 2;
+  a.dK = static_cast<uint8_t*>(dK->p); a.dk_tok = dK->token * 2; a.dk_head = dK->head * 2;
+  a.dV = static_cast<uint8_t*>(dV->p); a.dv_tok = dV->token * 2; a.dv_head = dV->head * 2;
+  a.lse = const_cast<float*>(lse);
+  a.neg_lse = static_cast<float*>(ws);
+  a.neg_delta = a.neg_lse + (size_t)a.heads * a.tq;
+  return from_hip(dqt::launch_attn_bwd(d->d, a, static_cast<hipStream_t>(stream)));
+}
+
 dqt_status dqt_act_quant_batch(int32_t n, const dqt_act_io* io, int32_t x_t, int64_t M,
                                int32_t act_q, void* stream) {
   if (n < 0 || n > DQT_MAX_BATCH) return DQT_ERR_SHAPE;

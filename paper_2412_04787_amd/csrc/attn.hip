@@ -1,0 +1,602 @@
+// Softmax attention over packed sequences, forward and backward (bf16).
+//
+// Query i of a sequence of lq queries and lk keys sees key j when j < lk and,
+// causal, j <= i + lk - lq.  For one query head h and its key head h / G
+// (G = heads / kv_heads query heads share a key head), with c = scale:
+//   z_ij = c q_i . k_j,  lse_i = log sum_j exp(z_ij),  p_ij = exp(z_ij - lse_i)
+//   o_i = sum_j p_ij v_j
+//   dv_j = sum_i p_ij do_i,  g_ij = p_ij (do_i . v_j - do_i . o_i)
+//   dq_i = c sum_j g_ij k_j,  dk_j = c sum_i g_ij q_i      (i over all G heads)
+// The scores never reach memory: the forward keeps a running maximum and sum
+// per row, the backward forms p again from lse.
+//
+// Rows.  The G query heads of a key head and the tokens of a sequence form
+// one list of rows, row r = token r / G, head r % G, so that a tile of rows
+// reads the keys and values once for all the heads that share them, a single
+// new token fills G rows of a tile, and dk and dv of a shared head are summed
+// over its query heads in registers (fixed order, no atomics).
+//
+// Matrix layout (v_mfma_f32_32x32x16_bf16).  A operand: lane l holds row
+// l % 32, 8 values of the reduction from 8 (l / 32); B the same for columns;
+// result register i of lane l is row 8 (i / 4) + 4 (l / 32) + i % 4 of column
+// l % 32.  The forward and dq form the scores transposed (A = keys, B = rows
+// of Q), so that a lane holds scores of one query: the softmax statistics
+// need one exchange between lane halves, and the scaling of o is per lane.
+// The second product takes the score registers as its B operand as they are:
+// registers 8 kk .. 8 kk + 7 of the two lane halves are keys
+// 16 kk + 8 (j / 4) + 4 (l / 32) + j % 4, and the order of a reduction is free
+// as long as the A operand (V or K, transposed by ds_read_b64_tr_b16) takes
+// the same one.  dk/dv run the other way round (A = rows of Q, B = keys).
+#include "dqt_launch.h"
+
+namespace dqt {
+
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+using lds_i32x4 = __attribute__((address_space(3))) i32x4;
+using lds_f32x4 = __attribute__((address_space(3))) f32x4;
+
+constexpr int kBM = 128;      // rows per block of the forward and dq, keys per block of dk/dv
+constexpr int kKT = 64;       // keys (forward, dq) or rows (dk/dv) per staged tile
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// A staged tile: kKT rows of D bf16 values, 16-byte chunk c of row r at chunk
+// c ^ swz(r).  With swz, the 16 rows that a straight read takes at one chunk,
+// and the 4 x 4 chunks that a transposing read takes of 4 rows, each fall on
+// all 64 banks once.
+template <int D>
+__device__ __forceinline__ int swz(int r) {
+  return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 2) << 1) | ((r >> 2) & 3);
+}
+
+struct Seq {
+  int q0, lq, k0, lk;   // first token and length, of queries and keys
+  int tile;             // this block's tile within the sequence
+};
+
+// Sequence s's tiles start at index start * mul / kBM + s (rounded down): the
+// sequence's tiles always fit before the next one's, so blocks find their
+// sequence from the starts alone, whatever the lengths.  Lane-parallel search
+// of the last sequence that starts at or before tile t; false when there is
+// none.  Starts are clamped to the tensors: no value in them leads out of
+// bounds.
+__device__ __forceinline__ int clamp_to(int x, int n) { return x < 0 ? 0 : x > n ? n : x; }
+__device__ __forceinline__ int64_t tile0_of(int start, int n, int mul, int s) {
+  return (int64_t)clamp_to(start, n) * mul / kBM + s;
+}
+template <bool KEYS>
+__device__ __forceinline__ bool find_seq(const AttnArgs& a, int t, Seq& q) {
+  const int32_t* starts = KEYS ? a.k_start : a.q_start;
+  const int n_tok = KEYS ? a.tk : a.tq, mul = KEYS ? 1 : a.group;
+  const int lane = threadIdx.x & (kWave - 1);
+  int lo = 0, hi = a.n_seq;
+  if (starts != nullptr) {
+    while (hi - lo > 1) {
+      const int step = (hi - lo + kWave - 1) / kWave;
+      const int s = lo + lane * step;
+      const bool at = s < hi && tile0_of(starts[s < hi ? s : lo], n_tok, mul, s) <= t;
+      const int cnt = __popcll(__ballot(at));
+      if (cnt == 0) return false;
+      lo = lo + (cnt - 1) * step;
+      hi = min(hi, lo + step);
+    }
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  auto span = [&](const int32_t* p, int n, int& first, int& len) {
+    const int b = p == nullptr ? 0 : clamp_to(p[lo], n), e = p == nullptr ? n : clamp_to(p[lo + 1], n);
+    first = __builtin_amdgcn_readfirstlane(b);
+    len = __builtin_amdgcn_readfirstlane(e > b ? e - b : 0);
+  };
+  span(a.q_start, a.tq, q.q0, q.lq);
+  span(a.k_start, a.tk, q.k0, q.lk);
+  const int64_t first = tile0_of(KEYS ? q.k0 : q.q0, n_tok, mul, lo);
+  q.tile = (int)(t - first);
+  return q.tile >= 0;
+}
+
+// row r of a sequence -> token and head within the group (r / G, r % G)
+__device__ __forceinline__ int row_token(const AttnArgs& a, int r) {
+  return a.group == 1 ? r : (int)(__umulhi((uint32_t)r, a.gmul) >> a.gshift);
+}
+
+// Blocks go to the 8 XCDs in turn; XCD x takes the x-th eighth of the list, so
+// that the blocks that read one head's keys share an L2.
+__device__ __forceinline__ int xcd_order(int b, int n) {
+  const int per = n / 8;
+  return b < 8 * per ? (b & 7) * per + (b >> 3) : b;
+}
+
+template <int D>
+__device__ __forceinline__ i32x4 read_straight(const lds_u8* tile, int rb, int ks) {
+  const int l = threadIdx.x & 63, row = rb + (l & 31);
+  return *(const lds_i32x4*)(tile + row * (2 * D) + (((2 * ks + (l >> 5)) ^ swz<D>(row & 15)) << 4));
+}
+// values [kb + {4 h + 0..3, 8 + 4 h + 0..3}] (h = lane half) of column
+// 32 db + lane % 32, kb a multiple of 16
+template <int D>
+__device__ __forceinline__ i32x4 read_transposed(const lds_u8* tile, int kb, int db) {
+  const int l = threadIdx.x & 63, h = l >> 5, i = l & 15;
+  const int c = 4 * db + ((l >> 3) & 2) + ((i >> 1) & 1);
+  auto half = [&](int e) {
+    const int row = kb + 8 * e + 4 * h + (i >> 2);
+    const int off = row * (2 * D) + ((c ^ swz<D>((8 * e + 4 * h + (i >> 2)) & 15)) << 4) + 8 * (i & 1);
+    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(tile + off));
+    return __builtin_bit_cast(u32x2, v);
+  };
+  const u32x2 lo = half(0), hi = half(1);
+  return i32x4{(int)lo[0], (int)lo[1], (int)hi[0], (int)hi[1]};
+}
+__device__ __forceinline__ f32x16 mfma(i32x4 a, i32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// 8 scores -> B operand (rounded to bf16, as every operand of the second
+// products: the matrix cores take 16-bit values)
+__device__ __forceinline__ i32x4 pack8(const f32x16& v, int at) {
+  return i32x4{(int)pack_bf16x2(v[at], v[at + 1]), (int)pack_bf16x2(v[at + 2], v[at + 3]),
+               (int)pack_bf16x2(v[at + 4], v[at + 5]), (int)pack_bf16x2(v[at + 6], v[at + 7])};
+}
+__device__ __forceinline__ f32x16 splat(float x) {
+  f32x16 v;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = x;
+  return v;
+}
+
+// One wave's quarter of a tile of kKT rows: row_ptr(r) is the address of the
+// tile's row r (in bounds for every r).
+template <int D, class F>
+__device__ __forceinline__ void stage(lds_u8* tile, F&& row_ptr) {
+  constexpr int CH = D / 8, N = kKT * CH / 256;
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int p = (w * N + n) * 64 + l, row = p / CH, c = (p % CH) ^ swz<D>(row & 15);
+    dma16(row_ptr(row) + 16 * c, tile + (w * N + n) * 1024);
+  }
+}
+
+// result columns (one row of the output per lane, 32 ND values) -> bf16
+template <int ND>
+__device__ __forceinline__ void store_cols(uint8_t* p, const f32x16 (&o)[ND], float f) {
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int db = 0; db < ND; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint2 v = make_uint2(pack_bf16x2(o[db][4 * q] * f, o[db][4 * q + 1] * f),
+                                 pack_bf16x2(o[db][4 * q + 2] * f, o[db][4 * q + 3] * f));
+      *reinterpret_cast<uint2*>(p + 2 * (32 * db + 8 * q + 4 * h)) = v;
+    }
+}
+
+// ------------------------------------------------------------------ forward
+template <int D>
+__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
+  constexpr int NK = D / 16, ND = D / 32, TB = kKT * D * 2;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2][TB];
+  lds_u8* lds = (lds_u8*)&smem[0][0][0];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, h = lane >> 5;
+  const int id = xcd_order(blockIdx.x, gridDim.x);
+  const int per_head = a.row_tiles * a.splits;
+  const int kvh = id / per_head, rem = id - kvh * per_head;
+  const int split = rem % a.splits;
+  Seq sq;
+  // (last tiles first: under a causal mask they are the longest)
+  if (!find_seq<false>(a, a.row_tiles - 1 - rem / a.splits, sq)) return;
+  const int rows = sq.lq * a.group, r0 = sq.tile * kBM;
+  if (r0 >= rows) return;
+  const int off = sq.lk - sq.lq;
+
+  // this lane's row
+  const int r = r0 + 32 * w + (lane & 31), rc = min(r, rows - 1);
+  const int tok = row_token(a, rc), head = kvh * a.group + (rc - tok * a.group);
+  const bool active = r0 + 32 * w < rows;
+  // keys of this block: all that its last row sees, of this split
+  int kend = sq.lk;
+  if (a.causal) kend = min(kend, row_token(a, min(r0 + kBM, rows) - 1) + off + 1);
+  int kbeg = 0;
+  if (a.splits > 1) {
+    const int per = ((sq.lk + a.splits - 1) / a.splits + kKT - 1) / kKT * kKT;
+    kbeg = (int)min((int64_t)split * per, (int64_t)sq.lk);
+    kend = min(kend, kbeg + per);
+  }
+  const int nt = kend > kbeg ? (kend - kbeg + kKT - 1) / kKT : 0;
+  const int lim = min(a.causal ? tok + off : sq.lk - 1, kend - 1);      // last key this row sees
+  const int lim_lo = __builtin_amdgcn_readlane(lim, 0), lim_hi = __builtin_amdgcn_readlane(lim, 31);
+
+  const uint8_t* kp = a.K + (int64_t)sq.k0 * a.k_tok + (int64_t)kvh * a.k_head;
+  const uint8_t* vp = a.V + (int64_t)sq.k0 * a.v_tok + (int64_t)kvh * a.v_head;
+  auto issue = [&](int t) {
+    lds_u8* s = lds + (t & 1) * 2 * TB;
+    const int k0 = kbeg + t * kKT;
+    stage<D>(s, [&](int row) { return kp + (int64_t)min(k0 + row, sq.lk - 1) * a.k_tok; });
+    stage<D>(s + TB, [&](int row) { return vp + (int64_t)min(k0 + row, sq.lk - 1) * a.v_tok; });
+  };
+  if (nt > 0) issue(0);
+
+  i32x4 qf[NK];
+  const uint8_t* qp = a.Q + (int64_t)(sq.q0 + tok) * a.q_tok + (int64_t)head * a.q_head;
+#pragma unroll
+  for (int ks = 0; ks < NK; ++ks) qf[ks] = *reinterpret_cast<const i32x4*>(qp + 32 * ks + 16 * h);
+
+  f32x16 o[ND];
+#pragma unroll
+  for (int db = 0; db < ND; ++db) o[db] = splat(0.0f);
+  const float c = a.scale * kLog2e;
+  float m = -__builtin_inff(), l = 0.0f;      // running maximum (of c q.k), sum of exp2
+
+  for (int t = 0; t < nt; ++t) {
+    wait_vm<0>();
+    __syncthreads();
+    if (t + 1 < nt) issue(t + 1);
+    const lds_u8* kt = lds + (t & 1) * 2 * TB;
+    const lds_u8* vt = kt + TB;
+    const int k0 = kbeg + t * kKT;
+    if (!active || k0 > lim_hi) continue;
+    f32x16 s[2] = {splat(0.0f), splat(0.0f)};
+#pragma unroll
+    for (int ks = 0; ks < NK; ++ks) {
+      s[0] = mfma(read_straight<D>(kt, 0, ks), qf[ks], s[0]);
+      s[1] = mfma(read_straight<D>(kt, 32, ks), qf[ks], s[1]);
+    }
+    if (k0 + kKT - 1 > lim_lo) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = k0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3);
+          s[b][i] = j <= lim ? s[b][i] : -__builtin_inff();
+        }
+    }
+    float mx = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, fmaxf(s[0][i], s[1][i]));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * c;
+    if (__any(mx > m)) {
+      const float mn = fmaxf(m, mx);
+      const float f = exp2_fast(m - (mn == -__builtin_inff() ? 0.0f : mn));
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int db = 0; db < ND; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= f;
+    }
+    const float mu = m == -__builtin_inff() ? 0.0f : m;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[b][i] = exp2_fast(__builtin_fmaf(s[b][i], c, -mu));
+        l += s[b][i];
+      }
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      const i32x4 p = pack8(s[kk >> 1], 8 * (kk & 1));
+#pragma unroll
+      for (int db = 0; db < ND; ++db) o[db] = mfma(read_transposed<D>(vt, 16 * kk, db), p, o[db]);
+    }
+  }
+  l += __shfl_xor(l, 32, kWave);
+  if (r >= rows) return;
+  const bool none = l == 0.0f;               // a row that sees no key: zeros
+  const float inv = none ? 0.0f : 1.0f / l, lse2 = none ? -__builtin_inff() : m + __log2f(l);
+  const int64_t at = (int64_t)head * a.tq + sq.q0 + tok;
+  if (a.splits == 1) {
+    store_cols<ND>(a.O + (int64_t)(sq.q0 + tok) * a.o_tok + (int64_t)head * a.o_head, o, inv);
+    if (h == 0 && a.lse != nullptr) a.lse[at] = lse2 * kLn2;
+  } else {
+    const int64_t all = (int64_t)a.heads * a.tq;
+    if (h == 0) a.part_lse[split * all + at] = lse2;
+    if (!none) {
+      float* p = a.part + (split * all + at) * D;
+#pragma unroll
+      for (int db = 0; db < ND; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<f32x4*>(p + 32 * db + 8 * q + 4 * h) =
+              f32x4{o[db][4 * q] * inv, o[db][4 * q + 1] * inv, o[db][4 * q + 2] * inv, o[db][4 * q + 3] * inv};
+    }
+  }
+}
+
+// o = sum_s 2^(lse_s - lse) o_s over the splits of a row: one wave per row.
+template <int D>
+__global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t all = (int64_t)a.heads * a.tq;
+  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at >= all) return;
+  const int head = (int)(at / a.tq), tok = (int)(at - (int64_t)head * a.tq);
+  if (a.q_start != nullptr && (tok < a.q_start[0] || tok >= a.q_start[a.n_seq])) return;
+  float mx = -__builtin_inff();
+  for (int s = lane; s < a.splits; s += 64) mx = fmaxf(mx, a.part_lse[s * all + at]);
+  mx = wave_max(mx);
+  constexpr int E = D / 64;
+  float o[E] = {}, sum = 0.0f;
+  if (mx == -__builtin_inff()) mx = 0.0f;
+  for (int s = 0; s < a.splits; ++s) {
+    const float ls = a.part_lse[s * all + at];
+    if (ls == -__builtin_inff()) continue;        // (its o was not written)
+    const float f = exp2_fast(ls - mx);
+    sum += f;
+    const float* p = a.part + (s * all + at) * D + E * lane;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] += f * p[e];
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  uint8_t* op = a.O + (int64_t)tok * a.o_tok + (int64_t)head * a.o_head;
+  if constexpr (E == 2) *reinterpret_cast<uint32_t*>(op + 4 * lane) = pack_bf16x2(o[0] * inv, o[1] * inv);
+  else *reinterpret_cast<uint16_t*>(op + 2 * lane) = (uint16_t)f32_to_bf16_bits(o[0] * inv);
+  if (lane == 0 && a.lse != nullptr) a.lse[at] = sum == 0.0f ? -__builtin_inff() : (mx + __log2f(sum)) * kLn2;
+}
+
+// ------------------------------------------------------------------ backward
+// Per row, in row order [kv head][token * G + head in group]: -lse / c, from
+// which a score's accumulator starts (so that the product ends as
+// q.k - lse / c), and -do.o, from which do.v starts.  16 lanes per row.
+template <int D>
+__global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
+  const int64_t all = (int64_t)a.heads * a.tq;
+  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int i = threadIdx.x & 15;
+  if (row >= all) return;
+  const int64_t per = (int64_t)a.tq * a.group;
+  const int kvh = (int)(row / per);
+  const int64_t rr = row - kvh * per;
+  const int tok = (int)(rr / a.group), head = kvh * a.group + (int)(rr - (int64_t)tok * a.group);
+  float s = 0.0f;
+  const uint8_t* op = a.O + (int64_t)tok * a.o_tok + (int64_t)head * a.o_head;
+  const uint8_t* gp = a.dO + (int64_t)tok * a.do_tok + (int64_t)head * a.do_head;
+  constexpr int E = D / 16;      // values per lane: 8 or 4
+#pragma unroll
+  for (int e = 0; e < E / 4; ++e) {
+    const uint2 x = *reinterpret_cast<const uint2*>(op + 2 * E * i + 8 * e);
+    const uint2 y = *reinterpret_cast<const uint2*>(gp + 2 * E * i + 8 * e);
+    s += bf16_bits_to_f32(x.x & 0xFFFFu) * bf16_bits_to_f32(y.x & 0xFFFFu);
+    s += bf16_bits_to_f32(x.x >> 16) * bf16_bits_to_f32(y.x >> 16);
+    s += bf16_bits_to_f32(x.y & 0xFFFFu) * bf16_bits_to_f32(y.y & 0xFFFFu);
+    s += bf16_bits_to_f32(x.y >> 16) * bf16_bits_to_f32(y.y >> 16);
+  }
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) s += __shfl_xor(s, d, 16);
+  if (i == 0) {
+    a.neg_lse[row] = -a.lse[(int64_t)head * a.tq + tok] / a.scale;
+    a.neg_delta[row] = -s;
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
+  constexpr int NK = D / 16, ND = D / 32, TB = kKT * D * 2;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2][TB];
+  lds_u8* lds = (lds_u8*)&smem[0][0][0];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, h = lane >> 5;
+  const int id = xcd_order(blockIdx.x, gridDim.x);
+  const int kvh = id / a.row_tiles;
+  Seq sq;
+  if (!find_seq<false>(a, a.row_tiles - 1 - (id - kvh * a.row_tiles), sq)) return;
+  const int rows = sq.lq * a.group, r0 = sq.tile * kBM;
+  if (r0 >= rows) return;
+  const int off = sq.lk - sq.lq;
+  const int r = r0 + 32 * w + (lane & 31), rc = min(r, rows - 1);
+  const int tok = row_token(a, rc), head = kvh * a.group + (rc - tok * a.group);
+  const bool active = r0 + 32 * w < rows;
+  int kend = sq.lk;
+  if (a.causal) kend = min(kend, row_token(a, min(r0 + kBM, rows) - 1) + off + 1);
+  const int nt = kend > 0 ? (kend + kKT - 1) / kKT : 0;
+  const int lim = min(a.causal ? tok + off : sq.lk - 1, kend - 1);
+  const int lim_lo = __builtin_amdgcn_readlane(lim, 0), lim_hi = __builtin_amdgcn_readlane(lim, 31);
+
+  const uint8_t* kp = a.K + (int64_t)sq.k0 * a.k_tok + (int64_t)kvh * a.k_head;
+  const uint8_t* vp = a.V + (int64_t)sq.k0 * a.v_tok + (int64_t)kvh * a.v_head;
+  auto issue = [&](int t) {
+    lds_u8* s = lds + (t & 1) * 2 * TB;
+    stage<D>(s, [&](int row) { return kp + (int64_t)min(t * kKT + row, sq.lk - 1) * a.k_tok; });
+    stage<D>(s + TB, [&](int row) { return vp + (int64_t)min(t * kKT + row, sq.lk - 1) * a.v_tok; });
+  };
+  if (nt > 0) issue(0);
+  i32x4 qf[NK], gf[NK];
+  const uint8_t* qp = a.Q + (int64_t)(sq.q0 + tok) * a.q_tok + (int64_t)head * a.q_head;
+  const uint8_t* gp = a.dO + (int64_t)(sq.q0 + tok) * a.do_tok + (int64_t)head * a.do_head;
+#pragma unroll
+  for (int ks = 0; ks < NK; ++ks) {
+    qf[ks] = *reinterpret_cast<const i32x4*>(qp + 32 * ks + 16 * h);
+    gf[ks] = *reinterpret_cast<const i32x4*>(gp + 32 * ks + 16 * h);
+  }
+  const int64_t at = ((int64_t)kvh * a.tq + sq.q0) * a.group + rc;
+  const float nl = a.neg_lse[at], nd = a.neg_delta[at];
+  const float c = a.scale * kLog2e;
+  f32x16 dq[ND];
+#pragma unroll
+  for (int db = 0; db < ND; ++db) dq[db] = splat(0.0f);
+
+  for (int t = 0; t < nt; ++t) {
+    wait_vm<0>();
+    __syncthreads();
+    if (t + 1 < nt) issue(t + 1);
+    const lds_u8* kt = lds + (t & 1) * 2 * TB;
+    const lds_u8* vt = kt + TB;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int k0 = t * kKT + 32 * b;
+      if (!active || k0 > lim_hi) continue;
+      f32x16 s = splat(nl), g = splat(nd);
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks) {
+        s = mfma(read_straight<D>(kt, 32 * b, ks), qf[ks], s);
+        g = mfma(read_straight<D>(vt, 32 * b, ks), gf[ks], g);
+      }
+      if (k0 + 31 > lim_lo) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          g[i] = k0 + 8 * (i >> 2) + 4 * h + (i & 3) <= lim ? exp2_fast(s[i] * c) * g[i] : 0.0f;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) g[i] *= exp2_fast(s[i] * c);
+      }
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        const i32x4 p = pack8(g, 8 * kk);
+#pragma unroll
+        for (int db = 0; db < ND; ++db) dq[db] = mfma(read_transposed<D>(kt, 32 * b + 16 * kk, db), p, dq[db]);
+      }
+    }
+  }
+  if (r >= rows) return;
+  store_cols<ND>(a.dQ + (int64_t)(sq.q0 + tok) * a.dq_tok + (int64_t)head * a.dq_head, dq, a.scale);
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
+  constexpr int NK = D / 16, ND = D / 32, TB = kKT * D * 2;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2][TB];
+  __shared__ __attribute__((aligned(256))) float stat[2][2][kKT];     // -lse / c, -do.o
+  lds_u8* lds = (lds_u8*)&smem[0][0][0];
+  lds_u8* slds = (lds_u8*)&stat[0][0][0];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, h = lane >> 5;
+  const int id = xcd_order(blockIdx.x, gridDim.x);
+  const int kvh = id / a.key_tiles;
+  Seq sq;
+  // (first tiles first: under a causal mask the most rows see them)
+  if (!find_seq<true>(a, id - kvh * a.key_tiles, sq)) return;
+  const int k0 = sq.tile * kBM;
+  if (k0 >= sq.lk) return;
+  const int rows = sq.lq * a.group, off = sq.lk - sq.lq;
+  const int kw = k0 + 32 * w, j = kw + (lane & 31), jc = min(j, sq.lk - 1);
+  const bool active = kw < sq.lk;
+  // first row that sees a key of this block
+  const int rlo = a.causal ? max(0, k0 - off) * a.group : 0;
+  const int nt = rows > rlo ? (rows - rlo + kKT - 1) / kKT : 0;
+
+  const uint8_t* qp = a.Q + (int64_t)sq.q0 * a.q_tok + (int64_t)kvh * a.group * a.q_head;
+  const uint8_t* gp = a.dO + (int64_t)sq.q0 * a.do_tok + (int64_t)kvh * a.group * a.do_head;
+  const int64_t at = ((int64_t)kvh * a.tq + sq.q0) * a.group;
+  auto issue = [&](int t) {
+    lds_u8* s = lds + (t & 1) * 2 * TB;
+    const int r0 = rlo + t * kKT;
+    auto ptr = [&](const uint8_t* p, int64_t tok_s, int64_t head_s, int row) {
+      const int rc = min(r0 + row, rows - 1), tok = row_token(a, rc);
+      return p + tok * tok_s + (rc - tok * a.group) * head_s;
+    };
+    stage<D>(s, [&](int row) { return ptr(qp, a.q_tok, a.q_head, row); });
+    stage<D>(s + TB, [&](int row) { return ptr(gp, a.do_tok, a.do_head, row); });
+    if (w < 2) {
+      const float* sp = (w == 0 ? a.neg_lse : a.neg_delta) + at + min(r0 + lane, rows - 1);
+      dma4(reinterpret_cast<const uint8_t*>(sp), slds + ((t & 1) * 2 + w) * (kKT * 4));
+    }
+  };
+  if (nt > 0) issue(0);
+  i32x4 kf[NK], vf[NK];
+  const uint8_t* kp = a.K + (int64_t)(sq.k0 + jc) * a.k_tok + (int64_t)kvh * a.k_head;
+  const uint8_t* vp = a.V + (int64_t)(sq.k0 + jc) * a.v_tok + (int64_t)kvh * a.v_head;
+#pragma unroll
+  for (int ks = 0; ks < NK; ++ks) {
+    kf[ks] = *reinterpret_cast<const i32x4*>(kp + 32 * ks + 16 * h);
+    vf[ks] = *reinterpret_cast<const i32x4*>(vp + 32 * ks + 16 * h);
+  }
+  const float c = a.scale * kLog2e;
+  f32x16 dk[ND], dv[ND];
+#pragma unroll
+  for (int db = 0; db < ND; ++db) dk[db] = dv[db] = splat(0.0f);
+
+  for (int t = 0; t < nt; ++t) {
+    wait_vm<0>();
+    __syncthreads();
+    if (t + 1 < nt) issue(t + 1);
+    const lds_u8* qt = lds + (t & 1) * 2 * TB;
+    const lds_u8* gt = qt + TB;
+    const lds_u8* st = slds + (t & 1) * 2 * (kKT * 4);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int r0 = rlo + t * kKT + 32 * b;
+      if (!active || r0 >= rows) continue;
+      // last key that the last row of these 32 sees; and the first row
+      if (a.causal && row_token(a, min(r0 + 31, rows - 1)) + off < kw) continue;
+      const bool whole = r0 + 31 < rows && kw + 31 < sq.lk && (!a.causal || kw + 31 <= row_token(a, r0) + off);
+      f32x16 s, g;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 x = *(const lds_f32x4*)(st + 4 * (32 * b + 8 * q + 4 * h));
+        const f32x4 y = *(const lds_f32x4*)(st + 4 * (kKT + 32 * b + 8 * q + 4 * h));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { s[4 * q + e] = x[e]; g[4 * q + e] = y[e]; }
+      }
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks) {
+        s = mfma(read_straight<D>(qt, 32 * b, ks), kf[ks], s);
+        g = mfma(read_straight<D>(gt, 32 * b, ks), vf[ks], g);
+      }
+      if (whole) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { s[i] = exp2_fast(s[i] * c); g[i] *= s[i]; }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int r = r0 + 8 * (i >> 2) + 4 * h + (i & 3);
+          const bool see = r < rows && j < sq.lk && (!a.causal || j <= row_token(a, min(r, rows - 1)) + off);
+          s[i] = see ? exp2_fast(s[i] * c) : 0.0f;
+          g[i] = see ? g[i] * s[i] : 0.0f;
+        }
+      }
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        const i32x4 p = pack8(s, 8 * kk), ds = pack8(g, 8 * kk);
+#pragma unroll
+        for (int db = 0; db < ND; ++db) {
+          dv[db] = mfma(read_transposed<D>(gt, 32 * b + 16 * kk, db), p, dv[db]);
+          dk[db] = mfma(read_transposed<D>(qt, 32 * b + 16 * kk, db), ds, dk[db]);
+        }
+      }
+    }
+  }
+  if (j >= sq.lk) return;
+  store_cols<ND>(a.dK + (int64_t)(sq.k0 + j) * a.dk_tok + (int64_t)kvh * a.dk_head, dk, a.scale);
+  store_cols<ND>(a.dV + (int64_t)(sq.k0 + j) * a.dv_tok + (int64_t)kvh * a.dv_head, dv, 1.0f);
+}
+
+}  // namespace
+
+// Tiles of all sequences at most: see find_seq.
+int64_t attn_row_tiles(int64_t tokens, int64_t mul, int64_t n_seq) { return tokens * mul / kBM + n_seq; }
+
+// Splits of the keys: few rows over many keys leave the chip empty, so the
+// keys are divided until there are about 8 blocks per CU, with at least 128
+// keys each on average.
+int attn_splits(int64_t tq, int64_t tk, int64_t n_seq, int heads, int kv_heads) {
+  const int64_t blocks = attn_row_tiles(tq, heads / kv_heads, n_seq) * kv_heads;
+  if (blocks >= 1024) return 1;
+  const int64_t want = (2048 + blocks - 1) / blocks, most = tk / n_seq / 128;
+  const int64_t s = want < most ? want : most;
+  return s < 1 ? 1 : (int)s;
+}
+
+hipError_t launch_attn_fwd(int d, AttnArgs a, hipStream_t stream) {
+  const dim3 grid((unsigned)((int64_t)a.row_tiles * a.splits * a.kv_heads)), block(256);
+  LaunchStatus st;
+  st << launch_kernel(d == 128 ? attn_fwd_kernel<128> : attn_fwd_kernel<64>, grid, block, stream, a);
+  if (a.splits > 1)
+    st << launch_kernel(d == 128 ? attn_combine_kernel<128> : attn_combine_kernel<64>,
+                        dim3((unsigned)(((int64_t)a.heads * a.tq + 3) / 4)), block, stream, a);
+  return st.e;
+}
+
+hipError_t launch_attn_bwd(int d, AttnArgs a, hipStream_t stream) {
+  const dim3 block(256);
+  LaunchStatus st;
+  if (a.tq > 0) {
+    st << launch_kernel(d == 128 ? attn_delta_kernel<128> : attn_delta_kernel<64>,
+                        dim3((unsigned)(((int64_t)a.heads * a.tq + 15) / 16)), block, stream, a);
+    st << launch_kernel(d == 128 ? attn_dq_kernel<128> : attn_dq_kernel<64>,
+                        dim3((unsigned)((int64_t)a.row_tiles * a.kv_heads)), block, stream, a);
+  }
+  if (a.tk > 0)
+    st << launch_kernel(d == 128 ? attn_dkv_kernel<128> : attn_dkv_kernel<64>,
+                        dim3((unsigned)((int64_t)a.key_tiles * a.kv_heads)), block, stream, a);
+  return st.e;
+}
+
+}  // namespace dqt

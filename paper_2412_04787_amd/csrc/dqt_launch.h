@@ -262,6 +262,65 @@ struct AdamHyper {
 hipError_t launch_adamw_sr(int cf, int n, const AdamTensor* t, const AdamHyper& hp,
                            uint64_t seed, uint32_t step, unsigned long long* counters,
                            hipStream_t stream);
+// Attention (attn.hip).  Strides in bytes.
+struct AttnArgs {
+  const uint8_t *Q, *K, *V, *dO;
+  uint8_t *O, *dQ, *dK, *dV;
+  float* lse;                  // [heads, tq]
+  int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head, do_tok, do_head;
+  int64_t dq_tok, dq_head, dk_tok, dk_head, dv_tok, dv_head;
+  const int32_t *q_start, *k_start;   // [n_seq + 1], or null: one sequence of all tokens
+  int tq, tk, n_seq, heads, kv_heads, group;
+  uint32_t gmul;               // r / group = umulhi(r, gmul) >> gshift (group > 1, r < 2^31)
+  int gshift;
+  float scale;
+  int causal;
+  int row_tiles, key_tiles;    // tiles of all sequences at most
+  int splits;                  // of the keys, forward
+  float *part, *part_lse;      // [splits, heads, tq, d], [splits, heads, tq]
+  float *neg_lse, *neg_delta;  // [kv_heads, tq * group]
+};
+int64_t attn_row_tiles(int64_t tokens, int64_t mul, int64_t n_seq);
+int attn_splits(int64_t tq, int64_t tk, int64_t n_seq, int heads, int kv_heads);
+hipError_t launch_attn_fwd(int d, AttnArgs a, hipStream_t stream);
+hipError_t launch_attn_bwd(int d, AttnArgs a, hipStream_t stream);
+
+// silu(G) * U and its 8-bit codes; with a checkpoint (Gq != null), the 8-bit
+// codes and scales of G and U.
+constexpr int kCkptGroup = 128;      // consecutive elements that share a scale
+struct Ckpt {
+  int8_t *Gq, *Uq;             // [M, K]
+  float *gs, *us;              // [M, ceil(K / kCkptGroup)]
+};
+hipError_t launch_swiglu_act_quant(const void* G, const void* U, bool x_bf16, int64_t M, int K, bool e4m3, void* Xq,
+                                   float* xdq, const Ckpt& ckpt, hipStream_t stream);
+// from G and U (ckpt.Gq == null) or from their checkpoint
+hipError_t launch_swiglu_backward(const void* dH, bool h_bf16, const void* G, const void* U, const Ckpt& ckpt, int64_t M,
+                                  int K, void* dG, void* dU, hipStream_t stream);
+
+// Log probabilities (logprob.hip).
+constexpr int kMaxTop = 32;
+struct LogprobArgs {
+  const void* x;               // logits [M, V], stride elements per row
+  int64_t stride, M;
+  int V;
+  const int64_t* targets;      // [M], nullable
+  float *logp, *lse, *entropy; // [M], nullable
+  float* stat;                 // [M, 2], nullable in the forward: maximum, log of the sum relative to it
+  int64_t* top_ids;            // [M, top]
+  float* top_logp;             // [M, top]
+  int top;
+  int splits;                  // blocks per row
+  float* part;                 // [M, splits, 4]: maximum, sum, weighted sum
+  uint64_t* part_top;          // [M, splits, top]
+  // gradient
+  const float *dlogp, *dent;   // [M], nullable
+  void* dx;
+  int64_t dx_stride;
+};
+int logprob_splits(int64_t M, int V);
+hipError_t launch_logprob_fwd(const LogprobArgs& a, bool bf16, hipStream_t stream);
+hipError_t launch_logprob_bwd(const LogprobArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_debug_rng(uint64_t seed, uint32_t step, uint32_t tensor_id, uint64_t i0,
                             int64_t n, uint32_t* out, hipStream_t stream);
 

@@ -1,0 +1,224 @@
+// The SwiGLU product of a LLaMA block and its 8-bit quantisation, in one
+// launch, and its backward from 8-bit checkpoints of its inputs:
+//   h = (g / (1 + exp(-g))) u,  m_row = max(max_k |h|, 1e-5)
+//   Xq = quantise(h fl(Q / m_row)), xdq = fl(m_row / Q)      (Q = 127 or 448)
+//   checkpoint of g and of u: groups of 128 consecutive elements of a row,
+//     a = max(max |x|, 1e-5), code = clamp(rint(x fl(127 / a))), scale = fl(a / 127)
+//   backward, with s = 1 / (1 + exp(-g)):
+//     dU = dH (g s),  dG = dH u s (1 + g (1 - s))
+// The forward's operations are correctly rounded fp32 (the exponential the
+// device library's), so codes and scales do not depend on how rows are spread
+// over threads.
+//
+// Forward: a block per row; h stays in registers between the row's maximum
+// and the codes (rows of up to 8 chunks of 8 elements per thread; longer ones
+// form h twice, from cache).  A checkpoint group is 16 neighbouring lanes.
+// HBM traffic per element (bf16): 4 bytes read, 1 written, 2 more with the
+// checkpoint; bound by it.
+// Backward: 8 elements per thread, 8 bytes of traffic per element (bf16 dH,
+// dG and dU, checkpoint); bound by it.
+#include "dqt_launch.h"
+
+namespace dqt {
+
+namespace {
+
+template <typename TX>
+__device__ __forceinline__ void load8(const TX* p, float (&v)[8]) {
+  if constexpr (sizeof(TX) == 2) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = bf16_bits_to_f32(w[i] & 0xFFFFu);
+      v[2 * i + 1] = bf16_bits_to_f32(w[i] >> 16);
+    }
+  } else {
+    const float4 a = *reinterpret_cast<const float4*>(p);
+    const float4 b = *reinterpret_cast<const float4*>(p + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+}
+template <typename TX>
+__device__ __forceinline__ void store8(TX* p, const float (&v)[8]) {
+  if constexpr (sizeof(TX) == 2) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                              pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+  } else {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  }
+}
+__device__ __forceinline__ float silu_mul(float g, float u) { return __fdiv_rn(g, 1.0f + expf(-g)) * u; }
+
+// The 8-bit checkpoint of 8 elements of a group held by 16 neighbouring lanes.
+__device__ __forceinline__ void ckpt8(const float (&v)[8], bool in, int8_t* q, float* scale) {
+  float a = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) a = fmaxf(a, fabsf(v[j]));
+  a = in ? a : 0.0f;
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) a = fmaxf(a, __shfl_xor(a, d, 16));
+  a = fmaxf(a, 1e-5f);
+  const float inv = __fdiv_rn(127.0f, a);
+  if (!in) return;
+  *reinterpret_cast<uint2*>(q) = make_uint2(f32x4_to_i8x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                                            f32x4_to_i8x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
+  if ((threadIdx.x & 15) == 0) *scale = __fdiv_rn(a, 127.0f);
+}
+
+// NCH chunks of 8 elements per thread in registers; NCH = 0: any row length.
+template <typename TX, bool E4M3, bool CKPT, int T, int NCH>
+__global__ __launch_bounds__(T) void swiglu_quant_kernel(const TX* __restrict__ G, const TX* __restrict__ U, int64_t M,
+                                                         int K, uint8_t* __restrict__ Xq, float* __restrict__ xdq,
+                                                         Ckpt ck) {
+  __shared__ float wmax[2][T / kWave];
+  const int nchunk = K / 8, ngroup = (K + kCkptGroup - 1) / kCkptGroup;
+  constexpr float qmax = E4M3 ? 448.0f : 127.0f;
+  int flip = 0;
+  for (int64_t row = blockIdx.x; row < M; row += gridDim.x, flip ^= 1) {
+    const TX* gr = G + row * (int64_t)K;
+    const TX* ur = U + row * (int64_t)K;
+    float hv[NCH > 0 ? NCH : 1][8];
+    float amax = 0.0f;
+    auto chunk = [&](int c, float (&hh)[8]) {
+      // (lanes without a chunk load the last one and do not use it)
+      const bool in = c < nchunk;
+      const int cc = in ? c : nchunk - 1;
+      float g[8], u[8];
+      load8(gr + 8 * cc, g);
+      load8(ur + 8 * cc, u);
+      float m = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        hh[j] = silu_mul(g[j], u[j]);
+        m = fmaxf(m, fabsf(hh[j]));
+      }
+      amax = in ? fmaxf(amax, m) : amax;
+      if constexpr (CKPT) {
+        const int64_t sg = row * ngroup + cc / 16;
+        ckpt8(g, in, ck.Gq + row * (int64_t)K + 8 * cc, ck.gs + sg);
+        ckpt8(u, in, ck.Uq + row * (int64_t)K + 8 * cc, ck.us + sg);
+      }
+    };
+    auto codes = [&](int c, const float (&hh)[8], float inv) {
+      if (c >= nchunk) return;
+      uint32_t w0, w1;
+      if constexpr (E4M3) {
+        w0 = f32x4_to_e4m3x4(hh[0] * inv, hh[1] * inv, hh[2] * inv, hh[3] * inv);
+        w1 = f32x4_to_e4m3x4(hh[4] * inv, hh[5] * inv, hh[6] * inv, hh[7] * inv);
+      } else {
+        w0 = f32x4_to_i8x4(hh[0] * inv, hh[1] * inv, hh[2] * inv, hh[3] * inv);
+        w1 = f32x4_to_i8x4(hh[4] * inv, hh[5] * inv, hh[6] * inv, hh[7] * inv);
+      }
+      *reinterpret_cast<uint2*>(Xq + row * (int64_t)K + 8 * c) = make_uint2(w0, w1);
+    };
+    if constexpr (NCH > 0) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) chunk(i * T + threadIdx.x, hv[i]);
+    } else {
+      for (int b = 0; b < nchunk; b += T) chunk(b + threadIdx.x, hv[0]);
+    }
+    amax = wave_max(amax);
+    if ((threadIdx.x & (kWave - 1)) == 0) wmax[flip][threadIdx.x / kWave] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < T / kWave; ++w) amax = fmaxf(amax, wmax[flip][w]);
+    amax = fmaxf(amax, 1e-5f);
+    const float inv = __fdiv_rn(qmax, amax);
+    if (threadIdx.x == 0) xdq[row] = __fdiv_rn(amax, qmax);
+    if constexpr (NCH > 0) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) codes(i * T + threadIdx.x, hv[i], inv);
+    } else {
+      for (int c = threadIdx.x; c < nchunk; c += T) {
+        float g[8], u[8];
+        load8(gr + 8 * c, g);
+        load8(ur + 8 * c, u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) hv[0][j] = silu_mul(g[j], u[j]);
+        codes(c, hv[0], inv);
+      }
+    }
+  }
+}
+
+template <typename TX, bool E4M3, bool CKPT>
+hipError_t launch_fwd(const TX* g, const TX* u, int64_t M, int K, uint8_t* q, float* xdq, const Ckpt& ck, hipStream_t s) {
+  const int nchunk = K / 8;
+  const dim3 grid((unsigned)(M < 65536 ? M : 65536));
+  auto go = [&](auto kernel, int t) { return launch_kernel(kernel, grid, dim3(t), s, g, u, M, K, q, xdq, ck); };
+  if (nchunk <= 256) return go(swiglu_quant_kernel<TX, E4M3, CKPT, 256, 1>, 256);
+  if (nchunk <= 512) return go(swiglu_quant_kernel<TX, E4M3, CKPT, 256, 2>, 256);
+  if (nchunk <= 768) return go(swiglu_quant_kernel<TX, E4M3, CKPT, 256, 3>, 256);
+  if (nchunk <= 1024) return go(swiglu_quant_kernel<TX, E4M3, CKPT, 512, 2>, 512);
+  if (nchunk <= 1536) return go(swiglu_quant_kernel<TX, E4M3, CKPT, 512, 3>, 512);
+  if (nchunk <= 2048) return go(swiglu_quant_kernel<TX, E4M3, CKPT, 512, 4>, 512);
+  return go(swiglu_quant_kernel<TX, E4M3, CKPT, 512, 0>, 512);
+}
+
+template <typename TH, bool CKPT>
+__global__ __launch_bounds__(256) void swiglu_bwd_kernel(const TH* __restrict__ dH, const TH* __restrict__ G,
+                                                         const TH* __restrict__ U, Ckpt ck, uint32_t n, uint32_t nchunk,
+                                                         TH* __restrict__ dG, TH* __restrict__ dU) {
+  const uint32_t ngroup = (nchunk + 15) / 16;
+  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
+    float d[8], g[8], u[8], og[8], ou[8];
+    load8(dH + 8 * i, d);
+    if constexpr (CKPT) {
+      const uint32_t row = (uint32_t)i / nchunk, c = (uint32_t)i - row * nchunk;
+      const uint64_t sg = (uint64_t)row * ngroup + c / 16;
+      const float a = ck.gs[sg], b = ck.us[sg];
+      const uint2 x = *reinterpret_cast<const uint2*>(ck.Gq + 8 * i), y = *reinterpret_cast<const uint2*>(ck.Uq + 8 * i);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        g[j] = (float)(int8_t)((j < 4 ? x.x : x.y) >> (8 * (j & 3))) * a;
+        u[j] = (float)(int8_t)((j < 4 ? y.x : y.y) >> (8 * (j & 3))) * b;
+      }
+    } else {
+      load8(G + 8 * i, g);
+      load8(U + 8 * i, u);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float s = __builtin_amdgcn_rcpf(1.0f + expf(-g[j]));    // (within one unit in the last place)
+      ou[j] = d[j] * (g[j] * s);
+      og[j] = d[j] * u[j] * (s * (1.0f + g[j] * (1.0f - s)));
+    }
+    store8(dG + 8 * i, og);
+    store8(dU + 8 * i, ou);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_swiglu_act_quant(const void* G, const void* U, bool x_bf16, int64_t M, int K, bool e4m3, void* Xq,
+                                   float* xdq, const Ckpt& ck, hipStream_t s) {
+  uint8_t* q = static_cast<uint8_t*>(Xq);
+  const bool c = ck.Gq != nullptr;
+  auto go = [&](auto t) {
+    using TX = decltype(t);
+    const TX* g = static_cast<const TX*>(G);
+    const TX* u = static_cast<const TX*>(U);
+    if (e4m3) return c ? launch_fwd<TX, true, true>(g, u, M, K, q, xdq, ck, s) : launch_fwd<TX, true, false>(g, u, M, K, q, xdq, ck, s);
+    return c ? launch_fwd<TX, false, true>(g, u, M, K, q, xdq, ck, s) : launch_fwd<TX, false, false>(g, u, M, K, q, xdq, ck, s);
+  };
+  return x_bf16 ? go(uint16_t{}) : go(float{});
+}
+
+hipError_t launch_swiglu_backward(const void* dH, bool h_bf16, const void* G, const void* U, const Ckpt& ck, int64_t M,
+                                  int K, void* dG, void* dU, hipStream_t s) {
+  const uint32_t nchunk = K / 8, n = (uint32_t)(M * nchunk);
+  const uint32_t blocks = n / 256 + (n % 256 != 0);
+  const dim3 grid(blocks < (1u << 20) ? blocks : 1u << 20), block(256);
+  auto go = [&](auto t) {
+    using TH = decltype(t);
+    auto* k = ck.Gq != nullptr ? swiglu_bwd_kernel<TH, true> : swiglu_bwd_kernel<TH, false>;
+    return launch_kernel(k, grid, block, s, static_cast<const TH*>(dH), static_cast<const TH*>(G),
+                         static_cast<const TH*>(U), ck, n, nchunk, static_cast<TH*>(dG), static_cast<TH*>(dU));
+  };
+  return h_bf16 ? go(uint16_t{}) : go(float{});
+}
+
+}  // namespace dqt

@@ -31,7 +31,9 @@ EXPORTS = (
     "dqt_update_variant_workspace", "dqt_update_variant_batch",
     "dqt_sr_update", "dqt_debug_rng", "dqt_absmean_init", "dqt_pack_ternary",
     "dqt_unpack_ternary", "dqt_pack_int4", "dqt_unpack_int4", "dqt_pack_int3", "dqt_unpack_int3", "dqt_launch_timer_start", "dqt_launch_timer_stop", "dqt_read_stream",
-    "dqt_status_string", "dqt_version",
+    "dqt_swiglu_act_quant", "dqt_swiglu_backward", "dqt_logprob_workspace", "dqt_logprob_fwd",
+    "dqt_logprob_bwd", "dqt_attn_fwd_workspace", "dqt_attn_fwd", "dqt_attn_bwd_workspace",
+    "dqt_attn_bwd", "dqt_status_string", "dqt_version",
 )
 
 
@@ -59,6 +61,23 @@ class DqtActIO(ctypes.Structure):
                 ("K", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class DqtCkptIO(ctypes.Structure):
+    _fields_ = [("Gq", ctypes.c_void_p), ("Uq", ctypes.c_void_p), ("gs", ctypes.c_void_p),
+                ("us", ctypes.c_void_p)]
+
+
+class DqtAttn(ctypes.Structure):
+    _fields_ = [("q_start", ctypes.c_void_p), ("k_start", ctypes.c_void_p),
+                ("q_tokens", ctypes.c_int64), ("k_tokens", ctypes.c_int64),
+                ("n_seq", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("scale", ctypes.c_float), ("causal", ctypes.c_int32),
+                ("reserved", ctypes.c_int64)]
+
+
+class DqtRows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
 def weight(d_out: int, d_in: int, wfmt: int, qmin: int, qmax: int, alpha: float,
            tensor_id: int = 0) -> DqtWeight:
     return DqtWeight(d_out, d_in, wfmt, qmin, qmax, float(alpha), tensor_id, 0)
@@ -81,6 +100,16 @@ _SIGS = {
     "dqt_act_quant_batch": (_i32, [_i32, _vp, _i32, _i64, _i32, _vp]),
     "dqt_rmsnorm_act_quant": (_i32, [_vp, _i32, _vp, _f32, _i64, _i32, _i32, _vp, _vp, _vp, _vp]),
     "dqt_rmsnorm_backward": (_i32, [_i32, _vp, _vp, _i32, _vp, _vp, _i64, _i32, _vp, _vp, _i32, _vp]),
+    "dqt_swiglu_act_quant": (_i32, [_vp, _vp, _i32, _i64, _i32, _i32, _vp, _vp, _vp, _vp]),
+    "dqt_swiglu_backward": (_i32, [_vp, _i32, _vp, _vp, _vp, _i64, _i32, _vp, _vp, _vp]),
+    "dqt_logprob_workspace": (ctypes.c_size_t, [_i64, _i32, _i32]),
+    "dqt_logprob_fwd": (_i32, [_vp, _i32, _i64, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp,
+                               _vp, ctypes.c_size_t, _vp]),
+    "dqt_logprob_bwd": (_i32, [_vp, _i32, _i64, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "dqt_attn_fwd_workspace": (ctypes.c_size_t, [_vp]),
+    "dqt_attn_fwd": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "dqt_attn_bwd_workspace": (ctypes.c_size_t, [_vp]),
+    "dqt_attn_bwd": (_i32, [_vp] * 11 + [ctypes.c_size_t, _vp]),
     "dqt_linear_fwd_workspace": (ctypes.c_size_t, [_wp]),
     "dqt_linear_fwd": (_i32, [_wp, _vp, _vp, _i32, _i64, _i32, _vp, _vp, _vp, _i32, _vp,
                               ctypes.c_size_t, _vp]),
@@ -164,6 +193,23 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _same(*ts):
+    """The shape [M, K] that contiguous tensors of one dtype share."""
+    for t in ts:
+        if t.shape != ts[0].shape or t.dtype != ts[0].dtype or not t.is_contiguous():
+            raise ValueError("expected contiguous tensors of one shape and dtype")
+    return ts[0].shape
+
+
+def _unit_stride(t):
+    if t.dim() != 2 or (t.stride(1) != 1 and t.numel() > 0 and t.shape[1] > 1):
+        raise ValueError("expected a [rows, columns] tensor with unit column stride")
+
+
 def _stream(stream=None):
     """The stream's handle; without one, that of torch's current stream on the
     current device.  (Asked for directly: building the Stream object of
@@ -204,6 +250,142 @@ def dqt_rmsnorm_backward(dYs, X, gamma, rinv, dX, gpart, stream=None):
            load().dqt_rmsnorm_backward(len(dYs), ptrs, _ptr(X), dtype_code(X), _ptr(gamma),
                                        _ptr(rinv), M, K, _ptr(dX), _ptr(gpart), gpart.shape[0],
                                        _stream(stream)))
+
+
+CKPT_GROUP = 128
+
+
+class SwigluCkpt:
+    """8-bit checkpoint of gate and up [M, K]: codes Gq, Uq (int8) and scales
+    gs, us (fp32, one for CKPT_GROUP consecutive elements of a row)."""
+
+    def __init__(self, Gq, Uq, gs, us):
+        self.Gq, self.Uq, self.gs, self.us = Gq, Uq, gs, us
+        self.io = DqtCkptIO(_addr(Gq), _addr(Uq), _addr(gs), _addr(us))
+
+
+def swiglu_ckpt(M: int, K: int, device="cuda:0") -> SwigluCkpt:
+    """Buffers for the checkpoint of a gate and an up of shape [M, K]."""
+    torch = _torch()
+    groups = (K + CKPT_GROUP - 1) // CKPT_GROUP
+    q = [torch.empty((M, K), dtype=torch.int8, device=device) for _ in range(2)]
+    s = [torch.empty((M, groups), dtype=torch.float32, device=device) for _ in range(2)]
+    return SwigluCkpt(*q, *s)
+
+
+def dqt_swiglu_act_quant(G, U, act_q: int, Xq, xdq, ckpt: SwigluCkpt | None = None, stream=None):
+    """G, U: contiguous [M, K] of one dtype."""
+    M, K = _same(G, U)
+    _check("dqt_swiglu_act_quant",
+           load().dqt_swiglu_act_quant(_ptr(G), _ptr(U), dtype_code(G), M, K, act_q, _ptr(Xq), _ptr(xdq),
+                                       None if ckpt is None else ctypes.byref(ckpt.io), _stream(stream)))
+
+
+def dqt_swiglu_backward(dH, G, U, dG, dU, stream=None):
+    """dH, G, U, dG, dU: contiguous [M, K] of one dtype."""
+    M, K = _same(dH, G, U, dG, dU)
+    _check("dqt_swiglu_backward",
+           load().dqt_swiglu_backward(_ptr(dH), dtype_code(dH), _ptr(G), _ptr(U), None, M, K, _ptr(dG),
+                                      _ptr(dU), _stream(stream)))
+
+
+def dqt_swiglu_backward_ckpt(dH, ckpt: SwigluCkpt, dG, dU, stream=None):
+    """dqt_swiglu_backward with gate and up from their 8-bit checkpoint."""
+    M, K = _same(dH, dG, dU)
+    _check("dqt_swiglu_backward",
+           load().dqt_swiglu_backward(_ptr(dH), dtype_code(dH), None, None, ctypes.byref(ckpt.io), M, K,
+                                      _ptr(dG), _ptr(dU), _stream(stream)))
+
+
+MAX_TOP = 32
+
+
+def dqt_logprob_workspace(M: int, V: int, top_k: int = 0) -> int:
+    return int(load().dqt_logprob_workspace(M, V, top_k))
+
+
+def dqt_logprob_fwd(X, targets, logp, lse=None, entropy=None, stat=None, top_ids=None, top_logp=None,
+                    ws=None, stream=None):
+    """X: [M, V] logits, rows of any stride; targets: int64 [M]; logp, lse,
+    entropy: fp32 [M], stat (for the backward): fp32 [M, 2], or None; top_ids (int64) and top_logp (fp32): [M, k],
+    or None."""
+    M, V = X.shape
+    _unit_stride(X)
+    top_k = 0 if top_ids is None else top_ids.shape[1]
+    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check("dqt_logprob_fwd",
+           load().dqt_logprob_fwd(_ptr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _ptr(targets),
+                                  _ptr(logp), _ptr(lse), _ptr(entropy), _ptr(stat), top_k,
+                                  _ptr(top_ids), _ptr(top_logp), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def dqt_logprob_bwd(X, targets, stat, dlogp, dX, entropy=None, dent=None, stream=None):
+    """dX: [M, V] of X's dtype (X itself is allowed); dlogp, dent: fp32 [M] or None."""
+    M, V = X.shape
+    _unit_stride(X)
+    _unit_stride(dX)
+    if dX.dtype != X.dtype or dX.shape != X.shape:
+        raise ValueError("dX must have X's dtype and shape")
+    _check("dqt_logprob_bwd",
+           load().dqt_logprob_bwd(_ptr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _ptr(targets),
+                                  _ptr(stat), _ptr(entropy), _ptr(dlogp), _ptr(dent), _ptr(dX),
+                                  dX.stride(0) if M > 1 else V, _stream(stream)))
+
+
+def attn(q_tokens: int, k_tokens: int, heads: int, kv_heads: int, d: int, q_start=None, k_start=None,
+         scale: float | None = None, causal: bool = True) -> DqtAttn:
+    """The descriptor of an attention call.  q_start, k_start: device int32
+    [n_seq + 1] (kept alive on the descriptor), or None for one sequence of
+    all tokens; scale: 1 / sqrt(d) by default."""
+    n = {t.numel() - 1 for t in (q_start, k_start) if t is not None} or {1}
+    if len(n) != 1:
+        raise ValueError("q_start and k_start must have the same length")
+    for t in (q_start, k_start):
+        if t is not None and (t.dtype != _torch().int32 or not t.is_contiguous()):
+            raise ValueError("q_start and k_start must be contiguous int32")
+    a = DqtAttn(_addr(q_start), _addr(k_start), q_tokens, k_tokens, n.pop(), heads, kv_heads, d,
+                d ** -0.5 if scale is None else scale, int(causal), 0)
+    a._keep = (q_start, k_start)
+    return a
+
+
+def _rows(t, tokens: int, heads: int, d: int):
+    """[tokens, heads, d] bf16 tensor (any token and head strides) -> dqt_rows."""
+    if t.dtype != _torch().bfloat16:
+        raise ValueError("attention takes bfloat16 tensors")
+    if tuple(t.shape) != (tokens, heads, d) or (t.stride(2) != 1 and t.numel() > 0):
+        raise ValueError(f"expected a [{tokens}, {heads}, {d}] tensor with unit last stride, got "
+                         f"{tuple(t.shape)} with strides {t.stride()}")
+    # (strides of a dimension of one do not matter)
+    return DqtRows(t.data_ptr(), t.stride(0) if tokens > 1 else heads * d, t.stride(1) if heads > 1 else d)
+
+
+def dqt_attn_fwd_workspace(a: DqtAttn) -> int:
+    return int(load().dqt_attn_fwd_workspace(ctypes.byref(a)))
+
+
+def dqt_attn_fwd(a: DqtAttn, Q, K, V, O, lse=None, ws=None, stream=None):
+    """Q, O: [q_tokens, heads, d]; K, V: [k_tokens, kv_heads, d], bf16 with any
+    token and head strides; lse: fp32 [heads, q_tokens] or None."""
+    qs, ks = (a.q_tokens, a.heads, a.d), (a.k_tokens, a.kv_heads, a.d)
+    r = [_rows(Q, *qs), _rows(K, *ks), _rows(V, *ks), _rows(O, *qs)]
+    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check("dqt_attn_fwd", load().dqt_attn_fwd(ctypes.byref(a), *map(ctypes.byref, r), _ptr(lse), _ptr(ws),
+                                               ws_bytes, _stream(stream)))
+
+
+def dqt_attn_bwd_workspace(a: DqtAttn) -> int:
+    return int(load().dqt_attn_bwd_workspace(ctypes.byref(a)))
+
+
+def dqt_attn_bwd(a: DqtAttn, Q, K, V, O, lse, dO, dQ, dK, dV, ws, stream=None):
+    """Shapes as dqt_attn_fwd; dO, dQ like Q, dK and dV like K."""
+    qs, ks = (a.q_tokens, a.heads, a.d), (a.k_tokens, a.kv_heads, a.d)
+    f = [_rows(Q, *qs), _rows(K, *ks), _rows(V, *ks), _rows(O, *qs)]
+    b = [_rows(dO, *qs), _rows(dQ, *qs), _rows(dK, *ks), _rows(dV, *ks)]
+    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check("dqt_attn_bwd", load().dqt_attn_bwd(ctypes.byref(a), *map(ctypes.byref, f), _ptr(lse),
+                                               *map(ctypes.byref, b), _ptr(ws), ws_bytes, _stream(stream)))
 
 
 def dqt_linear_fwd_workspace(w: DqtWeight) -> int:

@@ -1,0 +1,267 @@
+"""Attention over packed sequences (dqt_attn_fwd, dqt_attn_bwd) against a plain
+float64 implementation: head layouts, lengths from zero to thousands, rows that
+see nothing, strides, tokens outside every sequence; the gradients also against
+differences."""
+import numpy as np
+import pytest
+import torch
+
+import op_reference as R
+from gpu_util import DEV, log
+from paper_2412_04787_amd import dqt
+
+pytestmark = pytest.mark.gpu
+
+SENT = 1.25e4          # what outputs hold before a call
+
+
+def starts(lens, first=0):
+    return np.concatenate([[0], np.cumsum(lens)]).astype(np.int64) + first
+
+
+def tensors(gen, tokens, heads, d, layout, std=1.0):
+    """A [tokens, heads, d] bf16 view: contiguous, head-major, or a slice of a
+    wider buffer."""
+    x = (torch.randn((tokens, heads, d), generator=gen) * std).to(torch.bfloat16)
+    if layout == "heads":
+        buf = x.permute(1, 0, 2).contiguous().to(DEV)
+        return x, buf.permute(1, 0, 2)
+    if layout == "wide":
+        buf = torch.full((tokens, 3, heads + 1, d + 8), 7.0, dtype=torch.bfloat16)
+        buf[:, 1, :heads, :d] = x
+        return x, buf.to(DEV)[:, 1, :heads, :d]
+    return x, x.to(DEV)
+
+
+def like(view):
+    """An output with a view's strides, filled with SENT."""
+    n = 1 + sum((s - 1) * st for s, st in zip(view.shape, view.stride()))
+    return torch.full((n,), SENT, dtype=torch.bfloat16, device=DEV).as_strided(view.shape, view.stride())
+
+
+def close(name, got, ref, tol):
+    got = got.detach().double().cpu()
+    bad = ~((got - ref).abs() <= tol + 1e-30)
+    bad &= ~((got == ref) & torch.isinf(ref))
+    assert not bad.any(), (name, int(bad.sum()), tuple(bad.nonzero()[0].tolist()), float((got - ref).abs().max()))
+
+
+def run(d, heads, kvh, lq, lk, causal=True, layout="plain", scale=None, train=True, seed=0, before=0, behind=0, std=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    qs, ks = starts(lq, before), starts(lk, before)
+    tq, tk = int(qs[-1]) + behind, int(ks[-1]) + behind
+    Q, Qd = tensors(gen, tq, heads, d, layout, std)
+    K, Kd = tensors(gen, tk, kvh, d, layout)
+    V, Vd = tensors(gen, tk, kvh, d, layout)
+    dO, dOd = tensors(gen, tq, heads, d, layout, 1e-2)
+    dev32 = lambda s: torch.from_numpy(s.astype(np.int32)).to(DEV)
+    a = dqt.attn(tq, tk, heads, kvh, d, dev32(qs), dev32(ks), scale=scale, causal=causal)
+    O, lse = like(Qd), torch.full((heads, tq), SENT, dtype=torch.float32, device=DEV)
+    ws = dqt.workspace(dqt.dqt_attn_fwd_workspace(a))
+    if ws is not None:
+        ws.fill_(float("nan"))
+    dqt.dqt_attn_fwd(a, Qd, Kd, Vd, O, lse, ws)
+    torch.cuda.synchronize()
+    ref = R.attention(Q, K, V, qs, ks, d ** -0.5 if scale is None else scale, causal, dO if train else None)
+    own_q = torch.zeros(tq, dtype=torch.bool)
+    own_q[qs[0]:qs[-1]] = True
+    own_k = torch.zeros(tk, dtype=torch.bool)
+    own_k[ks[0]:ks[-1]] = True
+    close("O", O[own_q], ref["O"][own_q], ref["t_O"][own_q])
+    close("lse", lse[:, own_q], ref["lse"][:, own_q], ref["t_lse"][:, own_q])
+    assert (O[~own_q] == SENT).all() and (lse[:, ~own_q] == SENT).all()
+    if not train:
+        return
+    dQ, dK, dV = like(Qd), like(Kd), like(Vd)
+    ws = dqt.workspace(dqt.dqt_attn_bwd_workspace(a))
+    if ws is not None:
+        ws.fill_(float("nan"))
+    dqt.dqt_attn_bwd(a, Qd, Kd, Vd, O, lse, dOd, dQ, dK, dV, ws)
+    torch.cuda.synchronize()
+    for n, got, own in (("dQ", dQ, own_q), ("dK", dK, own_k), ("dV", dV, own_k)):
+        close(n, got[own], ref[n][own], ref["t_" + n][own])
+        assert (got[~own] == SENT).all(), n
+        if ref[n][own].norm() > 0:
+            err = (got[own].double().cpu() - ref[n][own]).norm() / ref[n][own].norm()
+            assert err < 1.5 * R.BF16, (n, float(err))
+
+
+LENGTHS = [
+    # (query lengths, key lengths)
+    ([1], [1]),
+    ([37], [37]),
+    ([64, 65, 1, 63], [64, 65, 1, 63]),
+    ([127, 128, 129], [127, 128, 129]),
+    ([300, 0, 17, 0], [300, 0, 17, 0]),
+    ([1, 1, 1, 1, 1, 1], [1, 2, 63, 64, 65, 1000]),             # new tokens
+    ([40, 3, 200, 130], [100, 500, 231, 129]),                  # chunks; the last one's first query sees nothing
+    ([50, 10, 0], [7, 0, 30]),                                  # rows that see nothing; no keys; no queries
+]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("li", range(len(LENGTHS)))
+@pytest.mark.parametrize("heads,kvh", [(2, 2), (6, 2), (8, 1)])
+def test_attention_matches_float64(lib, d, li, heads, kvh):
+    lq, lk = LENGTHS[li]
+    log(f"attention d={d} heads={heads}/{kvh} lq={lq} lk={lk}")
+    run(d, heads, kvh, lq, lk, seed=li)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_without_mask(lib, d):
+    log(f"attention not causal d={d}")
+    run(d, 4, 2, [1, 70, 129, 0], [200, 3, 129, 5], causal=False, seed=20)
+
+
+@pytest.mark.parametrize("layout", ["heads", "wide"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_strides(lib, layout, d):
+    log(f"attention layout={layout} d={d}")
+    run(d, 6, 3, [33, 100, 1], [90, 100, 300], layout=layout, seed=21)
+
+
+def test_attention_leaves_other_tokens(lib):
+    log("attention: tokens before the first and behind the last sequence")
+    run(128, 4, 2, [20, 75], [20, 80], before=13, behind=29, seed=22)
+    run(64, 4, 4, [1, 1], [700, 20], before=3, behind=5, seed=23)
+
+
+def test_attention_many_sequences(lib):
+    """More sequences than lanes, empty ones among them."""
+    rng = np.random.default_rng(3)
+    lq = rng.integers(0, 9, 200).tolist()
+    lk = [x + int(c) for x, c in zip(lq, rng.integers(0, 12, 200))]
+    log("attention: 200 sequences")
+    run(64, 3, 1, lq, lk, seed=24)
+    run(128, 2, 2, [1] * 130, rng.integers(1, 40, 130).tolist(), seed=25)
+
+
+def test_attention_long(lib):
+    log("attention: 1 x 2100 of 2 heads, one token over 9001 keys, a chunk over 5000")
+    run(128, 2, 1, [2100], [2100], seed=26)
+    run(128, 8, 2, [1], [9001], seed=27, train=False)
+    run(64, 4, 4, [129], [5000], seed=28)
+
+
+def test_attention_scale_and_large_scores(lib):
+    """Scores of several hundreds: the softmax is nearly one-hot; the running
+    maximum moves all along the row."""
+    log("attention: large scores")
+    run(64, 2, 2, [200], [200], scale=1.0, std=4.0, seed=29, train=False)
+    run(128, 2, 1, [90], [150], scale=0.01, seed=30)
+
+
+def test_attention_one_sequence_without_starts(lib):
+    gen = torch.Generator().manual_seed(5)
+    Q, Qd = tensors(gen, 77, 4, 64, "plain")
+    K, Kd = tensors(gen, 77, 2, 64, "plain")
+    V, Vd = tensors(gen, 77, 2, 64, "plain")
+    log("attention without starts")
+    a = dqt.attn(77, 77, 4, 2, 64)
+    O = torch.empty_like(Qd)
+    dqt.dqt_attn_fwd(a, Qd, Kd, Vd, O)           # (no lse)
+    torch.cuda.synchronize()
+    ref = R.attention(Q, K, V, [0, 77], [0, 77], 0.125, True)
+    close("O", O, ref["O"], ref["t_O"])
+
+
+def test_attention_infinite_scores_stay_in_their_sequence(lib):
+    """A sequence of infinities and NaN leaves the next one's results alone."""
+    gen = torch.Generator().manual_seed(6)
+    lens = [40, 100, 30]
+    s = starts(lens)
+    T = int(s[-1])
+    Q, Qd = tensors(gen, T, 2, 128, "plain")
+    K, Kd = tensors(gen, T, 2, 128, "plain")
+    V, Vd = tensors(gen, T, 2, 128, "plain")
+    G, Gd = tensors(gen, T, 2, 128, "plain", 1e-2)
+    st = torch.from_numpy(s.astype(np.int32)).to(DEV)
+    a = dqt.attn(T, T, 2, 2, 128, st, st)
+    ws = dqt.workspace(dqt.dqt_attn_bwd_workspace(a))
+
+    def both(q, k, v):
+        O, lse = torch.empty_like(q), torch.empty((2, T), dtype=torch.float32, device=DEV)
+        g = [torch.empty_like(q) for _ in range(3)]
+        dqt.dqt_attn_fwd(a, q, k, v, O, lse, dqt.workspace(dqt.dqt_attn_fwd_workspace(a)))
+        dqt.dqt_attn_bwd(a, q, k, v, O, lse, Gd, *g, ws)
+        torch.cuda.synchronize()
+        return [O, *g]
+
+    log("attention: non-finite neighbours")
+    good = both(Qd, Kd, Vd)
+    for t in (Qd, Kd, Vd):
+        t[s[1]:s[2]] = float("nan")
+        t[s[1] + 3] = float("inf")
+    bad = both(Qd, Kd, Vd)
+    for x, y in zip(good, bad):
+        for i in (0, 2):
+            assert torch.equal(x[s[i]:s[i + 1]], y[s[i]:s[i + 1]])
+
+
+def test_attention_gradient_against_differences(lib):
+    """The kernels' gradients along random directions against central
+    differences of the float64 forward (step 1e-4: truncation below 1e-7)."""
+    gen = torch.Generator().manual_seed(7)
+    lq, lk, heads, kvh, d = [33, 5], [40, 77], 4, 2, 64
+    qs, ks = starts(lq), starts(lk)
+    Q, Qd = tensors(gen, 38, heads, d, "plain")
+    K, Kd = tensors(gen, 117, kvh, d, "plain")
+    V, Vd = tensors(gen, 117, kvh, d, "plain")
+    dO, dOd = tensors(gen, 38, heads, d, "plain")
+    st = [torch.from_numpy(x.astype(np.int32)).to(DEV) for x in (qs, ks)]
+    a = dqt.attn(38, 117, heads, kvh, d, *st)
+    O, lse = torch.empty_like(Qd), torch.empty((heads, 38), dtype=torch.float32, device=DEV)
+    g = [torch.empty_like(t) for t in (Qd, Kd, Vd)]
+    log("attention: differences")
+    dqt.dqt_attn_fwd(a, Qd, Kd, Vd, O, lse, dqt.workspace(dqt.dqt_attn_fwd_workspace(a)))
+    dqt.dqt_attn_bwd(a, Qd, Kd, Vd, O, lse, dOd, *g, dqt.workspace(dqt.dqt_attn_bwd_workspace(a)))
+    torch.cuda.synchronize()
+    ref = R.attention(Q, K, V, qs, ks, 0.125, True, dO)
+    base = [t.double() for t in (Q, K, V)]
+    for i, n in enumerate(("dQ", "dK", "dV")):
+        r = torch.randn(base[i].shape, generator=gen, dtype=torch.float64)
+
+        def loss(h):
+            x = [b + (h * r if j == i else 0) for j, b in enumerate(base)]
+            return float((R.attention(*x, qs, ks, 0.125, True)["O"] * dO.double()).sum())
+
+        diff = (loss(1e-4) - loss(-1e-4)) / 2e-4
+        got = float((g[i].double().cpu() * r).sum())
+        tol = float((ref["t_" + n] * r.abs()).sum()) + 1e-5 * abs(diff)
+        assert abs(got - diff) <= tol, (n, got, diff, tol)
+
+
+def test_attention_is_reproducible_and_streams(lib):
+    """The same bits on every call, on two streams at once (a workspace each)."""
+    gen = torch.Generator().manual_seed(8)
+    lens = [700, 33, 260]
+    T = sum(lens)
+    st = torch.from_numpy(starts(lens).astype(np.int32)).to(DEV)
+    _, Qd = tensors(gen, T, 8, 128, "plain")
+    _, Kd = tensors(gen, T, 2, 128, "plain")
+    _, Vd = tensors(gen, T, 2, 128, "plain")
+    _, Gd = tensors(gen, T, 8, 128, "plain")
+    a = dqt.attn(T, T, 8, 2, 128, st, st)
+
+    def bufs():
+        return dict(O=torch.empty_like(Qd), lse=torch.empty((8, T), dtype=torch.float32, device=DEV),
+                    dQ=torch.empty_like(Qd), dK=torch.empty_like(Kd), dV=torch.empty_like(Vd),
+                    f=dqt.workspace(dqt.dqt_attn_fwd_workspace(a)), b=dqt.workspace(dqt.dqt_attn_bwd_workspace(a)))
+
+    def go(b, stream=None):
+        dqt.dqt_attn_fwd(a, Qd, Kd, Vd, b["O"], b["lse"], b["f"], stream=stream)
+        dqt.dqt_attn_bwd(a, Qd, Kd, Vd, b["O"], b["lse"], Gd, b["dQ"], b["dK"], b["dV"], b["b"], stream=stream)
+
+    log("attention: two streams")
+    first, x, y = bufs(), bufs(), bufs()
+    go(first)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        go(x, s1)
+        go(y, s2)
+    torch.cuda.synchronize()
+    for b in (x, y):
+        for k in ("O", "lse", "dQ", "dK", "dV"):
+            assert torch.equal(first[k], b[k]), k

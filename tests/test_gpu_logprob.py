@@ -1,0 +1,212 @@
+"""Token log probabilities, entropy, alternatives and the logits' gradient
+against plain float64 arithmetic."""
+import numpy as np
+import pytest
+import torch
+
+import op_reference as R
+from gpu_util import DEV, log
+from paper_2412_04787_amd import dqt
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+
+
+def forward(X, t, top=0, ent=True):
+    M, V = X.shape
+    f = lambda *s: torch.full(s, 777.0, dtype=torch.float32, device=DEV)
+    o = dict(logp=f(M), lse=f(M), entropy=f(M) if ent else None, stat=f(M, 2),
+             ids=torch.full((M, top), -7, dtype=torch.int64, device=DEV) if top else None, tl=f(M, top) if top else None)
+    ws = dqt.workspace(dqt.dqt_logprob_workspace(M, V, top))
+    if ws is not None:
+        ws.fill_(float("nan"))
+    dqt.dqt_logprob_fwd(X, t, o["logp"], o["lse"], o["entropy"], o["stat"], o["ids"], o["tl"], ws)
+    torch.cuda.synchronize()
+    return o
+
+
+def check(X, Xd, t, top, ent=True):
+    """X: the values on the host (fp32), Xd: the device tensor."""
+    V = X.shape[1]
+    o = forward(Xd, t.to(DEV), top, ent)
+    ref = R.logprob(X, t)
+    for n in ("lse", "logp") + (("entropy",) if ent else ()):
+        got = o[n].double().cpu()
+        bad = ~((got - ref[n]).abs() <= ref["t_" + n]) & (got != ref[n])
+        assert not bad.any(), (n, got[bad][:4], ref[n][bad][:4])
+    if top:
+        val, idx = torch.sort(X, dim=1, descending=True, stable=True)
+        assert torch.equal(o["ids"].cpu(), idx[:, :top]), "top ids"
+        want = ref["d"].gather(1, idx[:, :top])
+        want[torch.isinf(val[:, :top])] = -INF
+        got = o["tl"].double().cpu()
+        tol = ref["t_d"] + 2 * R.F32 * torch.nan_to_num(want.abs(), posinf=0)
+        assert (((got - want).abs() <= tol) | (got == want)).all()
+    return o, ref
+
+
+def logits(M, V, dt, seed, masked=True):
+    g = torch.Generator().manual_seed(seed)
+    X = torch.randn((M, V), generator=g) * 2
+    if masked and V > 3:
+        X[:, V - max(1, V // 64):] = -INF
+        X[M // 2, V // 2:] = -INF
+    X = X.to(dt)
+    t = torch.randint(0, max(1, V // 2), (M,), generator=g)
+    if M > 2:
+        t[1] = -100
+        t[2] = V
+    return X, t
+
+
+SIZES = [(1, 1), (2, 2), (5, 7), (3, 100), (17, 1000), (300, 1001), (4, 4096), (1, 8192), (3, 32000), (1, 128001),
+         (600, 4099)]
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("top", [0, 1, 5, 32])
+@pytest.mark.parametrize("M,V", SIZES)
+def test_logprob_forward(lib, dt, top, M, V):
+    top = min(top, V)
+    log(f"logprob M={M} V={V} top={top} {dt}")
+    X, t = logits(M, V, dt, V + top)
+    check(X.float(), X.to(DEV), t, top, ent=top != 1)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_logprob_strided_rows(lib, dt):
+    """Rows at every alignment, of a wider buffer."""
+    for pad in (1, 2, 3, 5, 8):
+        log(f"logprob stride {pad} {dt}")
+        X, t = logits(9, 517, dt, pad)
+        buf = torch.full((9, 517 + pad), 100.0, dtype=dt, device=DEV)
+        buf[:, :517] = X.to(DEV)
+        check(X.float(), buf[:, :517], t, 4)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M", [3, 530])
+def test_logprob_ties_and_masked_rows(lib, dt, M):
+    """Constant rows, rows of few distinct values, rows with fewer finite
+    logits than alternatives, rows of nothing but -inf, the lowest finite value."""
+    log(f"logprob ties {dt} M={M}")
+    V = 9000
+    X = torch.zeros((M, V))
+    X[1] = (torch.arange(V) % 3).float()
+    X[2] = -INF
+    X[2, 4000] = 1.5
+    X[2, 17] = 1.5
+    if M > 3:
+        X[3] = -INF
+        X[4] = float(torch.finfo(dt).min)
+        X[5, ::2] = float(torch.finfo(dt).min)
+        X[6] = torch.arange(V).float()
+        X[7] = -torch.arange(V).float()
+    X = X.to(dt)
+    t = torch.zeros((M,), dtype=torch.int64)
+    t[2] = 17
+    check(X.float(), X.to(DEV), t, 32)
+
+
+@pytest.mark.parametrize("M", [1, 600])
+def test_logprob_alternatives_of_adverse_rows(lib, M):
+    """The largest logits all lie where few threads read them: more candidates
+    reach the bound than LDS holds."""
+    log(f"logprob adverse rows M={M}")
+    V = 65536
+    g = torch.Generator().manual_seed(4)
+    X = torch.rand((M, V), generator=g)
+    piece = (torch.arange(V) // 4) % 256
+    X[:, piece < 80] += 5.0
+    check(X, X.to(DEV), torch.zeros((M,), dtype=torch.int64), 20)
+
+
+def test_logprob_non_finite_rows(lib):
+    """NaN and +inf reach their own row's results alone; alternatives stay
+    distinct tokens."""
+    log("logprob non-finite rows")
+    X, t = logits(6, 3000, torch.float32, 11)
+    clean = forward(X.to(DEV), t.to(DEV), 8)
+    Y = X.clone()
+    Y[0, 5] = float("nan")
+    Y[1] = float("nan")
+    Y[3, 9] = INF
+    Y[3, 10] = INF
+    Y[4, 70] = -float("nan")
+    got = forward(Y.to(DEV), t.to(DEV), 8)
+    for r in (0, 1, 3, 4):
+        assert torch.isnan(got["lse"][r]) and torch.isnan(got["entropy"][r])
+        ids = got["ids"][r].tolist()
+        assert len(set(ids)) == 8 and all(0 <= i < 3000 for i in ids)
+    for r in (2, 5):
+        for n in ("lse", "logp", "entropy", "ids", "tl"):
+            assert torch.equal(got[n][r], clean[n][r])
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("ent", [True, False])
+@pytest.mark.parametrize("M,V,pad", [(1, 1, 0), (5, 7, 0), (17, 1000, 0), (33, 1001, 0), (4, 32000, 0), (3, 20000, 3)])
+def test_logprob_backward(lib, dt, ent, M, V, pad):
+    log(f"logprob backward M={M} V={V} pad={pad} {dt} entropy={ent}")
+    X, t = logits(M, V, dt, V + 1)
+    if M > 3:
+        X[3] = -INF                      # a row without a finite logit
+        X[0] = float(torch.finfo(dt).min)    # all equal: p = 1 / V, whatever the value
+    Xd = torch.zeros((M, V + pad), dtype=dt, device=DEV)[:, :V]
+    Xd.copy_(X)
+    g = torch.Generator().manual_seed(2)
+    dl, de = torch.randn((M,), generator=g), torch.randn((M,), generator=g) * 0.1
+    o = forward(Xd, t.to(DEV))
+    ref = R.logprob(X.float(), t)
+    buf = torch.full((M, V + 5), 3.0, dtype=dt, device=DEV)      # (another stride: other alignments)
+    dX = buf[:, :V]
+    args = (t.to(DEV), o["stat"], dl.to(DEV))
+    kw = dict(entropy=o["entropy"], dent=de.to(DEV)) if ent else {}
+    dqt.dqt_logprob_bwd(Xd, *args, dX, **kw)
+    same = Xd.clone() if pad == 0 else torch.zeros((M, V + pad), dtype=dt, device=DEV)[:, :V].copy_(Xd)
+    dqt.dqt_logprob_bwd(same, *args, same, **kw)                 # in place
+    torch.cuda.synchronize()
+    assert torch.equal(same, dX) and (buf[:, V:] == 3.0).all()
+    gl = torch.where(ref["has"], dl.double(), torch.zeros(M, dtype=torch.float64))[:, None]
+    pick = torch.nn.functional.one_hot(t.clamp(0, V - 1), V).double() * ref["has"][:, None]
+    some = torch.isfinite(ref["lse"])[:, None]
+    want = torch.where(some, gl * (pick - ref["p"]), torch.zeros_like(ref["p"]))
+    e = de.double()[:, None] if ent else torch.zeros((M, 1), dtype=torch.float64)
+    want = want - torch.where(some, e * (ref["plogp"] + ref["p"] * ref["entropy"][:, None]), torch.zeros_like(want))
+    # p: the error of lse and of one exponent below 2^7; entropy's own; then 6 roundings
+    rel = torch.where(some, torch.full_like(some, ref["t_d"] + 128 * R.F32, dtype=torch.float64), torch.zeros_like(some, dtype=torch.float64))
+    terms = gl.abs() * pick + ref["p"] * (gl.abs() + e.abs() * (ref["entropy"].abs()[:, None] + 1)) + e.abs() * ref["plogp"].abs()
+    tol = (rel + 8 * R.F32) * terms + e.abs() * ref["p"] * torch.nan_to_num(ref["t_entropy"])[:, None]
+    half = R.BF16 if dt == torch.bfloat16 else R.F32
+    tol = tol + half * want.abs() * (1 + 2.0 ** -7) + 1e-37
+    err = (dX.double().cpu() - want).abs()
+    assert (err <= tol).all(), (float(err.max()), int((err > tol).sum()))
+
+
+def test_logprob_gradient_against_differences(lib):
+    M, V = 3, 50
+    X, t = logits(M, V, torch.float32, 5, masked=False)
+    t = torch.tensor([3, 0, 49])
+    dl, de = torch.tensor([1.0, -0.5, 2.0]), torch.tensor([0.3, 0.2, -0.7])
+    o = forward(X.to(DEV), t.to(DEV))
+    dX = torch.empty((M, V), dtype=torch.float32, device=DEV)
+    log("logprob: differences")
+    dqt.dqt_logprob_bwd(X.to(DEV), t.to(DEV), o["stat"], dl.to(DEV), dX, o["entropy"], de.to(DEV))
+    torch.cuda.synchronize()
+    h = 1e-5
+    for j in range(V):
+        Y = X.double()
+        up, down = Y.clone(), Y.clone()
+        up[:, j] += h
+        down[:, j] -= h
+        a, b = R.logprob(up, t), R.logprob(down, t)
+        diff = (dl.double() * (a["logp"] - b["logp"]) + de.double() * (a["entropy"] - b["entropy"])) / (2 * h)
+        assert ((dX[:, j].double().cpu() - diff).abs() <= 2e-6 * (1 + diff.abs())).all()
+
+
+def test_logprob_empty(lib):
+    e = torch.empty((0, 10), device=DEV)
+    v = torch.empty((0,), device=DEV)
+    dqt.dqt_logprob_fwd(e, v.long(), v, v)
+    dqt.dqt_logprob_bwd(e, v.long(), torch.empty((0, 2), device=DEV), v, e)

@@ -1,0 +1,137 @@
+"""SwiGLU fused with the 8-bit quantisation, its 8-bit checkpoints and its
+backward, against plain float64 / fp32 arithmetic."""
+import numpy as np
+import pytest
+import torch
+
+import op_reference as R
+from gpu_util import DEV, log
+from paper_2412_04787_amd import dqt
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [(1, 16), (3, 48), (5, 128), (9, 144), (130, 2048), (7, 2064), (33, 4096), (4, 5632), (3, 8192), (2, 11008),
+         (2, 16384), (2, 16400)]
+
+
+def inputs(M, K, dt, seed):
+    g = torch.Generator().manual_seed(seed)
+    G, U = (torch.randn((M, K), generator=g) for _ in range(2))
+    G *= torch.exp(torch.linspace(-3, 3, M))[:, None]       # magnitudes across rows
+    if M > 2:
+        U[M // 2] = 0.0                                     # a zero row
+        G[1, :8] = torch.tensor([-100.0, 100.0, -88.5, 0.0, -0.0, 30.0, -30.0, 1e-30])
+    dH = torch.randn((M, K), generator=g) * 1e-2
+    return [t.to(dt) for t in (G, U, dH)]
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("act", ["i8", "e4m3"])
+@pytest.mark.parametrize("M,K", SIZES)
+def test_swiglu_act_quant(lib, dt, act, M, K):
+    log(f"swiglu M={M} K={K} {dt} {act}")
+    G, U, _ = inputs(M, K, dt, K + M)
+    code = dqt.DQT_I8 if act == "i8" else dqt.DQT_FP8E4M3
+    outs = []
+    for ck in (None, dqt.swiglu_ckpt(M, K)):
+        Xq = torch.full((M, K), 77, dtype=torch.int8 if act == "i8" else torch.uint8, device=DEV)
+        xdq = torch.empty((M,), dtype=torch.float32, device=DEV)
+        dqt.dqt_swiglu_act_quant(G.to(DEV), U.to(DEV), code, Xq, xdq, ck)
+        torch.cuda.synchronize()
+        outs.append((Xq, xdq))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    h = R.swiglu(G, U)
+    top = 127.0 if act == "i8" else 448.0
+    m = h.abs().amax(1).clamp(min=float(np.float32(1e-5)))
+    d = outs[0][1].double().cpu()
+    assert ((d - m / top).abs() <= (R.H_REL + 2 * R.F32) * m / top).all()
+    y = h * (top / m)[:, None]
+    err = (2 * R.H_REL + 4 * R.F32) * top
+    if act == "i8":
+        got = outs[0][0].cpu().double()
+        assert ((got - y).abs() <= 0.5 + err).all(), float((got - y).abs().max())
+    else:
+        got = outs[0][0].cpu().view(torch.float8_e4m3fn).double()
+        assert ((got - y).abs() <= 2.0 ** -4 * y.abs() + 2.0 ** -10 + err * 2.0 ** -3).all()
+    for x, q, s in ((G, ck.Gq, ck.gs), (U, ck.Uq, ck.us)):
+        codes, scales = R.checkpoint(x)
+        assert np.array_equal(q.cpu().numpy(), codes)
+        assert np.array_equal(s.cpu().numpy(), scales)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("stored", [True, False])
+@pytest.mark.parametrize("M,K", SIZES)
+def test_swiglu_backward(lib, dt, stored, M, K):
+    log(f"swiglu backward M={M} K={K} {dt} checkpoint={stored}")
+    G, U, dH = inputs(M, K, dt, K + M + 1)
+    dG, dU = (torch.empty((M, K), dtype=dt, device=DEV) for _ in range(2))
+    if stored:
+        ck = dqt.swiglu_ckpt(M, K)
+        (a, b), (c, e) = R.checkpoint(G), R.checkpoint(U)
+        for t, v in ((ck.Gq, a), (ck.gs, b), (ck.Uq, c), (ck.us, e)):
+            t.copy_(torch.from_numpy(v))
+        g, u = R.checkpoint_values(a, b), R.checkpoint_values(c, e)
+        dqt.dqt_swiglu_backward_ckpt(dH.to(DEV), ck, dG, dU)
+    else:
+        g, u = G, U
+        dqt.dqt_swiglu_backward(dH.to(DEV), G.to(DEV), U.to(DEV), dG, dU)
+    torch.cuda.synchronize()
+    rg, ru, tg, tu = R.swiglu_backward(dH, g, u)
+    half = R.BF16 if dt == torch.bfloat16 else R.F32
+    for n, got, ref, t in (("dG", dG, rg, tg), ("dU", dU, ru, tu)):
+        err = (got.double().cpu() - ref).abs()
+        tol = half * ref.abs() * (1 + 2.0 ** -7) + t + 1e-37
+        assert (err <= tol).all(), (n, float(err.max()), int((err > tol).sum()))
+
+
+def test_swiglu_gradient_against_differences(lib):
+    M, K = 4, 96
+    G, U, dH = inputs(M, K, torch.float32, 3)
+    G[1, :8] = torch.linspace(-3, 3, 8)
+    dG, dU = (torch.empty((M, K), dtype=torch.float32, device=DEV) for _ in range(2))
+    log("swiglu: differences")
+    dqt.dqt_swiglu_backward(dH.to(DEV), G.to(DEV), U.to(DEV), dG, dU)
+    torch.cuda.synchronize()
+    h = 1e-5
+    for got, at in ((dG, 0), (dU, 1)):
+        x = [G.double(), U.double()]
+        up, down = list(x), list(x)
+        up[at], down[at] = x[at] + h, x[at] - h
+        diff = dH.double() * (R.swiglu(*up) - R.swiglu(*down)) / (2 * h)
+        # (central differences: h^2 / 6 times a third derivative below 4 |u|, and rounding 1e-16 / h |h|)
+        tol = 1e-5 * diff.abs() + dH.double().abs() * 1e-8 * (1 + G.double().abs()) * (1 + U.double().abs())
+        assert ((got.double().cpu() - diff).abs() <= tol).all()
+
+
+def test_swiglu_backward_in_place_and_empty(lib):
+    G, U, dH = inputs(5, 256, torch.bfloat16, 9)
+    a, b = torch.empty((5, 256), dtype=torch.bfloat16, device=DEV), torch.empty((5, 256), dtype=torch.bfloat16, device=DEV)
+    log("swiglu backward in place")
+    dqt.dqt_swiglu_backward(dH.to(DEV), G.to(DEV), U.to(DEV), a, b)
+    x = dH.to(DEV)
+    y = torch.empty_like(x)
+    dqt.dqt_swiglu_backward(x, G.to(DEV), U.to(DEV), y, x)
+    torch.cuda.synchronize()
+    assert torch.equal(a, y) and torch.equal(b, x)
+    e = torch.empty((0, 256), dtype=torch.bfloat16, device=DEV)
+    dqt.dqt_swiglu_act_quant(e, e, dqt.DQT_I8, e.to(torch.int8), torch.empty((0,), device=DEV))
+    dqt.dqt_swiglu_backward(e, e, e, e, e)
+
+
+def test_swiglu_matches_unfused_quantiser(lib):
+    """On rows whose product is exact in bf16, the fused call gives the codes of
+    dqt_act_quant (g large: silu(g) = g in fp32)."""
+    M, K = 6, 512
+    gen = torch.Generator().manual_seed(1)
+    G = torch.randint(32, 64, (M, K), generator=gen).to(torch.bfloat16).to(DEV)
+    U = torch.tensor([-2.0, -1.0, 0.5, 0.25])[torch.randint(0, 4, (M, K), generator=gen)].to(torch.bfloat16).to(DEV)
+    H = G * U
+    log("swiglu: fused against the quantiser alone")
+    for act, t in ((dqt.DQT_I8, torch.int8), (dqt.DQT_FP8E4M3, torch.uint8)):
+        q = [torch.empty((M, K), dtype=t, device=DEV) for _ in range(2)]
+        s = [torch.empty((M,), dtype=torch.float32, device=DEV) for _ in range(2)]
+        dqt.dqt_swiglu_act_quant(G, U, act, q[0], s[0])
+        dqt.dqt_act_quant(H, act, q[1], s[1])
+        torch.cuda.synchronize()
+        assert torch.equal(q[0], q[1]) and torch.equal(s[0], s[1])
