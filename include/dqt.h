@@ -292,9 +292,9 @@ dqt_status dqt_logprob_bwd(const void* X, int32_t x_t, int64_t M, int32_t V, int
  *   q_tokens * heads < 2^28; k_tokens and q_tokens * (heads / kv_heads) < 2^31.
  *   scale: 2^-20 .. 2^20.
  * Tensors are strided: token t's head h is the d consecutive values from
- * p + t * token + h * head (elements; both strides multiples of 8, at most
- * 2^31; 0 allowed for inputs).  Outputs alias neither an input nor each other,
- * and their rows do not overlap (DQT_ERR_SHAPE).  A non-finite value in K or V
+ * p + t * token + h * head (elements; multiples of 8, token at most 2^23, head
+ * at most 2^40; 0 allowed for inputs).  Outputs alias neither an input nor
+ * each other, and their rows do not overlap (DQT_ERR_SHAPE).  A non-finite value in K or V
  * may reach any query of its own sequence and head, masked or not, and one in
  * Q or dO any gradient of its sequence; none reaches another sequence.
  */

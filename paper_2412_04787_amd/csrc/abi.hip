@@ -260,6 +260,7 @@ dqt_status check_attn(const dqt_attn* d, dqt::AttnArgs* a) {
   a->heads = d->heads;
   a->kv_heads = d->kv_heads;
   a->group = (int)g;
+  a->gone = g == 1 ? ~0u : 0u;
   if (g > 1) {      // r / g = umulhi(r, m) >> (b - 1) with m = ceil(2^(31 + b) / g), b = ceil(log2 g), for r < 2^31
     int b = 1;
     while ((int64_t(1) << b) < g) ++b;
@@ -284,9 +285,8 @@ dqt_status check_rows(const dqt_rows* t, int64_t tokens, int32_t heads, int32_t 
   if (t == nullptr) return DQT_ERR_NULL;
   if (tokens > 0 && t->p == nullptr) return DQT_ERR_NULL;
   if (!aligned16(t->p) || (t->token & 7) != 0 || (t->head & 7) != 0) return DQT_ERR_ALIGN;
-  const int64_t most = int64_t(1) << 31;
-  if (t->token < 0 || t->head < 0 || t->token > most || t->head > most) return DQT_ERR_SHAPE;
-  if (tokens > 0 && (tokens - 1) * t->token + (heads - 1) * t->head > (int64_t(1) << 48)) return DQT_ERR_SHAPE;
+  // (the kernels take a tile's rows, up to 128 tokens, at 32-bit offsets)
+  if (t->token < 0 || t->head < 0 || t->token > (int64_t(1) << 23) || t->head > (int64_t(1) << 40)) return DQT_ERR_SHAPE;
   if (output && tokens > 0) {
     const bool by_token = (heads == 1 || t->head >= d) && (tokens == 1 || t->token >= (heads - 1) * t->head + d);
     const bool by_head = (tokens == 1 || t->token >= d) && (heads == 1 || t->head >= (tokens - 1) * t->token + d);

@@ -98,7 +98,7 @@ __device__ __forceinline__ bool find_seq(const AttnArgs& a, int t, Seq& q) {
 
 // row r of a sequence -> token and head within the group (r / G, r % G)
 __device__ __forceinline__ int row_token(const AttnArgs& a, int r) {
-  return a.group == 1 ? r : (int)(__umulhi((uint32_t)r, a.gmul) >> a.gshift);
+  return (int)((__umulhi((uint32_t)r, a.gmul) + ((uint32_t)r & a.gone)) >> a.gshift);
 }
 
 // Blocks go to the 8 XCDs in turn; XCD x takes the x-th eighth of the list, so
@@ -108,22 +108,35 @@ __device__ __forceinline__ int xcd_order(int b, int n) {
   return b < 8 * per ? (b & 7) * per + (b >> 3) : b;
 }
 
+// This lane's byte offsets of the operand reads from a tile.
 template <int D>
-__device__ __forceinline__ i32x4 read_straight(const lds_u8* tile, int rb, int ks) {
-  const int l = threadIdx.x & 63, row = rb + (l & 31);
-  return *(const lds_i32x4*)(tile + row * (2 * D) + (((2 * ks + (l >> 5)) ^ swz<D>(row & 15)) << 4));
+struct Lanes {
+  int sa[D / 16];         // straight: row lane % 32, values 16 ks + 8 (lane / 32) ..
+  int ta[2][D / 32];      // transposed: column 32 db + lane % 32, values 8 e + 4 (lane / 32) + 0..3
+  __device__ __forceinline__ Lanes() {
+    const int l = threadIdx.x & 63, h = l >> 5, i = l & 15;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) sa[ks] = (l & 31) * (2 * D) + (((2 * ks + h) ^ swz<D>(l & 15)) << 4);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        const int row = 8 * e + 4 * h + (i >> 2), c = 4 * db + ((l >> 3) & 2) + ((i >> 1) & 1);
+        ta[e][db] = row * (2 * D) + ((c ^ swz<D>(row)) << 4) + 8 * (i & 1);
+      }
+  }
+};
+template <int D>
+__device__ __forceinline__ i32x4 read_straight(const lds_u8* tile, const Lanes<D>& ln, int rb, int ks) {
+  return *(const lds_i32x4*)(tile + ln.sa[ks] + rb * (2 * D));
 }
 // values [kb + {4 h + 0..3, 8 + 4 h + 0..3}] (h = lane half) of column
 // 32 db + lane % 32, kb a multiple of 16
 template <int D>
-__device__ __forceinline__ i32x4 read_transposed(const lds_u8* tile, int kb, int db) {
-  const int l = threadIdx.x & 63, h = l >> 5, i = l & 15;
-  const int c = 4 * db + ((l >> 3) & 2) + ((i >> 1) & 1);
+__device__ __forceinline__ i32x4 read_transposed(const lds_u8* tile, const Lanes<D>& ln, int kb, int db) {
   auto half = [&](int e) {
-    const int row = kb + 8 * e + 4 * h + (i >> 2);
-    const int off = row * (2 * D) + ((c ^ swz<D>((8 * e + 4 * h + (i >> 2)) & 15)) << 4) + 8 * (i & 1);
-    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(tile + off));
-    return __builtin_bit_cast(u32x2, v);
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s16x4*)(tile + ln.ta[e][db] + kb * (2 * D))));
   };
   const u32x2 lo = half(0), hi = half(1);
   return i32x4{(int)lo[0], (int)lo[1], (int)hi[0], (int)hi[1]};
@@ -145,16 +158,73 @@ __device__ __forceinline__ f32x16 splat(float x) {
   return v;
 }
 
-// One wave's quarter of a tile of kKT rows: row_ptr(r) is the address of the
-// tile's row r (in bounds for every r).
-template <int D, class F>
-__device__ __forceinline__ void stage(lds_u8* tile, F&& row_ptr) {
-  constexpr int CH = D / 8, N = kKT * CH / 256;
-  const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+// One wave's quarter of a tile of R rows: off(r, c) is the byte offset from
+// base of the tile's row r, 16-byte chunk c.
+template <int D, int R>
+struct Stager {
+  static constexpr int CH = D / 8, N = R * CH / 256;
+  static_assert(N * 256 == R * CH, "whole waves");
+  uint32_t off[N];
+  template <class F>
+  __device__ __forceinline__ void set(F&& f) {
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int p = (w * N + n) * 64 + l, row = p / CH, c = (p % CH) ^ swz<D>(row & 15);
-    dma16(row_ptr(row) + 16 * c, tile + (w * N + n) * 1024);
+    for (int n = 0; n < N; ++n) {
+      const int p = (w * N + n) * 64 + l, row = p / CH;
+      off[n] = f(row) + 16 * ((p % CH) ^ swz<D>(row & 15));
+    }
+  }
+  __device__ __forceinline__ void issue(const uint8_t* base, lds_u8* tile) const {
+    const int w = threadIdx.x >> 6;
+#pragma unroll
+    for (int n = 0; n < N; ++n) dma16s(base, off[n], tile + (w * N + n) * 1024);
+  }
+  // the same from each row's own address
+  template <class F>
+  static __device__ __forceinline__ void issue_each(lds_u8* tile, F&& row_ptr) {
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int p = (w * N + n) * 64 + l, row = p / CH;
+      dma16(row_ptr(row) + 16 * ((p % CH) ^ swz<D>(row & 15)), tile + (w * N + n) * 1024);
+    }
+  }
+};
+// Keys and values of tile after tile: rows past the last key repeat it.
+template <int D>
+struct KeyStream {
+  const uint8_t *kp, *vp;
+  int64_t k_tok, v_tok;
+  int lk;
+  Stager<D, kKT> ks, vs;
+  __device__ __forceinline__ KeyStream(const AttnArgs& a, const Seq& q, int kvh)
+      : kp(a.K + (int64_t)q.k0 * a.k_tok + (int64_t)kvh * a.k_head),
+        vp(a.V + (int64_t)q.k0 * a.v_tok + (int64_t)kvh * a.v_head), k_tok(a.k_tok), v_tok(a.v_tok), lk(q.lk) {
+    ks.set([&](int row) { return (uint32_t)row * (uint32_t)k_tok; });
+    vs.set([&](int row) { return (uint32_t)row * (uint32_t)v_tok; });
+  }
+  __device__ __forceinline__ void issue(int k0, lds_u8* kt, lds_u8* vt) const {
+    const uint8_t *kb = kp + (int64_t)k0 * k_tok, *vb = vp + (int64_t)k0 * v_tok;
+    if (k0 + kKT <= lk) {
+      ks.issue(kb, kt);
+      vs.issue(vb, vt);
+    } else {
+      Stager<D, kKT> e;
+      const int last = lk - 1 - k0;
+      e.set([&](int row) { return (uint32_t)min(row, last) * (uint32_t)k_tok; });
+      e.issue(kb, kt);
+      e.set([&](int row) { return (uint32_t)min(row, last) * (uint32_t)v_tok; });
+      e.issue(vb, vt);
+    }
+  }
+};
+// f(t, stage) for t = 0 .. n - 1 with the stage t % 2 a constant, so that
+// tile addresses fold into the reads' offsets
+template <class F>
+__device__ __forceinline__ void staged_loop(int n, F&& f) {
+  for (int t = 0; t < n; t += 2) {
+    f(t, std::integral_constant<int, 0>{});
+    if (t + 1 < n) f(t + 1, std::integral_constant<int, 1>{});
   }
 }
 
@@ -178,7 +248,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   constexpr int NK = D / 16, ND = D / 32, TB = kKT * D * 2;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2][TB];
   lds_u8* lds = (lds_u8*)&smem[0][0][0];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, h = lane >> 5;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int id = xcd_order(blockIdx.x, gridDim.x);
   const int per_head = a.row_tiles * a.splits;
   const int kvh = id / per_head, rem = id - kvh * per_head;
@@ -207,15 +277,9 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   const int lim = min(a.causal ? tok + off : sq.lk - 1, kend - 1);      // last key this row sees
   const int lim_lo = __builtin_amdgcn_readlane(lim, 0), lim_hi = __builtin_amdgcn_readlane(lim, 31);
 
-  const uint8_t* kp = a.K + (int64_t)sq.k0 * a.k_tok + (int64_t)kvh * a.k_head;
-  const uint8_t* vp = a.V + (int64_t)sq.k0 * a.v_tok + (int64_t)kvh * a.v_head;
-  auto issue = [&](int t) {
-    lds_u8* s = lds + (t & 1) * 2 * TB;
-    const int k0 = kbeg + t * kKT;
-    stage<D>(s, [&](int row) { return kp + (int64_t)min(k0 + row, sq.lk - 1) * a.k_tok; });
-    stage<D>(s + TB, [&](int row) { return vp + (int64_t)min(k0 + row, sq.lk - 1) * a.v_tok; });
-  };
-  if (nt > 0) issue(0);
+  const Lanes<D> ln;
+  const KeyStream<D> keys(a, sq, kvh);
+  if (nt > 0) keys.issue(kbeg, lds, lds + TB);
 
   i32x4 qf[NK];
   const uint8_t* qp = a.Q + (int64_t)(sq.q0 + tok) * a.q_tok + (int64_t)head * a.q_head;
@@ -228,19 +292,19 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   const float c = a.scale * kLog2e;
   float m = -__builtin_inff(), l = 0.0f;      // running maximum (of c q.k), sum of exp2
 
-  for (int t = 0; t < nt; ++t) {
+  staged_loop(nt, [&](int t, auto stage) {
+    constexpr int S = decltype(stage)::value;
+    const lds_u8 *kt = lds + S * 2 * TB, *vt = kt + TB;
+    const int k0 = kbeg + t * kKT;
     wait_vm<0>();
     __syncthreads();
-    if (t + 1 < nt) issue(t + 1);
-    const lds_u8* kt = lds + (t & 1) * 2 * TB;
-    const lds_u8* vt = kt + TB;
-    const int k0 = kbeg + t * kKT;
-    if (!active || k0 > lim_hi) continue;
+    if (t + 1 < nt) keys.issue(k0 + kKT, lds + (1 - S) * 2 * TB, lds + (1 - S) * 2 * TB + TB);
+    if (!active || k0 > lim_hi) return;
     f32x16 s[2] = {splat(0.0f), splat(0.0f)};
 #pragma unroll
     for (int ks = 0; ks < NK; ++ks) {
-      s[0] = mfma(read_straight<D>(kt, 0, ks), qf[ks], s[0]);
-      s[1] = mfma(read_straight<D>(kt, 32, ks), qf[ks], s[1]);
+      s[0] = mfma(read_straight<D>(kt, ln, 0, ks), qf[ks], s[0]);
+      s[1] = mfma(read_straight<D>(kt, ln, 32, ks), qf[ks], s[1]);
     }
     if (k0 + kKT - 1 > lim_lo) {
 #pragma unroll
@@ -277,9 +341,9 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
     for (int kk = 0; kk < 4; ++kk) {
       const i32x4 p = pack8(s[kk >> 1], 8 * (kk & 1));
 #pragma unroll
-      for (int db = 0; db < ND; ++db) o[db] = mfma(read_transposed<D>(vt, 16 * kk, db), p, o[db]);
+      for (int db = 0; db < ND; ++db) o[db] = mfma(read_transposed<D>(vt, ln, 16 * kk, db), p, o[db]);
     }
-  }
+  });
   l += __shfl_xor(l, 32, kWave);
   if (r >= rows) return;
   const bool none = l == 0.0f;               // a row that sees no key: zeros
@@ -315,18 +379,35 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
   float mx = -__builtin_inff();
   for (int s = lane; s < a.splits; s += 64) mx = fmaxf(mx, a.part_lse[s * all + at]);
   mx = wave_max(mx);
+  if (mx == -__builtin_inff()) mx = 0.0f;
   constexpr int E = D / 64;
   float o[E] = {}, sum = 0.0f;
-  if (mx == -__builtin_inff()) mx = 0.0f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float ls = a.part_lse[s * all + at];
-    if (ls == -__builtin_inff()) continue;        // (its o was not written)
-    const float f = exp2_fast(ls - mx);
+  for (int s0 = 0; s0 < a.splits; s0 += 64) {
+    const int n = min(64, a.splits - s0);
+    // a lane's split: its weight, 0 for one that saw no key (its o was not written)
+    const float f = lane < n ? exp2_fast(a.part_lse[(s0 + lane) * all + at] - mx) : 0.0f;
+    unsigned long long some = __ballot(f != 0.0f);
     sum += f;
-    const float* p = a.part + (s * all + at) * D + E * lane;
+    while (some != 0) {
+      // up to 4 splits' partials in flight
+      float v[4][E], fs[4];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += f * p[e];
+      for (int k = 0; k < 4; ++k) {
+        const int s = some != 0 ? __builtin_ctzll(some) : 0;
+        fs[k] = some != 0 ? __shfl(f, s, kWave) : 0.0f;
+        const float* p = a.part + ((s0 + s) * all + at) * D + E * lane;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[k][e] = some != 0 ? p[e] : 0.0f;
+        some &= some - 1;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += fs[k] * v[k][e];
+    }
   }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, kWave);
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   uint8_t* op = a.O + (int64_t)tok * a.o_tok + (int64_t)head * a.o_head;
   if constexpr (E == 2) *reinterpret_cast<uint32_t*>(op + 4 * lane) = pack_bf16x2(o[0] * inv, o[1] * inv);
@@ -374,7 +455,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   constexpr int NK = D / 16, ND = D / 32, TB = kKT * D * 2;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2][TB];
   lds_u8* lds = (lds_u8*)&smem[0][0][0];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, h = lane >> 5;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int id = xcd_order(blockIdx.x, gridDim.x);
   const int kvh = id / a.row_tiles;
   Seq sq;
@@ -391,14 +472,9 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   const int lim = min(a.causal ? tok + off : sq.lk - 1, kend - 1);
   const int lim_lo = __builtin_amdgcn_readlane(lim, 0), lim_hi = __builtin_amdgcn_readlane(lim, 31);
 
-  const uint8_t* kp = a.K + (int64_t)sq.k0 * a.k_tok + (int64_t)kvh * a.k_head;
-  const uint8_t* vp = a.V + (int64_t)sq.k0 * a.v_tok + (int64_t)kvh * a.v_head;
-  auto issue = [&](int t) {
-    lds_u8* s = lds + (t & 1) * 2 * TB;
-    stage<D>(s, [&](int row) { return kp + (int64_t)min(t * kKT + row, sq.lk - 1) * a.k_tok; });
-    stage<D>(s + TB, [&](int row) { return vp + (int64_t)min(t * kKT + row, sq.lk - 1) * a.v_tok; });
-  };
-  if (nt > 0) issue(0);
+  const Lanes<D> ln;
+  const KeyStream<D> keys(a, sq, kvh);
+  if (nt > 0) keys.issue(0, lds, lds + TB);
   i32x4 qf[NK], gf[NK];
   const uint8_t* qp = a.Q + (int64_t)(sq.q0 + tok) * a.q_tok + (int64_t)head * a.q_head;
   const uint8_t* gp = a.dO + (int64_t)(sq.q0 + tok) * a.do_tok + (int64_t)head * a.do_head;
@@ -414,12 +490,12 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
 #pragma unroll
   for (int db = 0; db < ND; ++db) dq[db] = splat(0.0f);
 
-  for (int t = 0; t < nt; ++t) {
+  staged_loop(nt, [&](int t, auto stage) {
+    constexpr int S = decltype(stage)::value;
+    const lds_u8 *kt = lds + S * 2 * TB, *vt = kt + TB;
     wait_vm<0>();
     __syncthreads();
-    if (t + 1 < nt) issue(t + 1);
-    const lds_u8* kt = lds + (t & 1) * 2 * TB;
-    const lds_u8* vt = kt + TB;
+    if (t + 1 < nt) keys.issue((t + 1) * kKT, lds + (1 - S) * 2 * TB, lds + (1 - S) * 2 * TB + TB);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const int k0 = t * kKT + 32 * b;
@@ -427,37 +503,42 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
       f32x16 s = splat(nl), g = splat(nd);
 #pragma unroll
       for (int ks = 0; ks < NK; ++ks) {
-        s = mfma(read_straight<D>(kt, 32 * b, ks), qf[ks], s);
-        g = mfma(read_straight<D>(vt, 32 * b, ks), gf[ks], g);
+        s = mfma(read_straight<D>(kt, ln, 32 * b, ks), qf[ks], s);
+        g = mfma(read_straight<D>(vt, ln, 32 * b, ks), gf[ks], g);
       }
       if (k0 + 31 > lim_lo) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          g[i] = k0 + 8 * (i >> 2) + 4 * h + (i & 3) <= lim ? exp2_fast(s[i] * c) * g[i] : 0.0f;
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) g[i] *= exp2_fast(s[i] * c);
+        for (int i = 0; i < 16; ++i) s[i] = k0 + 8 * (i >> 2) + 4 * h + (i & 3) <= lim ? s[i] : -__builtin_inff();
       }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) g[i] *= exp2_fast(s[i] * c);
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
         const i32x4 p = pack8(g, 8 * kk);
 #pragma unroll
-        for (int db = 0; db < ND; ++db) dq[db] = mfma(read_transposed<D>(kt, 32 * b + 16 * kk, db), p, dq[db]);
+        for (int db = 0; db < ND; ++db) dq[db] = mfma(read_transposed<D>(kt, ln, 32 * b + 16 * kk, db), p, dq[db]);
       }
     }
-  }
+  });
   if (r >= rows) return;
   store_cols<ND>(a.dQ + (int64_t)(sq.q0 + tok) * a.dq_tok + (int64_t)head * a.dq_head, dq, a.scale);
 }
 
+// Keys and values stay with the block: those of a wave's 32 keys in registers
+// (D = 128: the values in LDS, where the registers of both would not leave room
+// for two waves per SIMD), rows of Q and dO pass through LDS.
 template <int D>
 __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
-  constexpr int NK = D / 16, ND = D / 32, TB = kKT * D * 2;
+  constexpr int NK = D / 16, ND = D / 32;
+  constexpr bool VL = D == 128;
+  constexpr int RT = D == 128 ? 32 : 64, TB = RT * D * 2;          // rows per staged tile, its bytes
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2][TB];
-  __shared__ __attribute__((aligned(256))) float stat[2][2][kKT];     // -lse / c, -do.o
+  __shared__ __attribute__((aligned(1024))) uint8_t vtile[VL ? kBM * D * 2 : 16];
+  __shared__ __attribute__((aligned(256))) float stat[2][2][64];     // -lse / c, -do.o
   lds_u8* lds = (lds_u8*)&smem[0][0][0];
   lds_u8* slds = (lds_u8*)&stat[0][0][0];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, h = lane >> 5;
+  lds_u8* vlds = (lds_u8*)&vtile[0];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int id = xcd_order(blockIdx.x, gridDim.x);
   const int kvh = id / a.key_tiles;
   Seq sq;
@@ -467,92 +548,139 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
   if (k0 >= sq.lk) return;
   const int rows = sq.lq * a.group, off = sq.lk - sq.lq;
   const int kw = k0 + 32 * w, j = kw + (lane & 31), jc = min(j, sq.lk - 1);
-  const bool active = kw < sq.lk;
-  // first row that sees a key of this block
-  const int rlo = a.causal ? max(0, k0 - off) * a.group : 0;
-  const int nt = rows > rlo ? (rows - rlo + kKT - 1) / kKT : 0;
+  // The rows that see key x are a suffix: under a causal mask those from token
+  // x - off on.  This block's first; this wave's first and the one from which
+  // on all its keys are seen; this lane's.
+  auto first_row = [&](int x) { return x >= sq.lk ? 0x7fffffff : a.causal ? max(0, x - off) * a.group : 0; };
+  const int rlo = first_row(k0), rw_lo = first_row(kw), rw_hi = first_row(kw + 31), rmin = first_row(j);
+  const int nt = rows > rlo ? (rows - rlo + RT - 1) / RT : 0;
 
   const uint8_t* qp = a.Q + (int64_t)sq.q0 * a.q_tok + (int64_t)kvh * a.group * a.q_head;
   const uint8_t* gp = a.dO + (int64_t)sq.q0 * a.do_tok + (int64_t)kvh * a.group * a.do_head;
   const int64_t at = ((int64_t)kvh * a.tq + sq.q0) * a.group;
-  auto issue = [&](int t) {
-    lds_u8* s = lds + (t & 1) * 2 * TB;
-    const int r0 = rlo + t * kKT;
-    auto ptr = [&](const uint8_t* p, int64_t tok_s, int64_t head_s, int row) {
-      const int rc = min(r0 + row, rows - 1), tok = row_token(a, rc);
-      return p + tok * tok_s + (rc - tok * a.group) * head_s;
-    };
-    stage<D>(s, [&](int row) { return ptr(qp, a.q_tok, a.q_head, row); });
-    stage<D>(s + TB, [&](int row) { return ptr(gp, a.do_tok, a.do_head, row); });
-    if (w < 2) {
+  // A tile of rows starts with a token's first head when the group divides RT
+  // (rlo is a token's first row): offsets from that token are the same for
+  // every tile (where the heads of a group lie within 32 bits of each other).
+  const bool even = RT % a.group == 0 && a.group * max(a.q_head, a.do_head) < (int64_t(1) << 31);
+  Stager<D, RT> qs, gs;
+  auto offs = [&](int row, int64_t tok_s, int64_t head_s) {
+    const int tok = row_token(a, row);
+    return (uint32_t)tok * (uint32_t)tok_s + (uint32_t)(row - tok * a.group) * (uint32_t)head_s;
+  };
+  qs.set([&](int row) { return offs(row, a.q_tok, a.q_head); });
+  gs.set([&](int row) { return offs(row, a.do_tok, a.do_head); });
+  auto each = [&](const uint8_t* p, int64_t tok_s, int64_t head_s, int r0, lds_u8* tile) {
+    Stager<D, RT>::issue_each(tile, [&](int row) {
+      const int r = min(r0 + row, rows - 1), tok = row_token(a, r);
+      return p + tok * tok_s + (r - tok * a.group) * head_s;
+    });
+  };
+  auto issue = [&](int t, int s) {
+    lds_u8 *qt = lds + s * 2 * TB, *gt = qt + TB;
+    const int r0 = rlo + t * RT;
+    if (even && r0 + RT <= rows) {
+      const int64_t t0 = row_token(a, r0);
+      qs.issue(qp + t0 * a.q_tok, qt);
+      gs.issue(gp + t0 * a.do_tok, gt);
+    } else {
+      each(qp, a.q_tok, a.q_head, r0, qt);
+      each(gp, a.do_tok, a.do_head, r0, gt);
+    }
+    if (w < 2) {      // (64 statistics; those behind a tile of 32 are not used)
       const float* sp = (w == 0 ? a.neg_lse : a.neg_delta) + at + min(r0 + lane, rows - 1);
-      dma4(reinterpret_cast<const uint8_t*>(sp), slds + ((t & 1) * 2 + w) * (kKT * 4));
+      dma4(reinterpret_cast<const uint8_t*>(sp), slds + (s * 2 + w) * 256);
     }
   };
-  if (nt > 0) issue(0);
-  i32x4 kf[NK], vf[NK];
+  const Lanes<D> ln;
+  if (nt > 0) issue(0, 0);
+  i32x4 kf[NK], vf[VL ? 1 : NK];
   const uint8_t* kp = a.K + (int64_t)(sq.k0 + jc) * a.k_tok + (int64_t)kvh * a.k_head;
-  const uint8_t* vp = a.V + (int64_t)(sq.k0 + jc) * a.v_tok + (int64_t)kvh * a.v_head;
 #pragma unroll
-  for (int ks = 0; ks < NK; ++ks) {
-    kf[ks] = *reinterpret_cast<const i32x4*>(kp + 32 * ks + 16 * h);
-    vf[ks] = *reinterpret_cast<const i32x4*>(vp + 32 * ks + 16 * h);
+  for (int ks = 0; ks < NK; ++ks) kf[ks] = *reinterpret_cast<const i32x4*>(kp + 32 * ks + 16 * h);
+  if constexpr (VL) {
+    const uint8_t* vb = a.V + (int64_t)(sq.k0 + k0) * a.v_tok + (int64_t)kvh * a.v_head;
+    Stager<D, kBM> e;
+    const int last = sq.lk - 1 - k0;
+    e.set([&](int row) { return (uint32_t)min(row, last) * (uint32_t)a.v_tok; });
+    e.issue(vb, vlds);
+  } else {
+    const uint8_t* vp = a.V + (int64_t)(sq.k0 + jc) * a.v_tok + (int64_t)kvh * a.v_head;
+#pragma unroll
+    for (int ks = 0; ks < NK; ++ks) vf[ks] = *reinterpret_cast<const i32x4*>(vp + 32 * ks + 16 * h);
   }
   const float c = a.scale * kLog2e;
   f32x16 dk[ND], dv[ND];
 #pragma unroll
   for (int db = 0; db < ND; ++db) dk[db] = dv[db] = splat(0.0f);
 
-  for (int t = 0; t < nt; ++t) {
+  staged_loop(nt, [&](int t, auto stage) {
+    constexpr int S = decltype(stage)::value;
+    const lds_u8 *qt = lds + S * 2 * TB, *gt = qt + TB, *st = slds + S * 512;
     wait_vm<0>();
     __syncthreads();
-    if (t + 1 < nt) issue(t + 1);
-    const lds_u8* qt = lds + (t & 1) * 2 * TB;
-    const lds_u8* gt = qt + TB;
-    const lds_u8* st = slds + (t & 1) * 2 * (kKT * 4);
+    if (t + 1 < nt) issue(t + 1, 1 - S);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int r0 = rlo + t * kKT + 32 * b;
-      if (!active || r0 >= rows) continue;
-      // last key that the last row of these 32 sees; and the first row
-      if (a.causal && row_token(a, min(r0 + 31, rows - 1)) + off < kw) continue;
-      const bool whole = r0 + 31 < rows && kw + 31 < sq.lk && (!a.causal || kw + 31 <= row_token(a, r0) + off);
+    for (int b = 0; b < RT / 32; ++b) {
+      const int r0 = rlo + t * RT + 32 * b;
+      if (r0 >= rows || r0 + 31 < rw_lo) continue;       // (rw_lo is the largest int without a key)
       f32x16 s, g;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const f32x4 x = *(const lds_f32x4*)(st + 4 * (32 * b + 8 * q + 4 * h));
-        const f32x4 y = *(const lds_f32x4*)(st + 4 * (kKT + 32 * b + 8 * q + 4 * h));
+        const f32x4 y = *(const lds_f32x4*)(st + 256 + 4 * (32 * b + 8 * q + 4 * h));
 #pragma unroll
         for (int e = 0; e < 4; ++e) { s[4 * q + e] = x[e]; g[4 * q + e] = y[e]; }
       }
+      // (operands one step ahead, and no further: the compiler would fetch so
+      // many at once that the keys' registers went to scratch)
+      // (the values' lane offset is formed again for every read: kept for all
+      // of them, it took the registers of the keys, whose reloads from scratch
+      // waited for the copies in flight)
+      int vsa = ln.sa[0] + w * 64 * D;
+      asm volatile("" : "+v"(vsa));
+      auto read_v = [&](int ks) { return *(const lds_i32x4*)(vlds + (vsa ^ (ks << 5))); };
+      i32x4 qa = read_straight<D>(qt, ln, 32 * b, 0), ga = read_straight<D>(gt, ln, 32 * b, 0), va;
+      if constexpr (VL) va = read_v(0);
 #pragma unroll
       for (int ks = 0; ks < NK; ++ks) {
-        s = mfma(read_straight<D>(qt, 32 * b, ks), kf[ks], s);
-        g = mfma(read_straight<D>(gt, 32 * b, ks), vf[ks], g);
+        i32x4 qn, gn, vn;
+        if (ks + 1 < NK) {
+          qn = read_straight<D>(qt, ln, 32 * b, ks + 1);
+          gn = read_straight<D>(gt, ln, 32 * b, ks + 1);
+          if constexpr (VL) vn = read_v(ks + 1);
+        }
+        s = mfma(qa, kf[ks], s);
+        g = mfma(ga, VL ? va : vf[VL ? 0 : ks], g);
+        qa = qn;
+        ga = gn;
+        va = vn;
+        __builtin_amdgcn_sched_barrier(0);
       }
-      if (whole) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) { s[i] = exp2_fast(s[i] * c); g[i] *= s[i]; }
-      } else {
+      if (r0 + 31 >= rows || r0 < rw_hi) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int r = r0 + 8 * (i >> 2) + 4 * h + (i & 3);
-          const bool see = r < rows && j < sq.lk && (!a.causal || j <= row_token(a, min(r, rows - 1)) + off);
-          s[i] = see ? exp2_fast(s[i] * c) : 0.0f;
-          g[i] = see ? g[i] * s[i] : 0.0f;
+          s[i] = (r >= rmin) & (r < rows) ? s[i] : -__builtin_inff();
         }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[i] = exp2_fast(s[i] * c);
+        g[i] *= s[i];
       }
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
         const i32x4 p = pack8(s, 8 * kk), ds = pack8(g, 8 * kk);
 #pragma unroll
         for (int db = 0; db < ND; ++db) {
-          dv[db] = mfma(read_transposed<D>(gt, 32 * b + 16 * kk, db), p, dv[db]);
-          dk[db] = mfma(read_transposed<D>(qt, 32 * b + 16 * kk, db), ds, dk[db]);
+          dv[db] = mfma(read_transposed<D>(gt, ln, 32 * b + 16 * kk, db), p, dv[db]);
+          dk[db] = mfma(read_transposed<D>(qt, ln, 32 * b + 16 * kk, db), ds, dk[db]);
+          if (db & 1) __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
-  }
+  });
+  if (nt == 0) wait_vm<0>();      // (the values' copies, before their LDS is another block's)
   if (j >= sq.lk) return;
   store_cols<ND>(a.dK + (int64_t)(sq.k0 + j) * a.dk_tok + (int64_t)kvh * a.dk_head, dk, a.scale);
   store_cols<ND>(a.dV + (int64_t)(sq.k0 + j) * a.dv_tok + (int64_t)kvh * a.dv_head, dv, 1.0f);
@@ -563,14 +691,20 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
 // Tiles of all sequences at most: see find_seq.
 int64_t attn_row_tiles(int64_t tokens, int64_t mul, int64_t n_seq) { return tokens * mul / kBM + n_seq; }
 
-// Splits of the keys: few rows over many keys leave the chip empty, so the
-// keys are divided until there are about 8 blocks per CU, with at least 128
-// keys each on average.
+// Splits of the keys.  The partial results are written and read once, at 8
+// bytes a value, and joined by another launch, so keys are divided
+//  - for balance, to about 8 blocks per CU of at least 128 keys, as far as the
+//    partials stay below an eighth of the keys' and values' bytes (new tokens
+//    over long contexts);
+//  - to fill the chip, to 2 blocks per CU, where each still gets 512 keys.
 int attn_splits(int64_t tq, int64_t tk, int64_t n_seq, int heads, int kv_heads) {
   const int64_t blocks = attn_row_tiles(tq, heads / kv_heads, n_seq) * kv_heads;
-  if (blocks >= 1024) return 1;
-  const int64_t want = (2048 + blocks - 1) / blocks, most = tk / n_seq / 128;
-  const int64_t s = want < most ? want : most;
+  if (tq == 0 || blocks >= 1024) return 1;
+  auto least = [](int64_t x, int64_t y) { return x < y ? x : y; };
+  const int64_t mean = tk / n_seq;
+  const int64_t even = least(least(2048 / blocks, mean / 128), tk * kv_heads / (16 * tq * heads));
+  const int64_t fill = blocks < 256 ? least(512 / blocks, mean / 512) : 1;
+  const int64_t s = even > fill ? even : fill;
   return s < 1 ? 1 : (int)s;
 }
 

@@ -271,7 +271,8 @@ struct AttnArgs {
   int64_t dq_tok, dq_head, dk_tok, dk_head, dv_tok, dv_head;
   const int32_t *q_start, *k_start;   // [n_seq + 1], or null: one sequence of all tokens
   int tq, tk, n_seq, heads, kv_heads, group;
-  uint32_t gmul;               // r / group = umulhi(r, gmul) >> gshift (group > 1, r < 2^31)
+  // r / group = (umulhi(r, gmul) + (r & gone)) >> gshift for r < 2^31
+  uint32_t gmul, gone;
   int gshift;
   float scale;
   int causal;

@@ -29,6 +29,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kCand = 1024;       // candidates held in LDS
+constexpr int kMaxSplits = 64;    // blocks per row: a lane each when they are joined
 
 __device__ __forceinline__ float inf() { return __builtin_inff(); }
 
@@ -308,28 +309,43 @@ __global__ __launch_bounds__(NT) void logprob_fwd_kernel(LogprobArgs a) {
   }
 }
 
-// Joins the splits of a row: one block per row.
+// Joins the splits of a row (at most 64): one wave per row, a lane per split.
+// Each split's alternatives are in order, so the row's are merged from the
+// lists' heads, one wave maximum each.
 template <typename T>
-__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a) {
-  __shared__ uint64_t cand[kCand];
+__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
+  __shared__ uint64_t lists[kMaxSplits * kMaxTop];
   const int64_t row = blockIdx.x;
-  Stat t{-inf(), 0.0f, 0.0f};
-  for (int s = 0; s < a.splits; ++s) {
-    const float* p = a.part + (row * a.splits + s) * 4;
-    t.join(Stat{p[0], p[1], p[2]});
-  }
-  if (threadIdx.x == 0) {
+  const int lane = threadIdx.x;
+  const bool in = lane < a.splits;
+  const float* p = a.part + (row * a.splits + (in ? lane : 0)) * 4;
+  Stat t{in ? p[0] : -inf(), in ? p[1] : 0.0f, in ? p[2] : 0.0f};
+  const int n = a.splits * a.top;
+  for (int i = lane; i < n; i += 64) lists[i] = a.part_top[row * n + i];
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) t.join(Stat{__shfl_xor(t.m, d, kWave), __shfl_xor(t.s, d, kWave), __shfl_xor(t.w, d, kWave)});
+  if (lane == 0) {
     bool has;
     const float xt = target_logit<T>(a, row, has);
     write_row(a, row, t, xt, has);
   }
   if (a.top == 0) return;
-  const int n = a.splits * a.top;      // at most kCand
-  for (int i = threadIdx.x; i < n; i += 256) cand[i] = a.part_top[row * n + i];
   __syncthreads();
-  rank_out<256>(cand, n, a.top, [&](int rank, uint64_t key) {
-    if (key != 0) write_top(a, row, t, rank, key);
-  });
+  int at = 0;
+  uint64_t head = in ? lists[lane * a.top] : 0;
+  for (int r = 0; r < a.top; ++r) {
+    uint64_t key = head;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+      const uint64_t o = __shfl_xor(key, d, kWave);
+      key = o > key ? o : key;
+    }
+    if (head == key && key != 0) {       // (keys are distinct: one lane)
+      write_top(a, row, t, r, key);
+      ++at;
+      head = at < a.top ? lists[lane * a.top + at] : 0;
+    }
+  }
 }
 
 template <typename T, bool ENT>
@@ -389,12 +405,11 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobArgs a, int seg
 
 }  // namespace
 
-// Blocks per row: enough for about 2 per CU, each of at least 4096 logits, and
-// so few that the joined candidates fit (32 alternatives each).
+// Blocks per row: enough for about 2 per CU, each of at least 4096 logits.
 int logprob_splits(int64_t M, int V) {
   const int64_t want = 512 / (M < 1 ? 1 : M), most = V / 4096;
   int64_t s = want < most ? want : most;
-  if (s > kCand / kMaxTop) s = kCand / kMaxTop;
+  if (s > kMaxSplits) s = kMaxSplits;
   return s < 1 ? 1 : (int)s;
 }
 
@@ -409,7 +424,7 @@ hipError_t launch_logprob_fwd(const LogprobArgs& a, bool bf16, hipStream_t strea
   LaunchStatus st;
   st << launch_kernel(bf16 ? pick(uint16_t{}) : pick(float{}), dim3((unsigned)(a.M * a.splits)), dim3(NT), stream, a);
   if (a.splits > 1)
-    st << launch_kernel(bf16 ? logprob_join_kernel<uint16_t> : logprob_join_kernel<float>, dim3((unsigned)a.M), dim3(256), stream, a);
+    st << launch_kernel(bf16 ? logprob_join_kernel<uint16_t> : logprob_join_kernel<float>, dim3((unsigned)a.M), dim3(64), stream, a);
   return st.e;
 }
 
