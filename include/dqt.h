@@ -289,7 +289,8 @@ dqt_status dqt_logprob_bwd(const void* X, int32_t x_t, int64_t M, int32_t V, int
  *      results but no access outside the tensors.  Tokens outside every
  *      sequence are neither read into another's result nor written.
  *   d: 64 or 128.  heads a multiple of kv_heads, at most 1024.
- *   q_tokens * heads < 2^28; k_tokens and q_tokens * (heads / kv_heads) < 2^31.
+ *   q_tokens * heads and k_tokens < 2^31, and the tiles of 128 rows (keys) of
+ *   all sequences and key heads fewer than 2^24.
  *   scale: 2^-20 .. 2^20.
  * Tensors are strided: token t's head h is the d consecutive values from
  * p + t * token + h * head (elements; multiples of 8, token at most 2^23, head

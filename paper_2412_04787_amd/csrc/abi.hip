@@ -242,8 +242,7 @@ dqt_status check_attn(const dqt_attn* d, dqt::AttnArgs* a) {
   if (d->n_seq < 1 || d->q_tokens < 0 || d->k_tokens < 0) return DQT_ERR_SHAPE;
   const int64_t g = d->heads / d->kv_heads, most = (int64_t(1) << 31) - 1;
   if (d->q_tokens > most || d->k_tokens > most || d->q_tokens * g > most) return DQT_ERR_SHAPE;
-  // (the delta pass has 16 rows per block)
-  if (d->q_tokens * d->heads / 16 >= kMaxBlocks) return DQT_ERR_SHAPE;
+  if (d->q_tokens * d->heads >= (int64_t(1) << 31)) return DQT_ERR_SHAPE;
   const int64_t rt = dqt::attn_row_tiles(d->q_tokens, g, d->n_seq), kt = dqt::attn_row_tiles(d->k_tokens, 1, d->n_seq);
   if (rt * d->kv_heads >= kMaxBlocks || kt * d->kv_heads >= kMaxBlocks) return DQT_ERR_SHAPE;
   if ((d->q_start == nullptr || d->k_start == nullptr) && d->n_seq != 1) return DQT_ERR_NULL;

@@ -56,56 +56,87 @@ struct Seq {
   int tile;             // this block's tile within the sequence
 };
 
-// Sequence s's tiles start at index start * mul / kBM + s (rounded down): the
-// sequence's tiles always fit before the next one's, so blocks find their
-// sequence from the starts alone, whatever the lengths.  Lane-parallel search
-// of the last sequence that starts at or before tile t; false when there is
-// none.  Starts are clamped to the tensors: no value in them leads out of
-// bounds.
 __device__ __forceinline__ int clamp_to(int x, int n) { return x < 0 ? 0 : x > n ? n : x; }
-__device__ __forceinline__ int64_t tile0_of(int start, int n, int mul, int s) {
-  return (int64_t)clamp_to(start, n) * mul / kBM + s;
+// First token and length of sequence s.  Starts are clamped to the tensor: no
+// value in them leads out of bounds.
+__device__ __forceinline__ void span(const int32_t* p, int n, int s, int& first, int& len) {
+  const int b = p == nullptr ? 0 : clamp_to(p[s], n), e = p == nullptr ? n : clamp_to(p[s + 1], n);
+  first = b;
+  len = e > b ? e - b : 0;
 }
+
+// The block's tile: the one of rank p among all sequences' (KEYS: tiles of
+// keys, else of rows), the longest first: under a causal mask row tile d of a
+// sequence reads about d + 1 tiles of keys, and key tile d from the end as many
+// of rows.  False when there are not so many.  (In the order of the sequences
+// the last one's long tiles began when all others had ended: dk/dv of 8 x 2048
+// tokens left 20 % of the chip idle.)
+//
+// Up to 64 sequences, one per lane: with n_s tiles each, sum_s max(0, n_s - d)
+// tiles have depth d or more; d is found by bisection.  More sequences: the
+// list in order, sequence s's tiles from index start * mul / kBM + s (rounded
+// down), which leaves room for all of them.
 template <bool KEYS>
-__device__ __forceinline__ bool find_seq(const AttnArgs& a, int t, Seq& q) {
+__device__ __forceinline__ bool find_tile(const AttnArgs& a, int p, Seq& q) {
+  const int lane = threadIdx.x & (kWave - 1);
   const int32_t* starts = KEYS ? a.k_start : a.q_start;
   const int n_tok = KEYS ? a.tk : a.tq, mul = KEYS ? 1 : a.group;
-  const int lane = threadIdx.x & (kWave - 1);
-  int lo = 0, hi = a.n_seq;
-  if (starts != nullptr) {
-    while (hi - lo > 1) {
-      const int step = (hi - lo + kWave - 1) / kWave;
-      const int s = lo + lane * step;
-      const bool at = s < hi && tile0_of(starts[s < hi ? s : lo], n_tok, mul, s) <= t;
-      const int cnt = __popcll(__ballot(at));
-      if (cnt == 0) return false;
-      lo = lo + (cnt - 1) * step;
-      hi = min(hi, lo + step);
+  if (a.n_seq <= kWave) {
+    Seq v{0, 0, 0, 0, 0};
+    if (lane < a.n_seq) {
+      span(a.q_start, a.tq, lane, v.q0, v.lq);
+      span(a.k_start, a.tk, lane, v.k0, v.lk);
     }
+    const int n = (int)(((int64_t)(KEYS ? v.lk : v.lq) * mul + kBM - 1) / kBM);
+    int bits = 0;                      // of the largest n
+    while (__ballot((n >> bits) != 0) != 0) ++bits;
+    // tiles of depth d or more, as a sum over the bits of n - d
+    auto count = [&](int d) {
+      const int x = max(0, n - d);
+      int64_t sum = 0;
+      for (int b = 0; b < bits; ++b) sum += (int64_t)__popcll(__ballot((x >> b) & 1)) << b;
+      return sum;
+    };
+    if (count(0) <= p) return false;
+    int d = 0;                         // the largest d with count(d) > p
+    for (int b = bits - 1; b >= 0; --b)
+      if (count(d + (1 << b)) > p) d += 1 << b;
+    const int at = (int)(p - count(d + 1));
+    const unsigned long long deep = __ballot(n > d);
+    const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(deep >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)deep, 0));
+    const int s = __builtin_ctzll(__ballot(n > d && before == at));
+    q.q0 = __builtin_amdgcn_readlane(v.q0, s);
+    q.lq = __builtin_amdgcn_readlane(v.lq, s);
+    q.k0 = __builtin_amdgcn_readlane(v.k0, s);
+    q.lk = __builtin_amdgcn_readlane(v.lk, s);
+    q.tile = KEYS ? __builtin_amdgcn_readlane(n, s) - 1 - d : d;
+    return true;
+  }
+  auto first_tile = [&](int s) { return (int64_t)clamp_to(starts[s], n_tok) * mul / kBM + s; };
+  int lo = 0, hi = a.n_seq;            // the last sequence whose tiles start at or before p
+  while (hi - lo > 1) {
+    const int step = (hi - lo + kWave - 1) / kWave;
+    const int s = lo + lane * step;
+    const int cnt = __popcll(__ballot(s < hi && first_tile(min(s, hi - 1)) <= p));
+    if (cnt == 0) return false;
+    lo = lo + (cnt - 1) * step;
+    hi = min(hi, lo + step);
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
-  auto span = [&](const int32_t* p, int n, int& first, int& len) {
-    const int b = p == nullptr ? 0 : clamp_to(p[lo], n), e = p == nullptr ? n : clamp_to(p[lo + 1], n);
-    first = __builtin_amdgcn_readfirstlane(b);
-    len = __builtin_amdgcn_readfirstlane(e > b ? e - b : 0);
-  };
-  span(a.q_start, a.tq, q.q0, q.lq);
-  span(a.k_start, a.tk, q.k0, q.lk);
-  const int64_t first = tile0_of(KEYS ? q.k0 : q.q0, n_tok, mul, lo);
-  q.tile = (int)(t - first);
+  int x[4];
+  span(a.q_start, a.tq, lo, x[0], x[1]);
+  span(a.k_start, a.tk, lo, x[2], x[3]);
+  q.q0 = __builtin_amdgcn_readfirstlane(x[0]);
+  q.lq = __builtin_amdgcn_readfirstlane(x[1]);
+  q.k0 = __builtin_amdgcn_readfirstlane(x[2]);
+  q.lk = __builtin_amdgcn_readfirstlane(x[3]);
+  q.tile = __builtin_amdgcn_readfirstlane((int)(p - first_tile(lo)));
   return q.tile >= 0;
 }
 
 // row r of a sequence -> token and head within the group (r / G, r % G)
 __device__ __forceinline__ int row_token(const AttnArgs& a, int r) {
   return (int)((__umulhi((uint32_t)r, a.gmul) + ((uint32_t)r & a.gone)) >> a.gshift);
-}
-
-// Blocks go to the 8 XCDs in turn; XCD x takes the x-th eighth of the list, so
-// that the blocks that read one head's keys share an L2.
-__device__ __forceinline__ int xcd_order(int b, int n) {
-  const int per = n / 8;
-  return b < 8 * per ? (b & 7) * per + (b >> 3) : b;
 }
 
 // This lane's byte offsets of the operand reads from a tile.
@@ -143,6 +174,12 @@ __device__ __forceinline__ i32x4 read_transposed(const lds_u8* tile, const Lanes
 }
 __device__ __forceinline__ f32x16 mfma(i32x4 a, i32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// (the builtin first makes every operand a quiet NaN: twice the instructions)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 // 8 scores -> B operand (rounded to bf16, as every operand of the second
@@ -191,32 +228,31 @@ struct Stager {
   }
 };
 // Keys and values of tile after tile: rows past the last key repeat it.
-template <int D>
+template <int D, int KT>
 struct KeyStream {
   const uint8_t *kp, *vp;
   int64_t k_tok, v_tok;
   int lk;
-  Stager<D, kKT> ks, vs;
+  Stager<D, KT> ks, vs;
   __device__ __forceinline__ KeyStream(const AttnArgs& a, const Seq& q, int kvh)
       : kp(a.K + (int64_t)q.k0 * a.k_tok + (int64_t)kvh * a.k_head),
         vp(a.V + (int64_t)q.k0 * a.v_tok + (int64_t)kvh * a.v_head), k_tok(a.k_tok), v_tok(a.v_tok), lk(q.lk) {
     ks.set([&](int row) { return (uint32_t)row * (uint32_t)k_tok; });
     vs.set([&](int row) { return (uint32_t)row * (uint32_t)v_tok; });
   }
-  __device__ __forceinline__ void issue(int k0, lds_u8* kt, lds_u8* vt) const {
-    const uint8_t *kb = kp + (int64_t)k0 * k_tok, *vb = vp + (int64_t)k0 * v_tok;
-    if (k0 + kKT <= lk) {
-      ks.issue(kb, kt);
-      vs.issue(vb, vt);
+  __device__ __forceinline__ void issue(const uint8_t* p, int64_t tok, const Stager<D, KT>& st, int k0, lds_u8* tile) const {
+    const uint8_t* base = p + (int64_t)k0 * tok;
+    if (k0 + KT <= lk) {
+      st.issue(base, tile);
     } else {
-      Stager<D, kKT> e;
+      Stager<D, KT> e;
       const int last = lk - 1 - k0;
-      e.set([&](int row) { return (uint32_t)min(row, last) * (uint32_t)k_tok; });
-      e.issue(kb, kt);
-      e.set([&](int row) { return (uint32_t)min(row, last) * (uint32_t)v_tok; });
-      e.issue(vb, vt);
+      e.set([&](int row) { return (uint32_t)min(row, last) * (uint32_t)tok; });
+      e.issue(base, tile);
     }
   }
+  __device__ __forceinline__ void issue_k(int k0, lds_u8* tile) const { issue(kp, k_tok, ks, k0, tile); }
+  __device__ __forceinline__ void issue_v(int k0, lds_u8* tile) const { issue(vp, v_tok, vs, k0, tile); }
 };
 // f(t, stage) for t = 0 .. n - 1 with the stage t % 2 a constant, so that
 // tile addresses fold into the reads' offsets
@@ -245,17 +281,16 @@ __device__ __forceinline__ void store_cols(uint8_t* p, const f32x16 (&o)[ND], fl
 // ------------------------------------------------------------------ forward
 template <int D>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
-  constexpr int NK = D / 16, ND = D / 32, TB = kKT * D * 2;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2][TB];
-  lds_u8* lds = (lds_u8*)&smem[0][0][0];
+  constexpr int NK = D / 16, ND = D / 32, KT = 64, NB = KT / 32, TB = KT * D * 2;
+  constexpr bool PIPE = D == 64;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[4][TB];       // keys of two tiles, values of two
+  lds_u8* lds = (lds_u8*)&smem[0][0];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const int id = xcd_order(blockIdx.x, gridDim.x);
-  const int per_head = a.row_tiles * a.splits;
-  const int kvh = id / per_head, rem = id - kvh * per_head;
-  const int split = rem % a.splits;
+  // (blocks go to the 8 XCDs in turn: with 8 or 16 key heads each head's keys
+  // stay with one XCD's L2)
+  const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.splits;
   Seq sq;
-  // (last tiles first: under a causal mask they are the longest)
-  if (!find_seq<false>(a, a.row_tiles - 1 - rem / a.splits, sq)) return;
+  if (!find_tile<false>(a, rest / a.splits, sq)) return;
   const int rows = sq.lq * a.group, r0 = sq.tile * kBM;
   if (r0 >= rows) return;
   const int off = sq.lk - sq.lq;
@@ -263,7 +298,6 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   // this lane's row
   const int r = r0 + 32 * w + (lane & 31), rc = min(r, rows - 1);
   const int tok = row_token(a, rc), head = kvh * a.group + (rc - tok * a.group);
-  const bool active = r0 + 32 * w < rows;
   // keys of this block: all that its last row sees, of this split
   int kend = sq.lk;
   if (a.causal) kend = min(kend, row_token(a, min(r0 + kBM, rows) - 1) + off + 1);
@@ -273,13 +307,14 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
     kbeg = (int)min((int64_t)split * per, (int64_t)sq.lk);
     kend = min(kend, kbeg + per);
   }
-  const int nt = kend > kbeg ? (kend - kbeg + kKT - 1) / kKT : 0;
+  const int nt = kend > kbeg ? (kend - kbeg + KT - 1) / KT : 0;
   const int lim = min(a.causal ? tok + off : sq.lk - 1, kend - 1);      // last key this row sees
-  const int lim_lo = __builtin_amdgcn_readlane(lim, 0), lim_hi = __builtin_amdgcn_readlane(lim, 31);
+  // (those of the wave's first and last row; a wave without rows sees none)
+  const int lim_lo = __builtin_amdgcn_readlane(lim, 0), lim_hi = r0 + 32 * w < rows ? __builtin_amdgcn_readlane(lim, 31) : -1;
 
   const Lanes<D> ln;
-  const KeyStream<D> keys(a, sq, kvh);
-  if (nt > 0) keys.issue(kbeg, lds, lds + TB);
+  const KeyStream<D, KT> keys(a, sq, kvh);
+  if (nt > 0) keys.issue_k(kbeg, lds);
 
   i32x4 qf[NK];
   const uint8_t* qp = a.Q + (int64_t)(sq.q0 + tok) * a.q_tok + (int64_t)head * a.q_head;
@@ -290,36 +325,66 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
 #pragma unroll
   for (int db = 0; db < ND; ++db) o[db] = splat(0.0f);
   const float c = a.scale * kLog2e;
-  float m = -__builtin_inff(), l = 0.0f;      // running maximum (of c q.k), sum of exp2
+  // m: what the exponents are relative to, a maximum of c q.k so far; l: their
+  // sum.  m moves only when the maximum passes it by 2^8: powers up to 2^8 lose
+  // nothing, and in every tile some row's maximum moves a little (scaling o
+  // each time was a fifth of the vector work).
+  constexpr float kSlack = 8.0f;
+  float m = -__builtin_inff(), l = 0.0f;
+  // tiles that a row of this wave sees
+  const int mine = min(nt, lim_hi < kbeg ? 0 : (lim_hi - kbeg) / KT + 1);
 
+  // D = 64 (PIPE): the scores of tile t + 1 are formed while those of tile t go
+  // through the exponential, keys staged two tiles ahead, values one (12 heads
+  // of packed documents 37 -> 35 us).  D = 128 leaves no registers for two
+  // tiles' scores (spilled 330 us, 32 keys a tile 231, one tile at a time 175 at
+  // 8 x 2048, 16 heads).
+  f32x16 s[NB];
+  auto scores = [&](const lds_u8* kt, f32x16 (&z)[NB]) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) z[b] = splat(0.0f);
+#pragma unroll
+    for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) z[b] = mfma(read_straight<D>(kt, ln, 32 * b, ks), qf[ks], z[b]);
+  };
+  if (nt > 0) {
+    keys.issue_v(kbeg, lds + 2 * TB);
+    if constexpr (PIPE) {
+      if (nt > 1) keys.issue_k(kbeg + KT, lds + TB);
+      wait_vm<0>();
+      __syncthreads();
+      if (mine > 0) scores(lds, s);
+    }
+  }
   staged_loop(nt, [&](int t, auto stage) {
     constexpr int S = decltype(stage)::value;
-    const lds_u8 *kt = lds + S * 2 * TB, *vt = kt + TB;
-    const int k0 = kbeg + t * kKT;
+    const lds_u8 *kn = lds + (PIPE ? 1 - S : S) * TB, *vt = lds + (2 + S) * TB;
+    const int k0 = kbeg + t * KT;
     wait_vm<0>();
-    __syncthreads();
-    if (t + 1 < nt) keys.issue(k0 + kKT, lds + (1 - S) * 2 * TB, lds + (1 - S) * 2 * TB + TB);
-    if (!active || k0 > lim_hi) return;
-    f32x16 s[2] = {splat(0.0f), splat(0.0f)};
+    __syncthreads();          // (t = 0: every wave has read the first keys)
+    if (t + 1 + PIPE < nt) keys.issue_k(k0 + (1 + PIPE) * KT, lds + (PIPE ? S : 1 - S) * TB);
+    if (t + 1 < nt) keys.issue_v(k0 + KT, lds + (3 - S) * TB);
+    if (t >= mine) return;
+    if constexpr (!PIPE) scores(kn, s);
+    if (k0 + KT - 1 > lim_lo) {
 #pragma unroll
-    for (int ks = 0; ks < NK; ++ks) {
-      s[0] = mfma(read_straight<D>(kt, ln, 0, ks), qf[ks], s[0]);
-      s[1] = mfma(read_straight<D>(kt, ln, 32, ks), qf[ks], s[1]);
-    }
-    if (k0 + kKT - 1 > lim_lo) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int j = k0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3);
           s[b][i] = j <= lim ? s[b][i] : -__builtin_inff();
         }
     }
-    float mx = fmaxf(s[0][0], s[1][0]);
+    float mx = max3(s[0][0], s[0][1], s[0][2]), my = max3(s[0][3], s[0][4], s[0][5]);
 #pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, fmaxf(s[0][i], s[1][i]));
+    for (int i = 6; i < 16 * NB; i += 4) {
+      mx = max3(mx, s[i / 16][i % 16], s[i / 16][i % 16 + 1]);
+      if (i + 2 < 16 * NB) my = max3(my, s[(i + 2) / 16][(i + 2) % 16], s[(i + 2) / 16][(i + 2) % 16 + 1]);
+    }
+    mx = fmaxf(mx, my);
     mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * c;
-    if (__any(mx > m)) {
+    if (__any(mx > m + kSlack)) {
       const float mn = fmaxf(m, mx);
       const float f = exp2_fast(m - (mn == -__builtin_inff() ? 0.0f : mn));
       m = mn;
@@ -329,20 +394,38 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] *= f;
     }
-    const float mu = m == -__builtin_inff() ? 0.0f : m;
+    const float mu0 = m == -__builtin_inff() ? 0.0f : m;
+    auto rest = [&](auto more) {
+      constexpr bool MORE = decltype(more)::value;
+      // (apart from each other: the compiler would take what both branches
+      // share, the exponentials, out of them and before the products)
+      float mu = mu0;
+      if constexpr (MORE) asm volatile("; more" : "+v"(mu));
+      else asm volatile("; last" : "+v"(mu));
+      f32x16 z[NB];
+      if constexpr (MORE) scores(kn, z);
+      float sum = 0.0f;
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[b][i] = exp2_fast(__builtin_fmaf(s[b][i], c, -mu));
-        l += s[b][i];
+        for (int i = 0; i < 16; ++i) {
+          s[b][i] = exp2_fast(__builtin_fmaf(s[b][i], c, -mu));
+          sum += s[b][i];
+        }
+      l += sum;
+#pragma unroll
+      for (int kk = 0; kk < 2 * NB; ++kk) {
+        const i32x4 p = pack8(s[kk >> 1], 8 * (kk & 1));
+#pragma unroll
+        for (int db = 0; db < ND; ++db) o[db] = mfma(read_transposed<D>(vt, ln, 16 * kk, db), p, o[db]);
       }
+      if constexpr (MORE) {
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      const i32x4 p = pack8(s[kk >> 1], 8 * (kk & 1));
-#pragma unroll
-      for (int db = 0; db < ND; ++db) o[db] = mfma(read_transposed<D>(vt, ln, 16 * kk, db), p, o[db]);
-    }
+        for (int b = 0; b < NB; ++b) s[b] = z[b];
+      }
+    };
+    if (PIPE && t + 1 < mine) rest(std::integral_constant<bool, PIPE>{});
+    else rest(std::false_type{});
   });
   l += __shfl_xor(l, 32, kWave);
   if (r >= rows) return;
@@ -416,50 +499,18 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
 }
 
 // ------------------------------------------------------------------ backward
-// Per row, in row order [kv head][token * G + head in group]: -lse / c, from
-// which a score's accumulator starts (so that the product ends as
-// q.k - lse / c), and -do.o, from which do.v starts.  16 lanes per row.
-template <int D>
-__global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
-  const int64_t all = (int64_t)a.heads * a.tq;
-  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  const int i = threadIdx.x & 15;
-  if (row >= all) return;
-  const int64_t per = (int64_t)a.tq * a.group;
-  const int kvh = (int)(row / per);
-  const int64_t rr = row - kvh * per;
-  const int tok = (int)(rr / a.group), head = kvh * a.group + (int)(rr - (int64_t)tok * a.group);
-  float s = 0.0f;
-  const uint8_t* op = a.O + (int64_t)tok * a.o_tok + (int64_t)head * a.o_head;
-  const uint8_t* gp = a.dO + (int64_t)tok * a.do_tok + (int64_t)head * a.do_head;
-  constexpr int E = D / 16;      // values per lane: 8 or 4
-#pragma unroll
-  for (int e = 0; e < E / 4; ++e) {
-    const uint2 x = *reinterpret_cast<const uint2*>(op + 2 * E * i + 8 * e);
-    const uint2 y = *reinterpret_cast<const uint2*>(gp + 2 * E * i + 8 * e);
-    s += bf16_bits_to_f32(x.x & 0xFFFFu) * bf16_bits_to_f32(y.x & 0xFFFFu);
-    s += bf16_bits_to_f32(x.x >> 16) * bf16_bits_to_f32(y.x >> 16);
-    s += bf16_bits_to_f32(x.y & 0xFFFFu) * bf16_bits_to_f32(y.y & 0xFFFFu);
-    s += bf16_bits_to_f32(x.y >> 16) * bf16_bits_to_f32(y.y >> 16);
-  }
-#pragma unroll
-  for (int d = 8; d > 0; d >>= 1) s += __shfl_xor(s, d, 16);
-  if (i == 0) {
-    a.neg_lse[row] = -a.lse[(int64_t)head * a.tq + tok] / a.scale;
-    a.neg_delta[row] = -s;
-  }
-}
-
+// dq, and per row, for dk/dv, in row order [kv head][token * G + head in
+// group]: -lse / c, from which a score's accumulator starts (so that the product
+// ends as q.k - lse / c), and -do.o, from which do.v starts.
 template <int D>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   constexpr int NK = D / 16, ND = D / 32, TB = kKT * D * 2;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2][TB];
   lds_u8* lds = (lds_u8*)&smem[0][0][0];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const int id = xcd_order(blockIdx.x, gridDim.x);
-  const int kvh = id / a.row_tiles;
+  const int kvh = blockIdx.x % a.kv_heads;
   Seq sq;
-  if (!find_seq<false>(a, a.row_tiles - 1 - (id - kvh * a.row_tiles), sq)) return;
+  if (!find_tile<false>(a, blockIdx.x / a.kv_heads, sq)) return;
   const int rows = sq.lq * a.group, r0 = sq.tile * kBM;
   if (r0 >= rows) return;
   const int off = sq.lk - sq.lq;
@@ -473,8 +524,11 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   const int lim_lo = __builtin_amdgcn_readlane(lim, 0), lim_hi = __builtin_amdgcn_readlane(lim, 31);
 
   const Lanes<D> ln;
-  const KeyStream<D> keys(a, sq, kvh);
-  if (nt > 0) keys.issue(0, lds, lds + TB);
+  const KeyStream<D, kKT> keys(a, sq, kvh);
+  if (nt > 0) {
+    keys.issue_k(0, lds);
+    keys.issue_v(0, lds + TB);
+  }
   i32x4 qf[NK], gf[NK];
   const uint8_t* qp = a.Q + (int64_t)(sq.q0 + tok) * a.q_tok + (int64_t)head * a.q_head;
   const uint8_t* gp = a.dO + (int64_t)(sq.q0 + tok) * a.do_tok + (int64_t)head * a.do_head;
@@ -483,8 +537,24 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     qf[ks] = *reinterpret_cast<const i32x4*>(qp + 32 * ks + 16 * h);
     gf[ks] = *reinterpret_cast<const i32x4*>(gp + 32 * ks + 16 * h);
   }
-  const int64_t at = ((int64_t)kvh * a.tq + sq.q0) * a.group + rc;
-  const float nl = a.neg_lse[at], nd = a.neg_delta[at];
+  float nd = 0.0f;
+  const uint8_t* op = a.O + (int64_t)(sq.q0 + tok) * a.o_tok + (int64_t)head * a.o_head;
+#pragma unroll
+  for (int ks = 0; ks < NK; ++ks) {
+    const i32x4 x = *reinterpret_cast<const i32x4*>(op + 32 * ks + 16 * h);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      nd -= bf16_bits_to_f32((uint32_t)x[e] & 0xFFFFu) * bf16_bits_to_f32((uint32_t)gf[ks][e] & 0xFFFFu);
+      nd -= __uint_as_float((uint32_t)x[e] & 0xFFFF0000u) * __uint_as_float((uint32_t)gf[ks][e] & 0xFFFF0000u);
+    }
+  }
+  nd += __shfl_xor(nd, 32, kWave);
+  const float nl = -a.lse[(int64_t)head * a.tq + sq.q0 + tok] / a.scale;
+  if (h == 0 && r < rows) {
+    const int64_t at = ((int64_t)kvh * a.tq + sq.q0) * a.group + r;
+    a.neg_lse[at] = nl;
+    a.neg_delta[at] = nd;
+  }
   const float c = a.scale * kLog2e;
   f32x16 dq[ND];
 #pragma unroll
@@ -495,29 +565,40 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     const lds_u8 *kt = lds + S * 2 * TB, *vt = kt + TB;
     wait_vm<0>();
     __syncthreads();
-    if (t + 1 < nt) keys.issue((t + 1) * kKT, lds + (1 - S) * 2 * TB, lds + (1 - S) * 2 * TB + TB);
+    if (t + 1 < nt) {
+      keys.issue_k((t + 1) * kKT, lds + (1 - S) * 2 * TB);
+      keys.issue_v((t + 1) * kKT, lds + (1 - S) * 2 * TB + TB);
+    }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const int k0 = t * kKT + 32 * b;
       if (!active || k0 > lim_hi) continue;
-      f32x16 s = splat(nl), g = splat(nd);
+      f32x16 s = splat(nl);
+      int sa = ln.sa[0];
+      if constexpr (D == 128) asm volatile("" : "+v"(sa));
+      auto straight = [&](const lds_u8* tile, int ks) { return *(const lds_i32x4*)(tile + (sa ^ (ks << 5)) + 64 * b * D); };
 #pragma unroll
-      for (int ks = 0; ks < NK; ++ks) {
-        s = mfma(read_straight<D>(kt, ln, 32 * b, ks), qf[ks], s);
-        g = mfma(read_straight<D>(vt, ln, 32 * b, ks), gf[ks], g);
-      }
+      for (int ks = 0; ks < NK; ++ks) s = mfma(straight(kt, ks), qf[ks], s);
       if (k0 + 31 > lim_lo) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = k0 + 8 * (i >> 2) + 4 * h + (i & 3) <= lim ? s[i] : -__builtin_inff();
       }
+      // do.v runs while p is formed
+      __builtin_amdgcn_sched_barrier(0);
+      f32x16 g = splat(nd);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) g[i] *= exp2_fast(s[i] * c);
+      for (int ks = 0; ks < NK; ++ks) g = mfma(straight(vt, ks), gf[ks], g);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = exp2_fast(s[i] * c);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) g[i] *= s[i];
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
         const i32x4 p = pack8(g, 8 * kk);
 #pragma unroll
         for (int db = 0; db < ND; ++db) dq[db] = mfma(read_transposed<D>(kt, ln, 32 * b + 16 * kk, db), p, dq[db]);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
   });
   if (r >= rows) return;
@@ -539,11 +620,9 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
   lds_u8* slds = (lds_u8*)&stat[0][0][0];
   lds_u8* vlds = (lds_u8*)&vtile[0];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const int id = xcd_order(blockIdx.x, gridDim.x);
-  const int kvh = id / a.key_tiles;
+  const int kvh = blockIdx.x % a.kv_heads;
   Seq sq;
-  // (first tiles first: under a causal mask the most rows see them)
-  if (!find_seq<true>(a, id - kvh * a.key_tiles, sq)) return;
+  if (!find_tile<true>(a, blockIdx.x / a.kv_heads, sq)) return;
   const int k0 = sq.tile * kBM;
   if (k0 >= sq.lk) return;
   const int rows = sq.lq * a.group, off = sq.lk - sq.lq;
@@ -623,39 +702,30 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
     for (int b = 0; b < RT / 32; ++b) {
       const int r0 = rlo + t * RT + 32 * b;
       if (r0 >= rows || r0 + 31 < rw_lo) continue;       // (rw_lo is the largest int without a key)
-      f32x16 s, g;
+      auto read_stat = [&](int off) {
+        f32x16 v;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x4 x = *(const lds_f32x4*)(st + 4 * (32 * b + 8 * q + 4 * h));
-        const f32x4 y = *(const lds_f32x4*)(st + 256 + 4 * (32 * b + 8 * q + 4 * h));
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 x = *(const lds_f32x4*)(st + off + 4 * (32 * b + 8 * q + 4 * h));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { s[4 * q + e] = x[e]; g[4 * q + e] = y[e]; }
-      }
-      // (operands one step ahead, and no further: the compiler would fetch so
-      // many at once that the keys' registers went to scratch)
-      // (the values' lane offset is formed again for every read: kept for all
-      // of them, it took the registers of the keys, whose reloads from scratch
-      // waited for the copies in flight)
-      int vsa = ln.sa[0] + w * 64 * D;
-      asm volatile("" : "+v"(vsa));
-      auto read_v = [&](int ks) { return *(const lds_i32x4*)(vlds + (vsa ^ (ks << 5))); };
-      i32x4 qa = read_straight<D>(qt, ln, 32 * b, 0), ga = read_straight<D>(gt, ln, 32 * b, 0), va;
-      if constexpr (VL) va = read_v(0);
-#pragma unroll
-      for (int ks = 0; ks < NK; ++ks) {
-        i32x4 qn, gn, vn;
-        if (ks + 1 < NK) {
-          qn = read_straight<D>(qt, ln, 32 * b, ks + 1);
-          gn = read_straight<D>(gt, ln, 32 * b, ks + 1);
-          if constexpr (VL) vn = read_v(ks + 1);
+          for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
         }
-        s = mfma(qa, kf[ks], s);
-        g = mfma(ga, VL ? va : vf[VL ? 0 : ks], g);
-        qa = qn;
-        ga = gn;
-        va = vn;
-        __builtin_amdgcn_sched_barrier(0);
-      }
+        return v;
+      };
+      // (D = 128: a straight read's lane offset is formed again each time; kept
+      // for all of them they would take the registers of the keys, whose reload
+      // from scratch waits for the copies in flight)
+      auto fresh = [&](int x) {
+        if constexpr (VL) asm volatile("" : "+v"(x));
+        return x;
+      };
+      auto straight = [&](const lds_u8* tile, int sa, int ks) {
+        return VL ? *(const lds_i32x4*)(tile + (sa ^ (ks << 5))) : read_straight<D>(tile, ln, 32 * b, ks);
+      };
+      f32x16 s = read_stat(0);
+      const int qsa = fresh(ln.sa[0]);
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks) s = mfma(straight(qt, qsa, ks), kf[ks], s);
       if (r0 + 31 >= rows || r0 < rw_hi) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -663,20 +733,31 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
           s[i] = (r >= rmin) & (r < rows) ? s[i] : -__builtin_inff();
         }
       }
+      const int gsa = fresh(ln.sa[0]), vsa = fresh(ln.sa[0] + w * 64 * D);
+      // From here on the matrix cores always have a product that does not wait
+      // for the arithmetic beside it: do.v while p is formed, dv while g is, dk.
+      __builtin_amdgcn_sched_barrier(0);
+      f32x16 g = read_stat(256);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[i] = exp2_fast(s[i] * c);
-        g[i] *= s[i];
+      for (int ks = 0; ks < NK; ++ks) {
+        const i32x4 vv = VL ? straight(vlds, vsa, ks) : vf[VL ? 0 : ks];
+        g = mfma(straight(gt, gsa, ks), vv, g);
       }
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        const i32x4 p = pack8(s, 8 * kk), ds = pack8(g, 8 * kk);
+      for (int i = 0; i < 16; ++i) s[i] = exp2_fast(s[i] * c);
 #pragma unroll
-        for (int db = 0; db < ND; ++db) {
-          dv[db] = mfma(read_transposed<D>(gt, ln, 32 * b + 16 * kk, db), p, dv[db]);
-          dk[db] = mfma(read_transposed<D>(qt, ln, 32 * b + 16 * kk, db), ds, dk[db]);
-          if (db & 1) __builtin_amdgcn_sched_barrier(0);
-        }
+      for (int kk = 0; kk < 2; ++kk) {
+        const i32x4 p = pack8(s, 8 * kk);
+#pragma unroll
+        for (int db = 0; db < ND; ++db) dv[db] = mfma(read_transposed<D>(gt, ln, 32 * b + 16 * kk, db), p, dv[db]);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) g[i] *= s[i];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        const i32x4 ds = pack8(g, 8 * kk);
+#pragma unroll
+        for (int db = 0; db < ND; ++db) dk[db] = mfma(read_transposed<D>(qt, ln, 32 * b + 16 * kk, db), ds, dk[db]);
       }
     }
   });
@@ -688,7 +769,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
 
 }  // namespace
 
-// Tiles of all sequences at most: see find_seq.
+// Tiles of all sequences at most (each has at most one that is not full).
 int64_t attn_row_tiles(int64_t tokens, int64_t mul, int64_t n_seq) { return tokens * mul / kBM + n_seq; }
 
 // Splits of the keys.  The partial results are written and read once, at 8
@@ -721,12 +802,9 @@ hipError_t launch_attn_fwd(int d, AttnArgs a, hipStream_t stream) {
 hipError_t launch_attn_bwd(int d, AttnArgs a, hipStream_t stream) {
   const dim3 block(256);
   LaunchStatus st;
-  if (a.tq > 0) {
-    st << launch_kernel(d == 128 ? attn_delta_kernel<128> : attn_delta_kernel<64>,
-                        dim3((unsigned)(((int64_t)a.heads * a.tq + 15) / 16)), block, stream, a);
+  if (a.tq > 0)
     st << launch_kernel(d == 128 ? attn_dq_kernel<128> : attn_dq_kernel<64>,
                         dim3((unsigned)((int64_t)a.row_tiles * a.kv_heads)), block, stream, a);
-  }
   if (a.tk > 0)
     st << launch_kernel(d == 128 ? attn_dkv_kernel<128> : attn_dkv_kernel<64>,
                         dim3((unsigned)((int64_t)a.key_tiles * a.kv_heads)), block, stream, a);
