@@ -730,7 +730,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int r = r0 + 8 * (i >> 2) + 4 * h + (i & 3);
-          s[i] = (r >= rmin) & (r < rows) ? s[i] : -__builtin_inff();
+          s[i] = (r >= rmin && r < rows) ? s[i] : -__builtin_inff();
         }
       }
       const int gsa = fresh(ln.sa[0]), vsa = fresh(ln.sa[0] + w * 64 * D);

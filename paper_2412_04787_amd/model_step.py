@@ -22,6 +22,13 @@ What runs where:
     trained by AdamW, as BitNet-style models keep them), causal attention
     (PyTorch's flash kernels), the rotary embedding, SiLU, the residual adds,
     the backward of the norms and the loss.
+  * With own_ops, attention, the SwiGLU product and the loss run in this
+    library too: dqt_attn_fwd / _bwd take documents of different lengths packed
+    into the batch and grouped key heads; dqt_swiglu_act_quant feeds the down
+    projection and keeps gate and up as 8-bit checkpoints, from which
+    dqt_swiglu_backward takes their gradients (2 bytes per element of a token's
+    feed-forward held for the backward, 6 in PyTorch); dqt_logprob_fwd / _bwd
+    give the loss and the logits' gradient.
 
 Initialisation (untimed): codes by Eq. 2-4 for the ternary grid from
 W0 ~ N(0, 0.02) (alpha = mean |W0|, q = Clip(Round(W0 / alpha), -1, 1));
@@ -50,6 +57,16 @@ class ModelConfig:
     eps: float = 1e-6
     rope_base: float = 10000.0
     seed: int = 0
+    kv_heads: int = 0          # key heads (0: as many as heads); fewer need own_ops
+    own_ops: bool = False      # attention, SwiGLU and loss in this library's kernels
+
+    def __post_init__(self):
+        if self.kv_heads and (self.heads % self.kv_heads or (self.kv_heads != self.heads and not self.own_ops)):
+            raise ValueError("kv_heads must divide heads, and grouped heads need own_ops")
+
+    @property
+    def n_kv(self) -> int:
+        return self.kv_heads or self.heads
 
     @property
     def tokens(self) -> int:
@@ -59,7 +76,8 @@ class ModelConfig:
         """(group name, [(linear name, d_in, d_out)]) of one block; linears in
         one group share their input."""
         h, f = self.hidden, self.ffn
-        return [("attn_in", [("q", h, h), ("k", h, h), ("v", h, h)]),
+        kv = h // self.heads * self.n_kv
+        return [("attn_in", [("q", h, h), ("k", h, kv), ("v", h, kv)]),
                 ("attn_out", [("o", h, h)]),
                 ("mlp_in", [("gate", h, f), ("up", h, f)]),
                 ("mlp_hidden", [("down", f, h)])]
@@ -86,6 +104,11 @@ MODELS = {
     # a small model of the same structure, for tests
     "tiny": ModelConfig(name="tiny", layers=2, hidden=256, heads=4, ffn=512, vocab=1000,
                         batch=2, seq=128, lr=3e-4),
+    # the same two with attention, SwiGLU and loss in this library's kernels
+    "llama24_h2048_ops": ModelConfig(name="llama24_h2048_ops", layers=24, hidden=2048, heads=16,
+                                     ffn=5632, vocab=32000, batch=8, seq=2048, lr=3e-4, own_ops=True),
+    "tiny_ops": ModelConfig(name="tiny_ops", layers=2, hidden=256, heads=4, kv_heads=2, ffn=512,
+                            vocab=1000, batch=2, seq=128, lr=3e-4, own_ops=True),
 }
 
 
@@ -125,6 +148,36 @@ class _Group:
             self.weights.append(dqt.weight(d_out, d_in, dqt.DQT_TERNARY2, -1, 1, alpha, tid))
 
 
+def _group_fwd(grp, Xq, xdq):
+    """The group's linears on their quantised input: bf16 outputs."""
+    torch = dqt._torch()
+    T = Xq.shape[0]
+    Ys = [torch.empty((T, d_out), dtype=torch.bfloat16, device=Xq.device) for d_out in grp.d_outs]
+    io = dqt.linear_io([dict(w=w, Wq=c, Xq=Xq, xdq=xdq, Y=Y)
+                        for w, c, Y in zip(grp.weights, grp.codes, Ys)])
+    dqt.dqt_linear_fwd_batch(io, T, dqt.DQT_I8, dqt.DQT_BF16,
+                             grp.model.workspace(dqt.dqt_linear_fwd_batch_workspace(io)))
+    return Ys
+
+
+def _group_bwd(grp, Xq, xdq, dYs):
+    """dX of each of the group's linears (bf16); the codes are updated by Eq. 5."""
+    torch = dqt._torch()
+    m = grp.model
+    T = Xq.shape[0]
+    dXs = [torch.empty((T, grp.d_in), dtype=torch.bfloat16, device=Xq.device) for _ in grp.d_outs]
+    ents = []
+    for w, c, dY, dX, d_out in zip(grp.weights, grp.codes, dYs, dXs, grp.d_outs):
+        if dY is None:
+            dY = torch.zeros((T, d_out), dtype=torch.bfloat16, device=Xq.device)
+        ents.append(dict(w=w, Wq=c, Xq=Xq, xdq=xdq, dY=dY.contiguous(), dX=dX))
+    io = dqt.linear_io(ents)
+    dqt.dqt_linear_bwd_sr_batch(io, T, dqt.DQT_I8, dqt.DQT_BF16, dqt.DQT_BF16, dqt.DQT_BF16, m.cfg.lr,
+                                m.cfg.seed, m.step_no, m.counters,
+                                m.workspace(dqt.dqt_linear_bwd_batch_workspace(io, T)))
+    return dXs
+
+
 class _DQTGroupFn:
     """Autograd function of one group: x (or RMSNorm(x) * gamma) is quantised
     to int8 per token and fed to the group's linears; the backward returns
@@ -152,12 +205,7 @@ class _DQTGroupFn:
                 else:
                     rinv = torch.empty((T,), dtype=torch.float32, device=x.device)
                     dqt.dqt_rmsnorm_act_quant(x, gamma, m.cfg.eps, dqt.DQT_I8, Xq, xdq, rinv)
-                Ys = [torch.empty((T, d_out), dtype=torch.bfloat16, device=x.device)
-                      for d_out in grp.d_outs]
-                io = dqt.linear_io([dict(w=w, Wq=c, Xq=Xq, xdq=xdq, Y=Y)
-                                    for w, c, Y in zip(grp.weights, grp.codes, Ys)])
-                dqt.dqt_linear_fwd_batch(io, T, dqt.DQT_I8, dqt.DQT_BF16,
-                                         m.workspace(dqt.dqt_linear_fwd_batch_workspace(io)))
+                Ys = _group_fwd(grp, Xq, xdq)
                 ctx.grp = grp
                 ctx.has_gamma = gamma is not None
                 if gamma is None:
@@ -168,23 +216,9 @@ class _DQTGroupFn:
 
             @staticmethod
             def backward(ctx, *dYs):
-                grp = ctx.grp
-                m = grp.model
                 saved = ctx.saved_tensors
                 Xq, xdq = saved[0], saved[1]
-                T = Xq.shape[0]
-                dXs = [torch.empty((T, grp.d_in), dtype=torch.bfloat16, device=Xq.device)
-                       for _ in grp.d_outs]
-                ents = []
-                for w, c, dY, dX, d_out in zip(grp.weights, grp.codes, dYs, dXs, grp.d_outs):
-                    if dY is None:
-                        dY = torch.zeros((T, d_out), dtype=torch.bfloat16, device=Xq.device)
-                    ents.append(dict(w=w, Wq=c, Xq=Xq, xdq=xdq, dY=dY.contiguous(), dX=dX))
-                io = dqt.linear_io(ents)
-                dqt.dqt_linear_bwd_sr_batch(io, T, dqt.DQT_I8, dqt.DQT_BF16, dqt.DQT_BF16,
-                                            dqt.DQT_BF16, m.cfg.lr, m.cfg.seed, m.step_no,
-                                            m.counters,
-                                            m.workspace(dqt.dqt_linear_bwd_batch_workspace(io, T)))
+                dXs = _group_bwd(ctx.grp, Xq, xdq, dYs)
                 if not ctx.has_gamma:
                     if len(dXs) == 1:
                         return dXs[0], None, None
@@ -204,6 +238,94 @@ class _DQTGroupFn:
 
         cls._cls = Fn
         return Fn
+
+
+class _OwnFns:
+    """Autograd functions of the operators that own_ops runs in this library."""
+
+    _cls = None
+
+    @classmethod
+    def get(cls):
+        if cls._cls is not None:
+            return cls._cls
+        torch = dqt._torch()
+
+        class Attn(torch.autograd.Function):
+            """softmax(q k^T / sqrt(d)) v, causal, per packed sequence; q
+            [T, heads, d], k and v [T, kv heads, d]."""
+
+            @staticmethod
+            def forward(ctx, q, k, v, starts, model):
+                T, nh, d = q.shape
+                a = dqt.attn(T, T, nh, k.shape[1], d, starts, starts)
+                o = torch.empty((T, nh, d), dtype=torch.bfloat16, device=q.device)
+                lse = torch.empty((nh, T), dtype=torch.float32, device=q.device)
+                dqt.dqt_attn_fwd(a, q, k, v, o, lse, model.workspace(dqt.dqt_attn_fwd_workspace(a)))
+                ctx.a, ctx.model = a, model
+                ctx.save_for_backward(q, k, v, o, lse)
+                return o
+
+            @staticmethod
+            def backward(ctx, do):
+                q, k, v, o, lse = ctx.saved_tensors
+                dq = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+                dk, dv = (torch.empty(k.shape, dtype=torch.bfloat16, device=q.device) for _ in range(2))
+                dqt.dqt_attn_bwd(ctx.a, q, k, v, o, lse, do.contiguous(), dq, dk, dv,
+                                 ctx.model.workspace(dqt.dqt_attn_bwd_workspace(ctx.a)))
+                return dq, dk, dv, None, None
+
+        class SwigluGroup(torch.autograd.Function):
+            """silu(gate) * up, quantised and fed to the group's linears (the
+            down projection); gate and up are kept as 8-bit checkpoints."""
+
+            @staticmethod
+            def forward(ctx, gate, up, grp):
+                T, K = gate.shape
+                Xq = torch.empty((T, K), dtype=torch.int8, device=gate.device)
+                xdq = torch.empty((T,), dtype=torch.float32, device=gate.device)
+                ckpt = dqt.swiglu_ckpt(T, K, gate.device)
+                dqt.dqt_swiglu_act_quant(gate.contiguous(), up.contiguous(), dqt.DQT_I8, Xq, xdq, ckpt)
+                ctx.grp = grp
+                ctx.save_for_backward(Xq, xdq, ckpt.Gq, ckpt.Uq, ckpt.gs, ckpt.us)
+                return tuple(_group_fwd(grp, Xq, xdq))
+
+            @staticmethod
+            def backward(ctx, *dYs):
+                Xq, xdq, *ckpt = ctx.saved_tensors
+                dXs = _group_bwd(ctx.grp, Xq, xdq, dYs)
+                dh = dXs[0]
+                for d in dXs[1:]:
+                    dh = dh + d
+                dg, du = torch.empty_like(dh), torch.empty_like(dh)
+                dqt.dqt_swiglu_backward_ckpt(dh, dqt.SwigluCkpt(*ckpt), dg, du)
+                return dg, du, None
+
+        class TokenLoss(torch.autograd.Function):
+            """Mean of -log p(target) over the rows that have a target (one in
+            0 .. V - 1)."""
+
+            @staticmethod
+            def forward(ctx, logits, targets, model):
+                M, V = logits.shape
+                logp = torch.empty((M,), dtype=torch.float32, device=logits.device)
+                stat = torch.empty((M, 2), dtype=torch.float32, device=logits.device)
+                dqt.dqt_logprob_fwd(logits, targets, logp, stat=stat,
+                                    ws=model.workspace(dqt.dqt_logprob_workspace(M, V)))
+                n = ((targets >= 0) & (targets < V)).sum().clamp(min=1).float()
+                ctx.save_for_backward(logits, targets, stat, n)
+                return -logp.sum() / n
+
+            @staticmethod
+            def backward(ctx, dloss):
+                logits, targets, stat, n = ctx.saved_tensors
+                dlogp = (-dloss.float() / n).expand(logits.shape[0]).contiguous()
+                dx = torch.empty_like(logits)
+                dqt.dqt_logprob_bwd(logits, targets, stat, dlogp, dx)
+                return dx, None, None
+
+        cls._cls = (Attn, SwigluGroup, TokenLoss)
+        return cls._cls
 
 
 class DQTModel:
@@ -235,9 +357,13 @@ class DQTModel:
         self.opt = torch.optim.AdamW(dense, lr=cfg.lr, betas=(0.9, 0.95), weight_decay=0.1)
         hd = H // cfg.heads
         inv = 1.0 / (cfg.rope_base ** (torch.arange(0, hd, 2, device=device, dtype=torch.float32) / hd))
-        ang = torch.arange(cfg.seq, device=device, dtype=torch.float32)[:, None] * inv[None, :]
-        self.cos = torch.cos(ang).to(torch.bfloat16)[None, None]   # [1, 1, S, hd/2]
+        # (packed documents may be as long as the batch)
+        rows = cfg.tokens if cfg.own_ops else cfg.seq
+        ang = torch.arange(rows, device=device, dtype=torch.float32)[:, None] * inv[None, :]
+        self.cos = torch.cos(ang).to(torch.bfloat16)[None, None]   # [1, 1, rows, hd/2]
         self.sin = torch.sin(ang).to(torch.bfloat16)[None, None]
+        # first token of each of the batch's sequences, and behind the last
+        self.starts = torch.arange(0, cfg.tokens + 1, cfg.seq, dtype=torch.int32, device=device)
 
     def next_tensor_id(self) -> int:
         t = self._tid
@@ -253,19 +379,23 @@ class DQTModel:
             self._ws = dqt.workspace(nbytes, self.dev)
         return self._ws
 
-    def _rope(self, x):
-        # x [B, nh, S, hd]: rotate the two halves of each head
+    def _rope(self, x, c=None, s=None):
+        # x [B, nh, S, hd] (or [T, nh, hd] with each token's c and s): rotate
+        # the two halves of each head
         h = x.shape[-1] // 2
         x1, x2 = x[..., :h], x[..., h:]
-        c, s = self.cos, self.sin
+        if c is None:
+            c, s = self.cos, self.sin
         return self._cat((x1 * c - x2 * s, x1 * s + x2 * c))
 
     @staticmethod
     def _cat(parts):
         return dqt._torch().cat(parts, dim=-1)
 
-    def loss(self, tokens, targets):
-        """Forward of one batch: mean next-token cross-entropy (fp32)."""
+    def logits(self, tokens, starts=None):
+        """Logits [tokens, vocab] (bf16) of one batch.  starts (own_ops): int32
+        on the device, the first token of each document packed into the batch and,
+        last, the number of tokens; by default the batch's sequences."""
         torch = dqt._torch()
         F = torch.nn.functional
         from torch.nn.attention import SDPBackend, sdpa_kernel
@@ -273,33 +403,73 @@ class DQTModel:
         B, S, H, nh = cfg.batch, cfg.seq, cfg.hidden, cfg.heads
         hd = H // nh
         fn = _DQTGroupFn.get()
+        if cfg.own_ops:
+            attn_fn, swiglu_fn, _ = _OwnFns.get()
+            starts = self.starts if starts is None else starts
+            tok = torch.arange(B * S, dtype=torch.int32, device=self.dev)
+            pos = (tok - starts[torch.searchsorted(starts[1:], tok, right=True)]).long()
+            cos, sin = self.cos[0, 0, pos][:, None], self.sin[0, 0, pos][:, None]
+        elif starts is not None:
+            raise ValueError("packed documents need own_ops")
         h = F.embedding(tokens.reshape(-1), self.emb.to(torch.bfloat16))     # [T, H] bf16
         for layer in range(cfg.layers):
             grp = self.groups[layer]
             n_attn, n_mlp = self.norms[layer]
             q, k, v = fn.apply(h, n_attn, grp["attn_in"])
-            q, k, v = (t.view(B, S, nh, hd).transpose(1, 2) for t in (q, k, v))
-            q, k = self._rope(q), self._rope(k)
-            # flash / memory-efficient kernels only (no fallback to the math path)
-            with sdpa_kernel([SDPBackend.FLASH_ATTENTION, SDPBackend.EFFICIENT_ATTENTION]):
-                a = F.scaled_dot_product_attention(q, k, v, is_causal=True)
-            a = a.transpose(1, 2).reshape(B * S, H)
+            if cfg.own_ops:
+                q, k, v = (t.view(B * S, -1, hd) for t in (q, k, v))
+                a = attn_fn.apply(self._rope(q, cos, sin), self._rope(k, cos, sin), v, starts, self)
+                a = a.view(B * S, H)
+            else:
+                q, k, v = (t.view(B, S, nh, hd).transpose(1, 2) for t in (q, k, v))
+                q, k = self._rope(q), self._rope(k)
+                # flash / memory-efficient kernels only (no fallback to the math path)
+                with sdpa_kernel([SDPBackend.FLASH_ATTENTION, SDPBackend.EFFICIENT_ATTENTION]):
+                    a = F.scaled_dot_product_attention(q, k, v, is_causal=True)
+                a = a.transpose(1, 2).reshape(B * S, H)
             (o,) = fn.apply(a, None, grp["attn_out"])
             h = h + o
             gt, up = fn.apply(h, n_mlp, grp["mlp_in"])
-            (d,) = fn.apply(F.silu(gt) * up, None, grp["mlp_hidden"])
+            if cfg.own_ops:
+                (d,) = swiglu_fn.apply(gt, up, grp["mlp_hidden"])
+            else:
+                (d,) = fn.apply(F.silu(gt) * up, None, grp["mlp_hidden"])
             h = h + d
         hn = F.rms_norm(h.float(), (H,), weight=self.final_norm, eps=cfg.eps).to(torch.bfloat16)
-        logits = hn @ self.head.to(torch.bfloat16).t()
-        return F.cross_entropy(logits.float(), targets.reshape(-1))
+        return hn @ self.head.to(torch.bfloat16).t()
 
-    def train_step(self, tokens, targets):
+    def loss(self, tokens, targets, starts=None):
+        """Forward of one batch: mean next-token cross-entropy (fp32)."""
+        logits = self.logits(tokens, starts)
+        if self.cfg.own_ops:
+            return _OwnFns.get()[2].apply(logits, targets.reshape(-1), self)
+        return dqt._torch().nn.functional.cross_entropy(logits.float(), targets.reshape(-1))
+
+    def score(self, tokens, targets, top_k=0, starts=None):
+        """Log probability of each target token (0 where it is outside the
+        vocabulary), the entropy of each prediction and, with top_k, the ids and
+        log probabilities of its most probable tokens, each [batch, seq(, top_k)].
+        A continuation's score is the sum of its tokens' log probabilities,
+        perplexity exp of their negated mean."""
+        torch = dqt._torch()
+        with torch.no_grad():
+            x = self.logits(tokens, starts)
+            M, V = x.shape
+            f = lambda *shape: torch.empty(shape, dtype=torch.float32, device=x.device)
+            out = dict(logp=f(M), entropy=f(M))
+            if top_k:
+                out.update(top_ids=torch.empty((M, top_k), dtype=torch.int64, device=x.device), top_logp=f(M, top_k))
+            dqt.dqt_logprob_fwd(x, targets.reshape(-1), out["logp"], None, out["entropy"], None, out.get("top_ids"),
+                                out.get("top_logp"), self.workspace(dqt.dqt_logprob_workspace(M, V, top_k)))
+        return {k: v.view(self.cfg.batch, self.cfg.seq, *v.shape[1:]) for k, v in out.items()}
+
+    def train_step(self, tokens, targets, starts=None):
         """One step: forward, backward (the DQT codes are updated by Eq. 5
         inside it, keyed by this step's number), AdamW on the dense
         parameters.  Returns the loss tensor (not synchronised)."""
         self.step_no += 1
         self.opt.zero_grad(set_to_none=True)
-        loss = self.loss(tokens, targets)
+        loss = self.loss(tokens, targets, starts)
         loss.backward()
         self.opt.step()
         return loss.detach()

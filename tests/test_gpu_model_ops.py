@@ -1,0 +1,187 @@
+"""The model with attention, SwiGLU and loss in this library's kernels
+(own_ops): against the same model in PyTorch, packed documents, scoring, and
+all of the operators' calls captured into a graph."""
+import dataclasses
+import math
+
+import pytest
+import torch
+
+from gpu_util import DEV, log
+from paper_2412_04787_amd import dqt, model_step as MS
+
+pytestmark = pytest.mark.gpu
+
+
+def test_gradients_match_the_model_in_pytorch(lib):
+    """Same weights, same batch: loss and dense gradients of the two paths.
+    They differ by bf16 roundings in other places (2^-8 each, of which a
+    layer has about ten), by int8 codes that fall to the other side, and by the
+    gate and up checkpoints (a group's maximum / 254 at most, about 1 % of the
+    gradients through them): 5 % of a gradient's norm covers two layers."""
+    own = MS.DQTModel(dataclasses.replace(MS.MODELS["tiny"], own_ops=True))
+    ref = MS.DQTModel(MS.MODELS["tiny"])
+    tok, tgt = MS.synthetic_batch(MS.MODELS["tiny"], 0)
+    log("model: own operators against PyTorch")
+    a, b = own.loss(tok, tgt), ref.loss(tok, tgt)
+    a.backward()
+    b.backward()
+    assert abs(float(a) - float(b)) < 2e-3 * float(b)
+    pairs = [("emb", own.emb, ref.emb), ("head", own.head, ref.head), ("final", own.final_norm, ref.final_norm)]
+    for i, (x, y) in enumerate(zip(own.norms, ref.norms)):
+        pairs += [(f"norm {i}.{j}", p, q) for j, (p, q) in enumerate(zip(x, y))]
+    for name, p, q in pairs:
+        err = float((p.grad - q.grad).norm() / q.grad.norm())
+        log(f"{name}: {err:.4f}")
+        assert err < 0.05, (name, err)
+
+
+def test_packed_documents_stay_apart(lib):
+    """A document's logits do not depend on the other documents of the batch,
+    nor on where it lies in it."""
+    cfg = MS.MODELS["tiny_ops"]
+    model = MS.DQTModel(cfg)
+    tok, _ = MS.synthetic_batch(cfg, 1)
+    tok = tok.reshape(-1)
+    lens = [100, 1, 0, 155]
+    starts = torch.tensor([0, 100, 101, 101, 256], dtype=torch.int32, device=DEV)
+    log("model: packed documents")
+    with torch.no_grad():
+        a = model.logits(tok, starts)
+        other = tok.clone()
+        other[:100] = (other[:100] + 7) % cfg.vocab
+        b = model.logits(other, starts)
+        assert torch.equal(a[100:], b[100:]) and not torch.equal(a[:100], b[:100])
+        docs = torch.split(tok, lens)
+        turned = torch.cat([docs[3], docs[0], docs[1]])
+        c = model.logits(turned, torch.tensor([0, 155, 255, 256], dtype=torch.int32, device=DEV))
+        # (only the LM head's library product may sum in another order: one bf16 step)
+        assert torch.allclose(c[:155].float(), a[101:].float(), rtol=2.0 ** -7, atol=2.0 ** -7 * float(a.float().abs().max()))
+
+
+def test_score_matches_log_softmax(lib):
+    cfg = MS.MODELS["tiny_ops"]
+    model = MS.DQTModel(cfg)
+    tok, tgt = MS.synthetic_batch(cfg, 2)
+    tgt[0, 5] = -100
+    log("model: score")
+    out = model.score(tok, tgt, top_k=7)
+    with torch.no_grad():
+        x = model.logits(tok).double()
+    lp = torch.log_softmax(x, -1)
+    want = lp.gather(1, tgt.reshape(-1, 1).clamp(min=0)).view(cfg.batch, cfg.seq)
+    want[0, 5] = 0.0
+    assert out["logp"].shape == (cfg.batch, cfg.seq) and out["top_ids"].shape == (cfg.batch, cfg.seq, 7)
+    assert float((out["logp"].double() - want).abs().max()) < 1e-5
+    assert float((out["entropy"].double() + (lp.exp() * lp).sum(-1).view_as(want)).abs().max()) < 1e-4
+    val, idx = torch.sort(x, dim=-1, descending=True, stable=True)
+    assert torch.equal(out["top_ids"].view(-1, 7), idx[:, :7])
+    # the PyTorch model scores too
+    ref = MS.DQTModel(MS.MODELS["tiny"])
+    assert ref.score(tok, tgt)["logp"].isfinite().all()
+
+
+def test_tiny_model_trains_on_packed_documents(lib):
+    cfg = MS.MODELS["tiny_ops"]
+    log(f"packed training steps {cfg}")
+    model = MS.DQTModel(cfg)
+    starts = torch.tensor([0, 37, 200, 201, 256], dtype=torch.int32, device=DEV)
+    losses = []
+    for s in range(3):
+        tok, tgt = MS.synthetic_batch(cfg, s)
+        tgt.view(-1)[torch.tensor([36, 199, 200, 255], device=DEV)] = -100    # no token follows a document's last
+        losses.append(float(model.train_step(tok, tgt, starts)))
+    assert all(math.isfinite(v) for v in losses) and abs(losses[0] - math.log(cfg.vocab)) < 0.5
+    changed, nonfinite = model.counters.tolist()
+    assert changed > 0 and nonfinite == 0
+
+
+def test_configuration_refusals():
+    with pytest.raises(ValueError):
+        dataclasses.replace(MS.MODELS["tiny"], kv_heads=2)
+    with pytest.raises(ValueError):
+        dataclasses.replace(MS.MODELS["tiny_ops"], kv_heads=3)
+
+
+def test_graph_replays_match_eager(lib):
+    """Forward and backward of the three operators, captured together: every
+    replay gives the eager results, with eager work between the replays (and
+    calls of another size on the same buffers' workspaces)."""
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    r = lambda *s, dt=torch.bfloat16: torch.randn(s, generator=gen, device=DEV).to(dt)
+    T, H, KV, D, K, V = 300, 8, 2, 64, 1040, 9001
+    st = torch.tensor([0, 120, 120, 300], dtype=torch.int32, device=DEV)
+    one = torch.tensor([0, 1], dtype=torch.int32, device=DEV)
+    long = torch.tensor([0, 9000], dtype=torch.int32, device=DEV)
+    a = dqt.attn(T, T, H, KV, D, st, st)
+    a1 = dqt.attn(1, 9000, H, KV, D, one, long)            # one token: keys split over blocks
+    assert dqt.dqt_attn_fwd_workspace(a1) > 0 and dqt.dqt_logprob_workspace(4, V, 5) > 0
+    q, k, v, do = r(T, H, D), r(T, KV, D), r(T, KV, D), r(T, H, D)
+    q1, k1, v1 = r(1, H, D), r(9000, KV, D), r(9000, KV, D)
+    G, U, dh = r(T, K), r(T, K), r(T, K)
+    X, tgt = r(4, V, dt=torch.float32), torch.tensor([3, -1, 9000, 77], device=DEV)
+    dl = torch.randn((4,), generator=gen, device=DEV)
+
+    def bufs():
+        f = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt, device=DEV)
+        bf = torch.bfloat16
+        return dict(O=f(T, H, D, dt=bf), lse=f(H, T), dQ=f(T, H, D, dt=bf), dK=f(T, KV, D, dt=bf), dV=f(T, KV, D, dt=bf),
+                    O1=f(1, H, D, dt=bf), Xq=f(T, K, dt=torch.int8), xdq=f(T), dG=f(T, K, dt=bf), dU=f(T, K, dt=bf),
+                    logp=f(4), stat=f(4, 2), ent=f(4), ids=f(4, 5, dt=torch.int64), tl=f(4, 5), dX=f(4, V))
+
+    ck = dqt.swiglu_ckpt(T, K)
+    ws = dqt.workspace(max(dqt.dqt_attn_bwd_workspace(a), dqt.dqt_attn_fwd_workspace(a), dqt.dqt_attn_fwd_workspace(a1),
+                           dqt.dqt_logprob_workspace(4, V, 5)))
+
+    def calls(b):
+        dqt.dqt_attn_fwd(a, q, k, v, b["O"], b["lse"], ws)
+        dqt.dqt_attn_bwd(a, q, k, v, b["O"], b["lse"], do, b["dQ"], b["dK"], b["dV"], ws)
+        dqt.dqt_attn_fwd(a1, q1, k1, v1, b["O1"], None, ws)
+        dqt.dqt_swiglu_act_quant(G, U, dqt.DQT_I8, b["Xq"], b["xdq"], ck)
+        dqt.dqt_swiglu_backward_ckpt(dh, ck, b["dG"], b["dU"])
+        dqt.dqt_logprob_fwd(X, tgt, b["logp"], None, b["ent"], b["stat"], b["ids"], b["tl"], ws)
+        dqt.dqt_logprob_bwd(X, tgt, b["stat"], dl, b["dX"])
+
+    eager, g = bufs(), bufs()
+    calls(eager)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(g)
+    torch.cuda.synchronize()
+    for rep in range(3):
+        log(f"graph replay {rep}")
+        for t in g.values():
+            t.zero_()
+        ws.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in g:
+            assert torch.equal(g[n], eager[n]), (rep, n)
+
+
+def test_calls_on_another_stream(lib):
+    """Each call takes the stream it is given; results equal the default stream's."""
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    G, U = (torch.randn((70, 512), generator=gen, device=DEV) for _ in range(2))
+    X = torch.randn((70, 3001), generator=gen, device=DEV)
+    t = torch.randint(0, 3001, (70,), generator=gen, device=DEV)
+
+    def go(stream):
+        o = dict(Xq=torch.zeros((70, 512), dtype=torch.uint8, device=DEV), xdq=torch.zeros((70,), device=DEV),
+                 logp=torch.zeros((70,), device=DEV), stat=torch.zeros((70, 2), device=DEV), dX=torch.zeros_like(X),
+                 dG=torch.zeros_like(G), dU=torch.zeros_like(G))
+        ws = dqt.workspace(dqt.dqt_logprob_workspace(70, 3001))
+        torch.cuda.synchronize()
+        dqt.dqt_swiglu_act_quant(G, U, dqt.DQT_FP8E4M3, o["Xq"], o["xdq"], stream=stream)
+        dqt.dqt_swiglu_backward(G, G, U, o["dG"], o["dU"], stream=stream)
+        dqt.dqt_logprob_fwd(X, t, o["logp"], stat=o["stat"], ws=ws, stream=stream)
+        dqt.dqt_logprob_bwd(X, t, o["stat"], o["logp"], o["dX"], stream=stream)
+        torch.cuda.synchronize()
+        return o
+
+    log("operators on another stream")
+    a, b = go(None), go(torch.cuda.Stream())
+    for n in a:
+        assert torch.equal(a[n], b[n]), n
