@@ -239,8 +239,8 @@ dqt_status dqt_swiglu_backward(const void* dH, int32_t h_t, const void* G, const
  *   targets: [M] int64, or NULL when logp is NULL.  A target outside 0 .. V-1
  *      (padding) gives logp = 0 and no gradient.
  *   logp, lse, entropy: [M] fp32, each may be NULL (not written).
- *   stat: NULL, or [M, 2] fp32, 8-byte aligned, for the backward: the row's
- *      largest logit and log sum_j exp(x_j - it).
+ *   stat: NULL, or [M, 2] fp32, 8-byte aligned, for the backward: a logit c
+ *      near the row's largest, and log sum_j exp(x_j - c).
  *   top_k: 0 .. DQT_MAX_TOP, at most V; top_ids [M, top_k] int64, top_logp
  *      [M, top_k] fp32 (NULL allowed when top_k is 0).
  *   ws: dqt_logprob_workspace(M, V, top_k) bytes (0 for many rows; rows are

@@ -307,7 +307,7 @@ struct LogprobArgs {
   int V;
   const int64_t* targets;      // [M], nullable
   float *logp, *lse, *entropy; // [M], nullable
-  float* stat;                 // [M, 2], nullable in the forward: maximum, log of the sum relative to it
+  float* stat;                 // [M, 2], nullable in the forward: reference, log of the sum relative to it
   int64_t* top_ids;            // [M, top]
   float* top_logp;             // [M, top]
   int top;

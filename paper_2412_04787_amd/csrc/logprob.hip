@@ -5,7 +5,7 @@
 //   dx_j = g [j = t] - p_j (g + e (x_j - lse + entropy))
 // with g, e the upstream gradients of logp and entropy.
 //
-// Forward: one pass over the row.  Each thread keeps a running maximum m, the
+// Forward: one pass over the row.  Each thread keeps m, a maximum so far, the
 // sum s of exp(x - m) and, for the entropy, w, the sum of exp(x - m) (x - m);
 // entropy = log s - w / s.  Rows are split over blocks when there are few; a
 // second launch joins them.
@@ -15,10 +15,11 @@
 // with fewer finite logits than alternatives need no care.  The block's
 // threads form 64 groups; the k-th largest of the groups' maxima (k <= 32) is
 // a bound that at least k elements reach and, unless the row is adverse, few
-// more (about 24 of random logits for k = 20): a second read of the row, from
-// cache, collects those that reach it in LDS and ranks them by comparing all
-// with all.  If they do not fit, k rounds of a whole-block maximum below the
-// last one take their place.
+// more (about 24 of random logits for k = 20): the pieces in whose round a
+// thread saw a value that large are read again, from cache, and the elements
+// that reach the bound collected in LDS and ranked by comparing all with all.
+// If they do not fit, k rounds of a whole-block maximum below the last one take
+// their place.
 //
 // Gradient: one read of the logits and one write.  Both bound by HBM.
 #include "dqt_launch.h"
@@ -30,6 +31,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kCand = 1024;       // candidates held in LDS
 constexpr int kMaxSplits = 64;    // blocks per row: a lane each when they are joined
+constexpr int kRounds = 16;       // rounds of a row whose maxima are kept (16 KB)
 
 __device__ __forceinline__ float inf() { return __builtin_inff(); }
 
@@ -77,30 +79,36 @@ struct Span {
   }
 };
 
-// calls f(values, count <= E, first index) for every piece of [lo, hi), each
-// thread's in ascending order of index but for the elements at the ends
-template <typename T, int NT, class F>
-__device__ __forceinline__ void for_row(const T* row, int lo, int hi, F&& f) {
+// Calls f(values, count <= E, first index) for every piece of [lo, hi) that this
+// thread reads: of round r (4 NT pieces of the row) pieces r 4 NT + k NT + tid,
+// k = 0 .. 3, if want(r); then, as round -1, up to one element outside the
+// body.  after(r) follows a round's pieces.
+template <typename T, int NT, class W, class F, class A>
+__device__ __forceinline__ void for_row(const T* row, int lo, int hi, W&& want, F&& f, A&& after) {
   constexpr int E = Span<T>::E, U = 4;
   const Span<T> sp(row, lo, hi);
   const int tid = threadIdx.x;
   const uint4* p = reinterpret_cast<const uint4*>(row + sp.body);
-  int c = tid;
-  for (; c + (U - 1) * NT < sp.pieces; c += U * NT) {
-    uint4 u[U];
-#pragma unroll
-    for (int k = 0; k < U; ++k) u[k] = p[c + k * NT];
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-      float v[E];
-      unpack<T>(u[k], v);
-      f(v, E, sp.body + (c + k * NT) * E);
-    }
-  }
-  for (; c < sp.pieces; c += NT) {
+  for (int r = 0, c0 = 0; c0 < sp.pieces; ++r, c0 += U * NT) {
+    if (!want(r)) continue;
+    const int c = c0 + tid;
     float v[E];
-    unpack<T>(p[c], v);
-    f(v, E, sp.body + c * E);
+    if (c0 + U * NT <= sp.pieces) {
+      uint4 u[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) u[k] = p[c + k * NT];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        unpack<T>(u[k], v);
+        f(v, E, sp.body + (c + k * NT) * E);
+      }
+    } else {
+      for (int k = c; k < sp.pieces; k += NT) {
+        unpack<T>(p[k], v);
+        f(v, E, sp.body + k * E);
+      }
+    }
+    after(r);
   }
   // up to 2 (E - 1) elements outside the body, one per thread
   const int head = sp.body - lo, n = head + hi - sp.tail;
@@ -112,6 +120,18 @@ __device__ __forceinline__ void for_row(const T* row, int lo, int hi, F&& f) {
   }
 }
 
+// (three at a time; the builtin would first quiet every operand's NaN)
+__device__ __forceinline__ float max_of(const float* v, int n) {
+  float m = v[0];
+  int j = 1;
+  for (; j + 1 < n; j += 2) asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(m), "v"(v[j]), "v"(v[j + 1]));
+  return j < n ? fmaxf(m, v[j]) : m;
+}
+
+// A thread's m moves only when a logit passes it by kSlack: sums of powers up
+// to e^8 lose nothing, and among 64 lanes some would move it at every piece
+// (and 25 operations each time).
+constexpr float kSlack = 8.0f;
 struct Stat {
   float m, s, w;
   // joins b into this one: sums relative to the larger maximum
@@ -203,6 +223,7 @@ __global__ __launch_bounds__(NT) void logprob_fwd_kernel(LogprobArgs a) {
   __shared__ Stat red[NT / 64];
   __shared__ uint64_t red64[64];
   __shared__ uint64_t cand[TOP ? kCand : 1];
+  __shared__ float round_max[TOP ? kRounds : 1][NT];
   __shared__ int ncand;
   const int tid = threadIdx.x, lane = tid & 63;
   const int64_t row = blockIdx.x / a.splits;
@@ -214,21 +235,25 @@ __global__ __launch_bounds__(NT) void logprob_fwd_kernel(LogprobArgs a) {
   Stat t{-inf(), 0.0f, 0.0f};
   float best = -inf();
   int best_at = -1;            // index behind the piece that holds best; -1: none yet
-  for_row<T, NT>(x, lo, hi, [&](const float* v, int n, int first) {
-    float cm = v[0];
-    for (int j = 1; j < n; ++j) cm = fmaxf(cm, v[j]);
+  const auto every = [](int) { return true; };
+  float rm = -inf();           // of this round
+  for_row<T, NT>(x, lo, hi, every, [&](const float* v, int n, int first) {
+    const float cm = max_of(v, n);
     if constexpr (TOP) {
+      rm = fmaxf(rm, cm);
       if (best_at < 0 || cm > best || (cm == best && first + n < best_at)) { best = cm; best_at = first + n; }
     }
-    if (cm > t.m) {
-      if constexpr (ENT) t.join(Stat{cm, 0.0f, 0.0f});
-      else { t.s *= __builtin_amdgcn_exp2f((t.m - cm) * kLog2e); t.m = cm; }
-    }
+    if (cm > t.m + kSlack) t.join(Stat{cm, 0.0f, 0.0f});
     const float m = t.m == -inf() ? 0.0f : t.m;
     for (int j = 0; j < n; ++j) {
       const float d = v[j] - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
       t.s += e;
-      if constexpr (ENT) t.w += e * fmaxf(d, -1e4f);      // (e is 0 long before; -inf would make it NaN)
+      if constexpr (ENT) t.w = __builtin_fmaf(e, fmaxf(d, -1e4f), t.w);      // (e is 0 long before; -inf would make it NaN)
+    }
+  }, [&](int r) {
+    if constexpr (TOP) {
+      if (r < kRounds) round_max[r][tid] = rm;
+      rm = -inf();
     }
   });
 #pragma unroll
@@ -270,10 +295,9 @@ __global__ __launch_bounds__(NT) void logprob_fwd_kernel(LogprobArgs a) {
     const int top = min(a.top, hi - lo);
     const uint64_t bound = kth_of_wave(red64[lane], top);
     const float bv = from_order((uint32_t)(bound >> 32));
-    for_row<T, NT>(x, lo, hi, [&](const float* v, int n, int first) {
-      float cm = v[0];
-      for (int j = 1; j < n; ++j) cm = fmaxf(cm, v[j]);
-      if (cm < bv) return;
+    for_row<T, NT>(x, lo, hi, [&](int r) { return r >= kRounds || !(round_max[r][tid] < bv); },
+                   [&](const float* v, int n, int first) {
+      if (max_of(v, n) < bv) return;
       for (int j = 0; j < n; ++j) {
         const uint64_t key = key_of(v[j], (uint32_t)(first + j));
         if (key >= bound) {
@@ -281,7 +305,7 @@ __global__ __launch_bounds__(NT) void logprob_fwd_kernel(LogprobArgs a) {
           if (at < kCand) cand[at] = key;
         }
       }
-    });
+    }, [](int) {});
     __syncthreads();
     const int n = ncand;
     auto out = [&](int rank, uint64_t key) {
@@ -294,12 +318,12 @@ __global__ __launch_bounds__(NT) void logprob_fwd_kernel(LogprobArgs a) {
       uint64_t last = ~0ull;
       for (int r = 0; r < top; ++r) {
         uint64_t key = 0;
-        for_row<T, NT>(x, lo, hi, [&](const float* v, int cnt, int first) {
+        for_row<T, NT>(x, lo, hi, every, [&](const float* v, int cnt, int first) {
           for (int j = 0; j < cnt; ++j) {
             const uint64_t o = key_of(v[j], (uint32_t)(first + j));
             key = o < last && o > key ? o : key;
           }
-        });
+        }, [](int) {});
         last = block_max<NT>(key, red64);
         if (tid == 0) out(r, last);
       }
@@ -309,43 +333,39 @@ __global__ __launch_bounds__(NT) void logprob_fwd_kernel(LogprobArgs a) {
   }
 }
 
-// Joins the splits of a row (at most 64): one wave per row, a lane per split.
-// Each split's alternatives are in order, so the row's are merged from the
-// lists' heads, one wave maximum each.
+// Joins the splits of a row (at most 64, a lane each; each wave joins all).
+// Each split's alternatives are in order: the k-th largest of the lists' heads
+// is reached by k of them, so the elements below it are out; the others are
+// ranked as above.
 template <typename T>
-__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
-  __shared__ uint64_t lists[kMaxSplits * kMaxTop];
+__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a) {
+  __shared__ uint64_t cand[kMaxSplits * kMaxTop];
+  __shared__ int ncand;
   const int64_t row = blockIdx.x;
-  const int lane = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63;
   const bool in = lane < a.splits;
   const float* p = a.part + (row * a.splits + (in ? lane : 0)) * 4;
   Stat t{in ? p[0] : -inf(), in ? p[1] : 0.0f, in ? p[2] : 0.0f};
-  const int n = a.splits * a.top;
-  for (int i = lane; i < n; i += 64) lists[i] = a.part_top[row * n + i];
+  const uint64_t* lists = a.part_top + row * a.splits * a.top;
+  const uint64_t head = in && a.top > 0 ? lists[lane * a.top] : 0;
+  if (tid == 0) ncand = 0;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) t.join(Stat{__shfl_xor(t.m, d, kWave), __shfl_xor(t.s, d, kWave), __shfl_xor(t.w, d, kWave)});
-  if (lane == 0) {
+  if (tid == 0) {
     bool has;
     const float xt = target_logit<T>(a, row, has);
     write_row(a, row, t, xt, has);
   }
   if (a.top == 0) return;
+  // (fewer lists than k: the bound is 0, which all reach; a list's padding is 0)
+  const uint64_t bound = kth_of_wave(head, a.top);
   __syncthreads();
-  int at = 0;
-  uint64_t head = in ? lists[lane * a.top] : 0;
-  for (int r = 0; r < a.top; ++r) {
-    uint64_t key = head;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-      const uint64_t o = __shfl_xor(key, d, kWave);
-      key = o > key ? o : key;
-    }
-    if (head == key && key != 0) {       // (keys are distinct: one lane)
-      write_top(a, row, t, r, key);
-      ++at;
-      head = at < a.top ? lists[lane * a.top + at] : 0;
-    }
+  for (int i = tid; i < a.splits * a.top; i += 256) {
+    const uint64_t key = lists[i];
+    if (key >= bound && key != 0) cand[atomicAdd(&ncand, 1)] = key;
   }
+  __syncthreads();
+  rank_out<256>(cand, ncand, a.top, [&](int rank, uint64_t key) { write_top(a, row, t, rank, key); });
 }
 
 template <typename T, bool ENT>
@@ -424,7 +444,7 @@ hipError_t launch_logprob_fwd(const LogprobArgs& a, bool bf16, hipStream_t strea
   LaunchStatus st;
   st << launch_kernel(bf16 ? pick(uint16_t{}) : pick(float{}), dim3((unsigned)(a.M * a.splits)), dim3(NT), stream, a);
   if (a.splits > 1)
-    st << launch_kernel(bf16 ? logprob_join_kernel<uint16_t> : logprob_join_kernel<float>, dim3((unsigned)a.M), dim3(64), stream, a);
+    st << launch_kernel(bf16 ? logprob_join_kernel<uint16_t> : logprob_join_kernel<float>, dim3((unsigned)a.M), dim3(256), stream, a);
   return st.e;
 }
 

@@ -197,6 +197,10 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
+def _nbytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
 def _same(*ts):
     """The shape [M, K] that contiguous tensors of one dtype share."""
     for t in ts:
@@ -277,7 +281,7 @@ def dqt_swiglu_act_quant(G, U, act_q: int, Xq, xdq, ckpt: SwigluCkpt | None = No
     """G, U: contiguous [M, K] of one dtype."""
     M, K = _same(G, U)
     _check("dqt_swiglu_act_quant",
-           load().dqt_swiglu_act_quant(_ptr(G), _ptr(U), dtype_code(G), M, K, act_q, _ptr(Xq), _ptr(xdq),
+           load().dqt_swiglu_act_quant(_addr(G), _addr(U), dtype_code(G), M, K, act_q, _addr(Xq), _addr(xdq),
                                        None if ckpt is None else ctypes.byref(ckpt.io), _stream(stream)))
 
 
@@ -285,16 +289,16 @@ def dqt_swiglu_backward(dH, G, U, dG, dU, stream=None):
     """dH, G, U, dG, dU: contiguous [M, K] of one dtype."""
     M, K = _same(dH, G, U, dG, dU)
     _check("dqt_swiglu_backward",
-           load().dqt_swiglu_backward(_ptr(dH), dtype_code(dH), _ptr(G), _ptr(U), None, M, K, _ptr(dG),
-                                      _ptr(dU), _stream(stream)))
+           load().dqt_swiglu_backward(_addr(dH), dtype_code(dH), _addr(G), _addr(U), None, M, K, _addr(dG),
+                                      _addr(dU), _stream(stream)))
 
 
 def dqt_swiglu_backward_ckpt(dH, ckpt: SwigluCkpt, dG, dU, stream=None):
     """dqt_swiglu_backward with gate and up from their 8-bit checkpoint."""
     M, K = _same(dH, dG, dU)
     _check("dqt_swiglu_backward",
-           load().dqt_swiglu_backward(_ptr(dH), dtype_code(dH), None, None, ctypes.byref(ckpt.io), M, K,
-                                      _ptr(dG), _ptr(dU), _stream(stream)))
+           load().dqt_swiglu_backward(_addr(dH), dtype_code(dH), None, None, ctypes.byref(ckpt.io), M, K,
+                                      _addr(dG), _addr(dU), _stream(stream)))
 
 
 MAX_TOP = 32
@@ -312,11 +316,10 @@ def dqt_logprob_fwd(X, targets, logp, lse=None, entropy=None, stat=None, top_ids
     M, V = X.shape
     _unit_stride(X)
     top_k = 0 if top_ids is None else top_ids.shape[1]
-    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check("dqt_logprob_fwd",
-           load().dqt_logprob_fwd(_ptr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _ptr(targets),
-                                  _ptr(logp), _ptr(lse), _ptr(entropy), _ptr(stat), top_k,
-                                  _ptr(top_ids), _ptr(top_logp), _ptr(ws), ws_bytes, _stream(stream)))
+           load().dqt_logprob_fwd(_addr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _addr(targets),
+                                  _addr(logp), _addr(lse), _addr(entropy), _addr(stat), top_k,
+                                  _addr(top_ids), _addr(top_logp), _addr(ws), _nbytes(ws), _stream(stream)))
 
 
 def dqt_logprob_bwd(X, targets, stat, dlogp, dX, entropy=None, dent=None, stream=None):
@@ -327,8 +330,8 @@ def dqt_logprob_bwd(X, targets, stat, dlogp, dX, entropy=None, dent=None, stream
     if dX.dtype != X.dtype or dX.shape != X.shape:
         raise ValueError("dX must have X's dtype and shape")
     _check("dqt_logprob_bwd",
-           load().dqt_logprob_bwd(_ptr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _ptr(targets),
-                                  _ptr(stat), _ptr(entropy), _ptr(dlogp), _ptr(dent), _ptr(dX),
+           load().dqt_logprob_bwd(_addr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _addr(targets),
+                                  _addr(stat), _addr(entropy), _addr(dlogp), _addr(dent), _addr(dX),
                                   dX.stride(0) if M > 1 else V, _stream(stream)))
 
 
@@ -346,18 +349,29 @@ def attn(q_tokens: int, k_tokens: int, heads: int, kv_heads: int, d: int, q_star
     a = DqtAttn(_addr(q_start), _addr(k_start), q_tokens, k_tokens, n.pop(), heads, kv_heads, d,
                 d ** -0.5 if scale is None else scale, int(causal), 0)
     a._keep = (q_start, k_start)
+    a._shapes = ((q_tokens, heads, d), (k_tokens, kv_heads, d))
     return a
 
 
-def _rows(t, tokens: int, heads: int, d: int):
-    """[tokens, heads, d] bf16 tensor (any token and head strides) -> dqt_rows."""
-    if t.dtype != _torch().bfloat16:
-        raise ValueError("attention takes bfloat16 tensors")
-    if tuple(t.shape) != (tokens, heads, d) or (t.stride(2) != 1 and t.numel() > 0):
-        raise ValueError(f"expected a [{tokens}, {heads}, {d}] tensor with unit last stride, got "
-                         f"{tuple(t.shape)} with strides {t.stride()}")
-    # (strides of a dimension of one do not matter)
-    return DqtRows(t.data_ptr(), t.stride(0) if tokens > 1 else heads * d, t.stride(1) if heads > 1 else d)
+def _rows(a: DqtAttn, tensors, kinds: str):
+    """The dqt_rows of bf16 tensors [q_tokens, heads, d] (kind "q") or
+    [k_tokens, kv_heads, d] ("k") with any token and head strides: an array of
+    (address, token stride, head stride), 24 bytes each, and their addresses."""
+    bf16 = _torch().bfloat16
+    v = []
+    for t, kind in zip(tensors, kinds):
+        shape = a._shapes[kind == "k"]
+        if t.dtype is not bf16 or t.shape != shape:
+            raise ValueError(f"expected a bfloat16 tensor of shape {shape}, got {t.dtype} {tuple(t.shape)}")
+        st, sh, sd = t.stride()
+        if sd != 1 and t.numel() > 0:
+            raise ValueError(f"expected unit last stride, got strides {t.stride()}")
+        n, h, d = shape
+        # (strides of a dimension of one do not matter)
+        v += (t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d)
+    arr = (ctypes.c_int64 * len(v))(*v)
+    first = ctypes.addressof(arr)
+    return arr, range(first, first + 8 * len(v), 24)
 
 
 def dqt_attn_fwd_workspace(a: DqtAttn) -> int:
@@ -367,11 +381,9 @@ def dqt_attn_fwd_workspace(a: DqtAttn) -> int:
 def dqt_attn_fwd(a: DqtAttn, Q, K, V, O, lse=None, ws=None, stream=None):
     """Q, O: [q_tokens, heads, d]; K, V: [k_tokens, kv_heads, d], bf16 with any
     token and head strides; lse: fp32 [heads, q_tokens] or None."""
-    qs, ks = (a.q_tokens, a.heads, a.d), (a.k_tokens, a.kv_heads, a.d)
-    r = [_rows(Q, *qs), _rows(K, *ks), _rows(V, *ks), _rows(O, *qs)]
-    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check("dqt_attn_fwd", load().dqt_attn_fwd(ctypes.byref(a), *map(ctypes.byref, r), _ptr(lse), _ptr(ws),
-                                               ws_bytes, _stream(stream)))
+    keep, r = _rows(a, (Q, K, V, O), "qkkq")
+    _check("dqt_attn_fwd", load().dqt_attn_fwd(ctypes.byref(a), *r, _addr(lse), _addr(ws), _nbytes(ws),
+                                               _stream(stream)))
 
 
 def dqt_attn_bwd_workspace(a: DqtAttn) -> int:
@@ -380,12 +392,9 @@ def dqt_attn_bwd_workspace(a: DqtAttn) -> int:
 
 def dqt_attn_bwd(a: DqtAttn, Q, K, V, O, lse, dO, dQ, dK, dV, ws, stream=None):
     """Shapes as dqt_attn_fwd; dO, dQ like Q, dK and dV like K."""
-    qs, ks = (a.q_tokens, a.heads, a.d), (a.k_tokens, a.kv_heads, a.d)
-    f = [_rows(Q, *qs), _rows(K, *ks), _rows(V, *ks), _rows(O, *qs)]
-    b = [_rows(dO, *qs), _rows(dQ, *qs), _rows(dK, *ks), _rows(dV, *ks)]
-    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check("dqt_attn_bwd", load().dqt_attn_bwd(ctypes.byref(a), *map(ctypes.byref, f), _ptr(lse),
-                                               *map(ctypes.byref, b), _ptr(ws), ws_bytes, _stream(stream)))
+    keep, r = _rows(a, (Q, K, V, O, dO, dQ, dK, dV), "qkkqqqkk")
+    _check("dqt_attn_bwd", load().dqt_attn_bwd(ctypes.byref(a), *r[:4], _addr(lse), *r[4:], _addr(ws), _nbytes(ws),
+                                               _stream(stream)))
 
 
 def dqt_linear_fwd_workspace(w: DqtWeight) -> int:
