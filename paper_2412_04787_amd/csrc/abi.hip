@@ -271,11 +271,18 @@ dqt_status check_attn(const dqt_attn* d, dqt::AttnArgs* a) {
   a->row_tiles = (int)rt;
   a->key_tiles = (int)kt;
   a->splits = dqt::attn_splits(d->q_tokens, d->k_tokens, d->n_seq, d->heads, d->kv_heads);
+  a->bwd_splits = dqt::attn_bwd_splits(d->q_tokens, d->k_tokens, d->n_seq, d->heads, d->kv_heads);
   return DQT_OK;
 }
 
 size_t attn_part_bytes(const dqt::AttnArgs& a, int d) {
   return a.splits == 1 ? 0 : (size_t)a.splits * a.heads * a.tq * (d + 1) * 4;
+}
+
+// Backward: the rows' statistics, then (16-byte aligned) the partial dk and dv.
+size_t attn_stat_bytes(const dqt::AttnArgs& a) { return ((size_t)a.heads * a.tq * 8 + 15) / 16 * 16; }
+size_t attn_bwd_bytes(const dqt::AttnArgs& a, int d) {
+  return attn_stat_bytes(a) + (a.bwd_splits == 1 ? 0 : (size_t)a.bwd_splits * 2 * a.tk * a.kv_heads * d * 4);
 }
 
 // A strided tensor [tokens, heads, d] of bf16: non-negative strides that keep
@@ -305,7 +312,7 @@ size_t dqt_attn_fwd_workspace(const dqt_attn* d) {
 size_t dqt_attn_bwd_workspace(const dqt_attn* d) {
   dqt::AttnArgs a;
   if (check_attn(d, &a) != DQT_OK) return 0;
-  return (size_t)a.heads * a.tq * 8;
+  return attn_bwd_bytes(a, d->d);
 }
 
 dqt_status dqt_attn_fwd(const dqt_attn* d, const dqt_rows* Q, const dqt_rows* K, const dqt_rows* V, const dqt_rows* O,
@@ -349,7 +356,7 @@ dqt_status dqt_attn_bwd(const dqt_attn* d, const dqt_rows* Q, const dqt_rows* K,
   if ((st = check_rows(dV, a.tk, a.kv_heads, d->d, true)) != DQT_OK) return st;
   if (a.tq > 0 && lse == nullptr) return DQT_ERR_NULL;
   if (!aligned4(lse) || !aligned16(ws)) return DQT_ERR_ALIGN;
-  const size_t need = (size_t)a.heads * a.tq * 8;
+  const size_t need = attn_bwd_bytes(a, d->d);
   if (need > 0 && (ws == nullptr || ws_bytes < need)) return DQT_ERR_WORKSPACE;
   a.Q = static_cast<const uint8_t*>(Q->p); a.q_tok = Q->token * 2; a.q_head = Q->head * 2;
   a.K = static_cast<const uint8_t*>(K->p); a.k_tok = K->token * 2; a.k_head = K->head * 2;
@@ -362,6 +369,7 @@ dqt_status dqt_attn_bwd(const dqt_attn* d, const dqt_rows* Q, const dqt_rows* K,
   a.lse = const_cast<float*>(lse);
   a.neg_lse = static_cast<float*>(ws);
   a.neg_delta = a.neg_lse + (size_t)a.heads * a.tq;
+  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + attn_stat_bytes(a));
   return from_hip(dqt::launch_attn_bwd(d->d, a, static_cast<hipStream_t>(stream)));
 }
 

@@ -37,6 +37,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 using lds_i32x4 = __attribute__((address_space(3))) i32x4;
 using lds_f32x4 = __attribute__((address_space(3))) f32x4;
+using lds_f32 = __attribute__((address_space(3))) float;
 
 constexpr int kBM = 128;      // rows per block of the forward and dq, keys per block of dk/dv
 constexpr int kKT = 64;       // keys (forward, dq) or rows (dk/dv) per staged tile
@@ -175,12 +176,9 @@ __device__ __forceinline__ i32x4 read_transposed(const lds_u8* tile, const Lanes
 __device__ __forceinline__ f32x16 mfma(i32x4 a, i32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-// (the builtin first makes every operand a quiet NaN: twice the instructions)
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
+// (not as inline asm, which would read a matrix result before it is written:
+// the compiler sees no operands to wait for there)
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 // 8 scores -> B operand (rounded to bf16, as every operand of the second
 // products: the matrix cores take 16-bit values)
@@ -199,12 +197,12 @@ __device__ __forceinline__ f32x16 splat(float x) {
 // base of the tile's row r, 16-byte chunk c.
 template <int D, int R>
 struct Stager {
-  static constexpr int CH = D / 8, N = R * CH / 256;
+  static constexpr int CH = D / 8, N = R * CH / 256;       // (the four waves of a group)
   static_assert(N * 256 == R * CH, "whole waves");
   uint32_t off[N];
   template <class F>
   __device__ __forceinline__ void set(F&& f) {
-    const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+    const int w = (threadIdx.x >> 6) & 3, l = threadIdx.x & 63;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const int p = (w * N + n) * 64 + l, row = p / CH;
@@ -212,14 +210,18 @@ struct Stager {
     }
   }
   __device__ __forceinline__ void issue(const uint8_t* base, lds_u8* tile) const {
-    const int w = threadIdx.x >> 6;
+    const int w = (threadIdx.x >> 6) & 3;
+    // (the copies take the base from scalar registers)
+    const uint64_t b = reinterpret_cast<uint64_t>(base);
+    base = reinterpret_cast<const uint8_t*>((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32 |
+                                            (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b));
 #pragma unroll
     for (int n = 0; n < N; ++n) dma16s(base, off[n], tile + (w * N + n) * 1024);
   }
   // the same from each row's own address
   template <class F>
   static __device__ __forceinline__ void issue_each(lds_u8* tile, F&& row_ptr) {
-    const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+    const int w = (threadIdx.x >> 6) & 3, l = threadIdx.x & 63;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const int p = (w * N + n) * 64 + l, row = p / CH;
@@ -264,12 +266,12 @@ __device__ __forceinline__ void staged_loop(int n, F&& f) {
   }
 }
 
-// result columns (one row of the output per lane, 32 ND values) -> bf16
-template <int ND>
-__device__ __forceinline__ void store_cols(uint8_t* p, const f32x16 (&o)[ND], float f) {
+// result columns (one row of the output per lane, N blocks of 32 values) -> bf16
+template <int N>
+__device__ __forceinline__ void store_cols(uint8_t* p, const f32x16 (&o)[N], float f) {
   const int h = (threadIdx.x & 63) >> 5;
 #pragma unroll
-  for (int db = 0; db < ND; ++db)
+  for (int db = 0; db < N; ++db)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const uint2 v = make_uint2(pack_bf16x2(o[db][4 * q] * f, o[db][4 * q + 1] * f),
@@ -278,14 +280,55 @@ __device__ __forceinline__ void store_cols(uint8_t* p, const f32x16 (&o)[ND], fl
     }
 }
 
+// the same in fp32, for a sum that is not complete
+template <int N>
+__device__ __forceinline__ void store_part(float* p, const f32x16 (&o)[N], float f) {
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int db = 0; db < N; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<f32x4*>(p + 32 * db + 8 * q + 4 * h) =
+          f32x4{o[db][4 * q] * f, o[db][4 * q + 1] * f, o[db][4 * q + 2] * f, o[db][4 * q + 3] * f};
+}
+
+// Two groups of four waves may share a block's rows (GR = 2), each taking every
+// second tile of keys: a block is done in half the time, which counts when the
+// longest block takes as long as the kernel.  At the end group g
+// finishes blocks g ND / 2 .. of the ND (own), with the other group's sums.
+constexpr int larger(int a, int b) { return a > b ? a : b; }
+constexpr int share_floats(int nd) { return 2 * 4 * (nd / 2) * 16 * 64; }
+template <int ND>
+__device__ __forceinline__ void join_groups(const f32x16 (&x)[ND], f32x16 (&own)[ND / 2], lds_f32* buf, int g, float f,
+                                            float f_other) {
+  const int w = (threadIdx.x >> 6) & 3, lane = threadIdx.x & 63;
+  constexpr int H = ND / 2;
+  __syncthreads();            // (what buf held is read)
+#pragma unroll
+  for (int d = 0; d < H; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      // (values selected, not places: an index would send the sums to scratch)
+      const float give = g == 0 ? x[H + d][i] : x[d][i], keep = g == 0 ? x[d][i] : x[H + d][i];
+      buf[(((g * 4 + w) * H + d) * 16 + i) * 64 + lane] = give;
+      own[d][i] = keep * f;
+    }
+  __syncthreads();
+#pragma unroll
+  for (int d = 0; d < H; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) own[d][i] += buf[((((1 - g) * 4 + w) * H + d) * 16 + i) * 64 + lane] * f_other;
+}
+
 // ------------------------------------------------------------------ forward
-template <int D>
-__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
+template <int D, int GR>
+__global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fwd_kernel(AttnArgs a) {
   constexpr int NK = D / 16, ND = D / 32, KT = 64, NB = KT / 32, TB = KT * D * 2;
-  constexpr bool PIPE = D == 64;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[4][TB];       // keys of two tiles, values of two
-  lds_u8* lds = (lds_u8*)&smem[0][0];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  constexpr int LDS = GR == 1 ? 4 * TB : larger(8 * TB, share_floats(ND) * 4 + 2048);
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS];        // a group's: keys of two tiles, values of two
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 3, g = wave >> 2;
+  lds_u8* lds = (lds_u8*)&smem[0] + g * 4 * TB;
   // (blocks go to the 8 XCDs in turn: with 8 or 16 key heads each head's keys
   // stay with one XCD's L2)
   const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.splits;
@@ -314,7 +357,10 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
 
   const Lanes<D> ln;
   const KeyStream<D, KT> keys(a, sq, kvh);
-  if (nt > 0) keys.issue_k(kbeg, lds);
+  if (g < nt) {
+    keys.issue_k(kbeg + g * KT, lds);
+    keys.issue_v(kbeg + g * KT, lds + 2 * TB);
+  }
 
   i32x4 qf[NK];
   const uint8_t* qp = a.Q + (int64_t)(sq.q0 + tok) * a.q_tok + (int64_t)head * a.q_head;
@@ -334,39 +380,24 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   // tiles that a row of this wave sees
   const int mine = min(nt, lim_hi < kbeg ? 0 : (lim_hi - kbeg) / KT + 1);
 
-  // D = 64 (PIPE): the scores of tile t + 1 are formed while those of tile t go
-  // through the exponential, keys staged two tiles ahead, values one (12 heads
-  // of packed documents 37 -> 35 us).  D = 128 leaves no registers for two
-  // tiles' scores (spilled 330 us, 32 keys a tile 231, one tile at a time 175 at
-  // 8 x 2048, 16 heads).
-  f32x16 s[NB];
-  auto scores = [&](const lds_u8* kt, f32x16 (&z)[NB]) {
+  staged_loop((nt + GR - 1) / GR, [&](int it, auto stage) {
+    constexpr int S = decltype(stage)::value;
+    const lds_u8 *kt = lds + S * TB, *vt = lds + (2 + S) * TB;
+    const int t = it * GR + g, k0 = kbeg + t * KT;
+    wait_vm<0>();
+    __syncthreads();
+    if (t + GR < nt) {
+      keys.issue_k(k0 + GR * KT, lds + (1 - S) * TB);
+      keys.issue_v(k0 + GR * KT, lds + (3 - S) * TB);
+    }
+    if (t >= mine) return;
+    f32x16 s[NB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) z[b] = splat(0.0f);
+    for (int b = 0; b < NB; ++b) s[b] = splat(0.0f);
 #pragma unroll
     for (int ks = 0; ks < NK; ++ks)
 #pragma unroll
-      for (int b = 0; b < NB; ++b) z[b] = mfma(read_straight<D>(kt, ln, 32 * b, ks), qf[ks], z[b]);
-  };
-  if (nt > 0) {
-    keys.issue_v(kbeg, lds + 2 * TB);
-    if constexpr (PIPE) {
-      if (nt > 1) keys.issue_k(kbeg + KT, lds + TB);
-      wait_vm<0>();
-      __syncthreads();
-      if (mine > 0) scores(lds, s);
-    }
-  }
-  staged_loop(nt, [&](int t, auto stage) {
-    constexpr int S = decltype(stage)::value;
-    const lds_u8 *kn = lds + (PIPE ? 1 - S : S) * TB, *vt = lds + (2 + S) * TB;
-    const int k0 = kbeg + t * KT;
-    wait_vm<0>();
-    __syncthreads();          // (t = 0: every wave has read the first keys)
-    if (t + 1 + PIPE < nt) keys.issue_k(k0 + (1 + PIPE) * KT, lds + (PIPE ? S : 1 - S) * TB);
-    if (t + 1 < nt) keys.issue_v(k0 + KT, lds + (3 - S) * TB);
-    if (t >= mine) return;
-    if constexpr (!PIPE) scores(kn, s);
+      for (int b = 0; b < NB; ++b) s[b] = mfma(read_straight<D>(kt, ln, 32 * b, ks), qf[ks], s[b]);
     if (k0 + KT - 1 > lim_lo) {
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -394,59 +425,59 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] *= f;
     }
-    const float mu0 = m == -__builtin_inff() ? 0.0f : m;
-    auto rest = [&](auto more) {
-      constexpr bool MORE = decltype(more)::value;
-      // (apart from each other: the compiler would take what both branches
-      // share, the exponentials, out of them and before the products)
-      float mu = mu0;
-      if constexpr (MORE) asm volatile("; more" : "+v"(mu));
-      else asm volatile("; last" : "+v"(mu));
-      f32x16 z[NB];
-      if constexpr (MORE) scores(kn, z);
-      float sum = 0.0f;
+    const float mu = m == -__builtin_inff() ? 0.0f : m;
+    float sum = 0.0f;
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[b][i] = exp2_fast(__builtin_fmaf(s[b][i], c, -mu));
-          sum += s[b][i];
-        }
-      l += sum;
-#pragma unroll
-      for (int kk = 0; kk < 2 * NB; ++kk) {
-        const i32x4 p = pack8(s[kk >> 1], 8 * (kk & 1));
-#pragma unroll
-        for (int db = 0; db < ND; ++db) o[db] = mfma(read_transposed<D>(vt, ln, 16 * kk, db), p, o[db]);
+      for (int i = 0; i < 16; ++i) {
+        s[b][i] = exp2_fast(__builtin_fmaf(s[b][i], c, -mu));
+        sum += s[b][i];
       }
-      if constexpr (MORE) {
+    l += sum;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) s[b] = z[b];
-      }
-    };
-    if (PIPE && t + 1 < mine) rest(std::integral_constant<bool, PIPE>{});
-    else rest(std::false_type{});
+    for (int kk = 0; kk < 2 * NB; ++kk) {
+      const i32x4 p = pack8(s[kk >> 1], 8 * (kk & 1));
+#pragma unroll
+      for (int db = 0; db < ND; ++db) o[db] = mfma(read_transposed<D>(vt, ln, 16 * kk, db), p, o[db]);
+    }
   });
   l += __shfl_xor(l, 32, kWave);
-  if (r >= rows) return;
-  const bool none = l == 0.0f;               // a row that sees no key: zeros
-  const float inv = none ? 0.0f : 1.0f / l, lse2 = none ? -__builtin_inff() : m + __log2f(l);
-  const int64_t at = (int64_t)head * a.tq + sq.q0 + tok;
-  if (a.splits == 1) {
-    store_cols<ND>(a.O + (int64_t)(sq.q0 + tok) * a.o_tok + (int64_t)head * a.o_head, o, inv);
-    if (h == 0 && a.lse != nullptr) a.lse[at] = lse2 * kLn2;
-  } else {
-    const int64_t all = (int64_t)a.heads * a.tq;
-    if (h == 0) a.part_lse[split * all + at] = lse2;
-    if (!none) {
-      float* p = a.part + (split * all + at) * D;
-#pragma unroll
-      for (int db = 0; db < ND; ++db)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<f32x4*>(p + 32 * db + 8 * q + 4 * h) =
-              f32x4{o[db][4 * q] * inv, o[db][4 * q + 1] * inv, o[db][4 * q + 2] * inv, o[db][4 * q + 3] * inv};
+  // the row's results from block `first` of 32 on
+  auto finish = [&](const auto& x, int first) {
+    if (r >= rows) return;
+    const bool none = l == 0.0f;               // a row that sees no key: zeros
+    const float inv = none ? 0.0f : 1.0f / l, lse2 = none ? -__builtin_inff() : m + __log2f(l);
+    const int64_t at = (int64_t)head * a.tq + sq.q0 + tok;
+    if (a.splits == 1) {
+      store_cols(a.O + (int64_t)(sq.q0 + tok) * a.o_tok + (int64_t)head * a.o_head + 64 * first, x, inv);
+      if (h == 0 && first == 0 && a.lse != nullptr) a.lse[at] = lse2 * kLn2;
+      return;
     }
+    const int64_t all = (int64_t)a.heads * a.tq;
+    if (h == 0 && first == 0) a.part_lse[split * all + at] = lse2;
+    if (none) return;
+    store_part(a.part + (split * all + at) * D + 32 * first, x, inv);
+  };
+  if constexpr (GR == 2) {
+    lds_f32* buf = (lds_f32*)&smem[0];
+    lds_f32* ml = buf + share_floats(ND) + (w * 64 + (lane & 31)) * 2;      // [wave][group][row]
+    __syncthreads();
+    if (h == 0) {
+      ml[g * 64] = m;
+      ml[g * 64 + 1] = l;
+    }
+    __syncthreads();
+    const float mo = ml[(1 - g) * 64], lo = ml[(1 - g) * 64 + 1];
+    const float mn = fmaxf(m, mo), mu = mn == -__builtin_inff() ? 0.0f : mn;
+    const float fs = exp2_fast(m - mu), fo = exp2_fast(mo - mu);
+    m = mn;
+    l = l * fs + lo * fo;
+    f32x16 own[ND / 2];
+    join_groups<ND>(o, own, buf, g, fs, fo);
+    finish(own, g * (ND / 2));
+  } else {
+    finish(o, 0);
   }
 }
 
@@ -505,8 +536,8 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
 template <int D>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   constexpr int NK = D / 16, ND = D / 32, TB = kKT * D * 2;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2][TB];
-  lds_u8* lds = (lds_u8*)&smem[0][0][0];
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * TB];
+  lds_u8* lds = (lds_u8*)&smem[0];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int kvh = blockIdx.x % a.kv_heads;
   Seq sq;
@@ -575,7 +606,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
       if (!active || k0 > lim_hi) continue;
       f32x16 s = splat(nl);
       int sa = ln.sa[0];
-      if constexpr (D == 128) asm volatile("" : "+v"(sa));
+      asm volatile("" : "+v"(sa));
       auto straight = [&](const lds_u8* tile, int ks) { return *(const lds_i32x4*)(tile + (sa ^ (ks << 5)) + 64 * b * D); };
 #pragma unroll
       for (int ks = 0; ks < NK; ++ks) s = mfma(straight(kt, ks), qf[ks], s);
@@ -601,8 +632,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
       __builtin_amdgcn_sched_barrier(0);
     }
   });
-  if (r >= rows) return;
-  store_cols<ND>(a.dQ + (int64_t)(sq.q0 + tok) * a.dq_tok + (int64_t)head * a.dq_head, dq, a.scale);
+  if (r < rows) store_cols(a.dQ + (int64_t)(sq.q0 + tok) * a.dq_tok + (int64_t)head * a.dq_head, dq, a.scale);
 }
 
 // Keys and values stay with the block: those of a wave's 32 keys in registers
@@ -613,16 +643,16 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
   constexpr int NK = D / 16, ND = D / 32;
   constexpr bool VL = D == 128;
   constexpr int RT = D == 128 ? 32 : 64, TB = RT * D * 2;          // rows per staged tile, its bytes
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2][TB];
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * TB];     // two stages of Q and dO
   __shared__ __attribute__((aligned(1024))) uint8_t vtile[VL ? kBM * D * 2 : 16];
-  __shared__ __attribute__((aligned(256))) float stat[2][2][64];     // -lse / c, -do.o
-  lds_u8* lds = (lds_u8*)&smem[0][0][0];
+  __shared__ __attribute__((aligned(256))) float stat[2][2][64];      // two stages of -lse / c and -do.o
+  lds_u8* lds = (lds_u8*)&smem[0];
   lds_u8* slds = (lds_u8*)&stat[0][0][0];
   lds_u8* vlds = (lds_u8*)&vtile[0];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const int kvh = blockIdx.x % a.kv_heads;
+  const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.bwd_splits;
   Seq sq;
-  if (!find_tile<true>(a, blockIdx.x / a.kv_heads, sq)) return;
+  if (!find_tile<true>(a, rest / a.bwd_splits, sq)) return;
   const int k0 = sq.tile * kBM;
   if (k0 >= sq.lk) return;
   const int rows = sq.lq * a.group, off = sq.lk - sq.lq;
@@ -632,7 +662,10 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
   // on all its keys are seen; this lane's.
   auto first_row = [&](int x) { return x >= sq.lk ? 0x7fffffff : a.causal ? max(0, x - off) * a.group : 0; };
   const int rlo = first_row(k0), rw_lo = first_row(kw), rw_hi = first_row(kw + 31), rmin = first_row(j);
-  const int nt = rows > rlo ? (rows - rlo + RT - 1) / RT : 0;
+  // this split's tiles of rows
+  const int all_t = rows > rlo ? (rows - rlo + RT - 1) / RT : 0;
+  const int t_lo = (int)((int64_t)all_t * split / a.bwd_splits);
+  const int nt = (int)((int64_t)all_t * (split + 1) / a.bwd_splits) - t_lo;
 
   const uint8_t* qp = a.Q + (int64_t)sq.q0 * a.q_tok + (int64_t)kvh * a.group * a.q_head;
   const uint8_t* gp = a.dO + (int64_t)sq.q0 * a.do_tok + (int64_t)kvh * a.group * a.do_head;
@@ -656,7 +689,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
   };
   auto issue = [&](int t, int s) {
     lds_u8 *qt = lds + s * 2 * TB, *gt = qt + TB;
-    const int r0 = rlo + t * RT;
+    const int r0 = rlo + (t_lo + t) * RT;
     if (even && r0 + RT <= rows) {
       const int64_t t0 = row_token(a, r0);
       qs.issue(qp + t0 * a.q_tok, qt);
@@ -700,7 +733,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
     if (t + 1 < nt) issue(t + 1, 1 - S);
 #pragma unroll
     for (int b = 0; b < RT / 32; ++b) {
-      const int r0 = rlo + t * RT + 32 * b;
+      const int r0 = rlo + (t_lo + t) * RT + 32 * b;
       if (r0 >= rows || r0 + 31 < rw_lo) continue;       // (rw_lo is the largest int without a key)
       auto read_stat = [&](int off) {
         f32x16 v;
@@ -716,16 +749,16 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
       // for all of them they would take the registers of the keys, whose reload
       // from scratch waits for the copies in flight)
       auto fresh = [&](int x) {
-        if constexpr (VL) asm volatile("" : "+v"(x));
+        asm volatile("" : "+v"(x));
         return x;
       };
       auto straight = [&](const lds_u8* tile, int sa, int ks) {
-        return VL ? *(const lds_i32x4*)(tile + (sa ^ (ks << 5))) : read_straight<D>(tile, ln, 32 * b, ks);
+        return *(const lds_i32x4*)(tile + (sa ^ (ks << 5)));
       };
       f32x16 s = read_stat(0);
       const int qsa = fresh(ln.sa[0]);
 #pragma unroll
-      for (int ks = 0; ks < NK; ++ks) s = mfma(straight(qt, qsa, ks), kf[ks], s);
+      for (int ks = 0; ks < NK; ++ks) s = mfma(straight(qt + 64 * b * D, qsa, ks), kf[ks], s);
       if (r0 + 31 >= rows || r0 < rw_hi) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -741,7 +774,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
 #pragma unroll
       for (int ks = 0; ks < NK; ++ks) {
         const i32x4 vv = VL ? straight(vlds, vsa, ks) : vf[VL ? 0 : ks];
-        g = mfma(straight(gt, gsa, ks), vv, g);
+        g = mfma(straight(gt + 64 * b * D, gsa, ks), vv, g);
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = exp2_fast(s[i] * c);
@@ -763,8 +796,31 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
   });
   if (nt == 0) wait_vm<0>();      // (the values' copies, before their LDS is another block's)
   if (j >= sq.lk) return;
-  store_cols<ND>(a.dK + (int64_t)(sq.k0 + j) * a.dk_tok + (int64_t)kvh * a.dk_head, dk, a.scale);
-  store_cols<ND>(a.dV + (int64_t)(sq.k0 + j) * a.dv_tok + (int64_t)kvh * a.dv_head, dv, 1.0f);
+  if (a.bwd_splits == 1) {
+    store_cols(a.dK + (int64_t)(sq.k0 + j) * a.dk_tok + (int64_t)kvh * a.dk_head, dk, a.scale);
+    store_cols(a.dV + (int64_t)(sq.k0 + j) * a.dv_tok + (int64_t)kvh * a.dv_head, dv, 1.0f);
+  } else {
+    const int64_t all = (int64_t)a.tk * a.kv_heads * D;
+    float* p = a.part + (2 * split) * all + ((int64_t)(sq.k0 + j) * a.kv_heads + kvh) * D;
+    store_part(p, dk, a.scale);
+    store_part(p + all, dv, 1.0f);
+  }
+}
+
+// dk, dv = the sums of the splits, in their order: 4 values per thread.
+__global__ __launch_bounds__(256) void attn_dkv_sum_kernel(AttnArgs a, int d) {
+  const int64_t all = (int64_t)a.tk * a.kv_heads * d;
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= 2 * all) return;
+  const bool v = i >= all;
+  const int64_t at = v ? i - all : i, row = at / d;
+  const int tok = (int)(row / a.kv_heads), kvh = (int)(row - (int64_t)tok * a.kv_heads), c = (int)(at - row * d);
+  if (a.k_start != nullptr && (tok < a.k_start[0] || tok >= a.k_start[a.n_seq])) return;
+  f32x4 s = *reinterpret_cast<const f32x4*>(a.part + i);
+  for (int k = 1; k < a.bwd_splits; ++k) s += *reinterpret_cast<const f32x4*>(a.part + 2 * k * all + i);
+  uint8_t* p = v ? a.dV + (int64_t)tok * a.dv_tok + (int64_t)kvh * a.dv_head
+                 : a.dK + (int64_t)tok * a.dk_tok + (int64_t)kvh * a.dk_head;
+  *reinterpret_cast<uint2*>(p + 2 * c) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
 }
 
 }  // namespace
@@ -790,24 +846,50 @@ int attn_splits(int64_t tq, int64_t tk, int64_t n_seq, int heads, int kv_heads) 
 }
 
 hipError_t launch_attn_fwd(int d, AttnArgs a, hipStream_t stream) {
-  const dim3 grid((unsigned)((int64_t)a.row_tiles * a.splits * a.kv_heads)), block(256);
+  const int64_t blocks = (int64_t)a.row_tiles * a.splits * a.kv_heads;
+  // Two groups of waves per block up to two blocks per CU, where a block's own
+  // length counts, for 128-wide heads.  One group -> two: 6 sequences of 100 to
+  // 2000 tokens, 8 heads on 2 key heads (406 blocks) 54.6 -> 45.7 us, chunks of
+  // 64 to 400 tokens over 500 to 2048 (264 blocks) 51.9 -> 42.9, 584 blocks 41.2
+  // -> 40.2, 704 blocks 56.9 -> 62.8; 64-wide, where three blocks of one group
+  // share a CU: 300 blocks 26.6 -> 28.5, 512 blocks 20.5 -> 25.1.
+  const bool two = d == 128 && a.splits == 1 && blocks <= 512;
+  auto* k = d == 64 ? attn_fwd_kernel<64, 1> : two ? attn_fwd_kernel<128, 2> : attn_fwd_kernel<128, 1>;
   LaunchStatus st;
-  st << launch_kernel(d == 128 ? attn_fwd_kernel<128> : attn_fwd_kernel<64>, grid, block, stream, a);
+  st << launch_kernel(k, dim3((unsigned)blocks), dim3(two ? 512 : 256), stream, a);
   if (a.splits > 1)
     st << launch_kernel(d == 128 ? attn_combine_kernel<128> : attn_combine_kernel<64>,
-                        dim3((unsigned)(((int64_t)a.heads * a.tq + 3) / 4)), block, stream, a);
+                        dim3((unsigned)(((int64_t)a.heads * a.tq + 3) / 4)), dim3(256), stream, a);
   return st.e;
 }
 
+// Splits of the rows in dk/dv: few key heads (grouped) over few tokens leave
+// the chip empty, so the rows are divided until there are about 2 blocks per CU,
+// with at least 256 rows each on average; the partial sums are fp32 and summed
+// by another launch.  Backward without -> with: 2 sequences of 1500 and 2500
+// tokens, 8 heads on one key head 400 -> 90 us; the 6 sequences above 329 -> 148;
+// 3 of 300 to 1200, 32 heads on 8 214 -> 124; 4 heads of their own, 2 x 2250
+// 158 -> 122.
+int attn_bwd_splits(int64_t tq, int64_t tk, int64_t n_seq, int heads, int kv_heads) {
+  const int64_t blocks = attn_row_tiles(tk, 1, n_seq) * kv_heads;
+  if (blocks >= 384) return 1;
+  const int64_t want = 512 / blocks, most = tq * (heads / kv_heads) / n_seq / 256;
+  const int64_t s = want < most ? want : most;
+  return s < 1 ? 1 : (int)s;
+}
+
 hipError_t launch_attn_bwd(int d, AttnArgs a, hipStream_t stream) {
-  const dim3 block(256);
   LaunchStatus st;
   if (a.tq > 0)
     st << launch_kernel(d == 128 ? attn_dq_kernel<128> : attn_dq_kernel<64>,
-                        dim3((unsigned)((int64_t)a.row_tiles * a.kv_heads)), block, stream, a);
-  if (a.tk > 0)
+                        dim3((unsigned)((int64_t)a.row_tiles * a.kv_heads)), dim3(256), stream, a);
+  if (a.tk > 0) {
     st << launch_kernel(d == 128 ? attn_dkv_kernel<128> : attn_dkv_kernel<64>,
-                        dim3((unsigned)((int64_t)a.key_tiles * a.kv_heads)), block, stream, a);
+                        dim3((unsigned)((int64_t)a.key_tiles * a.bwd_splits * a.kv_heads)), dim3(256), stream, a);
+    if (a.bwd_splits > 1)
+      st << launch_kernel(attn_dkv_sum_kernel, dim3((unsigned)(((int64_t)a.tk * a.kv_heads * d / 2 + 255) / 256)), dim3(256),
+                          stream, a, d);
+  }
   return st.e;
 }
 

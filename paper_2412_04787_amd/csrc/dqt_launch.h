@@ -278,11 +278,14 @@ struct AttnArgs {
   int causal;
   int row_tiles, key_tiles;    // tiles of all sequences at most
   int splits;                  // of the keys, forward
-  float *part, *part_lse;      // [splits, heads, tq, d], [splits, heads, tq]
+  int bwd_splits;              // of the rows, dk/dv
+  float *part, *part_lse;      // forward: [splits, heads, tq, d], [splits, heads, tq]
+                               // backward: [bwd_splits, 2 (dk, dv), tk, kv_heads, d]
   float *neg_lse, *neg_delta;  // [kv_heads, tq * group]
 };
 int64_t attn_row_tiles(int64_t tokens, int64_t mul, int64_t n_seq);
 int attn_splits(int64_t tq, int64_t tk, int64_t n_seq, int heads, int kv_heads);
+int attn_bwd_splits(int64_t tq, int64_t tk, int64_t n_seq, int heads, int kv_heads);
 hipError_t launch_attn_fwd(int d, AttnArgs a, hipStream_t stream);
 hipError_t launch_attn_bwd(int d, AttnArgs a, hipStream_t stream);
 

@@ -232,20 +232,23 @@ def test_attention_gradient_against_differences(lib):
         assert abs(got - diff) <= tol, (n, got, diff, tol)
 
 
-def test_attention_is_reproducible_and_streams(lib):
+# one block's rows shared by two groups of waves; 64-wide heads; rows of few
+# key heads split in the backward
+@pytest.mark.parametrize("lens,heads,kvh,d", [([700, 33, 260], 8, 2, 128), ([700, 33, 260], 8, 2, 64),
+                                              ([1500, 800], 8, 1, 64), ([1000], 4, 4, 128)])
+def test_attention_is_reproducible_and_streams(lib, lens, heads, kvh, d):
     """The same bits on every call, on two streams at once (a workspace each)."""
     gen = torch.Generator().manual_seed(8)
-    lens = [700, 33, 260]
     T = sum(lens)
     st = torch.from_numpy(starts(lens).astype(np.int32)).to(DEV)
-    _, Qd = tensors(gen, T, 8, 128, "plain")
-    _, Kd = tensors(gen, T, 2, 128, "plain")
-    _, Vd = tensors(gen, T, 2, 128, "plain")
-    _, Gd = tensors(gen, T, 8, 128, "plain")
-    a = dqt.attn(T, T, 8, 2, 128, st, st)
+    _, Qd = tensors(gen, T, heads, d, "plain")
+    _, Kd = tensors(gen, T, kvh, d, "plain")
+    _, Vd = tensors(gen, T, kvh, d, "plain")
+    _, Gd = tensors(gen, T, heads, d, "plain")
+    a = dqt.attn(T, T, heads, kvh, d, st, st)
 
     def bufs():
-        return dict(O=torch.empty_like(Qd), lse=torch.empty((8, T), dtype=torch.float32, device=DEV),
+        return dict(O=torch.empty_like(Qd), lse=torch.empty((heads, T), dtype=torch.float32, device=DEV),
                     dQ=torch.empty_like(Qd), dK=torch.empty_like(Kd), dV=torch.empty_like(Vd),
                     f=dqt.workspace(dqt.dqt_attn_fwd_workspace(a)), b=dqt.workspace(dqt.dqt_attn_bwd_workspace(a)))
 
@@ -253,15 +256,59 @@ def test_attention_is_reproducible_and_streams(lib):
         dqt.dqt_attn_fwd(a, Qd, Kd, Vd, b["O"], b["lse"], b["f"], stream=stream)
         dqt.dqt_attn_bwd(a, Qd, Kd, Vd, b["O"], b["lse"], Gd, b["dQ"], b["dK"], b["dV"], b["b"], stream=stream)
 
-    log("attention: two streams")
+    log(f"attention: two streams {lens} {heads}/{kvh} d={d}")
     first, x, y = bufs(), bufs(), bufs()
     go(first)
     torch.cuda.synchronize()
     s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
-    for _ in range(3):
+    for _ in range(4):
         go(x, s1)
         go(y, s2)
-    torch.cuda.synchronize()
-    for b in (x, y):
-        for k in ("O", "lse", "dQ", "dK", "dV"):
-            assert torch.equal(first[k], b[k]), k
+        torch.cuda.synchronize()
+        for b in (x, y):
+            for k in ("O", "lse", "dQ", "dK", "dV"):
+                assert torch.equal(first[k], b[k]), k
+
+
+@pytest.mark.parametrize("lens,heads,kvh,d", [([1500, 800], 8, 1, 64), ([900, 1100], 6, 2, 128)])
+def test_attention_split_rows_of_the_backward(lib, lens, heads, kvh, d):
+    """Few key heads: dk and dv of a key tile are formed by several blocks."""
+    log(f"attention: split rows {lens} {heads}/{kvh} d={d}")
+    T = sum(lens)
+    a = dqt.attn(T, T, heads, kvh, d, torch.zeros(len(lens) + 1, dtype=torch.int32, device=DEV),
+                 torch.zeros(len(lens) + 1, dtype=torch.int32, device=DEV))
+    assert dqt.dqt_attn_bwd_workspace(a) > 8 * T * heads
+    run(d, heads, kvh, lens, lens, seed=31, before=2, behind=3)
+
+
+def test_attention_offsets_past_32_bits(lib):
+    """Sequences at the end of 5 GB of keys and of values, and of 5 GB of
+    queries: the bits of the same call on copies at the start."""
+    log("attention: long tensors")
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    tk, kvh, d = 2_500_000, 8, 128
+    K, V, O = (torch.empty((tk, kvh, d), dtype=torch.bfloat16, device=DEV) for _ in range(3))
+    lens = [700, 300]
+    n = sum(lens)
+    for t in (K, V):
+        t[-n:] = torch.randn((n, kvh, d), generator=gen, device=DEV).to(torch.bfloat16)
+    Q = torch.empty((tk, kvh, d), dtype=torch.bfloat16, device=DEV)
+    Q[-n:] = torch.randn((n, kvh, d), generator=gen, device=DEV).to(torch.bfloat16)
+    G = Q * 0.01
+
+    def both(q, k, v, o, g, s):
+        st = torch.tensor(s, dtype=torch.int32, device=DEV)
+        T = q.shape[0]
+        a = dqt.attn(T, T, kvh, kvh, d, st, st)
+        lse = torch.empty((kvh, T), dtype=torch.float32, device=DEV)
+        out = [torch.empty_like(q) for _ in range(3)]
+        dqt.dqt_attn_fwd(a, q, k, v, o, lse, dqt.workspace(dqt.dqt_attn_fwd_workspace(a)))
+        dqt.dqt_attn_bwd(a, q, k, v, o, lse, g, *out, dqt.workspace(dqt.dqt_attn_bwd_workspace(a)))
+        torch.cuda.synchronize()
+        return [x[-n:].clone() for x in (o, *out)] + [lse[:, -n:].clone()]
+
+    far = both(Q, K, V, O, G, [tk - n, tk - n + lens[0], tk])
+    small = [t[-n:].clone() for t in (Q, K, V, O, G)]
+    near = both(*small, [0, lens[0], n])
+    for x, y in zip(far, near):
+        assert x.isfinite().all() and (x - y).abs().max() <= 2.0 ** -6 * y.abs().max()
