@@ -74,9 +74,10 @@ __device__ __forceinline__ void span(const int32_t* p, int n, int s, int& first,
 // tokens left 20 % of the chip idle.)
 //
 // Up to 64 sequences, one per lane: with n_s tiles each, sum_s max(0, n_s - d)
-// tiles have depth d or more; d is found by bisection.  More sequences: the
-// list in order, sequence s's tiles from index start * mul / kBM + s (rounded
-// down), which leaves room for all of them.
+// tiles have depth d or more; d is found with 64 candidates at a time, one per
+// lane.  (Bisection over scalar sums of ballots took 3 to 6 us of each block.)
+// More sequences: the list in order, sequence s's tiles from index
+// start * mul / kBM + s (rounded down), which leaves room for all of them.
 template <bool KEYS>
 __device__ __forceinline__ bool find_tile(const AttnArgs& a, int p, Seq& q) {
   const int lane = threadIdx.x & (kWave - 1);
@@ -89,22 +90,25 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, int p, Seq& q) {
       span(a.k_start, a.tk, lane, v.k0, v.lk);
     }
     const int n = (int)(((int64_t)(KEYS ? v.lk : v.lq) * mul + kBM - 1) / kBM);
-    int bits = 0;                      // of the largest n
-    while (__ballot((n >> bits) != 0) != 0) ++bits;
-    // tiles of depth d or more, as a sum over the bits of n - d
-    auto count = [&](int d) {
-      const int x = max(0, n - d);
-      int64_t sum = 0;
-      for (int b = 0; b < bits; ++b) sum += (int64_t)__popcll(__ballot((x >> b) & 1)) << b;
-      return sum;
-    };
-    if (count(0) <= p) return false;
-    int d = 0;                         // the largest d with count(d) > p
-    for (int b = bits - 1; b >= 0; --b)
-      if (count(d + (1 << b)) > p) d += 1 << b;
-    const int at = (int)(p - count(d + 1));
+    int step = 1;                      // 64 steps pass every depth
+    for (int64_t most = ((int64_t)n_tok * mul + kBM - 1) / kBM; most > (int64_t)kWave * step;) step *= kWave;
+    int d = 0, count;                  // the largest depth with count > p tiles at or below it
+    for (;; step /= kWave) {
+      const int x = d + lane * step;
+      int sum = 0;
+      for (int s = 0; s < a.n_seq; s += 8)      // (lanes behind the last sequence hold 0 tiles)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += max(0, __builtin_amdgcn_readlane(n, s + e) - x);
+      const unsigned long long more = __ballot(sum > p);
+      if (more == 0) return false;
+      const int at = __popcll(more) - 1;
+      d += at * step;
+      count = __builtin_amdgcn_readlane(sum, at);
+      if (step == 1) break;
+    }
     const unsigned long long deep = __ballot(n > d);
     const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(deep >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)deep, 0));
+    const int at = p - (count - __popcll(deep));        // among those of this depth
     const int s = __builtin_ctzll(__ballot(n > d && before == at));
     q.q0 = __builtin_amdgcn_readlane(v.q0, s);
     q.lq = __builtin_amdgcn_readlane(v.lq, s);
@@ -331,9 +335,10 @@ __global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fw
   lds_u8* lds = (lds_u8*)&smem[0] + g * 4 * TB;
   // (blocks go to the 8 XCDs in turn: with 8 or 16 key heads each head's keys
   // stay with one XCD's L2)
-  const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.splits;
+  const int at_tile = blockIdx.x / a.kv_heads, kvh = blockIdx.x - at_tile * a.kv_heads;
+  const int rank = a.splits == 1 ? at_tile : at_tile / a.splits, split = at_tile - rank * a.splits;
   Seq sq;
-  if (!find_tile<false>(a, rest / a.splits, sq)) return;
+  if (!find_tile<false>(a, rank, sq)) return;
   const int rows = sq.lq * a.group, r0 = sq.tile * kBM;
   if (r0 >= rows) return;
   const int off = sq.lk - sq.lq;
@@ -372,10 +377,10 @@ __global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fw
   for (int db = 0; db < ND; ++db) o[db] = splat(0.0f);
   const float c = a.scale * kLog2e;
   // m: what the exponents are relative to, a maximum of c q.k so far; l: their
-  // sum.  m moves only when the maximum passes it by 2^8: powers up to 2^8 lose
-  // nothing, and in every tile some row's maximum moves a little (scaling o
-  // each time was a fifth of the vector work).
-  constexpr float kSlack = 8.0f;
+  // sum.  m moves only when the maximum passes it by 2^8 (the sum of a tile's
+  // powers 2^16): large powers lose nothing, and in every tile some row's maximum
+  // moves a little (scaling o each time was a fifth of the vector work).
+  constexpr float kSlack = 8.0f, kMost = 65536.0f;
   float m = -__builtin_inff(), l = 0.0f;
   // tiles that a row of this wave sees
   const int mine = min(nt, lim_hi < kbeg ? 0 : (lim_hi - kbeg) / KT + 1);
@@ -407,15 +412,17 @@ __global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fw
           s[b][i] = j <= lim ? s[b][i] : -__builtin_inff();
         }
     }
-    float mx = max3(s[0][0], s[0][1], s[0][2]), my = max3(s[0][3], s[0][4], s[0][5]);
+    auto tile_max = [&] {
+      float mx = max3(s[0][0], s[0][1], s[0][2]), my = max3(s[0][3], s[0][4], s[0][5]);
 #pragma unroll
-    for (int i = 6; i < 16 * NB; i += 4) {
-      mx = max3(mx, s[i / 16][i % 16], s[i / 16][i % 16 + 1]);
-      if (i + 2 < 16 * NB) my = max3(my, s[(i + 2) / 16][(i + 2) % 16], s[(i + 2) / 16][(i + 2) % 16 + 1]);
-    }
-    mx = fmaxf(mx, my);
-    mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * c;
-    if (__any(mx > m + kSlack)) {
+      for (int i = 6; i < 16 * NB; i += 4) {
+        mx = max3(mx, s[i / 16][i % 16], s[i / 16][i % 16 + 1]);
+        if (i + 2 < 16 * NB) my = max3(my, s[(i + 2) / 16][(i + 2) % 16], s[(i + 2) / 16][(i + 2) % 16 + 1]);
+      }
+      mx = fmaxf(mx, my);
+      return fmaxf(mx, __shfl_xor(mx, 32, kWave)) * c;
+    };
+    auto move = [&](float mx) {
       const float mn = fmaxf(m, mx);
       const float f = exp2_fast(m - (mn == -__builtin_inff() ? 0.0f : mn));
       m = mn;
@@ -424,22 +431,46 @@ __global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fw
       for (int db = 0; db < ND; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] *= f;
-    }
-    const float mu = m == -__builtin_inff() ? 0.0f : m;
-    float sum = 0.0f;
+    };
+    i32x4 p[2 * NB];
+    float sum;
+    auto powers = [&] {
+      const float mu = m == -__builtin_inff() ? 0.0f : m;
+      sum = 0.0f;
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+      for (int kk = 0; kk < 2 * NB; ++kk) {
+        float e[8];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[b][i] = exp2_fast(__builtin_fmaf(s[b][i], c, -mu));
-        sum += s[b][i];
+        for (int i = 0; i < 8; ++i) {
+          e[i] = exp2_fast(__builtin_fmaf(s[kk >> 1][8 * (kk & 1) + i], c, -mu));
+          sum += e[i];
+        }
+        p[kk] = i32x4{(int)pack_bf16x2(e[0], e[1]), (int)pack_bf16x2(e[2], e[3]), (int)pack_bf16x2(e[4], e[5]),
+                      (int)pack_bf16x2(e[6], e[7])};
       }
+    };
+    if constexpr (D == 64) {
+      // the sums show as well whether m is far behind, and cost nothing: the
+      // maxima (a tenth of the vector work) only of the first tile and where the
+      // sums ask for them
+      if (t == g) move(tile_max());
+      powers();
+      if (__any(!(sum <= kMost))) {
+        move(tile_max());
+        powers();
+      }
+    } else {
+      // (128-wide, the matrix products of o take the time of the maxima, and would
+      // have to wait for the check of the sums)
+      const float mx = tile_max();
+      if (__any(mx > m + kSlack)) move(mx);
+      powers();
+    }
     l += sum;
 #pragma unroll
     for (int kk = 0; kk < 2 * NB; ++kk) {
-      const i32x4 p = pack8(s[kk >> 1], 8 * (kk & 1));
 #pragma unroll
-      for (int db = 0; db < ND; ++db) o[db] = mfma(read_transposed<D>(vt, ln, 16 * kk, db), p, o[db]);
+      for (int db = 0; db < ND; ++db) o[db] = mfma(read_transposed<D>(vt, ln, 16 * kk, db), p[kk], o[db]);
     }
   });
   l += __shfl_xor(l, 32, kWave);
@@ -539,9 +570,9 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * TB];
   lds_u8* lds = (lds_u8*)&smem[0];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const int kvh = blockIdx.x % a.kv_heads;
+  const int rank = blockIdx.x / a.kv_heads, kvh = blockIdx.x - rank * a.kv_heads;
   Seq sq;
-  if (!find_tile<false>(a, blockIdx.x / a.kv_heads, sq)) return;
+  if (!find_tile<false>(a, rank, sq)) return;
   const int rows = sq.lq * a.group, r0 = sq.tile * kBM;
   if (r0 >= rows) return;
   const int off = sq.lk - sq.lq;
@@ -674,9 +705,10 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
   lds_u8* slds = (lds_u8*)&stat[0][0][0];
   lds_u8* vlds = (lds_u8*)&vtile[0];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.bwd_splits;
+  const int at_tile = blockIdx.x / a.kv_heads, kvh = blockIdx.x - at_tile * a.kv_heads;
+  const int rank = a.bwd_splits == 1 ? at_tile : at_tile / a.bwd_splits, split = at_tile - rank * a.bwd_splits;
   Seq sq;
-  if (!find_tile<true>(a, rest / a.bwd_splits, sq)) return;
+  if (!find_tile<true>(a, rank, sq)) return;
   const int k0 = sq.tile * kBM;
   if (k0 >= sq.lk) return;
   const int rows = sq.lq * a.group, off = sq.lk - sq.lq;
@@ -688,8 +720,8 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
   const int rlo = first_row(k0), rw_lo = first_row(kw), rw_hi = first_row(kw + 31), rmin = first_row(j);
   // this split's tiles of rows
   const int all_t = rows > rlo ? (rows - rlo + RT - 1) / RT : 0;
-  const int t_lo = (int)((int64_t)all_t * split / a.bwd_splits);
-  const int nt = (int)((int64_t)all_t * (split + 1) / a.bwd_splits) - t_lo;
+  const int per = a.bwd_splits == 1 ? all_t : (all_t + a.bwd_splits - 1) / a.bwd_splits;
+  const int t_lo = min(split * per, all_t), nt = min(per, all_t - t_lo);
 
   const uint8_t* qp = a.Q + (int64_t)sq.q0 * a.q_tok + (int64_t)kvh * a.group * a.q_head;
   const uint8_t* gp = a.dO + (int64_t)sq.q0 * a.do_tok + (int64_t)kvh * a.group * a.do_head;
