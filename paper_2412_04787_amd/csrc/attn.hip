@@ -270,18 +270,29 @@ __device__ __forceinline__ void staged_loop(int n, F&& f) {
   }
 }
 
-// result columns (one row of the output per lane, N blocks of 32 values) -> bf16
-template <int N>
-__device__ __forceinline__ void store_cols(uint8_t* p, const f32x16 (&o)[N], float f) {
-  const int h = (threadIdx.x & 63) >> 5;
+// A wave's result columns (one of 32 rows of the output per lane, N blocks of 32
+// values, times f) -> bf16 rows.  Through the wave's 32 x 64 N bytes of LDS, so
+// that a store writes whole rows: 8 bytes of 32 rows each kept the block's last
+// stores waiting (8 x 2048 tokens, 16 heads of 128: backward 528 -> 506 us,
+// forward 180 -> 177).
+// Chunks of a row are swizzled over the banks.
+template <int N, class F>
+__device__ __forceinline__ void store_rows(lds_u8* buf, const f32x16 (&o)[N], float f, int rows, F&& row_ptr) {
+  constexpr int CH = 4 * N;
+  const int lane = threadIdx.x & 63, h = lane >> 5, r = lane & 31;
+  auto at = [](int row, int c) { return row * 16 * CH + ((c ^ ((CH == 16 ? row : row >> 1) & (CH - 1))) << 4); };
 #pragma unroll
   for (int db = 0; db < N; ++db)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint2 v = make_uint2(pack_bf16x2(o[db][4 * q] * f, o[db][4 * q + 1] * f),
-                                 pack_bf16x2(o[db][4 * q + 2] * f, o[db][4 * q + 3] * f));
-      *reinterpret_cast<uint2*>(p + 2 * (32 * db + 8 * q + 4 * h)) = v;
-    }
+    for (int q = 0; q < 4; ++q)
+      *(__attribute__((address_space(3))) u32x2*)(buf + at(r, 4 * db + q) + 8 * h) =
+          u32x2{pack_bf16x2(o[db][4 * q] * f, o[db][4 * q + 1] * f), pack_bf16x2(o[db][4 * q + 2] * f, o[db][4 * q + 3] * f)};
+#pragma unroll
+  for (int i = 0; i < CH / 2; ++i) {
+    const int p = i * 64 + lane, row = p / CH, c = p % CH;
+    const i32x4 v = *(const lds_i32x4*)(buf + at(row, c));
+    if (row < rows) *reinterpret_cast<i32x4*>(row_ptr(row) + 16 * c) = v;
+  }
 }
 
 // the same in fp32, for a sum that is not complete
@@ -476,15 +487,21 @@ __global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fw
   l += __shfl_xor(l, 32, kWave);
   // the row's results from block `first` of 32 on
   auto finish = [&](const auto& x, int first) {
-    if (r >= rows) return;
     const bool none = l == 0.0f;               // a row that sees no key: zeros
     const float inv = none ? 0.0f : 1.0f / l, lse2 = none ? -__builtin_inff() : m + __log2f(l);
     const int64_t at = (int64_t)head * a.tq + sq.q0 + tok;
     if (a.splits == 1) {
-      store_cols(a.O + (int64_t)(sq.q0 + tok) * a.o_tok + (int64_t)head * a.o_head + 64 * first, x, inv);
-      if (h == 0 && first == 0 && a.lse != nullptr) a.lse[at] = lse2 * kLn2;
+      __syncthreads();            // (the tiles are read)
+      constexpr int N = sizeof(x) / sizeof(f32x16);
+      const int rw = r0 + 32 * w;
+      store_rows<N>((lds_u8*)&smem[0] + wave * 2048 * N, x, inv, rows - rw, [&](int i) {
+        const int t = row_token(a, rw + i);
+        return a.O + (int64_t)(sq.q0 + t) * a.o_tok + (int64_t)(kvh * a.group + (rw + i - t * a.group)) * a.o_head + 64 * first;
+      });
+      if (r < rows && h == 0 && first == 0 && a.lse != nullptr) a.lse[at] = lse2 * kLn2;
       return;
     }
+    if (r >= rows) return;
     const int64_t all = (int64_t)a.heads * a.tq;
     if (h == 0 && first == 0) a.part_lse[split * all + at] = lse2;
     if (none) return;
@@ -687,7 +704,12 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     a.neg_delta[at] = nd;
   }
   pass(std::false_type{});
-  if (r < rows) store_cols(a.dQ + (int64_t)(sq.q0 + tok) * a.dq_tok + (int64_t)head * a.dq_head, dq, a.scale);
+  __syncthreads();            // (the tiles are read)
+  const int rw = r0 + 32 * w;
+  store_rows<ND>(lds + w * 2048 * ND, dq, a.scale, rows - rw, [&](int i) {
+    const int t = row_token(a, rw + i);
+    return a.dQ + (int64_t)(sq.q0 + t) * a.dq_tok + (int64_t)(kvh * a.group + (rw + i - t * a.group)) * a.dq_head;
+  });
 }
 
 // Keys and values stay with the block: those of a wave's 32 keys in registers
@@ -851,11 +873,14 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
     }
   });
   if (nt == 0) wait_vm<0>();      // (the values' copies, before their LDS is another block's)
-  if (j >= sq.lk) return;
   if (a.bwd_splits == 1) {
-    store_cols(a.dK + (int64_t)(sq.k0 + j) * a.dk_tok + (int64_t)kvh * a.dk_head, dk, a.scale);
-    store_cols(a.dV + (int64_t)(sq.k0 + j) * a.dv_tok + (int64_t)kvh * a.dv_head, dv, 1.0f);
-  } else {
+    __syncthreads();            // (the tiles are read)
+    lds_u8* buf = lds + w * 2048 * ND;
+    store_rows<ND>(buf, dk, a.scale, sq.lk - kw,
+                   [&](int i) { return a.dK + (int64_t)(sq.k0 + kw + i) * a.dk_tok + (int64_t)kvh * a.dk_head; });
+    store_rows<ND>(buf, dv, 1.0f, sq.lk - kw,
+                   [&](int i) { return a.dV + (int64_t)(sq.k0 + kw + i) * a.dv_tok + (int64_t)kvh * a.dv_head; });
+  } else if (j < sq.lk) {
     const int64_t all = (int64_t)a.tk * a.kv_heads * D;
     float* p = a.part + (2 * split) * all + ((int64_t)(sq.k0 + j) * a.kv_heads + kvh) * D;
     store_part(p, dk, a.scale);
