@@ -34,12 +34,13 @@
  *    value, M = 0 is a no-op except that dW is then written as zeros).
  *    Base pointers must be 16-byte aligned; per-row fp32 outputs 4-byte.
  *  - Non-finite values in X or dY are not checked.
- *  - Workspaces (dqt_linear_fwd / dqt_linear_bwd and their batches) are
- *    caller-owned device buffers of at least the size the matching
- *    *_workspace() call returns.  Their contents on entry do not matter:
- *    the first 256 bytes hold the library's tile counters, which every call
- *    clears on its stream before the kernels that use them.  Calls that
- *    share a workspace must not run concurrently.
+ *  - Workspaces (dqt_linear_fwd / dqt_linear_bwd and their batches, attention,
+ *    log probabilities) are caller-owned device buffers of at least the size
+ *    the matching *_workspace() call returns.  Their contents on entry do not
+ *    matter: the first 256 bytes hold the tile counters of the linears, which
+ *    every such call clears on its stream before the kernels that use them.
+ *    Calls that share a workspace must not run concurrently, captured ones
+ *    included; in order on one stream they may share it.
  */
 #ifndef DQT_H
 #define DQT_H
@@ -295,9 +296,10 @@ dqt_status dqt_logprob_bwd(const void* X, int32_t x_t, int64_t M, int32_t V, int
  * Tensors are strided: token t's head h is the d consecutive values from
  * p + t * token + h * head (elements; multiples of 8, token at most 2^23, head
  * at most 2^40; 0 allowed for inputs).  Outputs alias neither an input nor
- * each other, and their rows do not overlap (DQT_ERR_SHAPE).  A non-finite value in K or V
- * may reach any query of its own sequence and head, masked or not, and one in
- * Q or dO any gradient of its sequence; none reaches another sequence.
+ * each other, and their rows do not overlap (DQT_ERR_SHAPE).  A non-finite
+ * value in K or V may reach any query of its own sequence and head, masked or
+ * not, and one in Q or dO any gradient of its sequence; none reaches another
+ * sequence.
  */
 typedef struct {
   const int32_t* q_start;

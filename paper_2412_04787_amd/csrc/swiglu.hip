@@ -158,10 +158,10 @@ hipError_t launch_fwd(const TX* g, const TX* u, int64_t M, int K, uint8_t* q, fl
   return go(swiglu_quant_kernel<TX, E4M3, CKPT, 512, 0>, 512);
 }
 
+// (dG or dU may be dH: no __restrict__ on them)
 template <typename TH, bool CKPT>
-__global__ __launch_bounds__(256) void swiglu_bwd_kernel(const TH* __restrict__ dH, const TH* __restrict__ G,
-                                                         const TH* __restrict__ U, Ckpt ck, uint32_t n, uint32_t nchunk,
-                                                         TH* __restrict__ dG, TH* __restrict__ dU) {
+__global__ __launch_bounds__(256) void swiglu_bwd_kernel(const TH* dH, const TH* __restrict__ G, const TH* __restrict__ U,
+                                                         Ckpt ck, uint32_t n, uint32_t nchunk, TH* dG, TH* dU) {
   const uint32_t ngroup = (nchunk + 15) / 16;
   for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
     float d[8], g[8], u[8], og[8], ou[8];

@@ -395,7 +395,10 @@ class DQTModel:
     def logits(self, tokens, starts=None):
         """Logits [tokens, vocab] (bf16) of one batch.  starts (own_ops): int32
         on the device, the first token of each document packed into the batch and,
-        last, the number of tokens; by default the batch's sequences."""
+        last, the token behind the last document; by default the batch's sequences.
+        Tokens behind it (or before the first document) pad the batch: they see
+        each other alone, and take no part in a loss whose targets there are
+        outside the vocabulary."""
         torch = dqt._torch()
         F = torch.nn.functional
         from torch.nn.attention import SDPBackend, sdpa_kernel
@@ -405,7 +408,10 @@ class DQTModel:
         fn = _DQTGroupFn.get()
         if cfg.own_ops:
             attn_fn, swiglu_fn, _ = _OwnFns.get()
-            starts = self.starts if starts is None else starts
+            if starts is None:
+                starts = self.starts
+            else:      # (padding forms sequences of its own, mostly empty: every row is written)
+                starts = torch.cat((self.starts[:1], starts, self.starts[-1:]))
             tok = torch.arange(B * S, dtype=torch.int32, device=self.dev)
             pos = (tok - starts[torch.searchsorted(starts[1:], tok, right=True)]).long()
             cos, sin = self.cos[0, 0, pos][:, None], self.sin[0, 0, pos][:, None]

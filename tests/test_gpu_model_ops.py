@@ -60,6 +60,30 @@ def test_packed_documents_stay_apart(lib):
         assert torch.allclose(c[:155].float(), a[101:].float(), rtol=2.0 ** -7, atol=2.0 ** -7 * float(a.float().abs().max()))
 
 
+def test_padded_batch(lib):
+    """Tokens outside every document change nothing in the documents, and with
+    targets outside the vocabulary nothing in the loss or the weights."""
+    cfg = MS.MODELS["tiny_ops"]
+    tok, tgt = MS.synthetic_batch(cfg, 3)
+    tgt.view(-1)[:16] = -100
+    tgt.view(-1)[200:] = -100
+    s32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    log("model: a padded batch")
+    got = []
+    for starts, pad in ((s32(16, 100, 200), 5), (s32(16, 100, 200), 77), (s32(0, 16, 100, 200, 256), 5)):
+        model = MS.DQTModel(cfg)
+        t = tok.clone().view(-1)
+        t[:16] = pad
+        t[200:] = pad
+        loss = model.train_step(t.view_as(tok), tgt, starts)
+        codes = [c.clone() for layer in model.groups for g in layer.values() for c in g.codes]
+        assert int(model.counters[1]) == 0 and bool(loss.isfinite())
+        got.append((loss, codes))
+    for loss, codes in got[1:]:
+        assert torch.equal(loss, got[0][0])
+        assert all(torch.equal(a, b) for a, b in zip(codes, got[0][1]))
+
+
 def test_score_matches_log_softmax(lib):
     cfg = MS.MODELS["tiny_ops"]
     model = MS.DQTModel(cfg)
