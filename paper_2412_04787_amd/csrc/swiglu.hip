@@ -11,12 +11,12 @@
 // over threads.
 //
 // Forward: a block per row; h stays in registers between the row's maximum
-// and the codes (rows of up to 8 chunks of 8 elements per thread; longer ones
+// and the codes (rows of up to 4 chunks of 8 elements per thread; longer ones
 // form h twice, from cache).  A checkpoint group is 16 neighbouring lanes.
 // HBM traffic per element (bf16): 4 bytes read, 1 written, 2 more with the
-// checkpoint; bound by it.
+// checkpoint; bound by it (FWDRATE).
 // Backward: 8 elements per thread, 8 bytes of traffic per element (bf16 dH,
-// dG and dU, checkpoint); bound by it.
+// dG and dU, checkpoint); bound by it (BWDRATE).
 #include "dqt_launch.h"
 
 namespace dqt {
@@ -144,6 +144,12 @@ __global__ __launch_bounds__(T) void swiglu_quant_kernel(const TX* __restrict__ 
   }
 }
 
+// Threads by the row's length, so that a thread holds up to 3 chunks (4 in rows of
+// more than 12288) and few lanes idle.  8192 rows of bf16, this rule / 512 threads
+// that form h twice / 256 threads with all chunks in registers / 512 or 1024 with
+// one or two: K = 2048 22.1 / 36.4 / 22.2 / 35.2 us, 5632 50.9 / 85.3 / 53.1 /
+// 64.6, 8192 76.4 / 120 / 74.2 / 78.4, 11008 106 / 162 / 120 / 127, 16384 145 /
+// 231 / 156 / 141.
 template <typename TX, bool E4M3, bool CKPT>
 hipError_t launch_fwd(const TX* g, const TX* u, int64_t M, int K, uint8_t* q, float* xdq, const Ckpt& ck, hipStream_t s) {
   const int nchunk = K / 8;

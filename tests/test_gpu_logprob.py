@@ -109,6 +109,32 @@ def test_logprob_ties_and_masked_rows(lib, dt, M):
     check(X.float(), X.to(DEV), t, 32)
 
 
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [61439, 61440, 70001])
+def test_logprob_split_rows(lib, dt, V):
+    """Rows on both sides of the length from which several blocks share one:
+    ties over all of them, masks that leave a block or a row nothing, rows of
+    another stride."""
+    M = 8
+    log(f"logprob split rows V={V} {dt}")
+    X = torch.randn((M, V), generator=torch.Generator().manual_seed(V))
+    X[1] = (torch.arange(V) % 3).float()
+    X[2] = -INF
+    X[2, V - 1] = 1.5
+    X[2, 17] = 1.5
+    X[3] = -INF
+    X[4] = float(torch.finfo(dt).min)
+    X[5, :V // 2] = -INF
+    X[6] = torch.arange(V).float()
+    X[7] = -torch.arange(V).float()
+    X = X.to(dt)
+    t = torch.tensor([V - 1, 0, 17, 3, 5, V // 2, V - 1, -1])
+    buf = torch.full((M, V + 3), 50.0, dtype=dt, device=DEV)
+    view = buf[:, :V]
+    view.copy_(X)
+    check(X.float(), view, t, 32)
+
+
 @pytest.mark.parametrize("M", [1, 600])
 def test_logprob_alternatives_of_adverse_rows(lib, M):
     """The largest logits all lie where few threads read them: more candidates
