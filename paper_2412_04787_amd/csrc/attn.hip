@@ -581,12 +581,13 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
 // dq, and per row, for dk/dv, in row order [kv head][token * G + head in
 // group]: -lse / c, from which a score's accumulator starts (so that the product
 // ends as q.k - lse / c), and -do.o, from which do.v starts.
-template <int D>
-__global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
+template <int D, int GR>
+__global__ __launch_bounds__(256 * GR, 2) void attn_dq_kernel(AttnArgs a) {
   constexpr int NK = D / 16, ND = D / 32, TB = kKT * D * 2;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * TB];
-  lds_u8* lds = (lds_u8*)&smem[0];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[GR == 1 ? 4 * TB : larger(8 * TB, share_floats(ND) * 4)];
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 3, g = wave >> 2;
+  lds_u8* lds = (lds_u8*)&smem[0] + g * 4 * TB;
   const int rank = blockIdx.x / a.kv_heads, kvh = blockIdx.x - rank * a.kv_heads;
   Seq sq;
   if (!find_tile<false>(a, rank, sq)) return;
@@ -604,10 +605,13 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
 
   const Lanes<D> ln;
   const KeyStream<D, kKT> keys(a, sq, kvh);
-  if (nt > 0) {
-    keys.issue_k(0, lds);
-    keys.issue_v(0, lds + TB);
-  }
+  auto issue = [&](int t, lds_u8* stage) {
+    if (t >= nt) return;
+    keys.issue_k(t * kKT, stage);
+    keys.issue_v(t * kKT, stage + TB);
+  };
+  const bool exact = nt <= 2;
+  issue(exact ? 0 : g, lds);
   i32x4 qf[NK], gf[NK];
   const uint8_t* qp = a.Q + (int64_t)(sq.q0 + tok) * a.q_tok + (int64_t)head * a.q_head;
   const uint8_t* gp = a.dO + (int64_t)(sq.q0 + tok) * a.do_tok + (int64_t)head * a.do_head;
@@ -635,16 +639,16 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   for (int db = 0; db < ND; ++db) dq[db] = splat(0.0f);
 
   float miss = 0.0f;
-  auto pass = [&](auto exact) {
-    staged_loop(nt, [&](int t, auto stage) {
+  // (tiles t0, t0 + step ..: both groups run the same number of rounds)
+  auto pass = [&](auto exact, int t0, int step) {
+    staged_loop((nt + step - 1) / step, [&](int it, auto stage) {
       constexpr int S = decltype(stage)::value;
+      const int t = t0 + it * step;
       const lds_u8 *kt = lds + S * 2 * TB, *vt = kt + TB;
       wait_vm<0>();
       __syncthreads();
-      if (t + 1 < nt) {
-        keys.issue_k((t + 1) * kKT, lds + (1 - S) * 2 * TB);
-        keys.issue_v((t + 1) * kKT, lds + (1 - S) * 2 * TB + TB);
-      }
+      issue(t + step, lds + (1 - S) * 2 * TB);
+      if (t >= nt) return;
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const int k0 = t * kKT + 32 * b;
@@ -661,21 +665,21 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
         }
         // do.v runs while p is formed
         __builtin_amdgcn_sched_barrier(0);
-        f32x16 g = splat(nd);
+        f32x16 ds = splat(nd);
 #pragma unroll
-        for (int ks = 0; ks < NK; ++ks) g = mfma(straight(vt, ks), gf[ks], g);
+        for (int ks = 0; ks < NK; ++ks) ds = mfma(straight(vt, ks), gf[ks], ds);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = exp2_fast(s[i] * c);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) g[i] *= s[i];
+        for (int i = 0; i < 16; ++i) ds[i] *= s[i];
         if constexpr (decltype(exact)::value) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) miss += g[i];
+          for (int i = 0; i < 16; ++i) miss += ds[i];
           continue;
         }
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
-          const i32x4 p = pack8(g, 8 * kk);
+          const i32x4 p = pack8(ds, 8 * kk);
 #pragma unroll
           for (int db = 0; db < ND; ++db) dq[db] = mfma(read_transposed<D>(kt, ln, 32 * b + 16 * kk, db), p, dq[db]);
         }
@@ -689,44 +693,52 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   // error itself (relative error of dq and dk of packed documents 0.0025 ->
   // 0.0024, where rounding the exact result to bf16 gives 0.0017 and rounding g
   // as well sqrt(2) of that; no measurable time).
-  if (nt <= 2) {
-    pass(std::true_type{});
+  if (exact) {
+    pass(std::true_type{}, 0, 1);
     nd -= miss + __shfl_xor(miss, 32, kWave);
     __syncthreads();
-    if (nt > 0) {
-      keys.issue_k(0, lds);
-      keys.issue_v(0, lds + TB);
-    }
+    issue(g, lds);
   }
-  if (h == 0 && r < rows) {
+  if (h == 0 && g == 0 && r < rows) {
     const int64_t at = ((int64_t)kvh * a.tq + sq.q0) * a.group + r;
     a.neg_lse[at] = nl;
     a.neg_delta[at] = nd;
   }
-  pass(std::false_type{});
-  __syncthreads();            // (the tiles are read)
+  pass(std::false_type{}, g, GR);
   const int rw = r0 + 32 * w;
-  store_rows<ND>(lds + w * 2048 * ND, dq, a.scale, rows - rw, [&](int i) {
-    const int t = row_token(a, rw + i);
-    return a.dQ + (int64_t)(sq.q0 + t) * a.dq_tok + (int64_t)(kvh * a.group + (rw + i - t * a.group)) * a.dq_head;
-  });
+  auto finish = [&](const auto& x, int first) {       // from block `first` of 32 on
+    constexpr int N = sizeof(x) / sizeof(f32x16);
+    __syncthreads();            // (the tiles are read)
+    store_rows<N>((lds_u8*)&smem[0] + wave * 2048 * N, x, a.scale, rows - rw, [&](int i) {
+      const int t = row_token(a, rw + i);
+      return a.dQ + (int64_t)(sq.q0 + t) * a.dq_tok + (int64_t)(kvh * a.group + (rw + i - t * a.group)) * a.dq_head + 64 * first;
+    });
+  };
+  if constexpr (GR == 2) {
+    f32x16 own[ND / 2];
+    join_groups<ND>(dq, own, (lds_f32*)&smem[0], g, 1.0f, 1.0f);
+    finish(own, g * (ND / 2));
+  } else {
+    finish(dq, 0);
+  }
 }
 
 // Keys and values stay with the block: those of a wave's 32 keys in registers
 // (D = 128: the values in LDS, where the registers of both would not leave room
 // for two waves per SIMD), rows of Q and dO pass through LDS.
-template <int D>
-__global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
+template <int D, int GR>
+__global__ __launch_bounds__(256 * GR, 2) void attn_dkv_kernel(AttnArgs a) {
   constexpr int NK = D / 16, ND = D / 32;
   constexpr bool VL = D == 128;
   constexpr int RT = D == 128 ? 32 : 64, TB = RT * D * 2;          // rows per staged tile, its bytes
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * TB];     // two stages of Q and dO
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[GR == 1 ? 4 * TB : larger(8 * TB, share_floats(ND) * 4)];
   __shared__ __attribute__((aligned(1024))) uint8_t vtile[VL ? kBM * D * 2 : 16];
-  __shared__ __attribute__((aligned(256))) float stat[2][2][64];      // two stages of -lse / c and -do.o
-  lds_u8* lds = (lds_u8*)&smem[0];
-  lds_u8* slds = (lds_u8*)&stat[0][0][0];
+  __shared__ __attribute__((aligned(256))) float stat[GR][2][2][64];      // two stages of -lse / c and -do.o
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 3, g = wave >> 2;
+  lds_u8* lds = (lds_u8*)&smem[0] + g * 4 * TB;        // a group's: two stages of Q and dO
+  lds_u8* slds = (lds_u8*)&stat[g][0][0][0];
   lds_u8* vlds = (lds_u8*)&vtile[0];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int at_tile = blockIdx.x / a.kv_heads, kvh = blockIdx.x - at_tile * a.kv_heads;
   const int rank = a.bwd_splits == 1 ? at_tile : at_tile / a.bwd_splits, split = at_tile - rank * a.bwd_splits;
   Seq sq;
@@ -766,6 +778,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
     });
   };
   auto issue = [&](int t, int s) {
+    if (t >= nt) return;
     lds_u8 *qt = lds + s * 2 * TB, *gt = qt + TB;
     const int r0 = rlo + (t_lo + t) * RT;
     if (even && r0 + RT <= rows) {
@@ -782,7 +795,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
     }
   };
   const Lanes<D> ln;
-  if (nt > 0) issue(0, 0);
+  issue(g, 0);
   i32x4 kf[NK], vf[VL ? 1 : NK];
   const uint8_t* kp = a.K + (int64_t)(sq.k0 + jc) * a.k_tok + (int64_t)kvh * a.k_head;
 #pragma unroll
@@ -792,7 +805,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
     Stager<D, kBM> e;
     const int last = sq.lk - 1 - k0;
     e.set([&](int row) { return (uint32_t)min(row, last) * (uint32_t)a.v_tok; });
-    e.issue(vb, vlds);
+    if (g == 0) e.issue(vb, vlds);
   } else {
     const uint8_t* vp = a.V + (int64_t)(sq.k0 + jc) * a.v_tok + (int64_t)kvh * a.v_head;
 #pragma unroll
@@ -803,12 +816,14 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
 #pragma unroll
   for (int db = 0; db < ND; ++db) dk[db] = dv[db] = splat(0.0f);
 
-  staged_loop(nt, [&](int t, auto stage) {
+  staged_loop((nt + GR - 1) / GR, [&](int it, auto stage) {
     constexpr int S = decltype(stage)::value;
+    const int t = it * GR + g;
     const lds_u8 *qt = lds + S * 2 * TB, *gt = qt + TB, *st = slds + S * 512;
     wait_vm<0>();
     __syncthreads();
-    if (t + 1 < nt) issue(t + 1, 1 - S);
+    issue(t + GR, 1 - S);
+    if (t >= nt) return;
 #pragma unroll
     for (int b = 0; b < RT / 32; ++b) {
       const int r0 = rlo + (t_lo + t) * RT + 32 * b;
@@ -848,11 +863,11 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
       // From here on the matrix cores always have a product that does not wait
       // for the arithmetic beside it: do.v while p is formed, dv while g is, dk.
       __builtin_amdgcn_sched_barrier(0);
-      f32x16 g = read_stat(256);
+      f32x16 ds = read_stat(256);
 #pragma unroll
       for (int ks = 0; ks < NK; ++ks) {
         const i32x4 vv = VL ? straight(vlds, vsa, ks) : vf[VL ? 0 : ks];
-        g = mfma(straight(gt + 64 * b * D, gsa, ks), vv, g);
+        ds = mfma(straight(gt + 64 * b * D, gsa, ks), vv, ds);
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = exp2_fast(s[i] * c);
@@ -863,28 +878,40 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
         for (int db = 0; db < ND; ++db) dv[db] = mfma(read_transposed<D>(gt, ln, 32 * b + 16 * kk, db), p, dv[db]);
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) g[i] *= s[i];
+      for (int i = 0; i < 16; ++i) ds[i] *= s[i];
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
-        const i32x4 ds = pack8(g, 8 * kk);
+        const i32x4 gg = pack8(ds, 8 * kk);
 #pragma unroll
-        for (int db = 0; db < ND; ++db) dk[db] = mfma(read_transposed<D>(qt, ln, 32 * b + 16 * kk, db), ds, dk[db]);
+        for (int db = 0; db < ND; ++db) dk[db] = mfma(read_transposed<D>(qt, ln, 32 * b + 16 * kk, db), gg, dk[db]);
       }
     }
   });
   if (nt == 0) wait_vm<0>();      // (the values' copies, before their LDS is another block's)
-  if (a.bwd_splits == 1) {
-    __syncthreads();            // (the tiles are read)
-    lds_u8* buf = lds + w * 2048 * ND;
-    store_rows<ND>(buf, dk, a.scale, sq.lk - kw,
-                   [&](int i) { return a.dK + (int64_t)(sq.k0 + kw + i) * a.dk_tok + (int64_t)kvh * a.dk_head; });
-    store_rows<ND>(buf, dv, 1.0f, sq.lk - kw,
-                   [&](int i) { return a.dV + (int64_t)(sq.k0 + kw + i) * a.dv_tok + (int64_t)kvh * a.dv_head; });
-  } else if (j < sq.lk) {
-    const int64_t all = (int64_t)a.tk * a.kv_heads * D;
-    float* p = a.part + (2 * split) * all + ((int64_t)(sq.k0 + j) * a.kv_heads + kvh) * D;
-    store_part(p, dk, a.scale);
-    store_part(p + all, dv, 1.0f);
+  // dk and dv from block `first` of 32 on
+  auto finish = [&](const auto& xk, const auto& xv, int first) {
+    if (a.bwd_splits == 1) {
+      constexpr int N = sizeof(xk) / sizeof(f32x16);
+      __syncthreads();            // (the tiles are read)
+      lds_u8* buf = (lds_u8*)&smem[0] + wave * 2048 * N;
+      store_rows<N>(buf, xk, a.scale, sq.lk - kw,
+                    [&](int i) { return a.dK + (int64_t)(sq.k0 + kw + i) * a.dk_tok + (int64_t)kvh * a.dk_head + 64 * first; });
+      store_rows<N>(buf, xv, 1.0f, sq.lk - kw,
+                    [&](int i) { return a.dV + (int64_t)(sq.k0 + kw + i) * a.dv_tok + (int64_t)kvh * a.dv_head + 64 * first; });
+    } else if (j < sq.lk) {
+      const int64_t all = (int64_t)a.tk * a.kv_heads * D;
+      float* p = a.part + (2 * split) * all + ((int64_t)(sq.k0 + j) * a.kv_heads + kvh) * D + 32 * first;
+      store_part(p, xk, a.scale);
+      store_part(p + all, xv, 1.0f);
+    }
+  };
+  if constexpr (GR == 2) {
+    f32x16 ok[ND / 2], ov[ND / 2];
+    join_groups<ND>(dk, ok, (lds_f32*)&smem[0], g, 1.0f, 1.0f);
+    join_groups<ND>(dv, ov, (lds_f32*)&smem[0], g, 1.0f, 1.0f);
+    finish(ok, ov, g * (ND / 2));
+  } else {
+    finish(dk, dv, 0);
   }
 }
 
@@ -945,15 +972,16 @@ hipError_t launch_attn_fwd(int d, AttnArgs a, hipStream_t stream) {
 }
 
 // Splits of the rows in dk/dv: few key heads (grouped) over few tokens leave
-// the chip empty, so the rows are divided until there are about 2 blocks per CU,
-// with at least 256 rows each on average; the partial sums are fp32 and summed
-// by another launch.  Backward without -> with: 2 sequences of 1500 and 2500
-// tokens, 8 heads on one key head 400 -> 90 us; the 6 sequences above 329 -> 148;
-// 3 of 300 to 1200, 32 heads on 8 214 -> 124; 4 heads of their own, 2 x 2250
-// 158 -> 122.
+// the chip empty, so below 192 blocks the rows are divided until there are about
+// 2 blocks per CU, with at least 256 rows each on average; the partial sums are
+// fp32 and summed by another launch.  Backward without -> with: 2 sequences of
+// 1500 and 2500 tokens, 8 heads on one key head 400 -> 90 us; 6 of 100 to 2000,
+// 8 on 2 329 -> 148; 3 of 300 to 1200, 32 on 8 214 -> 124.  With 192 blocks or
+// more two groups of waves in each do better: 2 of 1000 and 1500, 12 heads of
+// their own 62 -> 53 without splits, one of 2000, 16 heads 74 -> 64.
 int attn_bwd_splits(int64_t tq, int64_t tk, int64_t n_seq, int heads, int kv_heads) {
   const int64_t blocks = attn_row_tiles(tk, 1, n_seq) * kv_heads;
-  if (blocks >= 384) return 1;
+  if (blocks >= 192) return 1;
   const int64_t want = 512 / blocks, most = tq * (heads / kv_heads) / n_seq / 256;
   const int64_t s = want < most ? want : most;
   return s < 1 ? 1 : (int)s;
@@ -961,12 +989,22 @@ int attn_bwd_splits(int64_t tq, int64_t tk, int64_t n_seq, int heads, int kv_hea
 
 hipError_t launch_attn_bwd(int d, AttnArgs a, hipStream_t stream) {
   LaunchStatus st;
-  if (a.tq > 0)
-    st << launch_kernel(d == 128 ? attn_dq_kernel<128> : attn_dq_kernel<64>,
-                        dim3((unsigned)((int64_t)a.row_tiles * a.kv_heads)), dim3(256), stream, a);
+  // Two groups of waves per block up to two blocks per CU, as in the forward, of
+  // both widths, where sequences have 256 keys (rows) or more on average.  One
+  // group -> two: 6 sequences of 100 to 2000 tokens, 8 heads of 128 on 2 key heads
+  // 159 -> 135 us, 3 of 300 to 1200, 32 on 8 133 -> 123, 2 of 1500 and 2500, 8 heads
+  // of 64 on one 92 -> 80; above: 876 blocks 87 -> 114; short sequences: 4 of 30 to
+  // 300 23.7 -> 25.8, 8 of 200 to 300 34.4 -> 36.3.
+  const int64_t rb = (int64_t)a.row_tiles * a.kv_heads, kb = (int64_t)a.key_tiles * a.bwd_splits * a.kv_heads;
+  if (a.tq > 0) {
+    const bool two = rb <= 512 && a.tk >= 256 * (int64_t)a.n_seq;
+    auto* k = d == 128 ? (two ? attn_dq_kernel<128, 2> : attn_dq_kernel<128, 1>) : (two ? attn_dq_kernel<64, 2> : attn_dq_kernel<64, 1>);
+    st << launch_kernel(k, dim3((unsigned)rb), dim3(two ? 512 : 256), stream, a);
+  }
   if (a.tk > 0) {
-    st << launch_kernel(d == 128 ? attn_dkv_kernel<128> : attn_dkv_kernel<64>,
-                        dim3((unsigned)((int64_t)a.key_tiles * a.bwd_splits * a.kv_heads)), dim3(256), stream, a);
+    const bool two = kb <= 512 && (int64_t)a.tq * a.group >= 256 * (int64_t)a.n_seq * a.bwd_splits;
+    auto* k = d == 128 ? (two ? attn_dkv_kernel<128, 2> : attn_dkv_kernel<128, 1>) : (two ? attn_dkv_kernel<64, 2> : attn_dkv_kernel<64, 1>);
+    st << launch_kernel(k, dim3((unsigned)kb), dim3(two ? 512 : 256), stream, a);
     if (a.bwd_splits > 1)
       st << launch_kernel(attn_dkv_sum_kernel, dim3((unsigned)(((int64_t)a.tk * a.kv_heads * d / 2 + 255) / 256)), dim3(256),
                           stream, a, d);

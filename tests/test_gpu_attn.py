@@ -281,6 +281,15 @@ def test_attention_split_rows_of_the_backward(lib, lens, heads, kvh, d):
     run(d, heads, kvh, lens, lens, seed=31, before=2, behind=3)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,kvh", [(12, 12), (30, 30), (16, 8)])
+def test_attention_blocks_of_one_and_two_groups(lib, heads, kvh, d):
+    """Numbers of blocks on both sides of the rules for two groups of waves
+    per block and for split rows, with lengths of odd numbers of tiles."""
+    log(f"attention: groups of waves, {heads}/{kvh} heads d={d}")
+    run(d, heads, kvh, [1217, 1, 640], [1217, 1, 640], seed=32, before=1, behind=2)
+
+
 def test_attention_offsets_past_32_bits(lib):
     """Sequences at the end of 5 GB of keys and of values, and of 5 GB of
     queries: the bits of the same call on copies at the start."""

@@ -134,7 +134,7 @@ def test_graph_replays_match_eager(lib):
     calls of another size on the same buffers' workspaces)."""
     gen = torch.Generator(device=DEV).manual_seed(3)
     r = lambda *s, dt=torch.bfloat16: torch.randn(s, generator=gen, device=DEV).to(dt)
-    T, H, KV, D, K, V = 300, 8, 2, 64, 1040, 9001
+    T, H, KV, D, K, V = 300, 8, 2, 64, 1040, 70001
     st = torch.tensor([0, 120, 120, 300], dtype=torch.int32, device=DEV)
     one = torch.tensor([0, 1], dtype=torch.int32, device=DEV)
     long = torch.tensor([0, 9000], dtype=torch.int32, device=DEV)
