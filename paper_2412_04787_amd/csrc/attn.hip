@@ -941,28 +941,34 @@ int64_t attn_row_tiles(int64_t tokens, int64_t mul, int64_t n_seq) { return toke
 //  - for balance, to about 8 blocks per CU of at least 128 keys, as far as the
 //    partials stay below an eighth of the keys' and values' bytes (new tokens
 //    over long contexts);
-//  - to fill the chip, to 2 blocks per CU, where each still gets 512 keys.
+//  - below 96 blocks, to fill the chip, to 2 blocks per CU, where each still gets
+//    512 keys (one sequence of 2600 tokens, 4 heads of 128, 84 blocks: without ->
+//    with 42.1 -> 38.1 us; from about 100 blocks on two groups of waves in each do
+//    better: 1500 tokens, 8 heads, 104 blocks, with splits 32.6 -> two groups 29.0,
+//    2 of 1000 and 1500, 12 heads of 64, 250 blocks 32.9 -> 21.1).
 int attn_splits(int64_t tq, int64_t tk, int64_t n_seq, int heads, int kv_heads) {
   const int64_t blocks = attn_row_tiles(tq, heads / kv_heads, n_seq) * kv_heads;
   if (tq == 0 || blocks >= 1024) return 1;
   auto least = [](int64_t x, int64_t y) { return x < y ? x : y; };
   const int64_t mean = tk / n_seq;
   const int64_t even = least(least(2048 / blocks, mean / 128), tk * kv_heads / (16 * tq * heads));
-  const int64_t fill = blocks < 256 ? least(512 / blocks, mean / 512) : 1;
+  const int64_t fill = blocks < 96 ? least(512 / blocks, mean / 512) : 1;
   const int64_t s = even > fill ? even : fill;
   return s < 1 ? 1 : (int)s;
 }
 
 hipError_t launch_attn_fwd(int d, AttnArgs a, hipStream_t stream) {
   const int64_t blocks = (int64_t)a.row_tiles * a.splits * a.kv_heads;
-  // Two groups of waves per block up to two blocks per CU, where a block's own
-  // length counts, for 128-wide heads.  One group -> two: 6 sequences of 100 to
-  // 2000 tokens, 8 heads on 2 key heads (406 blocks) 54.6 -> 45.7 us, chunks of
-  // 64 to 400 tokens over 500 to 2048 (264 blocks) 51.9 -> 42.9, 584 blocks 41.2
-  // -> 40.2, 704 blocks 56.9 -> 62.8; 64-wide, where three blocks of one group
-  // share a CU: 300 blocks 26.6 -> 28.5, 512 blocks 20.5 -> 25.1.
-  const bool two = d == 128 && a.splits == 1 && blocks <= 512;
-  auto* k = d == 64 ? attn_fwd_kernel<64, 1> : two ? attn_fwd_kernel<128, 2> : attn_fwd_kernel<128, 1>;
+  // Two groups of waves per block up to two blocks per CU (64-wide: one, or two
+  // where sequences are long), where a block's own length counts.  One group ->
+  // two, 128-wide: 6 sequences of 100 to 2000 tokens, 8 heads on 2 key heads (406
+  // blocks) 54.6 -> 45.7 us, 584 blocks 41.2 -> 40.2, 704 blocks 56.9 -> 62.8;
+  // 64-wide: one of 2000, 16 heads (256 blocks) 32.6 -> 26.6, 2 of 2000, 12 heads
+  // (384) 32.7 -> 27.8, but 8 of 300 to 600, 12 heads (420) 15.3 -> 17.5.  Sequences
+  // of fewer than 256 keys on average have nothing to divide: 16 of 128, 2 heads
+  // on one 9.7 -> 11.6.
+  const bool two = a.splits == 1 && blocks <= 512 && a.tk >= (d == 128 || blocks <= 256 ? 256 : 1024) * (int64_t)a.n_seq;
+  auto* k = d == 64 ? (two ? attn_fwd_kernel<64, 2> : attn_fwd_kernel<64, 1>) : two ? attn_fwd_kernel<128, 2> : attn_fwd_kernel<128, 1>;
   LaunchStatus st;
   st << launch_kernel(k, dim3((unsigned)blocks), dim3(two ? 512 : 256), stream, a);
   if (a.splits > 1)
