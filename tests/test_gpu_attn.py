@@ -290,6 +290,46 @@ def test_attention_blocks_of_one_and_two_groups(lib, heads, kvh, d):
     run(d, heads, kvh, [1217, 1, 640], [1217, 1, 640], seed=32, before=1, behind=2)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_many_long_sequences(lib, d):
+    """More sequences than lanes, of up to several tiles, and keys that queries
+    of any position see."""
+    rng = np.random.default_rng(4)
+    lens = rng.integers(0, 640, 70).tolist()
+    log(f"attention: 70 sequences of up to 640 tokens d={d}")
+    run(d, 2, 1, lens, lens, seed=33, behind=4)
+    run(d, 9, 9, [700, 130, 1], [300, 900, 500], causal=False, seed=34)
+
+
+def test_attention_starts_out_of_range_stay_in_the_tensors(lib):
+    """Starts that break the rules give wrong results but touch nothing outside:
+    they are clamped to the tensors, and descending ones are empty."""
+    T, heads, kvh, d, pad = 300, 4, 2, 64, 64
+    gen = torch.Generator().manual_seed(35)
+
+    def inner(n, fill):
+        buf = torch.full((T + 2 * pad, n, d), fill, dtype=torch.bfloat16, device=DEV)
+        return buf, buf[pad:pad + T]
+
+    ins = [inner(n, 0.0) for n in (heads, kvh, kvh, heads)]
+    for _, x in ins:
+        x.copy_(torch.randn(x.shape, generator=gen).to(torch.bfloat16))
+    for bad in ([0, 500, 900, 300], [-70, 40, 20, 290], [250, 100, 400, -5], [300, 300, 300, 301]):
+        log(f"attention: starts {bad}")
+        st = torch.tensor(bad, dtype=torch.int32, device=DEV)
+        a = dqt.attn(T, T, heads, kvh, d, st, st)
+        outs = [inner(n, SENT) for n in (heads, heads, kvh, kvh)]
+        lse = torch.zeros((heads, T), dtype=torch.float32, device=DEV)
+        q, k, v, do = (x for _, x in ins)
+        o, dq, dk, dv = (x for _, x in outs)
+        ws = dqt.workspace(max(dqt.dqt_attn_fwd_workspace(a), dqt.dqt_attn_bwd_workspace(a)))
+        dqt.dqt_attn_fwd(a, q, k, v, o, lse, ws)
+        dqt.dqt_attn_bwd(a, q, k, v, o, lse, do, dq, dk, dv, ws)
+        torch.cuda.synchronize()
+        for buf, _ in outs:
+            assert (buf[:pad] == SENT).all() and (buf[pad + T:] == SENT).all()
+
+
 def test_attention_offsets_past_32_bits(lib):
     """Sequences at the end of 5 GB of keys and of values, and of 5 GB of
     queries: the bits of the same call on copies at the start."""

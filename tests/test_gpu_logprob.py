@@ -231,6 +231,26 @@ def test_logprob_gradient_against_differences(lib):
         assert ((dX[:, j].double().cpu() - diff).abs() <= 2e-6 * (1 + diff.abs())).all()
 
 
+def test_logprob_more_rows_than_blocks(lib):
+    """Rows past the largest grid of the gradient give what they give alone."""
+    M, V, tail = 1_050_001, 9, 3000
+    X = torch.randn((M, V), generator=torch.Generator().manual_seed(12)).to(torch.bfloat16).to(DEV)
+    t = (torch.arange(M, device=DEV) % 11) - 1
+    g = torch.linspace(-1, 1, M, device=DEV)
+    log("logprob: 1050001 rows")
+
+    def go(x, t, g):
+        o = forward(x, t)
+        dX = torch.empty_like(x)
+        dqt.dqt_logprob_bwd(x, t, o["stat"], g, dX, o["entropy"], g)
+        torch.cuda.synchronize()
+        return [o["logp"], o["lse"], o["entropy"], dX]
+
+    # (the tail's rows as a tensor of their own: their alignment differs, not their values)
+    for x, y in zip(go(X, t, g), go(X[-tail:].clone(), t[-tail:].clone(), g[-tail:].clone())):
+        assert (x[-tail:].float() - y.float()).abs().max() <= 2.0 ** -7 * y.float().abs().max()
+
+
 def test_logprob_empty(lib):
     e = torch.empty((0, 10), device=DEV)
     v = torch.empty((0,), device=DEV)

@@ -119,6 +119,25 @@ def test_swiglu_backward_in_place_and_empty(lib):
     dqt.dqt_swiglu_backward(e, e, e, e, e)
 
 
+def test_swiglu_more_rows_than_blocks(lib):
+    """Rows past the largest grid give what the same rows give on their own."""
+    M, K = 70001, 32
+    G, U, _ = inputs(M, K, torch.bfloat16, 7)
+    G, U = G.to(DEV), U.to(DEV)
+    log("swiglu: 70001 rows")
+
+    def go(g, u):
+        m = g.shape[0]
+        Xq, xdq = torch.empty((m, K), dtype=torch.int8, device=DEV), torch.empty((m,), dtype=torch.float32, device=DEV)
+        ck = dqt.swiglu_ckpt(m, K)
+        dqt.dqt_swiglu_act_quant(g, u, dqt.DQT_I8, Xq, xdq, ck)
+        torch.cuda.synchronize()
+        return [Xq, xdq, ck.Gq, ck.Uq, ck.gs, ck.us]
+
+    for x, y in zip(go(G, U), go(G[65000:].contiguous(), U[65000:].contiguous())):
+        assert torch.equal(x[65000:], y)
+
+
 def test_swiglu_matches_unfused_quantiser(lib):
     """On rows whose product is exact in bf16, the fused call gives the codes of
     dqt_act_quant (g large: silu(g) = g in fp32)."""

@@ -176,3 +176,19 @@ def test_tensors_checked_in_python():
         dqt.dqt_logprob_fwd(x.t(), None, None)
     with pytest.raises(ValueError):
         dqt.dqt_logprob_bwd(x, None, None, None, y)
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    class T:
+        is_cuda = True
+
+        def __init__(self, i):
+            self.i = i
+
+        def get_device(self):
+            return self.i
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    dqt._here(T(0))
+    with pytest.raises(ValueError):
+        dqt._here(T(1))
