@@ -343,9 +343,9 @@ __device__ __forceinline__ void join_groups(const f32x16 (&x)[ND], f32x16 (&own)
 // (775 TFLOP/s; one sequence of 8192 tokens 930): within a block's loop the matrix
 // cores are busy 0.6 of the cycles at the 1.7 to 1.9 GHz that the power limit
 // leaves, and a block's first data arrive 4 to 5 us after its start.  64-wide, 4 x
-// 4096 tokens, 16 heads: 160 us, the vector units busy 0.7 of the cycles; three
+// 4096 tokens, 16 heads: 160 us, bound by the vector units first; three
 // waves per SIMD (four, at 128 registers: 29.1 -> 31.1 us for 8 x 1024, 12 heads).
-// New tokens over long contexts are bound by HBM: 32 tokens over up to 4096 keys, 8
+// New tokens over long contexts are bound by HBM: 32 tokens over 1 to 8192 keys, 8
 // key heads: 108 us for 0.54 GB, 5.0 TB/s.
 template <int D, int GR>
 __global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fwd_kernel(AttnArgs a) {
@@ -541,7 +541,7 @@ __global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fw
 }
 
 // o = sum_s 2^(lse_s - lse) o_s over the splits of a row: one wave per row, up to
-// four splits' partials in flight (5 us for 1024 rows of 16 splits, most of it the
+// four splits' partials in flight (5 us for 1024 rows of 7 splits, most of it the
 // launch).
 template <int D>
 __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
@@ -744,8 +744,8 @@ __global__ __launch_bounds__(256 * GR, 2) void attn_dq_kernel(AttnArgs a) {
 // for two waves per SIMD), rows of Q and dO pass through LDS.  Four products, dk
 // and dv in registers for the whole loop (a pass over the keys by rows would need
 // atomics, whose order changes results): 8 x 2048 tokens, 16 heads of 128: 290 us
-// for 275 GFLOP (950 TFLOP/s), bound as the forward is, with twice its reads of
-// LDS (active 0.37 of the cycles, without bank conflicts).
+// for 275 GFLOP (950 TFLOP/s), bound as the forward is, with more reads of LDS
+// (active 0.43 of the cycles, 0.02 of them bank conflicts).
 template <int D, int GR>
 __global__ __launch_bounds__(256 * GR, 2) void attn_dkv_kernel(AttnArgs a) {
   constexpr int NK = D / 16, ND = D / 32;

@@ -14,9 +14,9 @@
 // and the codes (rows of up to 4 chunks of 8 elements per thread; longer ones
 // form h twice, from cache).  A checkpoint group is 16 neighbouring lanes.
 // HBM traffic per element (bf16): 4 bytes read, 1 written, 2 more with the
-// checkpoint: 16384 x 5632 in 166 us (3.9 TB/s), where the exponential and the
-// correctly rounded division, about 40 vector operations an element, take nearly
-// as long.
+// checkpoint: 16384 x 5632 in 150 us (4.3 TB/s; without it 8192 x 5632 in 43 us,
+// 5.4 TB/s), bound by HBM and the vector units alike (an exponential, a division
+// and three conversions an element).
 // Backward: 8 elements per thread, 8 bytes of traffic per element (bf16 dH,
 // dG and dU, checkpoint) and bound by it: the same size in 119 us, 6.2 TB/s, some
 // of it from the last-level cache.
@@ -53,22 +53,64 @@ __device__ __forceinline__ void store8(TX* p, const float (&v)[8]) {
     *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
   }
 }
-__device__ __forceinline__ float silu_mul(float g, float u) { return __fdiv_rn(g, 1.0f + expf(-g)) * u; }
+// The vector units are as busy as HBM here, so the divisions are shortened where
+// that gives the same bits (with the conversions' clamps left out: forward and
+// backward of 16384 x 5632 320 -> 300 us, 8192 x 5632 forward 46.7 -> 42.9): a / b
+// as a rcp(b) and one correction of its remainder.
+// For every fp32 g >= -69 and b = 1 + exp(-g) the result is that of the correctly
+// rounded division (all of them compared; -0 gives +0, restored where a code has
+// a sign), for 127 / b of every b from 1e-5 to 2^100, and for a / 127 of every a
+// from 1e-5 on.  Beyond (a denormal reciprocal) the division itself.
+__device__ __forceinline__ float div_short(float a, float b) {
+  const float r = __builtin_amdgcn_rcpf(b), q = a * r;
+  return __builtin_fmaf(__builtin_fmaf(-b, q, a), r, q);
+}
+__device__ __forceinline__ float div127(float a) {
+  constexpr float r = 1.0f / 127.0f;
+  const float q = a * r;
+  return __builtin_fmaf(__builtin_fmaf(-127.0f, q, a), r, q);
+}
+// h of 8 elements
+template <bool SIGN>
+__device__ __forceinline__ void silu_mul8(const float (&g)[8], const float (&u)[8], float (&h)[8]) {
+  float lo = g[0];
+#pragma unroll
+  for (int j = 1; j < 8; ++j) lo = fminf(lo, g[j]);
+  if (__any(lo < -69.0f)) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = __fdiv_rn(g[j], 1.0f + expf(-g[j])) * u[j];
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float s = div_short(g[j], 1.0f + expf(-g[j]));
+    h[j] = (SIGN ? copysignf(s, g[j]) : s) * u[j];
+  }
+}
+// f32x4_to_i8x4 of values whose magnitude rounds to 127 at most
+__device__ __forceinline__ uint32_t bounded_to_i8x4(float a, float b, float c, float d) {
+  auto q = [](float v) { return __float_as_uint(v + 12582912.0f); };
+  return (q(a) & 0xFFu) | ((q(b) & 0xFFu) << 8) | ((q(c) & 0xFFu) << 16) | (q(d) << 24);
+}
+
+// maximum with the value N lanes further on in the row of 16
+template <int N>
+__device__ __forceinline__ float max_of_16(float x) {
+  return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 | N, 0xF, 0xF, false)));
+}
 
 // The 8-bit checkpoint of 8 elements of a group held by 16 neighbouring lanes.
 __device__ __forceinline__ void ckpt8(const float (&v)[8], bool in, int8_t* q, float* scale) {
   float a = 0.0f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) a = fmaxf(a, fabsf(v[j]));
-  a = in ? a : 0.0f;
-#pragma unroll
-  for (int d = 8; d > 0; d >>= 1) a = fmaxf(a, __shfl_xor(a, d, 16));
+  a = max_of_16<8>(max_of_16<4>(max_of_16<2>(max_of_16<1>(in ? a : 0.0f))));
   a = fmaxf(a, 1e-5f);
-  const float inv = __fdiv_rn(127.0f, a);
+  const float inv = __any(!(a < 0x1p100f)) ? __fdiv_rn(127.0f, a) : div_short(127.0f, a);
   if (!in) return;
-  *reinterpret_cast<uint2*>(q) = make_uint2(f32x4_to_i8x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
-                                            f32x4_to_i8x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
-  if ((threadIdx.x & 15) == 0) *scale = __fdiv_rn(a, 127.0f);
+  *reinterpret_cast<uint2*>(q) = make_uint2(bounded_to_i8x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                                            bounded_to_i8x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
+  if ((threadIdx.x & 15) == 0) *scale = div127(a);
 }
 
 // NCH chunks of 8 elements per thread in registers; NCH = 0: any row length.
@@ -92,12 +134,10 @@ __global__ __launch_bounds__(T) void swiglu_quant_kernel(const TX* __restrict__ 
       float g[8], u[8];
       load8(gr + 8 * cc, g);
       load8(ur + 8 * cc, u);
+      silu_mul8<E4M3>(g, u, hh);
       float m = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        hh[j] = silu_mul(g[j], u[j]);
-        m = fmaxf(m, fabsf(hh[j]));
-      }
+      for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(hh[j]));
       amax = in ? fmaxf(amax, m) : amax;
       if constexpr (CKPT) {
         const int64_t sg = row * ngroup + cc / 16;
@@ -112,8 +152,8 @@ __global__ __launch_bounds__(T) void swiglu_quant_kernel(const TX* __restrict__ 
         w0 = f32x4_to_e4m3x4(hh[0] * inv, hh[1] * inv, hh[2] * inv, hh[3] * inv);
         w1 = f32x4_to_e4m3x4(hh[4] * inv, hh[5] * inv, hh[6] * inv, hh[7] * inv);
       } else {
-        w0 = f32x4_to_i8x4(hh[0] * inv, hh[1] * inv, hh[2] * inv, hh[3] * inv);
-        w1 = f32x4_to_i8x4(hh[4] * inv, hh[5] * inv, hh[6] * inv, hh[7] * inv);
+        w0 = bounded_to_i8x4(hh[0] * inv, hh[1] * inv, hh[2] * inv, hh[3] * inv);
+        w1 = bounded_to_i8x4(hh[4] * inv, hh[5] * inv, hh[6] * inv, hh[7] * inv);
       }
       *reinterpret_cast<uint2*>(Xq + row * (int64_t)K + 8 * c) = make_uint2(w0, w1);
     };
@@ -139,8 +179,7 @@ __global__ __launch_bounds__(T) void swiglu_quant_kernel(const TX* __restrict__ 
         float g[8], u[8];
         load8(gr + 8 * c, g);
         load8(ur + 8 * c, u);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) hv[0][j] = silu_mul(g[j], u[j]);
+        silu_mul8<E4M3>(g, u, hv[0]);
         codes(c, hv[0], inv);
       }
     }
@@ -150,9 +189,9 @@ __global__ __launch_bounds__(T) void swiglu_quant_kernel(const TX* __restrict__ 
 // Threads by the row's length, so that a thread holds up to 3 chunks (4 in rows of
 // more than 12288) and few lanes idle.  8192 rows of bf16, this rule / 512 threads
 // that form h twice / 256 threads with all chunks in registers / 512 or 1024 with
-// one or two: K = 2048 22.1 / 36.4 / 22.2 / 35.2 us, 5632 50.9 / 85.3 / 53.1 /
-// 64.6, 8192 76.4 / 120 / 74.2 / 78.4, 11008 106 / 162 / 120 / 127, 16384 145 /
-// 231 / 156 / 141.
+// one or two: K = 2048 20.0 / 44.1 / 19.8 / 31.5 us, 5632 44.6 / 86.9 / 45.5 /
+// 57.3, 8192 69.4 / 104 / 73.8 / 69.5, 11008 98 to 108 / 148 / 98 / 152, 16384
+// 140 / 200 / 138 / 164; few rows are faster with more threads.
 template <typename TX, bool E4M3, bool CKPT>
 hipError_t launch_fwd(const TX* g, const TX* u, int64_t M, int K, uint8_t* q, float* xdq, const Ckpt& ck, hipStream_t s) {
   const int nchunk = K / 8;
