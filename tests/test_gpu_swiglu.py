@@ -119,6 +119,38 @@ def test_swiglu_backward_in_place_and_empty(lib):
     dqt.dqt_swiglu_backward(e, e, e, e, e)
 
 
+@pytest.mark.parametrize("act", ["i8", "e4m3"])
+def test_swiglu_codes_are_those_of_single_operations(lib, act):
+    """Every finite bf16 gate, bit for bit against the same fp32 operations one
+    by one; -0, gates whose exponential is huge, and tiny rows among them."""
+    g = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    g[~torch.isfinite(g) | (g.float().abs() > 1e4)] = 0.0
+    gen = torch.Generator().manual_seed(21)
+    G = torch.cat([g.view(256, 256), g[torch.randperm(65536, generator=gen)].view(256, 256)])
+    U = torch.randn(G.shape, generator=gen).to(torch.bfloat16)
+    U[::7] *= 1e-6
+    G, U = G.to(DEV), U.to(DEV)
+    M, K = G.shape
+    log(f"swiglu: every bf16 gate, {act}")
+    Xq = torch.empty((M, K), dtype=torch.int8 if act == "i8" else torch.uint8, device=DEV)
+    xdq = torch.empty((M,), dtype=torch.float32, device=DEV)
+    ck = dqt.swiglu_ckpt(M, K)
+    dqt.dqt_swiglu_act_quant(G, U, dqt.DQT_I8 if act == "i8" else dqt.DQT_FP8E4M3, Xq, xdq, ck)
+    gf, uf = G.float(), U.float()
+    h = (gf / (1.0 + torch.exp(-gf))) * uf
+    top = torch.tensor(127.0 if act == "i8" else 448.0, device=DEV)
+    m = h.abs().amax(1).clamp(min=float(np.float32(1e-5)))
+    y = h * (top / m)[:, None]
+    want = (torch.round(y).clamp(-128, 127).to(torch.int8) if act == "i8"
+            else y.clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8))
+    torch.cuda.synchronize()
+    assert torch.equal(xdq, m / top)
+    assert torch.equal(Xq, want)
+    for x, q, s in ((G, ck.Gq, ck.gs), (U, ck.Uq, ck.us)):
+        codes, scales = R.checkpoint(x.cpu())
+        assert np.array_equal(q.cpu().numpy(), codes) and np.array_equal(s.cpu().numpy(), scales)
+
+
 def test_swiglu_more_rows_than_blocks(lib):
     """Rows past the largest grid give what the same rows give on their own."""
     M, K = 70001, 32
