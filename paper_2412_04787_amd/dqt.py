@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -203,10 +204,13 @@ def _nbytes(t):
 
 def _same(*ts):
     """The shape [M, K] that contiguous tensors of one dtype share."""
-    for t in ts:
-        if t.shape != ts[0].shape or t.dtype != ts[0].dtype or not t.is_contiguous():
-            raise ValueError("expected contiguous tensors of one shape and dtype")
-    return ts[0].shape
+    shape, dtype = ts[0].shape, ts[0].dtype
+    ok = ts[0].is_contiguous()
+    for t in ts[1:]:
+        ok = ok and t.dtype is dtype and t.shape == shape and t.is_contiguous()
+    if not ok:
+        raise ValueError("expected contiguous tensors of one shape and dtype")
+    return shape
 
 
 def _here(t):
@@ -234,10 +238,15 @@ def _stream(stream=None):
     return ctypes.c_void_p(c._cuda_getCurrentRawStream(c._cuda_getDevice()))
 
 
+_DTYPE_CODES = {}       # (filled on first use: torch is imported late)
+
+
 def dtype_code(t) -> int:
-    torch = _torch()
-    return {torch.float32: DQT_F32, torch.bfloat16: DQT_BF16, torch.int8: DQT_I8,
-            torch.float8_e4m3fn: DQT_FP8E4M3, torch.uint8: DQT_FP8E4M3}[t.dtype]
+    if not _DTYPE_CODES:
+        torch = _torch()
+        _DTYPE_CODES.update({torch.float32: DQT_F32, torch.bfloat16: DQT_BF16, torch.int8: DQT_I8,
+                             torch.float8_e4m3fn: DQT_FP8E4M3, torch.uint8: DQT_FP8E4M3})
+    return _DTYPE_CODES[t.dtype]
 
 
 def dqt_act_quant(X, act_q: int, Xq, xdq, stream=None):
@@ -361,19 +370,21 @@ def attn(q_tokens: int, k_tokens: int, heads: int, kv_heads: int, d: int, q_star
     a = DqtAttn(_addr(q_start), _addr(k_start), q_tokens, k_tokens, n.pop(), heads, kv_heads, d,
                 d ** -0.5 if scale is None else scale, int(causal), 0)
     a._keep = (q_start, k_start)
-    a._shapes = ((q_tokens, heads, d), (k_tokens, kv_heads, d))
+    a._shapes = {"q": (q_tokens, heads, d), "k": (k_tokens, kv_heads, d)}
     return a
 
 
+_pack_rows = struct.Struct("3q").pack
+
+
 def _rows(a: DqtAttn, tensors, kinds: str):
-    """The dqt_rows of bf16 tensors [q_tokens, heads, d] (kind "q") or
-    [k_tokens, kv_heads, d] ("k") with any token and head strides: an array of
-    (address, token stride, head stride), 24 bytes each, and their addresses."""
-    bf16 = _torch().bfloat16
+    """The dqt_rows (as bytes) of bf16 tensors [q_tokens, heads, d] (kind "q") or
+    [k_tokens, kv_heads, d] ("k") with any token and head strides."""
+    bf16, shapes = _torch().bfloat16, a._shapes
     _here(tensors[0])
-    v = []
+    rows = []
     for t, kind in zip(tensors, kinds):
-        shape = a._shapes[kind == "k"]
+        shape = shapes[kind]
         if t.dtype is not bf16 or t.shape != shape:
             raise ValueError(f"expected a bfloat16 tensor of shape {shape}, got {t.dtype} {tuple(t.shape)}")
         st, sh, sd = t.stride()
@@ -381,10 +392,8 @@ def _rows(a: DqtAttn, tensors, kinds: str):
             raise ValueError(f"expected unit last stride, got strides {t.stride()}")
         n, h, d = shape
         # (strides of a dimension of one do not matter)
-        v += (t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d)
-    arr = (ctypes.c_int64 * len(v))(*v)
-    first = ctypes.addressof(arr)
-    return arr, range(first, first + 8 * len(v), 24)
+        rows.append(_pack_rows(t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d))
+    return rows
 
 
 def dqt_attn_fwd_workspace(a: DqtAttn) -> int:
@@ -394,7 +403,7 @@ def dqt_attn_fwd_workspace(a: DqtAttn) -> int:
 def dqt_attn_fwd(a: DqtAttn, Q, K, V, O, lse=None, ws=None, stream=None):
     """Q, O: [q_tokens, heads, d]; K, V: [k_tokens, kv_heads, d], bf16 with any
     token and head strides; lse: fp32 [heads, q_tokens] or None."""
-    keep, r = _rows(a, (Q, K, V, O), "qkkq")
+    r = _rows(a, (Q, K, V, O), "qkkq")
     _check("dqt_attn_fwd", load().dqt_attn_fwd(ctypes.byref(a), *r, _addr(lse), _addr(ws), _nbytes(ws),
                                                _stream(stream)))
 
@@ -405,7 +414,7 @@ def dqt_attn_bwd_workspace(a: DqtAttn) -> int:
 
 def dqt_attn_bwd(a: DqtAttn, Q, K, V, O, lse, dO, dQ, dK, dV, ws, stream=None):
     """Shapes as dqt_attn_fwd; dO, dQ like Q, dK and dV like K."""
-    keep, r = _rows(a, (Q, K, V, O, dO, dQ, dK, dV), "qkkqqqkk")
+    r = _rows(a, (Q, K, V, O, dO, dQ, dK, dV), "qkkqqqkk")
     _check("dqt_attn_bwd", load().dqt_attn_bwd(ctypes.byref(a), *r[:4], _addr(lse), *r[4:], _addr(ws), _nbytes(ws),
                                                _stream(stream)))
 
