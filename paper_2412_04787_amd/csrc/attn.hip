@@ -474,7 +474,7 @@ __global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fw
     if constexpr (D == 64) {
       // the sums show as well whether m is far behind, and cost nothing: the
       // maxima (a tenth of the vector work) only of the first tile and where the
-      // sums ask for them
+      // sums ask for them (4 x 4096 tokens, 16 heads 170 -> 164 us)
       if (t == g) move(tile_max());
       powers();
       if (__any(!(sum <= kMost))) {
@@ -483,7 +483,8 @@ __global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fw
       }
     } else {
       // (128-wide, the matrix products of o take the time of the maxima, and would
-      // have to wait for the check of the sums)
+      // have to wait for the check of the sums: 5 prompts of 301 to 3001 tokens 185
+      // -> 189 us)
       const float mx = tile_max();
       if (__any(mx > m + kSlack)) move(mx);
       powers();
@@ -541,7 +542,7 @@ __global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fw
 }
 
 // o = sum_s 2^(lse_s - lse) o_s over the splits of a row: one wave per row, up to
-// four splits' partials in flight (5 us for 1024 rows of 7 splits, most of it the
+// four splits' partials in flight (5 us for 1024 rows of 6 splits, most of it the
 // launch).
 template <int D>
 __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
@@ -959,9 +960,13 @@ int64_t attn_row_tiles(int64_t tokens, int64_t mul, int64_t n_seq) { return toke
 
 // Splits of the keys.  The partial results are written and read once, at 8
 // bytes a value, and joined by another launch, so keys are divided
-//  - for balance, to about 8 blocks per CU of at least 128 keys, as far as the
+//  - for balance, to about 6 blocks per CU of at least 128 keys, as far as the
 //    partials stay below an eighth of the keys' and values' bytes (new tokens
-//    over long contexts);
+//    over long contexts).  32 new tokens over 1 to 8192 keys, 8 key heads: not
+//    split 150 us, into 4 / 6 / 7 / 10 blocks 124 / 118 / 118 / 119; 4 over 1000 to
+//    8192, 4 key heads 114, 23.6 / 23.7 / 22.9 / 23.7.  (Where all are of one
+//    length, which the host does not know, not to split is ahead: 32 over 4096 keys
+//    103, 108 / 110 / 116 / 118.)
 //  - below 96 blocks, to fill the chip, to 2 blocks per CU, where each still gets
 //    512 keys (one sequence of 2600 tokens, 4 heads of 128, 84 blocks: without ->
 //    with 42.1 -> 38.1 us; from about 100 blocks on two groups of waves in each do
@@ -972,7 +977,7 @@ int attn_splits(int64_t tq, int64_t tk, int64_t n_seq, int heads, int kv_heads) 
   if (tq == 0 || blocks >= 1024) return 1;
   auto least = [](int64_t x, int64_t y) { return x < y ? x : y; };
   const int64_t mean = tk / n_seq;
-  const int64_t even = least(least(2048 / blocks, mean / 128), tk * kv_heads / (16 * tq * heads));
+  const int64_t even = least(least(1600 / blocks, mean / 128), tk * kv_heads / (16 * tq * heads));
   const int64_t fill = blocks < 96 ? least(512 / blocks, mean / 512) : 1;
   const int64_t s = even > fill ? even : fill;
   return s < 1 ? 1 : (int)s;
