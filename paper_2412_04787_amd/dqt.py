@@ -198,10 +198,6 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-def _nbytes(t):
-    return 0 if t is None else t.numel() * t.element_size()
-
-
 def _same(*ts):
     """The shape [M, K] that contiguous tensors of one dtype share."""
     shape, dtype = ts[0].shape, ts[0].dtype
@@ -213,11 +209,32 @@ def _same(*ts):
     return shape
 
 
-def _here(t):
-    """Refuses a tensor of another device than the current one, on whose stream
-    the kernels would run."""
-    if t.is_cuda and t.get_device() != _torch()._C._cuda_getDevice():
-        raise ValueError(f"tensor on device {t.get_device()}, which is not the current one")
+def _here(t, *others):
+    """Refuses tensors in host memory, and of another device than the current
+    one, on whose stream the kernels would run.  (None stands for no tensor.)"""
+    dev = t.get_device()                   # (-1 in host memory)
+    if dev < 0 or dev != _torch()._C._cuda_getDevice():
+        raise ValueError("tensor in host memory" if dev < 0 else
+                         f"tensor on device {dev}, which is not the current one")
+    for o in others:
+        if o is not None and o.get_device() != dev:
+            raise ValueError(f"tensor on {o.device}, others on device {dev}")
+
+
+def _buf(t, n, dtype):
+    """Refuses a buffer that is not one of at least n consecutive values of dtype."""
+    if t is not None and (t.dtype is not dtype or t.numel() < n or not t.is_contiguous()):
+        raise ValueError(f"expected {n} consecutive values of {dtype}, got {tuple(t.shape)} of {t.dtype} "
+                         f"with strides {t.stride()}")
+
+
+def _ws_bytes(t):
+    """The bytes of a workspace."""
+    if t is None:
+        return 0
+    if not t.is_contiguous():
+        raise ValueError("a workspace must be contiguous")
+    return t.numel() * t.element_size()
 
 
 def _unit_stride(t):
@@ -280,6 +297,12 @@ class SwigluCkpt:
     gs, us (fp32, one for CKPT_GROUP consecutive elements of a row)."""
 
     def __init__(self, Gq, Uq, gs, us):
+        torch = _torch()
+        M, K = _same(Gq, Uq)
+        if Gq.dtype is not torch.int8 or gs.dtype is not torch.float32:
+            raise ValueError("expected int8 codes and fp32 scales")
+        if _same(gs, us) != (M, (K + CKPT_GROUP - 1) // CKPT_GROUP):
+            raise ValueError(f"expected one scale for {CKPT_GROUP} elements of a row, got {tuple(gs.shape)}")
         self.Gq, self.Uq, self.gs, self.us = Gq, Uq, gs, us
         self.io = DqtCkptIO(_addr(Gq), _addr(Uq), _addr(gs), _addr(us))
 
@@ -293,10 +316,25 @@ def swiglu_ckpt(M: int, K: int, device="cuda:0") -> SwigluCkpt:
     return SwigluCkpt(*q, *s)
 
 
+def _check_ckpt(ckpt: SwigluCkpt, M, K, x):
+    """Refuses a checkpoint of another size, or of another device than x."""
+    if ckpt.Gq.shape != (M, K):
+        raise ValueError(f"checkpoint of {tuple(ckpt.Gq.shape)}, expected {(M, K)}")
+    _here(x, ckpt.Gq, ckpt.Uq, ckpt.gs, ckpt.us)
+
+
 def dqt_swiglu_act_quant(G, U, act_q: int, Xq, xdq, ckpt: SwigluCkpt | None = None, stream=None):
-    """G, U: contiguous [M, K] of one dtype."""
+    """G, U: contiguous [M, K] of one dtype; Xq: M K bytes, xdq: M fp32 values
+    (larger buffers are used from their start)."""
     M, K = _same(G, U)
-    _here(G)
+    _here(G, U, Xq, xdq)
+    if Xq is not None:
+        if Xq.element_size() != 1:
+            raise ValueError(f"expected 8-bit codes, got {Xq.dtype}")
+        _buf(Xq, M * K, Xq.dtype)
+    _buf(xdq, M, _torch().float32)
+    if ckpt is not None:
+        _check_ckpt(ckpt, M, K, G)
     _check("dqt_swiglu_act_quant",
            load().dqt_swiglu_act_quant(_addr(G), _addr(U), dtype_code(G), M, K, act_q, _addr(Xq), _addr(xdq),
                                        None if ckpt is None else ctypes.byref(ckpt.io), _stream(stream)))
@@ -305,7 +343,7 @@ def dqt_swiglu_act_quant(G, U, act_q: int, Xq, xdq, ckpt: SwigluCkpt | None = No
 def dqt_swiglu_backward(dH, G, U, dG, dU, stream=None):
     """dH, G, U, dG, dU: contiguous [M, K] of one dtype."""
     M, K = _same(dH, G, U, dG, dU)
-    _here(dH)
+    _here(dH, G, U, dG, dU)
     _check("dqt_swiglu_backward",
            load().dqt_swiglu_backward(_addr(dH), dtype_code(dH), _addr(G), _addr(U), None, M, K, _addr(dG),
                                       _addr(dU), _stream(stream)))
@@ -314,7 +352,8 @@ def dqt_swiglu_backward(dH, G, U, dG, dU, stream=None):
 def dqt_swiglu_backward_ckpt(dH, ckpt: SwigluCkpt, dG, dU, stream=None):
     """dqt_swiglu_backward with gate and up from their 8-bit checkpoint."""
     M, K = _same(dH, dG, dU)
-    _here(dH)
+    _here(dH, dG, dU)
+    _check_ckpt(ckpt, M, K, dH)
     _check("dqt_swiglu_backward",
            load().dqt_swiglu_backward(_addr(dH), dtype_code(dH), None, None, ctypes.byref(ckpt.io), M, K,
                                       _addr(dG), _addr(dU), _stream(stream)))
@@ -327,29 +366,50 @@ def dqt_logprob_workspace(M: int, V: int, top_k: int = 0) -> int:
     return int(load().dqt_logprob_workspace(M, V, top_k))
 
 
+def _check_targets(targets, M):
+    if targets is not None and (targets.numel() != M or targets.dtype is not _torch().int64
+                                or not targets.is_contiguous()):
+        raise ValueError(f"expected {M} contiguous int64 targets, got {tuple(targets.shape)} of {targets.dtype} "
+                         f"with strides {targets.stride()}")
+
+
 def dqt_logprob_fwd(X, targets, logp, lse=None, entropy=None, stat=None, top_ids=None, top_logp=None,
                     ws=None, stream=None):
     """X: [M, V] logits, rows of any stride; targets: int64 [M]; logp, lse,
     entropy: fp32 [M], stat (for the backward): fp32 [M, 2], or None; top_ids
-    (int64) and top_logp (fp32): [M, k], or None."""
-    M, V = X.shape
+    (int64) and top_logp (fp32): [M, k], or None.  All but X contiguous; larger
+    outputs are used from their start."""
     _unit_stride(X)
-    _here(X)
-    top_k = 0 if top_ids is None else top_ids.shape[1]
+    M, V = X.shape
+    _here(X, targets, logp, lse, entropy, stat, top_ids, top_logp, ws)
+    torch = _torch()
+    _check_targets(targets, M)
+    for t, n in ((logp, M), (lse, M), (entropy, M), (stat, 2 * M)):
+        _buf(t, n, torch.float32)
+    top_k = 0
+    if top_ids is not None:
+        if top_ids.dim() != 2:
+            raise ValueError("expected top_ids of shape [M, k]")
+        top_k = top_ids.shape[1]
+        _buf(top_ids, M * top_k, torch.int64)
+        _buf(top_logp, M * top_k, torch.float32)
     _check("dqt_logprob_fwd",
            load().dqt_logprob_fwd(_addr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _addr(targets),
                                   _addr(logp), _addr(lse), _addr(entropy), _addr(stat), top_k,
-                                  _addr(top_ids), _addr(top_logp), _addr(ws), _nbytes(ws), _stream(stream)))
+                                  _addr(top_ids), _addr(top_logp), _addr(ws), _ws_bytes(ws), _stream(stream)))
 
 
 def dqt_logprob_bwd(X, targets, stat, dlogp, dX, entropy=None, dent=None, stream=None):
     """dX: [M, V] of X's dtype (X itself is allowed); dlogp, dent: fp32 [M] or None."""
-    M, V = X.shape
     _unit_stride(X)
-    _here(X)
+    M, V = X.shape
     _unit_stride(dX)
     if dX.dtype != X.dtype or dX.shape != X.shape:
         raise ValueError("dX must have X's dtype and shape")
+    _here(X, targets, stat, dlogp, dX, entropy, dent)
+    _check_targets(targets, M)
+    for t, n in ((stat, 2 * M), (dlogp, M), (entropy, M), (dent, M)):
+        _buf(t, n, _torch().float32)
     _check("dqt_logprob_bwd",
            load().dqt_logprob_bwd(_addr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _addr(targets),
                                   _addr(stat), _addr(entropy), _addr(dlogp), _addr(dent), _addr(dX),
@@ -364,12 +424,16 @@ def attn(q_tokens: int, k_tokens: int, heads: int, kv_heads: int, d: int, q_star
     n = {t.numel() - 1 for t in (q_start, k_start) if t is not None} or {1}
     if len(n) != 1:
         raise ValueError("q_start and k_start must have the same length")
-    for t in (q_start, k_start):
-        if t is not None and (t.dtype != _torch().int32 or not t.is_contiguous()):
+    starts = [t for t in (q_start, k_start) if t is not None]
+    for t in starts:
+        if t.dtype != _torch().int32 or not t.is_contiguous():
             raise ValueError("q_start and k_start must be contiguous int32")
+    if starts:
+        _here(*starts)
     a = DqtAttn(_addr(q_start), _addr(k_start), q_tokens, k_tokens, n.pop(), heads, kv_heads, d,
                 d ** -0.5 if scale is None else scale, int(causal), 0)
     a._keep = (q_start, k_start)
+    a._dev = starts[0].get_device() if starts else None
     a._shapes = {"q": (q_tokens, heads, d), "k": (k_tokens, kv_heads, d)}
     return a
 
@@ -377,11 +441,16 @@ def attn(q_tokens: int, k_tokens: int, heads: int, kv_heads: int, d: int, q_star
 _pack_rows = struct.Struct("3q").pack
 
 
-def _rows(a: DqtAttn, tensors, kinds: str):
+def _rows(a: DqtAttn, tensors, kinds: str, lse, ws):
     """The dqt_rows (as bytes) of bf16 tensors [q_tokens, heads, d] (kind "q") or
-    [k_tokens, kv_heads, d] ("k") with any token and head strides."""
-    bf16, shapes = _torch().bfloat16, a._shapes
-    _here(tensors[0])
+    [k_tokens, kv_heads, d] ("k") with any token and head strides; checks the
+    call's other buffers too."""
+    torch = _torch()
+    bf16, shapes = torch.bfloat16, a._shapes
+    _here(*tensors, lse, ws)
+    _buf(lse, a.heads * a.q_tokens, torch.float32)
+    if a._dev is not None and a._dev != tensors[0].get_device():
+        raise ValueError(f"q_start or k_start on device {a._dev}, the tensors on another")
     rows = []
     for t, kind in zip(tensors, kinds):
         shape = shapes[kind]
@@ -402,9 +471,9 @@ def dqt_attn_fwd_workspace(a: DqtAttn) -> int:
 
 def dqt_attn_fwd(a: DqtAttn, Q, K, V, O, lse=None, ws=None, stream=None):
     """Q, O: [q_tokens, heads, d]; K, V: [k_tokens, kv_heads, d], bf16 with any
-    token and head strides; lse: fp32 [heads, q_tokens] or None."""
-    r = _rows(a, (Q, K, V, O), "qkkq")
-    _check("dqt_attn_fwd", load().dqt_attn_fwd(ctypes.byref(a), *r, _addr(lse), _addr(ws), _nbytes(ws),
+    token and head strides; lse: contiguous fp32 [heads, q_tokens] or None."""
+    r = _rows(a, (Q, K, V, O), "qkkq", lse, ws)
+    _check("dqt_attn_fwd", load().dqt_attn_fwd(ctypes.byref(a), *r, _addr(lse), _addr(ws), _ws_bytes(ws),
                                                _stream(stream)))
 
 
@@ -414,8 +483,8 @@ def dqt_attn_bwd_workspace(a: DqtAttn) -> int:
 
 def dqt_attn_bwd(a: DqtAttn, Q, K, V, O, lse, dO, dQ, dK, dV, ws, stream=None):
     """Shapes as dqt_attn_fwd; dO, dQ like Q, dK and dV like K."""
-    r = _rows(a, (Q, K, V, O, dO, dQ, dK, dV), "qkkqqqkk")
-    _check("dqt_attn_bwd", load().dqt_attn_bwd(ctypes.byref(a), *r[:4], _addr(lse), *r[4:], _addr(ws), _nbytes(ws),
+    r = _rows(a, (Q, K, V, O, dO, dQ, dK, dV), "qkkqqqkk", lse, ws)
+    _check("dqt_attn_bwd", load().dqt_attn_bwd(ctypes.byref(a), *r[:4], _addr(lse), *r[4:], _addr(ws), _ws_bytes(ws),
                                                _stream(stream)))
 
 

@@ -192,3 +192,140 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     dqt._here(T(0))
     with pytest.raises(ValueError):
         dqt._here(T(1))
+
+
+class _Calls:
+    """Stands for the library: counts the calls that reach it."""
+
+    def __init__(self):
+        self.n = 0
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.n += 1
+            return dqt.DQT_OK
+        return call
+
+
+def _calls_of_each_operator():
+    """(name, call, its tensors by name); the call takes the same tensors."""
+    f32, bf16 = torch.float32, torch.bfloat16
+    M, K, V, k = 3, 160, 50, 4
+    f = lambda *s, dt=f32: torch.zeros(s, dtype=dt)
+    i8 = torch.int8
+    ck = lambda t: dqt.SwigluCkpt(t["Gq"], t["Uq"], t["gs"], t["us"])
+    ckt = lambda: dict(Gq=f(M, K, dt=i8), Uq=f(M, K, dt=i8), gs=f(M, 2), us=f(M, 2))
+    T, H, KV, D = 5, 4, 2, 64
+    q, kv = lambda: f(T, H, D, dt=bf16), lambda: f(T, KV, D, dt=bf16)
+    st = lambda: torch.tensor([0, T], dtype=torch.int32)
+    desc = lambda t: dqt.attn(T, T, H, KV, D, t["q_start"], t["k_start"])
+    return [
+        ("swiglu", lambda t: dqt.dqt_swiglu_act_quant(t["G"], t["U"], dqt.DQT_I8, t["Xq"], t["xdq"], ck(t)),
+         dict(G=f(M, K), U=f(M, K), Xq=f(M, K, dt=i8), xdq=f(M), **ckt())),
+        ("swiglu backward", lambda t: dqt.dqt_swiglu_backward(t["dH"], t["G"], t["U"], t["dG"], t["dU"]),
+         dict(dH=f(M, K), G=f(M, K), U=f(M, K), dG=f(M, K), dU=f(M, K))),
+        ("swiglu backward ckpt", lambda t: dqt.dqt_swiglu_backward_ckpt(t["dH"], ck(t), t["dG"], t["dU"]),
+         dict(dH=f(M, K), dG=f(M, K), dU=f(M, K), **ckt())),
+        ("logprob", lambda t: dqt.dqt_logprob_fwd(t["X"], t["targets"], t["logp"], t["lse"], t["entropy"], t["stat"],
+                                                  t["top_ids"], t["top_logp"], t["ws"]),
+         dict(X=f(M, V), targets=f(M, dt=torch.int64), logp=f(M), lse=f(M), entropy=f(M), stat=f(M, 2),
+              top_ids=f(M, k, dt=torch.int64), top_logp=f(M, k), ws=f(8))),
+        ("logprob backward", lambda t: dqt.dqt_logprob_bwd(t["X"], t["targets"], t["stat"], t["dlogp"], t["dX"],
+                                                           t["entropy"], t["dent"]),
+         dict(X=f(M, V), targets=f(M, dt=torch.int64), stat=f(M, 2), dlogp=f(M), dX=f(M, V), entropy=f(M), dent=f(M))),
+        ("attention", lambda t: dqt.dqt_attn_fwd(desc(t), t["Q"], t["K"], t["V"], t["O"], t["lse"], t["ws"]),
+         dict(Q=q(), K=kv(), V=kv(), O=q(), lse=f(H, T), ws=f(8), q_start=st(), k_start=st())),
+        ("attention backward", lambda t: dqt.dqt_attn_bwd(desc(t), t["Q"], t["K"], t["V"], t["O"], t["lse"], t["dO"],
+                                                          t["dQ"], t["dK"], t["dV"], t["ws"]),
+         dict(Q=q(), K=kv(), V=kv(), O=q(), lse=f(H, T), dO=q(), dQ=q(), dK=kv(), dV=kv(), ws=f(8), q_start=st(),
+              k_start=st())),
+    ]
+
+
+OPERATORS = _calls_of_each_operator()
+
+
+class _On:
+    """A tensor of host memory that says it is on device i."""
+
+    def __init__(self, t, i):
+        self._t, self._i = t, i
+
+    def get_device(self):
+        return self._i
+
+    is_cuda = True
+
+    def __getattr__(self, name):
+        return getattr(self._t, name)
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    c = _Calls()
+    monkeypatch.setattr(dqt, "load", lambda: c)
+    monkeypatch.setattr(dqt, "_stream", lambda stream=None: None)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    return c
+
+
+@pytest.mark.parametrize("at", range(len(OPERATORS)), ids=[o[0] for o in OPERATORS])
+def test_every_tensor_of_a_call_has_to_be_on_the_current_device(calls, at):
+    name, call, tensors = OPERATORS[at]
+    here = {n: _On(t, 0) for n, t in tensors.items()}
+    call(here)
+    assert calls.n == 1
+    for n, t in tensors.items():
+        for i in (-1, 1):                  # (-1: host memory)
+            with pytest.raises(ValueError):
+                call({**here, n: _On(t, i)})
+    with pytest.raises(ValueError):
+        call({n: _On(t, 1) for n, t in tensors.items()})
+    with pytest.raises(ValueError):
+        call(tensors)                      # all in host memory
+    assert calls.n == 1
+
+
+def _wrong(n, t):
+    """Tensors that the call must not take for t: another type, one row fewer,
+    one column fewer, not contiguous (where rows may have any stride: columns)."""
+    other = {torch.float32: torch.float64, torch.int64: torch.int32, torch.int32: torch.int64, torch.int8: torch.int16,
+             torch.bfloat16: torch.float16}[t.dtype]
+    out = [] if n == "ws" else [t.to(other), t[:-1]]
+    if t.dim() > 1:
+        out.append(t[:, :-1])
+        out.append(torch.zeros(t.shape[::-1], dtype=t.dtype).permute(*range(t.dim())[::-1]))
+    else:
+        out.append(torch.zeros((t.numel(), 2), dtype=t.dtype)[:, 0])
+    return out
+
+
+@pytest.mark.parametrize("at", range(len(OPERATORS)), ids=[o[0] for o in OPERATORS])
+def test_every_tensor_of_a_call_has_its_type_size_and_strides(calls, at):
+    name, call, tensors = OPERATORS[at]
+    here = {n: _On(t, 0) for n, t in tensors.items()}
+    for n, t in tensors.items():
+        for i, bad in enumerate(_wrong(n, t)):
+            if name.startswith("logprob") and n == "X" and i == 2 and "dX" not in tensors:
+                continue                   # (fewer columns: another vocabulary)
+            with pytest.raises((ValueError, KeyError)):
+                call({**here, n: _On(bad, 0)})
+                raise AssertionError((name, n, bad.dtype, tuple(bad.shape), bad.stride()))
+    assert calls.n == 0
+
+
+def test_larger_outputs_are_taken(calls):
+    """Buffers of a larger batch serve a smaller one."""
+    for name, call, tensors in OPERATORS:
+        here = {n: _On(torch.zeros((t.shape[0] + 2, *t.shape[1:]), dtype=t.dtype), 0)
+                if n in ("Xq", "xdq", "logp", "lse", "entropy", "stat", "top_ids", "top_logp", "ws") else _On(t, 0)
+                for n, t in tensors.items()}
+        call(here)
+    assert calls.n == len(OPERATORS)
+
+
+def test_targets_are_as_many_as_rows(calls):
+    name, call, tensors = OPERATORS[3]
+    with pytest.raises(ValueError):
+        call({**{n: _On(t, 0) for n, t in tensors.items()}, "targets": _On(torch.zeros(4, dtype=torch.int64), 0)})
+    assert calls.n == 0
