@@ -445,10 +445,13 @@ class DQTModel:
         return hn @ self.head.to(torch.bfloat16).t()
 
     def loss(self, tokens, targets, starts=None):
-        """Forward of one batch: mean next-token cross-entropy (fp32)."""
+        """Forward of one batch: mean next-token cross-entropy (fp32).  targets:
+        int64 on the device, one a token, of any strides.  With own_ops every
+        target outside the vocabulary is padding (the PyTorch form takes -100 alone
+        and refuses others), and a batch of nothing else has loss 0 (there NaN)."""
         logits = self.logits(tokens, starts)
         if self.cfg.own_ops:
-            return _OwnFns.get()[2].apply(logits, targets.reshape(-1), self)
+            return _OwnFns.get()[2].apply(logits, targets.reshape(-1).contiguous(), self)
         return dqt._torch().nn.functional.cross_entropy(logits.float(), targets.reshape(-1))
 
     def score(self, tokens, targets, top_k=0, starts=None):
@@ -465,7 +468,7 @@ class DQTModel:
             out = dict(logp=f(M), entropy=f(M))
             if top_k:
                 out.update(top_ids=torch.empty((M, top_k), dtype=torch.int64, device=x.device), top_logp=f(M, top_k))
-            dqt.dqt_logprob_fwd(x, targets.reshape(-1), out["logp"], None, out["entropy"], None, out.get("top_ids"),
+            dqt.dqt_logprob_fwd(x, targets.reshape(-1).contiguous(), out["logp"], None, out["entropy"], None, out.get("top_ids"),
                                 out.get("top_logp"), self.workspace(dqt.dqt_logprob_workspace(M, V, top_k)))
         return {k: v.view(self.cfg.batch, self.cfg.seq, *v.shape[1:]) for k, v in out.items()}
 

@@ -210,3 +210,21 @@ def test_calls_on_another_stream(lib):
     a, b = go(None), go(torch.cuda.Stream())
     for n in a:
         assert torch.equal(a[n], b[n]), n
+
+
+def test_strided_targets(lib):
+    """Targets that are every second value of a tensor: loss, gradients and
+    scores of their contiguous copy."""
+    cfg = MS.MODELS["tiny_ops"]
+    tok, tgt = MS.synthetic_batch(cfg, 4)
+    both = torch.stack((tok, tgt), dim=-1)
+    log("model: strided targets")
+    got = []
+    for t in (tgt, both[..., 1]):
+        model = MS.DQTModel(cfg)
+        out = model.score(tok, t, top_k=2)
+        loss = model.loss(tok, t)
+        loss.backward()
+        got.append([loss.detach(), model.head.grad, model.emb.grad, *out.values()])
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
