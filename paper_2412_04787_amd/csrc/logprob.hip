@@ -37,9 +37,11 @@ constexpr int kRounds = 16;       // rounds of a row whose maxima are kept (16 K
 
 __device__ __forceinline__ float inf() { return __builtin_inff(); }
 
-// fp32 bits as an unsigned integer of the same order
+// fp32 bits as an unsigned integer of the same order, the two zeros as one (by an
+// integer select: as x + 0 the compiler may drop it)
 __device__ __forceinline__ uint32_t order_bits(float x) {
-  const uint32_t u = __float_as_uint(x);
+  uint32_t u = __float_as_uint(x);
+  u = u == 0x80000000u ? 0u : u;
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float from_order(uint32_t o) {

@@ -256,3 +256,33 @@ def test_logprob_empty(lib):
     v = torch.empty((0,), device=DEV)
     dqt.dqt_logprob_fwd(e, v.long(), v, v)
     dqt.dqt_logprob_bwd(e, v.long(), torch.empty((0, 2), device=DEV), v, e)
+
+
+def zeros_of_both_signs(M, V, dt):
+    """Rows whose largest logits are zeros of either sign: ties over the k-th
+    place, in one thread's piece and far apart."""
+    X = torch.full((M, V), -1.0)
+    X[0, :3] = torch.tensor([-0.0, 0.0, -1.0])
+    X[1] = torch.where(torch.arange(V) % 2 == 0, -0.0, 0.0)
+    X[2] = torch.where(torch.arange(V) < V // 2, -0.0, 0.0)
+    X[3, V - 1] = 0.0
+    X[3, 7] = -0.0
+    X[3, V // 2] = 2.0
+    X[4] = -0.0
+    X[4, V - 2] = 0.0
+    X[5, ::3] = -0.0
+    X[5, 1::3] = 0.0
+    X[5, 5] = 1e-30
+    X[5, 6] = -1e-30
+    return X.to(dt)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [9, 1000, 9000, 70001])
+def test_logprob_zeros_of_either_sign_are_equal(lib, dt, V):
+    """The lower id comes first among them, in one block's row and in split rows."""
+    X = zeros_of_both_signs(6, V, dt)
+    t = torch.tensor([0, 1, V - 1, 7, V - 2, 0])
+    for top in (1, 2, 5, min(V, 32)):
+        log(f"logprob zeros of either sign V={V} top={top} {dt}")
+        check(X.float(), X.to(DEV), t, top)
