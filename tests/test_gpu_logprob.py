@@ -286,3 +286,57 @@ def test_logprob_zeros_of_either_sign_are_equal(lib, dt, V):
     for top in (1, 2, 5, min(V, 32)):
         log(f"logprob zeros of either sign V={V} top={top} {dt}")
         check(X.float(), X.to(DEV), t, top)
+
+
+def gradient(X, t, dl, de=None):
+    o = forward(X, t)
+    dX = torch.full_like(X, 5.0)
+    kw = {} if de is None else dict(entropy=o["entropy"], dent=de)
+    dqt.dqt_logprob_bwd(X, t, o["stat"], dl, dX, **kw)
+    torch.cuda.synchronize()
+    return dX
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("ent", [False, True])
+@pytest.mark.parametrize("V", [40, 3000, 70001])
+def test_logprob_gradient_of_non_finite_rows(lib, dt, ent, V):
+    """A row with a NaN or +inf has no finite gradient, whatever else it holds:
+    one NaN, NaN alone, NaN and -inf, +inf.  A row of -inf alone gets 0, and
+    the other rows what they get without such neighbours."""
+    log(f"logprob gradient of non-finite rows V={V} {dt} entropy={ent}")
+    X, _ = logits(7, V, dt, V + 3, masked=False)
+    t = torch.tensor([3, 0, 5, V - 1, 2, 7, 8]).to(DEV)
+    dl = torch.linspace(-1.5, 1.0, 7).to(DEV)
+    de = torch.linspace(0.1, 0.7, 7).to(DEV) if ent else None
+    clean = gradient(X.to(DEV), t, dl, de)
+    Y = X.clone()
+    Y[0, V // 2] = float("nan")
+    Y[1] = float("nan")
+    Y[2] = -INF
+    Y[2, V - 2] = float("nan")
+    Y[3, 11] = INF
+    Y[4] = -INF
+    got = gradient(Y.to(DEV), t, dl, de)
+    for r in (0, 1, 2, 3):
+        assert torch.isnan(got[r]).all(), r
+    assert (got[4] == 0).all()
+    for r in (5, 6):
+        assert torch.equal(got[r], clean[r])
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_logprob_gradient_of_a_masked_target(lib, dt):
+    """A target whose logit is masked: its own column takes g (p is 0 there),
+    the others -p g, as the formula says; other masked columns 0."""
+    log(f"logprob gradient of a masked target {dt}")
+    X = torch.tensor([[0.0, 1.0, -INF, 2.0, -INF, -1.0]]).to(dt)
+    t, g = torch.tensor([2]).to(DEV), 0.75
+    got = gradient(X.to(DEV), t, torch.tensor([g]).to(DEV)).double().cpu()[0]
+    p = torch.softmax(X.double(), 1)[0]
+    want = -g * p
+    want[2] = g
+    half = R.BF16 if dt == torch.bfloat16 else R.F32
+    # (p: some 16 fp32 roundings of an exponent of at most 4 and of its sum)
+    assert ((got - want).abs() <= (half + 64 * R.F32) * want.abs()).all() and got[4] == 0
+    assert float(forward(X.to(DEV), t)["logp"][0]) == -INF
