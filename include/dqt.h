@@ -260,7 +260,8 @@ dqt_status dqt_logprob_fwd(const void* X, int32_t x_t, int64_t M, int32_t V, int
  *   dX_j = g [j = t] - p_j (g + e (x_j - lse + entropy))
  * with g = dlogp of the row (0 for a row without a target) and e = dent; rounded
  * once to x_t.  A masked logit gets 0, or g where it is the target's (p = 0 there);
- * a row of nothing else gets 0, a row with a +inf or a NaN gets NaN.
+ * a row of nothing else gets 0, a row with a +inf or a NaN gets NaN.  A row without
+ * a target whose dent is 0 gets 0, whatever its logits are.
  *   stat, entropy: the forward's (entropy may be NULL when dent is).
  *   dlogp, dent: [M] fp32 upstream gradients, NULL for zero.
  *   dX: [M, V] of type x_t with stride dx_stride >= V; may be X itself (same

@@ -386,9 +386,10 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobArgs a, int seg
     const float m = st.x, ls = st.y;
     const float g = has && a.dlogp != nullptr ? a.dlogp[row] : 0.0f;
     const float e = ENT ? a.dent[row] : 0.0f, eh = ENT ? e * a.entropy[row] : 0.0f;
-    // a row of nothing but -inf (one of NaN, or of NaN and -inf, has no reference
-    // either, but a NaN sum: its gradient is NaN)
-    const bool none = m == -inf() && ls == 0.0f;
+    // Zeros: a row of nothing but -inf (one of NaN, or of NaN and -inf, has no
+    // reference either, but a NaN sum: its gradient is NaN), and a row without a
+    // target or an entropy's gradient, whatever its logits are.
+    const bool none = (m == -inf() && ls == 0.0f) || (!has && e == 0.0f);
     auto grad = [&](float v, int j) {
       const float d = (v - m) - ls, p = none ? 0.0f : __builtin_amdgcn_exp2f(d * kLog2e);
       float y = g + eh;

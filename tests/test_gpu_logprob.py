@@ -326,6 +326,27 @@ def test_logprob_gradient_of_non_finite_rows(lib, dt, ent, V):
 
 
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_logprob_gradient_of_padding(lib, dt):
+    """A row without a target has the gradient 0, whatever its logits are; its
+    entropy's gradient still counts where that is asked for."""
+    log(f"logprob gradient of padding rows {dt}")
+    M, V = 6, 5000
+    X, _ = logits(M, V, dt, 41, masked=False)
+    X[1] = float("nan")
+    X[2, 4] = INF
+    X[3] = -INF
+    X[4, 9] = float("nan")
+    t = torch.tensor([-100, -1, V, V + 7, 2 ** 40, 3]).to(DEV)
+    dl = torch.full((M,), -0.25).to(DEV)
+    got = gradient(X.to(DEV), t, dl)
+    assert (got[:5] == 0).all() and (got[5] != 0).any()
+    de = torch.zeros((M,))
+    de[0] = 0.5
+    both = gradient(X.to(DEV), t, dl, de.to(DEV))
+    assert (both[1:5] == 0).all() and torch.isfinite(both[0]).all() and (both[0] != 0).any()
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
 def test_logprob_gradient_of_a_masked_target(lib, dt):
     """A target whose logit is masked: its own column takes g (p is 0 there),
     the others -p g, as the formula says; other masked columns 0."""
