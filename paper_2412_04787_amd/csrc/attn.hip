@@ -373,9 +373,10 @@ __global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fw
   if (a.causal) kend = min(kend, row_token(a, min(r0 + kBM, rows) - 1) + off + 1);
   int kbeg = 0;
   if (a.splits > 1) {
-    const int per = ((sq.lk + a.splits - 1) / a.splits + kKT - 1) / kKT * kKT;
+    // (keys up to the largest count: neither sum fits 31 bits)
+    const uint32_t per = (((uint32_t)sq.lk + a.splits - 1) / a.splits + kKT - 1) / kKT * kKT;
     kbeg = (int)min((int64_t)split * per, (int64_t)sq.lk);
-    kend = min(kend, kbeg + per);
+    kend = (int)min((int64_t)kend, (int64_t)kbeg + per);
   }
   const int nt = kend > kbeg ? (kend - kbeg + KT - 1) / KT : 0;
   const int lim = min(a.causal ? tok + off : sq.lk - 1, kend - 1);      // last key this row sees

@@ -361,3 +361,29 @@ def test_attention_offsets_past_32_bits(lib):
     near = both(*small, [0, lens[0], n])
     for x, y in zip(far, near):
         assert x.isfinite().all() and (x - y).abs().max() <= 2.0 ** -6 * y.abs().max()
+
+
+@pytest.mark.parametrize("tk", [(1 << 31) - 129, (1 << 31) - 2000, (1 << 30) + 7])
+def test_attention_over_the_largest_number_of_keys(lib, tk):
+    """One new token over as many keys as a call takes, all of them one row of
+    memory (token stride 0).  With q = 0 every key counts alike: o = v, and lse =
+    log tk shows that none is lost (one split's share would move it by 6e-4).  v
+    are powers of two, so that the sums are exact."""
+    log(f"attention: {tk} keys")
+    heads, d = 2, 64
+    gen = torch.Generator().manual_seed(36)
+    K = torch.randn((1, 1, d), generator=gen).to(torch.bfloat16).to(DEV)
+    V = (2.0 ** torch.randint(-3, 4, (1, 1, d), generator=gen) * (torch.randint(0, 2, (1, 1, d), generator=gen) * 2 - 1))
+    V = V.to(torch.bfloat16).to(DEV)
+    Q = torch.zeros((1, heads, d), dtype=torch.bfloat16, device=DEV)
+    a = dqt.attn(1, tk, heads, 1, d)
+    O, lse = torch.full_like(Q, SENT), torch.zeros((heads, 1), dtype=torch.float32, device=DEV)
+    n = dqt.dqt_attn_fwd_workspace(a)
+    assert n > 0
+    ws = dqt.workspace(n)
+    ws.fill_(float("nan"))
+    dqt.dqt_attn_fwd(a, Q, K.expand(tk, 1, d), V.expand(tk, 1, d), O, lse, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(O, V.expand(1, heads, d))
+    # log2 of a part and of their sum, below 2^5: a few roundings of 2^-19 / 2
+    assert (lse.double().cpu() - float(np.log(float(tk)))).abs().max() < 8 * 2.0 ** -20 + 22 * R.F32
