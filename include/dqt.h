@@ -215,7 +215,8 @@ dqt_status dqt_swiglu_act_quant(const void* G, const void* U, int32_t x_t, int64
  * Backward of the SwiGLU product (the quantiser passes the gradient through,
  * as everywhere).  With s = 1 / (1 + exp(-g)), in fp32, rounded once:
  *   dU = dH (g s),   dG = dH u s (1 + g (1 - s))
- *   dH, dG, dU: [M, K], h_t = DQT_F32 or DQT_BF16; dG or dU may be dH's buffer.
+ *   dH, dG, dU: [M, K], h_t = DQT_F32 or DQT_BF16; one of dG and dU may be dH's
+ *   buffer, not both (DQT_ERR_SHAPE).
  *   g, u: from the checkpoint of the forward (code times scale; G and U NULL),
  *   or, with ckpt NULL, from G and U [M, K] of type h_t.
  *   Both given: DQT_ERR_UNSUPPORTED.  Sizes as for dqt_swiglu_act_quant.

@@ -161,6 +161,7 @@ dqt_status dqt_swiglu_backward(const void* dH, int32_t h_t, const void* G, const
   if (ckpt == nullptr && (G == nullptr || U == nullptr)) return DQT_ERR_NULL;
   if (ckpt != nullptr && (G != nullptr || U != nullptr)) return DQT_ERR_UNSUPPORTED;
   if (!aligned16(dH) || !aligned16(G) || !aligned16(U) || !aligned16(dG) || !aligned16(dU)) return DQT_ERR_ALIGN;
+  if (dG == dU) return DQT_ERR_SHAPE;
   return from_hip(dqt::launch_swiglu_backward(dH, h_t == DQT_BF16, G, U, c, M, K, dG, dU,
                                               static_cast<hipStream_t>(stream)));
 }

@@ -329,3 +329,13 @@ def test_targets_are_as_many_as_rows(calls):
     with pytest.raises(ValueError):
         call({**{n: _On(t, 0) for n, t in tensors.items()}, "targets": _On(torch.zeros(4, dtype=torch.int64), 0)})
     assert calls.n == 0
+
+
+def test_swiglu_gradients_are_two_buffers():
+    """dG or dU may be dH's buffer, not both: one would overwrite the other."""
+    lib, other, third = dqt.load(), FAKE * 2, FAKE * 3
+    c = ck()
+    for dG, dU in ((FAKE, FAKE), (other, other)):
+        assert lib.dqt_swiglu_backward(FAKE, dqt.DQT_BF16, third, third, None, 4, 64, dG, dU, None) == S
+        assert lib.dqt_swiglu_backward(FAKE, dqt.DQT_BF16, None, None, ctypes.byref(c), 4, 64, dG, dU, None) == S
+    assert lib.dqt_swiglu_backward(FAKE, dqt.DQT_BF16, FAKE, FAKE, None, 0, 64, FAKE, FAKE, None) == dqt.DQT_OK
