@@ -387,3 +387,64 @@ def test_attention_over_the_largest_number_of_keys(lib, tk):
     assert torch.equal(O, V.expand(1, heads, d))
     # log2 of a part and of their sum, below 2^5: a few roundings of 2^-19 / 2
     assert (lse.double().cpu() - float(np.log(float(tk)))).abs().max() < 8 * 2.0 ** -20 + 22 * R.F32
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lq,lk,heads,kvh", [([1, 2, 17, 40], [1, 2, 17, 40], 2, 2), ([64, 33, 128], [64, 33, 128], 4, 2),
+                                             ([1, 3, 20, 9], [1, 100, 128, 65], 8, 1)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_gradients_of_few_keys_do_not_take_delta_from_o(lib, d, lq, lk, heads, kvh, causal):
+    """Rows of at most 128 keys: do.o is found from p and v, not from the bf16 O,
+    whose error would count beside do.v - do.o.  O handed to the backward is off
+    by 2 % of its largest value at random, and dQ, dK stay what p and g in bf16
+    and the final rounding allow; taken from that O, do.o would
+    move some of them by more (checked below on the reference)."""
+    log(f"attention: few keys, O perturbed, d={d} lq={lq} lk={lk} {heads}/{kvh} causal={causal}")
+    gen = torch.Generator().manual_seed(40 + d)
+    qs, ks = starts(lq), starts(lk)
+    Q, Qd = tensors(gen, int(qs[-1]), heads, d, "plain")
+    K, Kd = tensors(gen, int(ks[-1]), kvh, d, "plain")
+    V, Vd = tensors(gen, int(ks[-1]), kvh, d, "plain")
+    dO, dOd = tensors(gen, int(qs[-1]), heads, d, "plain", 1e-2)
+    st = [torch.from_numpy(x.astype(np.int32)).to(DEV) for x in (qs, ks)]
+    a = dqt.attn(Q.shape[0], K.shape[0], heads, kvh, d, *st, causal=causal)
+    O, lse = torch.empty_like(Qd), torch.empty((heads, Q.shape[0]), dtype=torch.float32, device=DEV)
+    dqt.dqt_attn_fwd(a, Qd, Kd, Vd, O, lse, dqt.workspace(dqt.dqt_attn_fwd_workspace(a)))
+    off = torch.randn(O.shape, generator=gen) * 0.02 * float(O.float().abs().max())
+    bent = (O.float().cpu() + off).to(torch.bfloat16)
+    g = [torch.empty_like(t) for t in (Qd, Kd, Vd)]
+    dqt.dqt_attn_bwd(a, Qd, Kd, Vd, bent.to(DEV), lse, dOd, *g, dqt.workspace(dqt.dqt_attn_bwd_workspace(a)))
+    torch.cuda.synchronize()
+    # per sequence: exact gradients; what roundings of g (BF16), of p and its
+    # exponent (SLACK, on each term of g; where p's sum is off by it, the O that was
+    # handed over counts with it) and of the result allow; and the gradients with
+    # do.o from that O
+    scale, SLACK = d ** -0.5, 2.0 ** -12
+    z = dict(dtype=torch.float64)
+    want = [torch.zeros(t.shape, **z) for t in (Q, K)]
+    tol = [torch.zeros(t.shape, **z) for t in (Q, K)]
+    worse = [torch.zeros(t.shape, **z) for t in (Q, K)]
+    for s in range(len(lq)):
+        A, B = slice(qs[s], qs[s + 1]), slice(ks[s], ks[s + 1])
+        see = torch.ones((lq[s], lk[s]), dtype=torch.bool)
+        if causal:
+            see = torch.arange(lk[s])[None, :] <= torch.arange(lq[s])[:, None] + lk[s] - lq[s]
+        for h in range(heads):
+            j = h // (heads // kvh)
+            q, k, v, do = Q[A, h].double(), K[B, j].double(), V[B, j].double(), dO[A, h].double()
+            p = torch.softmax((scale * q @ k.T).masked_fill(~see, -np.inf), 1)
+            dp = do @ v.T
+            mag = do.abs() @ v.abs().T
+            ds = p * (dp - (p * dp).sum(1, keepdim=True))
+            ob = bent[A, h].double()
+            t_ds = R.BF16 * ds.abs() + SLACK * p * (mag + (p * mag).sum(1, keepdim=True)
+                                                    + (do * ob).abs().sum(1, keepdim=True))
+            bad = p * (dp - (do * ob).sum(1, keepdim=True))
+            want[0][A, h], tol[0][A, h], worse[0][A, h] = scale * ds @ k, scale * t_ds @ k.abs(), scale * bad @ k
+            want[1][B, j] += scale * ds.T @ q
+            tol[1][B, j] += scale * t_ds.T @ q.abs()
+            worse[1][B, j] += scale * bad.T @ q
+    for n, got, w, t, o in zip(("dQ", "dK"), g, want, tol, worse):
+        t = t + R.BF16 * w.abs() * (1 + 2.0 ** -7)
+        close(n, got, w, t)
+        assert ((o - w).abs() > t).double().mean() > 0.03, n
