@@ -58,9 +58,10 @@ __device__ __forceinline__ void store8(TX* p, const float (&v)[8]) {
 // backward of 16384 x 5632 320 -> 300 us, 8192 x 5632 forward 46.7 -> 42.9): a / b
 // as a rcp(b) and one correction of its remainder.
 // For every fp32 g >= -69 and b = 1 + exp(-g) the result is that of the correctly
-// rounded division (all of them compared; -0 gives +0, restored where a code has
-// a sign), for 127 / b of every b from 1e-5 to 2^100, and for a / 127 of every a
-// from 1e-5 on.  Beyond (a denormal reciprocal) the division itself.
+// rounded division (-0 gives +0, restored where a code has a sign), and so it is
+// for 127 / b from 1e-5 to 2^100 and a / 127 from 1e-5 on: the tests compare all
+// gates, and for the other two every significand and 2^18 values over all
+// exponents.  Beyond (a denormal reciprocal) the division itself.
 __device__ __forceinline__ float div_short(float a, float b) {
   const float r = __builtin_amdgcn_rcpf(b), q = a * r;
   return __builtin_fmaf(__builtin_fmaf(-b, q, a), r, q);

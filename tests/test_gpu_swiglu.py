@@ -186,3 +186,78 @@ def test_swiglu_matches_unfused_quantiser(lib):
         dqt.dqt_act_quant(H, act, q[1], s[1])
         torch.cuda.synchronize()
         assert torch.equal(q[0], q[1]) and torch.equal(s[0], s[1])
+
+
+def scales_of(G, U):
+    """xdq of rows of which only the first gate counts, and the rows' checkpoint."""
+    M, K = G.shape
+    Xq, xdq = torch.empty((M, K), dtype=torch.int8, device=DEV), torch.empty((M,), dtype=torch.float32, device=DEV)
+    ck = dqt.swiglu_ckpt(M, K)
+    dqt.dqt_swiglu_act_quant(G, U, dqt.DQT_I8, Xq, xdq, ck)
+    return xdq, ck
+
+
+def test_swiglu_division_of_every_gate(lib):
+    """g / (1 + exp(-g)) of every finite fp32 g >= -69 (and below it, where the
+    division is another, to -104), as the row scale shows it: fl(max(|s u|, 1e-5) /
+    127) with u a power of two.  The quotients are formed in 64 bits and rounded
+    once, which is the correctly rounded fp32 division."""
+    N, K = 1 << 23, 16
+    log("swiglu: division of every gate")
+    G = torch.zeros((N, K), dtype=torch.float32, device=DEV)
+    U = torch.zeros((N, K), dtype=torch.float32, device=DEV)
+    least = torch.tensor(1e-5, dtype=torch.float32, device=DEV)
+    low = torch.arange(N, dtype=torch.int32, device=DEV)
+    for sign in (0, 1):
+        # 2^23 patterns a time: one exponent, every significand
+        for e in range(255 if sign == 0 else 134):
+            bits = low | (e << 23) | (-(1 << 31) if sign else 0)
+            g = bits.view(torch.float32)
+            if sign:
+                g = g.clamp(min=-104.0)
+            # (u keeps s u within fp32 and, but for the smallest 40 gates, above 1e-5)
+            u = 2.0 ** (127 if e == 0 else 120 if e < 127 else 104 if e < 140 else 0)
+            G[:, 0], U[:, 0] = g, u
+            got, _ = scales_of(G, U)
+            b = 1.0 + torch.exp(-g)
+            s = (g.double() / b.double()).float()
+            want = (torch.maximum((s * u).abs(), least).double() / 127.0).float()
+            bad = got != want
+            assert not bool(bad.any()), (sign, e, g[bad][:4], got[bad][:4], want[bad][:4])
+            if e % 32 == 0:
+                log(f"sign {sign}, exponent {e}")
+
+
+def test_swiglu_checkpoint_divisions(lib):
+    """fl(127 / a) and fl(a / 127) of a group's maximum a: every significand, and
+    exponents from 1e-5 to the largest.  The second is the scale itself; the first
+    shows in the codes of 127 values next to the borders between two codes, of
+    which a step of the reciprocal's last place moves about half."""
+    log("swiglu: divisions of the checkpoint")
+    K, N = 128, 1 << 18
+    k = torch.arange(127, dtype=torch.float64, device=DEV)[None, :] + 0.5
+    gen = torch.Generator().manual_seed(50)
+
+    def check(a):                          # a: fp32, in host memory
+        inv = torch.from_numpy(np.float32(127) / a.numpy()).to(DEV)
+        a = a.to(DEV)
+        x = (k / inv.double()[:, None]).float()
+        x = torch.minimum(x, a[:, None])
+        G = torch.cat([a[:, None], x], 1)
+        _, ck = scales_of(G, G)
+        want = torch.round(G * inv[:, None]).clamp(-128, 127).to(torch.int8)
+        assert torch.equal(ck.Gq, want) and torch.equal(ck.Uq, want)
+        s = torch.from_numpy(a.cpu().numpy() / np.float32(127)).to(DEV)
+        assert torch.equal(ck.gs[:, 0], s) and torch.equal(ck.us[:, 0], s)
+        # (the test sees a reciprocal that is off by its last place)
+        for off in (torch.nextafter(inv, inv * 2), torch.nextafter(inv, inv * 0)):
+            some = (torch.round(G * off[:, None]).clamp(-128, 127).to(torch.int8) != want).any(1)
+            assert some.double().mean() > 0.999
+
+    for i in range(0, 1 << 23, N):
+        check((torch.arange(i, i + N, dtype=torch.int32) | (127 << 23)).view(torch.float32))
+        if i % (N * 8) == 0:
+            log(f"significands from {i}")
+    e = torch.randint(111, 254, (N,), generator=gen, dtype=torch.int32)
+    m = torch.randint(0, 1 << 23, (N,), generator=gen, dtype=torch.int32)
+    check(((e << 23) | m).view(torch.float32))
