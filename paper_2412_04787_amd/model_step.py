@@ -27,8 +27,9 @@ What runs where:
     into the batch and grouped key heads; dqt_swiglu_act_quant feeds the down
     projection and keeps gate and up as 8-bit checkpoints, from which
     dqt_swiglu_backward takes their gradients (2 bytes per element of a token's
-    feed-forward held for the backward, 6 in PyTorch); dqt_logprob_fwd / _bwd
-    give the loss and the logits' gradient.
+    feed-forward held for the backward, 6 in PyTorch; with ckpt8 = False gate and
+    up themselves, 4 bytes); dqt_logprob_fwd / _bwd give the loss and the logits'
+    gradient.
 
 Initialisation (untimed): codes by Eq. 2-4 for the ternary grid from
 W0 ~ N(0, 0.02) (alpha = mean |W0|, q = Clip(Round(W0 / alpha), -1, 1));
@@ -59,6 +60,10 @@ class ModelConfig:
     seed: int = 0
     kv_heads: int = 0          # key heads (0: as many as heads); fewer need own_ops
     own_ops: bool = False      # attention, SwiGLU and loss in this library's kernels
+    # own_ops: gate and up are held for the backward in 8 bits, one scale for 128
+    # elements (their gradients, and no other step's result, are off by 0.7 % rms
+    # for normal values); False: as they are, in bf16
+    ckpt8: bool = True
 
     def __post_init__(self):
         if self.kv_heads and (self.heads % self.kv_heads or (self.kv_heads != self.heads and not self.own_ops)):
@@ -277,28 +282,34 @@ class _OwnFns:
 
         class SwigluGroup(torch.autograd.Function):
             """silu(gate) * up, quantised and fed to the group's linears (the
-            down projection); gate and up are kept as 8-bit checkpoints."""
+            down projection); gate and up are kept as 8-bit checkpoints, or as
+            they are (ckpt8 = False)."""
 
             @staticmethod
             def forward(ctx, gate, up, grp):
                 T, K = gate.shape
                 Xq = torch.empty((T, K), dtype=torch.int8, device=gate.device)
                 xdq = torch.empty((T,), dtype=torch.float32, device=gate.device)
-                ckpt = dqt.swiglu_ckpt(T, K, gate.device)
-                dqt.dqt_swiglu_act_quant(gate.contiguous(), up.contiguous(), dqt.DQT_I8, Xq, xdq, ckpt)
+                gate, up = gate.contiguous(), up.contiguous()
+                ckpt = dqt.swiglu_ckpt(T, K, gate.device) if grp.model.cfg.ckpt8 else None
+                dqt.dqt_swiglu_act_quant(gate, up, dqt.DQT_I8, Xq, xdq, ckpt)
                 ctx.grp = grp
-                ctx.save_for_backward(Xq, xdq, ckpt.Gq, ckpt.Uq, ckpt.gs, ckpt.us)
+                kept = (gate, up) if ckpt is None else (ckpt.Gq, ckpt.Uq, ckpt.gs, ckpt.us)
+                ctx.save_for_backward(Xq, xdq, *kept)
                 return tuple(_group_fwd(grp, Xq, xdq))
 
             @staticmethod
             def backward(ctx, *dYs):
-                Xq, xdq, *ckpt = ctx.saved_tensors
+                Xq, xdq, *kept = ctx.saved_tensors
                 dXs = _group_bwd(ctx.grp, Xq, xdq, dYs)
                 dh = dXs[0]
                 for d in dXs[1:]:
                     dh = dh + d
                 dg, du = torch.empty_like(dh), torch.empty_like(dh)
-                dqt.dqt_swiglu_backward_ckpt(dh, dqt.SwigluCkpt(*ckpt), dg, du)
+                if len(kept) == 2:
+                    dqt.dqt_swiglu_backward(dh, *kept, dg, du)
+                else:
+                    dqt.dqt_swiglu_backward_ckpt(dh, dqt.SwigluCkpt(*kept), dg, du)
                 return dg, du, None
 
         class TokenLoss(torch.autograd.Function):

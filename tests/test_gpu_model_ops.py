@@ -7,6 +7,7 @@ import math
 import pytest
 import torch
 
+import op_reference as R
 from gpu_util import DEV, log
 from paper_2412_04787_amd import dqt, model_step as MS
 
@@ -229,3 +230,33 @@ def test_strided_targets(lib):
     for x, y in zip(*got):
         # (the head's gradient: a library product, which may sum in another order, to bf16)
         assert torch.equal(x, y) if x is not got[0][-1] else (x - y).norm() <= 2.0 ** -7 * x.norm()
+
+
+@pytest.mark.parametrize("ckpt8", [True, False])
+def test_what_the_feed_forward_holds_for_its_backward(lib, monkeypatch, ckpt8):
+    """Gradients of gate and up: of their values in bf16, or of those that the
+    8-bit checkpoints hold; the forward is the same."""
+    cfg = dataclasses.replace(MS.MODELS["tiny_ops"], ckpt8=ckpt8)
+    model = MS.DQTModel(cfg)
+    gen = torch.Generator().manual_seed(60)
+    gate, up = (torch.randn((200, cfg.ffn), generator=gen).to(torch.bfloat16) for _ in range(2))
+    dy = (torch.randn((200, cfg.hidden), generator=gen) * 1e-2).to(torch.bfloat16).to(DEV)
+    seen = []
+    plain = MS._group_bwd
+    monkeypatch.setattr(MS, "_group_bwd", lambda *a: seen.append(plain(*a)) or seen[-1])
+    g, u = (t.to(DEV).requires_grad_() for t in (gate, up))
+    grp = model.groups[0]["mlp_hidden"]
+    log(f"model: feed-forward held in 8 bits: {ckpt8}")
+    with torch.no_grad():
+        Xq, xdq = torch.empty((200, cfg.ffn), dtype=torch.int8, device=DEV), torch.empty((200,), device=DEV)
+        dqt.dqt_swiglu_act_quant(g, u, dqt.DQT_I8, Xq, xdq)
+        (want,) = MS._group_fwd(grp, Xq, xdq)
+    (y,) = MS._OwnFns.get()[1].apply(g, u, grp)
+    assert torch.equal(y, want)
+    y.backward(dy)
+    if ckpt8:
+        gate, up = (R.checkpoint_values(*R.checkpoint(t)) for t in (gate, up))
+    (dh,) = seen[0]
+    rg, ru, tg, tu = R.swiglu_backward(dh.cpu(), gate, up)
+    for got, ref, t in ((g.grad, rg, tg), (u.grad, ru, tu)):
+        assert ((got.double().cpu() - ref).abs() <= R.BF16 * ref.abs() * (1 + 2.0 ** -7) + t + 1e-37).all()
