@@ -185,9 +185,15 @@ def version() -> int:
 
 # ----------------------------------------------------------------- tensors
 
+_TORCH = None           # (imported late)
+
+
 def _torch():
-    import torch
-    return torch
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _TORCH = torch
+    return _TORCH
 
 
 def _ptr(t):
@@ -210,30 +216,32 @@ def _same(*ts):
 
 
 def _here(t, *others):
-    """Refuses tensors in host memory, and of another device than the current
-    one, on whose stream the kernels would run.  (None stands for no tensor.)"""
+    """The current device, on whose stream the kernels run: refuses tensors of
+    another one and in host memory."""
     dev = t.get_device()                   # (-1 in host memory)
     if dev < 0 or dev != _torch()._C._cuda_getDevice():
-        raise ValueError("tensor in host memory" if dev < 0 else
-                         f"tensor on device {dev}, which is not the current one")
+        raise ValueError("tensor in host memory" if dev < 0 else f"tensor on device {dev}, which is not the current one")
     for o in others:
-        if o is not None and o.get_device() != dev:
+        if o.get_device() != dev:
             raise ValueError(f"tensor on {o.device}, others on device {dev}")
+    return dev
 
 
-def _buf(t, n, dtype):
-    """Refuses a buffer that is not one of at least n consecutive values of dtype."""
-    if t is not None and (t.dtype is not dtype or t.numel() < n or not t.is_contiguous()):
-        raise ValueError(f"expected {n} consecutive values of {dtype}, got {tuple(t.shape)} of {t.dtype} "
-                         f"with strides {t.stride()}")
+def _bufs(dev, *bufs):
+    """Refuses a buffer (tensor or None, n, dtype) that is not one of at least n
+    consecutive values of dtype on device dev."""
+    for t, n, dtype in bufs:
+        if t is not None and (t.get_device() != dev or t.dtype is not dtype or t.numel() < n or not t.is_contiguous()):
+            raise ValueError(f"expected {n} consecutive values of {dtype} on device {dev}, got {tuple(t.shape)} of "
+                             f"{t.dtype} with strides {t.stride()} on {t.device}")
 
 
-def _ws_bytes(t):
-    """The bytes of a workspace."""
+def _ws_bytes(dev, t):
+    """The bytes of a workspace on device dev."""
     if t is None:
         return 0
-    if not t.is_contiguous():
-        raise ValueError("a workspace must be contiguous")
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous workspace on device {dev}, got strides {t.stride()} on {t.device}")
     return t.numel() * t.element_size()
 
 
@@ -243,16 +251,16 @@ def _unit_stride(t):
 
 
 def _stream(stream=None):
-    """The stream's handle; without one, that of torch's current stream on the
+    """The stream's handle (an integer); without one, that of torch's current stream on the
     current device.  (Asked for directly: building the Stream object of
     torch.cuda.current_stream() was a third of a small call's host time.)"""
     if stream is not None:
-        return ctypes.c_void_p(stream.cuda_stream)
+        return stream.cuda_stream
     torch = _torch()
     if not torch.cuda.is_initialized():
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        return torch.cuda.current_stream().cuda_stream
     c = torch._C
-    return ctypes.c_void_p(c._cuda_getCurrentRawStream(c._cuda_getDevice()))
+    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
 
 
 _DTYPE_CODES = {}       # (filled on first use: torch is imported late)
@@ -327,12 +335,12 @@ def dqt_swiglu_act_quant(G, U, act_q: int, Xq, xdq, ckpt: SwigluCkpt | None = No
     """G, U: contiguous [M, K] of one dtype; Xq: M K bytes, xdq: M fp32 values
     (larger buffers are used from their start)."""
     M, K = _same(G, U)
-    _here(G, U, Xq, xdq)
+    dev = _here(G, U)
     if Xq is not None:
         if Xq.element_size() != 1:
             raise ValueError(f"expected 8-bit codes, got {Xq.dtype}")
-        _buf(Xq, M * K, Xq.dtype)
-    _buf(xdq, M, _torch().float32)
+        _bufs(dev, (Xq, M * K, Xq.dtype))
+    _bufs(dev, (xdq, M, _torch().float32))
     if ckpt is not None:
         _check_ckpt(ckpt, M, K, G)
     _check("dqt_swiglu_act_quant",
@@ -366,11 +374,9 @@ def dqt_logprob_workspace(M: int, V: int, top_k: int = 0) -> int:
     return int(load().dqt_logprob_workspace(M, V, top_k))
 
 
-def _check_targets(targets, M):
-    if targets is not None and (targets.numel() != M or targets.dtype is not _torch().int64
-                                or not targets.is_contiguous()):
-        raise ValueError(f"expected {M} contiguous int64 targets, got {tuple(targets.shape)} of {targets.dtype} "
-                         f"with strides {targets.stride()}")
+def _as_many(targets, M):
+    if targets is not None and targets.numel() != M:
+        raise ValueError(f"expected {M} targets, got {targets.numel()}")
 
 
 def dqt_logprob_fwd(X, targets, logp, lse=None, entropy=None, stat=None, top_ids=None, top_logp=None,
@@ -381,22 +387,19 @@ def dqt_logprob_fwd(X, targets, logp, lse=None, entropy=None, stat=None, top_ids
     outputs are used from their start."""
     _unit_stride(X)
     M, V = X.shape
-    _here(X, targets, logp, lse, entropy, stat, top_ids, top_logp, ws)
-    torch = _torch()
-    _check_targets(targets, M)
-    for t, n in ((logp, M), (lse, M), (entropy, M), (stat, 2 * M)):
-        _buf(t, n, torch.float32)
-    top_k = 0
+    dev, torch = _here(X), _torch()
+    f32, i64, top_k = torch.float32, torch.int64, 0
     if top_ids is not None:
         if top_ids.dim() != 2:
             raise ValueError("expected top_ids of shape [M, k]")
         top_k = top_ids.shape[1]
-        _buf(top_ids, M * top_k, torch.int64)
-        _buf(top_logp, M * top_k, torch.float32)
+    _bufs(dev, (targets, M, i64), (logp, M, f32), (lse, M, f32), (entropy, M, f32), (stat, 2 * M, f32),
+          (top_ids, M * top_k, i64), (top_logp, M * top_k, f32))
+    _as_many(targets, M)
     _check("dqt_logprob_fwd",
            load().dqt_logprob_fwd(_addr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _addr(targets),
                                   _addr(logp), _addr(lse), _addr(entropy), _addr(stat), top_k,
-                                  _addr(top_ids), _addr(top_logp), _addr(ws), _ws_bytes(ws), _stream(stream)))
+                                  _addr(top_ids), _addr(top_logp), _addr(ws), _ws_bytes(dev, ws), _stream(stream)))
 
 
 def dqt_logprob_bwd(X, targets, stat, dlogp, dX, entropy=None, dent=None, stream=None):
@@ -406,10 +409,10 @@ def dqt_logprob_bwd(X, targets, stat, dlogp, dX, entropy=None, dent=None, stream
     _unit_stride(dX)
     if dX.dtype != X.dtype or dX.shape != X.shape:
         raise ValueError("dX must have X's dtype and shape")
-    _here(X, targets, stat, dlogp, dX, entropy, dent)
-    _check_targets(targets, M)
-    for t, n in ((stat, 2 * M), (dlogp, M), (entropy, M), (dent, M)):
-        _buf(t, n, _torch().float32)
+    f32 = _torch().float32
+    _bufs(_here(X, dX), (targets, M, _torch().int64), (stat, 2 * M, f32), (dlogp, M, f32), (entropy, M, f32),
+          (dent, M, f32))
+    _as_many(targets, M)
     _check("dqt_logprob_bwd",
            load().dqt_logprob_bwd(_addr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _addr(targets),
                                   _addr(stat), _addr(entropy), _addr(dlogp), _addr(dent), _addr(dX),
@@ -441,16 +444,15 @@ def attn(q_tokens: int, k_tokens: int, heads: int, kv_heads: int, d: int, q_star
 _pack_rows = struct.Struct("3q").pack
 
 
-def _rows(a: DqtAttn, tensors, kinds: str, lse, ws):
-    """The dqt_rows (as bytes) of bf16 tensors [q_tokens, heads, d] (kind "q") or
-    [k_tokens, kv_heads, d] ("k") with any token and head strides; checks the
-    call's other buffers too."""
+def _rows(a: DqtAttn, tensors, kinds: str, lse):
+    """(Their device, the dqt_rows (as bytes)) of bf16 tensors [q_tokens, heads, d]
+    (kind "q") or [k_tokens, kv_heads, d] ("k") with any token and head strides."""
     torch = _torch()
     bf16, shapes = torch.bfloat16, a._shapes
-    _here(*tensors, lse, ws)
-    _buf(lse, a.heads * a.q_tokens, torch.float32)
-    if a._dev is not None and a._dev != tensors[0].get_device():
-        raise ValueError(f"q_start or k_start on device {a._dev}, the tensors on another")
+    dev = _here(*tensors)
+    _bufs(dev, (lse, a.heads * a.q_tokens, torch.float32))
+    if a._dev is not None and a._dev != dev:
+        raise ValueError(f"q_start or k_start on device {a._dev}, the tensors on device {dev}")
     rows = []
     for t, kind in zip(tensors, kinds):
         shape = shapes[kind]
@@ -462,7 +464,7 @@ def _rows(a: DqtAttn, tensors, kinds: str, lse, ws):
         n, h, d = shape
         # (strides of a dimension of one do not matter)
         rows.append(_pack_rows(t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d))
-    return rows
+    return dev, rows
 
 
 def dqt_attn_fwd_workspace(a: DqtAttn) -> int:
@@ -472,8 +474,8 @@ def dqt_attn_fwd_workspace(a: DqtAttn) -> int:
 def dqt_attn_fwd(a: DqtAttn, Q, K, V, O, lse=None, ws=None, stream=None):
     """Q, O: [q_tokens, heads, d]; K, V: [k_tokens, kv_heads, d], bf16 with any
     token and head strides; lse: contiguous fp32 [heads, q_tokens] or None."""
-    r = _rows(a, (Q, K, V, O), "qkkq", lse, ws)
-    _check("dqt_attn_fwd", load().dqt_attn_fwd(ctypes.byref(a), *r, _addr(lse), _addr(ws), _ws_bytes(ws),
+    dev, r = _rows(a, (Q, K, V, O), "qkkq", lse)
+    _check("dqt_attn_fwd", load().dqt_attn_fwd(ctypes.byref(a), *r, _addr(lse), _addr(ws), _ws_bytes(dev, ws),
                                                _stream(stream)))
 
 
@@ -483,8 +485,8 @@ def dqt_attn_bwd_workspace(a: DqtAttn) -> int:
 
 def dqt_attn_bwd(a: DqtAttn, Q, K, V, O, lse, dO, dQ, dK, dV, ws, stream=None):
     """Shapes as dqt_attn_fwd; dO, dQ like Q, dK and dV like K."""
-    r = _rows(a, (Q, K, V, O, dO, dQ, dK, dV), "qkkqqqkk", lse, ws)
-    _check("dqt_attn_bwd", load().dqt_attn_bwd(ctypes.byref(a), *r[:4], _addr(lse), *r[4:], _addr(ws), _ws_bytes(ws),
+    dev, r = _rows(a, (Q, K, V, O, dO, dQ, dK, dV), "qkkqqqkk", lse)
+    _check("dqt_attn_bwd", load().dqt_attn_bwd(ctypes.byref(a), *r[:4], _addr(lse), *r[4:], _addr(ws), _ws_bytes(dev, ws),
                                                _stream(stream)))
 
 

@@ -57,7 +57,7 @@ def headless(monkeypatch):
     cfg = MS.MODELS["tiny_ops"]
     lib = _Library(cfg.tokens)
     monkeypatch.setattr(dqt, "load", lambda: lib)
-    monkeypatch.setattr(dqt, "_here", lambda *t: None)
+    monkeypatch.setattr(dqt, "_here", lambda *t: -1)
     monkeypatch.setattr(dqt, "_stream", lambda stream=None: None)
     model = MS.DQTModel.__new__(MS.DQTModel)
     model.cfg, model._ws = cfg, None
