@@ -32,7 +32,10 @@
  *    the caller's next synchronisation.  Nothing throws or aborts.
  *  - Shapes: d_in and d_out are multiples of 16 and at least 16; M >= 0 (any
  *    value, M = 0 is a no-op except that dW is then written as zeros).
- *    Base pointers must be 16-byte aligned; per-row fp32 outputs 4-byte.
+ *    Base pointers must be 16-byte aligned, those of the activations' scales
+ *    (xdq) among them.  Other vectors of one value a row (rinv, lse, logp,
+ *    entropy, their gradients, targets) and the alternatives need their type's
+ *    alignment, stat 8 bytes.
  *  - Non-finite values in X or dY are not checked.
  *  - Workspaces (dqt_linear_fwd / dqt_linear_bwd and their batches, attention,
  *    log probabilities) are caller-owned device buffers of at least the size
@@ -285,8 +288,10 @@ dqt_status dqt_logprob_bwd(const void* X, int32_t x_t, int64_t M, int32_t V, int
  * kv_heads).  Per query and head:
  *   z_j = scale q.k_j,  lse = log sum exp(z_j),  O = sum_j exp(z_j - lse) v_j
  * over the keys it sees; O = 0 and lse = -inf when it sees none.  Operands and
- * results are bf16; scores, softmax and sums fp32; probabilities are rounded
- * to bf16 for the matrix cores.
+ * results are bf16; scores, softmax and sums fp32.  What the matrix cores
+ * multiply again is rounded to bf16: p in O and dV, p (dO.v - dO.O) in dQ and
+ * dK; and dO.O is taken from the bf16 O, but for tiles of 128 rows (query tokens
+ * times heads / kv_heads) of which none sees more than 128 keys.
  *   q_start, k_start: device int32 [n_seq + 1], ascending, 0 <= start <=
  *      tokens; either may be NULL when n_seq = 1 (one sequence of all tokens).
  *      Empty sequences are allowed.  Values that break these rules give wrong

@@ -339,3 +339,15 @@ def test_swiglu_gradients_are_two_buffers():
         assert lib.dqt_swiglu_backward(FAKE, dqt.DQT_BF16, third, third, None, 4, 64, dG, dU, None) == S
         assert lib.dqt_swiglu_backward(FAKE, dqt.DQT_BF16, None, None, ctypes.byref(c), 4, 64, dG, dU, None) == S
     assert lib.dqt_swiglu_backward(FAKE, dqt.DQT_BF16, FAKE, FAKE, None, 0, 64, FAKE, FAKE, None) == dqt.DQT_OK
+
+
+def test_alignment_of_vectors_of_one_value_a_row():
+    """xdq 16 bytes as every other base, the rest its type's: a call with those
+    is refused for its missing workspace, not for them."""
+    lib = dqt.load()
+    assert lib.dqt_act_quant(FAKE, dqt.DQT_BF16, 4, 64, dqt.DQT_I8, FAKE, ODD, None) == A
+    assert lib.dqt_swiglu_act_quant(FAKE, FAKE, dqt.DQT_BF16, 4, 64, dqt.DQT_I8, FAKE, ODD, None, None) == A
+    ids = FAKE + 8
+    assert lib.dqt_logprob_fwd(FAKE, dqt.DQT_F32, 2, 128000, 128000, ids, ODD, ODD, ODD, ids, 5, ids, ODD, None, 0,
+                               None) == W
+    assert bwd(desc(), lse=ODD, ws=None) == W
