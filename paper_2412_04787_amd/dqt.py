@@ -229,10 +229,10 @@ def _here(t, *others):
 
 def _bufs(dev, *bufs):
     """Refuses a buffer (tensor or None, n, dtype) that is not one of at least n
-    consecutive values of dtype on device dev."""
+    consecutive bytes, values of dtype, on device dev."""
     for t, n, dtype in bufs:
-        if t is not None and (t.get_device() != dev or t.dtype is not dtype or t.numel() < n or not t.is_contiguous()):
-            raise ValueError(f"expected {n} consecutive values of {dtype} on device {dev}, got {tuple(t.shape)} of "
+        if t is not None and (t.get_device() != dev or t.dtype is not dtype or t.nbytes < n or not t.is_contiguous()):
+            raise ValueError(f"expected {n} consecutive bytes, {dtype}, on device {dev}, got {tuple(t.shape)} of "
                              f"{t.dtype} with strides {t.stride()} on {t.device}")
 
 
@@ -242,7 +242,7 @@ def _ws_bytes(dev, t):
         return 0
     if t.get_device() != dev or not t.is_contiguous():
         raise ValueError(f"expected a contiguous workspace on device {dev}, got strides {t.stride()} on {t.device}")
-    return t.numel() * t.element_size()
+    return t.nbytes
 
 
 def _unit_stride(t):
@@ -336,11 +336,9 @@ def dqt_swiglu_act_quant(G, U, act_q: int, Xq, xdq, ckpt: SwigluCkpt | None = No
     (larger buffers are used from their start)."""
     M, K = _same(G, U)
     dev = _here(G, U)
-    if Xq is not None:
-        if Xq.element_size() != 1:
-            raise ValueError(f"expected 8-bit codes, got {Xq.dtype}")
-        _bufs(dev, (Xq, M * K, Xq.dtype))
-    _bufs(dev, (xdq, M, _torch().float32))
+    if Xq is not None and Xq.element_size() != 1:
+        raise ValueError(f"expected 8-bit codes, got {Xq.dtype}")
+    _bufs(dev, (Xq, M * K, None if Xq is None else Xq.dtype), (xdq, 4 * M, _torch().float32))
     if ckpt is not None:
         _check_ckpt(ckpt, M, K, G)
     _check("dqt_swiglu_act_quant",
@@ -393,8 +391,8 @@ def dqt_logprob_fwd(X, targets, logp, lse=None, entropy=None, stat=None, top_ids
         if top_ids.dim() != 2:
             raise ValueError("expected top_ids of shape [M, k]")
         top_k = top_ids.shape[1]
-    _bufs(dev, (targets, M, i64), (logp, M, f32), (lse, M, f32), (entropy, M, f32), (stat, 2 * M, f32),
-          (top_ids, M * top_k, i64), (top_logp, M * top_k, f32))
+    _bufs(dev, (targets, 8 * M, i64), (logp, 4 * M, f32), (lse, 4 * M, f32), (entropy, 4 * M, f32), (stat, 8 * M, f32),
+          (top_ids, 8 * M * top_k, i64), (top_logp, 4 * M * top_k, f32))
     _as_many(targets, M)
     _check("dqt_logprob_fwd",
            load().dqt_logprob_fwd(_addr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _addr(targets),
@@ -410,8 +408,8 @@ def dqt_logprob_bwd(X, targets, stat, dlogp, dX, entropy=None, dent=None, stream
     if dX.dtype != X.dtype or dX.shape != X.shape:
         raise ValueError("dX must have X's dtype and shape")
     f32 = _torch().float32
-    _bufs(_here(X, dX), (targets, M, _torch().int64), (stat, 2 * M, f32), (dlogp, M, f32), (entropy, M, f32),
-          (dent, M, f32))
+    _bufs(_here(X, dX), (targets, 8 * M, _torch().int64), (stat, 8 * M, f32), (dlogp, 4 * M, f32),
+          (entropy, 4 * M, f32), (dent, 4 * M, f32))
     _as_many(targets, M)
     _check("dqt_logprob_bwd",
            load().dqt_logprob_bwd(_addr(X), dtype_code(X), M, V, X.stride(0) if M > 1 else V, _addr(targets),
@@ -450,7 +448,7 @@ def _rows(a: DqtAttn, tensors, kinds: str, lse):
     torch = _torch()
     bf16, shapes = torch.bfloat16, a._shapes
     dev = _here(*tensors)
-    _bufs(dev, (lse, a.heads * a.q_tokens, torch.float32))
+    _bufs(dev, (lse, 4 * a.heads * a.q_tokens, torch.float32))
     if a._dev is not None and a._dev != dev:
         raise ValueError(f"q_start or k_start on device {a._dev}, the tensors on device {dev}")
     rows = []
