@@ -184,8 +184,11 @@ __device__ __forceinline__ f32x16 mfma(i32x4 a, i32x4 b, f32x16 c) {
 // the compiler sees no operands to wait for there)
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-// 8 scores -> B operand (rounded to bf16, as every operand of the second
-// products: the matrix cores take 16-bit values)
+// 8 scores -> B operand of the second products (p for o and dv, g for dq and dk),
+// rounded to bf16: the matrix cores take 16-bit values, and operands in fp32 would
+// run at a sixteenth of their rate.  Each rounding is off by 2^-8 of its own p or g
+// at most, independently of the others (0.0012 of o's norm and 0.0017 of the
+// gradients', beside 0.0016 for rounding the results).
 __device__ __forceinline__ i32x4 pack8(const f32x16& v, int at) {
   return i32x4{(int)pack_bf16x2(v[at], v[at + 1]), (int)pack_bf16x2(v[at + 2], v[at + 3]),
                (int)pack_bf16x2(v[at + 4], v[at + 5]), (int)pack_bf16x2(v[at + 6], v[at + 7])};
@@ -338,13 +341,14 @@ __device__ __forceinline__ void join_groups(const f32x16 (&x)[ND], f32x16 (&own)
 // ------------------------------------------------------------------ forward
 // A block: 128 rows, 32 per wave; keys and values pass through LDS in tiles of 64,
 // two stages, copied while the tile before is worked on.  Scores, powers and sums
-// stay in registers.  Bound by matrix and vector work side by side: 8 x 2048
+// stay in registers.  Bound by matrix and vector work that take turns: 8 x 2048
 // tokens, 16 heads of 128, causal, 177 us for the 137 GFLOP that the mask leaves
-// (775 TFLOP/s; one sequence of 8192 tokens 930): within a block's loop the matrix
-// cores are busy 0.6 of the cycles at the 1.7 to 1.9 GHz that the power limit
-// leaves, and a block's first data arrive 4 to 5 us after its start.  64-wide, 4 x
-// 4096 tokens, 16 heads: 160 us, bound by the vector units first; three
-// waves per SIMD (four, at 128 registers: 29.1 -> 31.1 us for 8 x 1024, 12 heads).
+// (775 TFLOP/s; one sequence of 8192 tokens 930), the matrix cores busy 0.45 and
+// the vector units 0.50 of the busy units' cycles at the 1.7 to 1.9 GHz that the
+// power limit leaves; a block's first data arrive 4 to 5 us after its start.
+// Without the mask 1.53 times the time for twice the work (950 TFLOP/s).  64-wide,
+// 4 x 4096 tokens, 16 heads: 160 us; three waves per SIMD (four, at 128 registers: 29.1 -> 31.1 us
+// for 8 x 1024, 12 heads).
 // New tokens over long contexts are bound by HBM: 32 tokens over 1 to 8192 keys, 8
 // key heads: 108 us for 0.54 GB, 5.0 TB/s.
 template <int D, int GR>
@@ -466,7 +470,7 @@ __global__ __launch_bounds__(256 * GR, GR == 2 || D == 128 ? 2 : 3) void attn_fw
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           e[i] = exp2_fast(__builtin_fmaf(s[kk >> 1][8 * (kk & 1) + i], c, -mu));
-          sum += e[i];
+          sum += e[i];          // (in fp32: lse is the sum of the powers themselves)
         }
         p[kk] = i32x4{(int)pack_bf16x2(e[0], e[1]), (int)pack_bf16x2(e[2], e[3]), (int)pack_bf16x2(e[4], e[5]),
                       (int)pack_bf16x2(e[6], e[7])};
@@ -706,9 +710,9 @@ __global__ __launch_bounds__(256 * GR, 2) void attn_dq_kernel(AttnArgs a) {
     });
   };
   // do.o is formed from o in bf16.  Where a row sees few keys, its error counts
-  // beside do.v - do.o (for one key that is zero): the rows of the first 128 keys
-  // take a pass of their own that finds sum_j p_ij (do_i.v_j - do_i.o_i), the
-  // error itself (relative error of dq and dk of packed documents 0.0025 ->
+  // beside do.v - do.o (for one key that is zero): blocks whose rows see no more
+  // than 128 keys take a pass of their own that finds sum_j p_ij (do_i.v_j -
+  // do_i.o_i), the error itself (relative error of dq and dk of packed documents 0.0025 ->
   // 0.0024, where rounding the exact result to bf16 gives 0.0017 and rounding g
   // as well sqrt(2) of that; no measurable time).
   if (exact) {
