@@ -400,7 +400,8 @@ def run_model(args):
         "config": {
             "workload": f"{cfg.name}: {cfg.layers}-layer LLaMA-shaped model, hidden {cfg.hidden}, "
                         f"{cfg.heads} heads, FFN {cfg.ffn}, vocab {cfg.vocab}, RMSNorm, RoPE; "
-                        + ("attention, SwiGLU and loss in this library's kernels; " if cfg.own_ops else "")
+                        + ("attention, SwiGLU and loss in this library's kernels, gate and up held in "
+                           f"{'8 bits' if cfg.ckpt8 else 'bf16'} for the backward; " if cfg.own_ops else "")
                         + f"all {7 * cfg.layers} block linears DQT ternary (int8 activations, "
                         f"bf16 environment); batch {cfg.batch} x seq {cfg.seq}; lr {cfg.lr}",
             "tokens": cfg.tokens, "dqt_weights": cfg.dqt_weights,
