@@ -340,7 +340,9 @@ dqt_status dqt_attn_fwd(const dqt_attn* a, const dqt_rows* Q, const dqt_rows* K,
 /* Backward: dQ, dK, dV of the forward's O for the upstream gradient dO, from
  * the forward's O and lse.  Gradients of a key head are summed over the query
  * heads that share it, in fp32 and a fixed order (bit-reproducible).  Keys
- * that no query sees get 0. */
+ * that no query sees get 0.  The probabilities are formed again from q.k and the
+ * fp32 lse, whose roundings move them by up to |lse| 2^-20 of themselves: nothing
+ * beside bf16 for scores of hundreds, but not for millions. */
 size_t dqt_attn_bwd_workspace(const dqt_attn* a);
 dqt_status dqt_attn_bwd(const dqt_attn* a, const dqt_rows* Q, const dqt_rows* K,
                         const dqt_rows* V, const dqt_rows* O, const float* lse,

@@ -448,3 +448,62 @@ def test_attention_gradients_of_few_keys_do_not_take_delta_from_o(lib, d, lq, lk
         t = t + R.BF16 * w.abs() * (1 + 2.0 ** -7)
         close(n, got, w, t)
         assert ((o - w).abs() > t).double().mean() > 0.03, n
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,kvh", [(5, 1), (14, 2), (96, 1), (130, 2), (1024, 1)])
+def test_attention_odd_and_large_groups(lib, heads, kvh, d):
+    """Groups that do not divide a tile of rows, or fill several by themselves."""
+    log(f"attention: groups of {heads // kvh} d={d}")
+    lq, lk = ([9, 1, 30], [9, 40, 31]) if heads < 1000 else ([3, 1], [5, 70])
+    run(d, heads, kvh, lq, lk, seed=37, before=1, behind=1)
+
+
+def call(a, q, k, v, do):
+    """Forward and backward: [O, lse, dQ, dK, dV]."""
+    tq, heads = q.shape[:2]
+    new = lambda t: torch.full(t.shape, SENT, dtype=torch.bfloat16, device=DEV)
+    O, lse, g = new(q), torch.full((heads, tq), SENT, dtype=torch.float32, device=DEV), [new(t) for t in (q, k, v)]
+    dqt.dqt_attn_fwd(a, q, k, v, O, lse, dqt.workspace(dqt.dqt_attn_fwd_workspace(a)))
+    dqt.dqt_attn_bwd(a, q, k, v, O, lse, do, *g, dqt.workspace(dqt.dqt_attn_bwd_workspace(a)))
+    torch.cuda.synchronize()
+    return [O, lse, *g]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_inputs_of_stride_zero(lib, d):
+    """Heads or tokens that share memory give the bits of their copies."""
+    gen = torch.Generator(device=DEV).manual_seed(38)
+    r = lambda *s: torch.randn(s, generator=gen, device=DEV).to(torch.bfloat16)
+    T, heads, kvh = 200, 6, 3
+    st = torch.tensor([0, 70, 200], dtype=torch.int32, device=DEV)
+    a = dqt.attn(T, T, heads, kvh, d, st, st)
+    q, k, v, do = r(T, 1, d), r(T, 1, d), r(1, kvh, d), r(T, heads, d)
+    views = [q.expand(T, heads, d), k.expand(T, kvh, d), v.expand(T, kvh, d), do[:1].expand(T, heads, d)]
+    log(f"attention: inputs of stride zero d={d}")
+    for x, y in zip(call(a, *views), call(a, *[t.contiguous() for t in views])):
+        assert torch.equal(x, y)
+
+
+def test_attention_one_start_alone(lib):
+    """Starts of the queries or of the keys alone: the other is all tokens."""
+    gen = torch.Generator(device=DEV).manual_seed(39)
+    r = lambda *s: torch.randn(s, generator=gen, device=DEV).to(torch.bfloat16)
+    q, k, v, do = r(50, 4, 64), r(90, 2, 64), r(90, 2, 64), r(50, 4, 64)
+    s = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    log("attention: one start alone")
+    want = call(dqt.attn(50, 90, 4, 2, 64, s(0, 50), s(0, 90)), q, k, v, do)
+    for qs, ks in ((s(0, 50), None), (None, s(0, 90)), (None, None)):
+        for x, y in zip(call(dqt.attn(50, 90, 4, 2, 64, qs, ks), q, k, v, do), want):
+            assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_without_queries_or_keys(lib, d):
+    """No key: O and dQ 0, lse -inf.  No query: dK and dV 0."""
+    e, x = (torch.ones((n, 2, d), dtype=torch.bfloat16, device=DEV) for n in (0, 140))
+    log(f"attention: no queries, no keys d={d}")
+    O, lse, dQ, dK, dV = call(dqt.attn(140, 0, 2, 2, d), x, e, e, x)
+    assert (O == 0).all() and (dQ == 0).all() and (lse == -float("inf")).all() and dK.numel() == dV.numel() == 0
+    O, lse, dQ, dK, dV = call(dqt.attn(0, 140, 2, 2, d), e, x, x, e)
+    assert (dK == 0).all() and (dV == 0).all() and O.numel() == lse.numel() == dQ.numel() == 0

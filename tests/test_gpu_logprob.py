@@ -361,3 +361,30 @@ def test_logprob_gradient_of_a_masked_target(lib, dt):
     # (p: some 16 fp32 roundings of an exponent of at most 4 and of its sum)
     assert ((got - want).abs() <= (half + 64 * R.F32) * want.abs()).all() and got[4] == 0
     assert float(forward(X.to(DEV), t)["logp"][0]) == -INF
+
+
+def test_logprob_of_the_largest_vocabulary(lib):
+    """A row of 2^28 logits, all zero but a few: sums, alternatives and the
+    gradient in closed form."""
+    V = 1 << 28
+    log("logprob: 2^28 logits")
+    X = torch.zeros((1, V), dtype=torch.bfloat16, device=DEV)
+    some = {V - 1: 6.0, V - 2: 4.0, 5: 5.0, 1 << 27: 3.0}
+    for i, x in some.items():
+        X[0, i] = x
+    t = torch.tensor([V - 1], device=DEV)
+    o = forward(X, t, 6)
+    s = V - 4 + sum(np.exp(x) for x in some.values())
+    lse, ent = np.log(s), np.log(s) - sum(x * np.exp(x) for x in some.values()) / s
+    # (64 blocks of 256 threads sum 2^14 terms of 1 each, exactly up to 2^24)
+    assert abs(float(o["lse"][0]) - lse) < 1e-5 and abs(float(o["logp"][0]) - (6.0 - lse)) < 1e-5
+    assert abs(float(o["entropy"][0]) - ent) < 1e-4
+    assert o["ids"][0].tolist() == [V - 1, 5, V - 2, 1 << 27, 0, 1]
+    dX = torch.full_like(X, 7.0)
+    dqt.dqt_logprob_bwd(X, t, o["stat"], torch.tensor([1.0], device=DEV), dX)
+    torch.cuda.synchronize()
+    assert abs(float(dX[0, V - 1]) - (1 - np.exp(6.0) / s)) <= 2.0 ** -8
+    for i in (5, V - 2, 1 << 27):
+        assert abs(float(dX[0, i]) + np.exp(some[i]) / s) <= 2.0 ** -7 * np.exp(some[i]) / s
+    dX[0, list(some)] = dX[0, 0].clone()
+    assert (dX == dX[0, 0]).all() and abs(float(dX[0, 0]) * s + 1) <= 2.0 ** -7
