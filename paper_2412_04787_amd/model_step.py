@@ -61,8 +61,8 @@ class ModelConfig:
     kv_heads: int = 0          # key heads (0: as many as heads); fewer need own_ops
     own_ops: bool = False      # attention, SwiGLU and loss in this library's kernels
     # own_ops: gate and up are held for the backward in 8 bits, one scale for 128
-    # elements (their gradients, and no other step's result, are off by 0.7 % rms
-    # for normal values); False: as they are, in bf16
+    # elements (the forward is the same; gradients through the product are off by
+    # 0.7 % rms for normal values); False: as they are, in bf16
     ckpt8: bool = True
 
     def __post_init__(self):
