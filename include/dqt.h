@@ -349,6 +349,210 @@ dqt_status dqt_attn_bwd(const dqt_attn* a, const dqt_rows* Q, const dqt_rows* K,
                         const dqt_rows* dO, const dqt_rows* dQ, const dqt_rows* dK,
                         const dqt_rows* dV, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * Rotary positions (the LLaMA blocks of Sec. 4.1 turn each query and key by its
+ * position).  The first `rot` values of a head form rot / 2 pairs (a, b): values
+ * i and i + rot / 2 (pairs = 0), or 2 i and 2 i + 1 (pairs = 1).  At position p
+ * pair i turns by t = p freq[i] 2^-64 turns:
+ *   a' = a cos - b sin,  b' = a sin + b cos,  cos and sin times amp,
+ * the rest of the head is copied.  freq holds turns per position as 64-bit
+ * fractions of a turn, so p freq modulo 2^64 is the exact fraction at any
+ * position, negative ones among them; cos and sin are formed in double and rounded
+ * to fp32, a' and b' are three fp32 operations, rounded once to the tensor's type.
+ *   freq: device uint64 [rot / 2], 8-byte aligned.
+ *   d: the head's width, a multiple of 16, at most 1024; rot: a multiple of 16,
+ *      16 .. d.  amp: finite.
+ */
+typedef struct {
+  const uint64_t* freq;
+  int32_t d;
+  int32_t rot;
+  int32_t pairs;        /* 0 or 1                                              */
+  int32_t reserved;     /* must be 0                                           */
+  double amp;
+} dqt_rope;
+
+/* One tensor [tokens, heads, d] and where its rotated form goes: Y is X itself
+ * (same strides), or overlaps no X.  Strides as for the attention (elements). */
+typedef struct {
+  dqt_rows X;
+  dqt_rows Y;
+  int32_t heads;        /* 1 .. 1024                                           */
+  int32_t reserved;     /* must be 0                                           */
+} dqt_rope_io;
+
+/* The frequencies of a model (host, no GPU): f_i = base^(-2 i / rot) / (2 pi)
+ * turns per position, for a context stretched by `factor` blended with f_i /
+ * factor by how often the pair turns in the original context,
+ *   k = clamp((context f_i - slow) / (fast - slow), 0, 1),
+ *   freq[i] = round(2^64 f_i (k + (1 - k) / factor)):
+ * pairs of more than `fast` turns are kept, of fewer than `slow` stretched.
+ * slow = fast stretches every pair alike (k = 0; positions divided by factor).
+ *   freq: host uint64 [rot / 2].  base > 1, factor >= 1, context >= 0,
+ *   0 <= slow <= fast, all finite; DQT_ERR_RANGE otherwise. */
+dqt_status dqt_rope_freqs(int32_t rot, double base, double factor, double context,
+                          double slow, double fast, uint64_t* freq);
+
+/* Rotates n (1 .. DQT_MAX_ROPE) tensors of x_t = DQT_F32 or DQT_BF16, as a rule
+ * queries and keys, in one launch.
+ *   pos: device int32 [tokens], the position of each, or NULL: 0, 1, 2 ...
+ *   tokens < 2^31, tokens times d below 2^36.
+ * dqt_rope_bwd turns back (the transposed rotation): X holds the gradient of the
+ * rotated values, Y receives that of the values. */
+#define DQT_MAX_ROPE 4
+dqt_status dqt_rope_fwd(const dqt_rope* r, int32_t n, const dqt_rope_io* io, int32_t x_t,
+                        int64_t tokens, const int32_t* pos, void* stream);
+dqt_status dqt_rope_bwd(const dqt_rope* r, int32_t n, const dqt_rope_io* io, int32_t x_t,
+                        int64_t tokens, const int32_t* pos, void* stream);
+
+/*
+ * A layer's cache of keys and values in 8 bits, for attention of new tokens over
+ * what came before.  A page holds DQT_KV_PAGE = 64 consecutive tokens of one
+ * sequence, for all key heads:
+ *   K:  [pages, kv_heads, 64, d] codes,  V: [pages, kv_heads, d, 64] codes (a
+ *       value channel's tokens are consecutive, as the second product reads them),
+ *   scales: [pages, kv_heads, 2] fp32, of the keys and the values of that page
+ *       and head.  A code stands for its number times the scale.
+ *   fmt = DQT_FP8E4M3 or DQT_I8 (-127 .. 127).
+ * A scale is the smallest power of two s in 2^-64 .. 2^112 with |x| <= top s for
+ * all finite x that were written to that page and head since its first token was
+ * (top = 448 for e4m3, 127 for int8).  A power of two, so that codes that stand in
+ * the page when the scale grows move to the new one with hardly a loss: e4m3 codes
+ * exactly, unless they fall below its normal range, int8 codes are rounded again,
+ * once for each doubling.
+ *   pages < 2^31, kv_heads 1 .. 1024, d: 64 or 128.  K, V 16-byte aligned, scales
+ *   8-byte.
+ */
+#define DQT_KV_PAGE 64
+typedef struct {
+  void* K;
+  void* V;
+  float* scales;
+  int64_t pages;
+  int32_t kv_heads;
+  int32_t d;
+  int32_t fmt;          /* DQT_FP8E4M3 or DQT_I8                               */
+  int32_t reserved;     /* must be 0                                           */
+} dqt_kv_cache;
+
+/*
+ * The new tokens of a batch of sequences over such a cache.  Sequence s has
+ * kv_len[s] tokens, the new ones included, which are its last; token t lies in
+ * page table[s, t / 64], row t % 64.  Its new tokens are rows q_start[s] ..
+ * q_start[s + 1] - 1 of the batch's tensors.
+ *   table: device int32 [n_seq, table_stride]; kv_len: device int32 [n_seq];
+ *   q_start: device int32 [n_seq + 1], ascending, or NULL: one new token for each
+ *      sequence (q_tokens = n_seq).  Values that break these rules give wrong
+ *      results but no access outside the tensors: lengths are clamped to 0 ..
+ *      max_len, pages outside the cache (-1 for instance) hold no tokens (what
+ *      is written to them is lost), new tokens that come before position 0 see
+ *      nothing, and neither they nor their rotated queries are written.
+ *   max_len: no kv_len is larger; at most 64 table_stride and 2^31 - 64.  The work
+ *      is laid out for it (which a captured graph keeps), so close is better.
+ *   heads: query heads, a multiple of the cache's kv_heads, at most 1024; query
+ *      head h reads key head h / (heads / kv_heads).  q_tokens * heads < 2^31.
+ *   scale, causal: as for dqt_attn (causal = 0: every new token sees all).
+ */
+typedef struct {
+  const int32_t* table;
+  const int32_t* kv_len;
+  const int32_t* q_start;
+  int64_t q_tokens;
+  int64_t max_len;
+  int32_t n_seq;
+  int32_t table_stride;
+  int32_t heads;
+  int32_t causal;       /* 0 or 1                                              */
+  float scale;
+  int32_t reserved;     /* must be 0                                           */
+} dqt_kv_batch;
+
+/*
+ * Writes the new tokens to the cache and, with `rope`, rotates their keys (before
+ * they are written, in fp32) and queries by the positions kv_len[s] - lq .. kv_len[s]
+ * - 1 in the same launch.
+ *   K, V: [q_tokens, kv_heads, d] bf16.  rope: NULL, or of the same d.
+ *   Q, Qr: NULL (both), or the queries [q_tokens, heads, d] bf16 and where their
+ *      rotated form goes (Q itself, or no overlap); they need rope.
+ * A page whose row 0 is written starts a new scale; otherwise its scale stays or
+ * grows over the codes that stand in it.  Rows behind a sequence's last token are
+ * left as they are.  An infinite value is held as the largest code of its sign, a
+ * NaN as 0; neither counts for the scale, nor do values beyond top 2^112.
+ * A page that receives tokens belongs to one sequence of the batch (dqt_kv_pool_
+ * extend sees to that).  The scale, batch and attention fields that it does not
+ * need (scale, causal) are checked all the same.
+ */
+dqt_status dqt_kv_append(const dqt_kv_cache* c, const dqt_kv_batch* b, const dqt_rows* K,
+                         const dqt_rows* V, const dqt_rope* rope, const dqt_rows* Q,
+                         const dqt_rows* Qr, void* stream);
+
+/*
+ * Attention of the new tokens' queries over the cache, which holds their own keys
+ * and values too: query i of a sequence of lq sees key j when j <= i + kv_len - lq
+ * (causal) or always.  Formulas, O = 0 and lse = -inf for a query that sees nothing,
+ * strides and lse as for dqt_attn_fwd.  Q and O are bf16.  Codes enter the matrix
+ * products as they are, in 16-bit floating point which holds them exactly; the
+ * queries on a power of two of their largest value (exactly, but for values below
+ * 2^-31 of it), the probabilities times the values' scale relative to the largest such
+ * product so far (each off by 2^-11 of itself at most, those below 2^-22 of the
+ * largest by 2^-33 of it); sums are fp32.
+ * The values' scales of one sequence and head lie within 2^100 of each other.
+ * A NaN code in the cache (dqt_kv_append writes none) may reach any query of its
+ * sequence and head; what lies behind a sequence's last token reaches none.
+ *   ws: dqt_kv_attn_workspace() bytes, which depend on sizes alone.
+ */
+size_t dqt_kv_attn_workspace(const dqt_kv_cache* c, const dqt_kv_batch* b);
+dqt_status dqt_kv_attn(const dqt_kv_cache* c, const dqt_kv_batch* b, const dqt_rows* Q,
+                       const dqt_rows* O, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Copies page src[i] to page dst[i] (codes and scales), i = 0 .. n - 1, in each of
+ * n_caches caches (a model's layers) of the same sizes and format.  src, dst: host
+ * int32 [n], read before the call returns; every page in range, no page twice in
+ * dst and none of dst in src (DQT_ERR_RANGE).  One launch for up to 32 caches and
+ * 256 pages. */
+dqt_status dqt_kv_copy(int32_t n_caches, const dqt_kv_cache* c, int32_t n, const int32_t* src,
+                       const int32_t* dst, void* stream);
+
+/*
+ * Who holds which page (host memory, no GPU).  Sequences that were forked share
+ * pages; refs counts the holders of each.  A sequence's row of the page table is
+ * host int32 [row_pages], its length the caller's; unused entries are -1.  All
+ * arrays are the caller's.  A call that returns an error has changed nothing.
+ *   init: all pages free (page 0 is given out first).
+ *   extend: pages for tokens len .. new_len - 1 of a sequence, to be written: new
+ *      pages are taken, and a partly filled last page that others hold too is
+ *      replaced by a new one, for which the copy *src -> *dst has to be made
+ *      (dqt_kv_copy) before it is written; *src = -1 when there is none.
+ *      DQT_ERR_WORKSPACE: too few free pages; DQT_ERR_SHAPE: row too short.
+ *   fork: another sequence, of the row `to`, holds the same pages.
+ *   trim: keeps the first new_len <= len tokens; pages without holders are free
+ *      (new_len = 0 ends the sequence).  A scale that a dropped token raised stays
+ *      until its page starts anew.
+ *   compact: all pages in use move to 0 .. used - 1, table [n_seq, row_pages] (each
+ *      sequence's row, with every reference to the pool's pages) is rewritten, and
+ *      *n copies src[i] -> dst[i] have to be made before the cache is used.  src,
+ *      dst: host int32 [pages].
+ *   DQT_ERR_RANGE: a row does not hold what its length says, or holds a page that
+ *   is not in use; for compact also when the table's references are not those
+ *   that refs counts.
+ */
+typedef struct {
+  int32_t* refs;        /* host [pages]: holders of each page                  */
+  int32_t* free_pages;  /* host [pages]: the first n_free are free, last first */
+  int32_t pages;
+  int32_t n_free;
+} dqt_kv_pool;
+
+dqt_status dqt_kv_pool_init(dqt_kv_pool* p, int32_t pages, int32_t* refs, int32_t* free_pages);
+dqt_status dqt_kv_pool_extend(dqt_kv_pool* p, int32_t* row, int32_t row_pages, int64_t len,
+                              int64_t new_len, int32_t* src, int32_t* dst);
+dqt_status dqt_kv_pool_fork(dqt_kv_pool* p, const int32_t* row, int32_t row_pages, int64_t len,
+                            int32_t* to);
+dqt_status dqt_kv_pool_trim(dqt_kv_pool* p, int32_t* row, int32_t row_pages, int64_t len,
+                            int64_t new_len);
+dqt_status dqt_kv_pool_compact(dqt_kv_pool* p, int32_t* table, int32_t n_seq, int32_t row_pages,
+                               int32_t* src, int32_t* dst, int32_t* n);
+
 /* Bytes of device workspace for the fastest form of dqt_linear_fwd on this
  * weight: the 256 counter bytes, plus, for ternary, 3-bit and 4-bit codes,
  * d_out * d_in bytes the codes are expanded into (int8 or e4m3 bytes, or

@@ -4,16 +4,13 @@
 #include <math.h>
 #include <string.h>
 
-#include "../../include/dqt.h"
-#include "dqt_launch.h"
+#include "abi_check.h"
 
 namespace {
 
 constexpr int32_t kVersion = 1 * 10000 + 0 * 100 + 0;
 // |acc| <= 128 * 128 * d_in must stay below 2^31 for the int32 forward.
 constexpr int64_t kMaxDin = 65536;
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 dqt_status check_weight(const dqt_weight* w) {
   if (w == nullptr) return DQT_ERR_NULL;
@@ -40,10 +37,6 @@ dqt_status check_weight(const dqt_weight* w) {
 int code_format(int32_t wfmt) {
   return wfmt == DQT_TERNARY2 ? 1 : wfmt == DQT_INT4 ? 2 : wfmt == DQT_INT3 ? 3 : 0;
 }
-
-bool is_float_type(int32_t t) { return t == DQT_F32 || t == DQT_BF16; }
-
-dqt_status from_hip(hipError_t e) { return e == hipSuccess ? DQT_OK : DQT_ERR_HIP; }
 
 }  // namespace
 
@@ -112,9 +105,6 @@ dqt_status dqt_rmsnorm_backward(int32_t n_dy, const void* const* dY, const void*
 }
 
 namespace {
-
-bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
-bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // A checkpoint is given as a whole or not at all.
 dqt_status check_ckpt(const dqt_ckpt_io* c, dqt::Ckpt* out) {
@@ -233,8 +223,6 @@ dqt_status dqt_logprob_bwd(const void* X, int32_t x_t, int64_t M, int32_t V, int
 
 namespace {
 
-constexpr int64_t kMaxBlocks = int64_t(1) << 24;      // of 256 threads: the runtime's grids end at 2^32 threads
-
 // Checks the descriptor and fills the sizes of the launch arguments.
 dqt_status check_attn(const dqt_attn* d, dqt::AttnArgs* a) {
   if (d == nullptr) return DQT_ERR_NULL;
@@ -260,13 +248,7 @@ dqt_status check_attn(const dqt_attn* d, dqt::AttnArgs* a) {
   a->heads = d->heads;
   a->kv_heads = d->kv_heads;
   a->group = (int)g;
-  a->gone = g == 1 ? ~0u : 0u;
-  if (g > 1) {      // r / g = umulhi(r, m) >> (b - 1) with m = ceil(2^(31 + b) / g), b = ceil(log2 g), for r < 2^31
-    int b = 1;
-    while ((int64_t(1) << b) < g) ++b;
-    a->gmul = (uint32_t)(((uint64_t(1) << (31 + b)) + g - 1) / g);
-    a->gshift = b - 1;
-  }
+  group_division(g, &a->gmul, &a->gone, &a->gshift);
   a->scale = d->scale;
   a->causal = d->causal;
   a->row_tiles = (int)rt;
@@ -284,22 +266,6 @@ size_t attn_part_bytes(const dqt::AttnArgs& a, int d) {
 size_t attn_stat_bytes(const dqt::AttnArgs& a) { return ((size_t)a.heads * a.tq * 8 + 15) / 16 * 16; }
 size_t attn_bwd_bytes(const dqt::AttnArgs& a, int d) {
   return attn_stat_bytes(a) + (a.bwd_splits == 1 ? 0 : (size_t)a.bwd_splits * 2 * a.tk * a.kv_heads * d * 4);
-}
-
-// A strided tensor [tokens, heads, d] of bf16: non-negative strides that keep
-// 16-byte alignment; an output's rows must not overlap.
-dqt_status check_rows(const dqt_rows* t, int64_t tokens, int32_t heads, int32_t d, bool output) {
-  if (t == nullptr) return DQT_ERR_NULL;
-  if (tokens > 0 && t->p == nullptr) return DQT_ERR_NULL;
-  if (!aligned16(t->p) || (t->token & 7) != 0 || (t->head & 7) != 0) return DQT_ERR_ALIGN;
-  // (the kernels take a tile's rows, up to 128 tokens, at 32-bit offsets)
-  if (t->token < 0 || t->head < 0 || t->token > (int64_t(1) << 23) || t->head > (int64_t(1) << 40)) return DQT_ERR_SHAPE;
-  if (output && tokens > 0) {
-    const bool by_token = (heads == 1 || t->head >= d) && (tokens == 1 || t->token >= (heads - 1) * t->head + d);
-    const bool by_head = (tokens == 1 || t->token >= d) && (heads == 1 || t->head >= (tokens - 1) * t->token + d);
-    if (!by_token && !by_head) return DQT_ERR_SHAPE;
-  }
-  return DQT_OK;
 }
 
 }  // namespace

@@ -1,0 +1,432 @@
+// Attention of new tokens over the 8-bit cache.
+//
+// Query row r of a sequence and key head (token r / G, head r % G of the G query heads
+// that share it) sees keys j <= token + lk - lq (causal).  With codes k_j, v_j of page
+// scales a_j, b_j = 2^ev (powers of two) and c = scale log2 e:
+//   u_j = c a_j q.k_j + ev,  M = max u_j so far,  w_j = 2^(u_j - M + 8),
+//   o = sum w_j v_j / l,  l = sum w_j 2^-ev,  lse = ln 2 (M - 8 + log2 l)
+// so that the values' scale rides in the exponent and o is summed from codes.
+//
+// Both products run on the matrix cores in 16-bit floating point (fp16), which holds
+// every code exactly; the row of Q is brought to 2^14 .. 2^15 by a power of two (bf16
+// values fit, those below 2^-31 of the row's largest lose bits), and w, at most 2^14,
+// is off by 2^-11 of itself (below 2^-14, which is 2^-22 of the largest, by 2^-25).
+// In bf16 it would be off by 2^-8, as much as the result's own rounding.
+#include "kv_common.h"
+
+namespace dqt {
+
+namespace {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+using lds_f32 = __attribute__((address_space(3))) float;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLift = 8.0f;        // w = 2^(u - M + kLift)
+constexpr float kSlack = 6.0f;       // M moves when u passes it by more: w <= 2^14
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ int row_token(const KvAttnArgs& a, int r) {
+  return (int)((__umulhi((uint32_t)r, a.gmul) + ((uint32_t)r & a.gone)) >> a.gshift);
+}
+
+// 4 codes -> 4 fp16 values, exactly
+template <bool E4M3>
+__device__ __forceinline__ uint2 widen4(uint32_t w) {
+  if constexpr (E4M3) {
+    return uint2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true))};
+  } else {
+    // x + 128 in the low byte of 1024.0 is 1024 + x + 128
+    const uint32_t u = w ^ 0x80808080u;
+    const f16x2 off = {(_Float16)1152, (_Float16)1152};
+    const f16x2 lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - off;
+    const f16x2 hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - off;
+    return uint2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+  }
+}
+template <bool E4M3>
+__device__ __forceinline__ f16x8 widen8(int w0, int w1) {
+  const uint2 a = widen4<E4M3>((uint32_t)w0), b = widen4<E4M3>((uint32_t)w1);
+  return __builtin_bit_cast(f16x8, i32x4{(int)a.x, (int)a.y, (int)b.x, (int)b.y});
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  const f32x2_t v = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+}
+// the power of two k with 2^14 <= most 2^-k < 2^15 (no less than -40: smaller rows
+// need no more)
+__device__ __forceinline__ int row_shift(float most) {
+  return max((int)(__float_as_uint(most) >> 23) - 127 - 14, -40);
+}
+__device__ __forceinline__ float finite_abs(uint32_t bits) {
+  const float a = fabsf(__uint_as_float(bits));
+  return a <= 3.402823466e38f ? a : 0.0f;
+}
+// 8 bf16 values times f -> fp16
+__device__ __forceinline__ f16x8 scaled_row(i32x4 x, float f) {
+  i32x4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    y[i] = (int)pack_f16x2(__uint_as_float((uint32_t)x[i] << 16) * f, __uint_as_float((uint32_t)x[i] & 0xFFFF0000u) * f);
+  return __builtin_bit_cast(f16x8, y);
+}
+__device__ __forceinline__ float row_most(i32x4 x) {
+  float m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    m = fmaxf(m, fmaxf(finite_abs((uint32_t)x[i] << 16), finite_abs((uint32_t)x[i] & 0xFFFF0000u)));
+  return m;
+}
+// bytes 4 i .. 4 i + 3 of 16, of which the first n count: a mask
+__device__ __forceinline__ uint32_t keep_bytes(int n, int i) {
+  const int k = n - 4 * i;
+  return k >= 4 ? ~0u : k <= 0 ? 0u : (1u << (8 * k)) - 1;
+}
+
+// One tile of rows of one sequence and key head.
+struct Tile {
+  KvSeq q;
+  int r0, rows;          // its first row, the sequence's rows
+  int nblk;              // pages that its last row sees
+};
+__device__ __forceinline__ Tile tile_at(const KvAttnArgs& a, const KvSeq& q, int item) {
+  Tile t{q, item * a.tile_rows, q.lq * a.c.group, 0};
+  if (item >= 0 && t.r0 < t.rows) {
+    const int last = a.causal ? row_token(a, min(t.r0 + a.tile_rows, t.rows) - 1) + q.lk - q.lq : q.lk - 1;
+    t.nblk = last < 0 ? 0 : last / kPage + 1;
+  }
+  return t;
+}
+
+// ------------------------------------------------------------------ few rows
+// 16 NT rows of a sequence and key head over a range of pages, which the block's four
+// waves take in turn and join at the end.  Codes go from memory to registers and into
+// the matrix cores, 16 consecutive bytes per lane and load, without LDS: a wave holds
+// a whole page (64 tokens) of keys and one of values, and the next page's keys are
+// loaded while this one's are worked on.
+//
+// v_mfma_f32_16x16x32_f16: A lane l holds row l % 16, 8 values of the reduction from
+// 8 (l / 16); B the same of columns; result register i is row 4 (l / 16) + i of column
+// l % 16.  Scores are formed transposed, 16 tokens x 16 rows.  A lane's 16 bytes of a
+// key row serve two steps of the reduction over d (Q is read in the same order), and
+// token 16 (m / 4) + 4 t + m % 4 of a page is row m of token tile t, so that a lane's
+// results of four tiles are tokens 16 (l / 16) + 0..15: those of the 16 bytes that
+// it loads of a value channel, and, as they are, the second product's B operand.
+template <int D, bool E4M3, int NT>
+__global__ __launch_bounds__(256, 2) void kv_attn_kernel(KvAttnArgs a) {
+  constexpr int KJ = D / 64, ND = D / 16, ROWS = 16 * NT, OROW = D + 4;
+  __shared__ float part_o[4][ROWS][OROW];
+  __shared__ float part_m[4][ROWS], part_l[4][ROWS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  int id = blockIdx.x, item;
+  const int kvh = id % a.c.kv_heads;
+  id /= a.c.kv_heads;
+  const int split = id / a.tiles;
+  const Tile t = tile_at(a, kv_find(a.c, id - split * a.tiles, a.c.group, ROWS, 1, item), item);
+  if (item < 0 || t.r0 >= t.rows) return;
+  const int first = split * a.chunk, end = min(first + a.chunk, t.nblk);
+  if (split > 0 && first >= t.nblk) return;
+  if (a.splits > 1 && t.nblk == 0) return;          // (the join writes the empty rows)
+
+  // the rows
+  i32x4 qraw[NT][2 * KJ];
+  int lim[NT], tok[NT], head[NT];
+  f16x8 qf[NT][2 * KJ];
+  float qc[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = min(t.r0 + 16 * nt + n, t.rows - 1);
+    tok[nt] = row_token(a, r);
+    head[nt] = kvh * a.c.group + (r - tok[nt] * a.c.group);
+    lim[nt] = a.causal ? tok[nt] + t.q.lk - t.q.lq : t.q.lk - 1;
+    const uint8_t* p = a.Q + (int64_t)(t.q.q0 + tok[nt]) * a.q_tok + head[nt] * a.q_head;
+#pragma unroll
+    for (int j = 0; j < KJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) qraw[nt][2 * j + e] = *reinterpret_cast<const i32x4*>(p + 2 * (64 * j + 16 * g + 8 * e));
+  }
+  const int lim_lo = __builtin_amdgcn_readfirstlane(lim[0]);
+
+  // this wave's pages of up to 256 of the block's, one per lane
+  int page;
+  float ks, vs;
+  auto find_pages = [&](int from) {
+    const int blk = from + wave + 4 * lane;
+    page = -1;
+    ks = vs = 1.0f;
+    if (blk < end) page = a.c.table[(int64_t)t.q.s * a.c.table_stride + blk];
+    if (page < 0 || page >= a.c.pages) page = -1;
+    if (page >= 0) {
+      const float2 s = *reinterpret_cast<const float2*>(a.c.scales + 2 * ((int64_t)page * a.c.kv_heads + kvh));
+      ks = s.x;
+      vs = s.y;
+    }
+  };
+
+  // page i of this wave -> its codes
+  const uint32_t koff = (16 * (n >> 2) + (n & 3)) * D + 16 * g, voff = n * kPage + 16 * g;
+  auto block_at = [&](int i) {
+    const int p = __builtin_amdgcn_readlane(page, i);
+    return ((int64_t)p * a.c.kv_heads + kvh) * (int64_t)(kPage * D);
+  };
+  i32x4 kraw[4][KJ], vraw[ND];
+  auto load_k = [&](int i) {
+    const uint8_t* p = a.c.K + block_at(i);
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) kraw[mt][j] = *reinterpret_cast<const i32x4*>(p + koff + 4 * D * mt + 64 * j);
+  };
+  auto load_v = [&](int i) {
+    const uint8_t* p = a.c.V + block_at(i);
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) vraw[dt] = *reinterpret_cast<const i32x4*>(p + voff + 16 * kPage * dt);
+  };
+
+  unsigned long long todo;
+  int i;
+  auto begin = [&](int from) {
+    find_pages(from);
+    todo = __ballot(page >= 0);
+    i = todo ? __builtin_ctzll(todo) : 0;
+    if (todo) {
+      load_k(i);
+      load_v(i);
+    }
+  };
+  begin(first);
+
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float most = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 2 * KJ; ++j) most = fmaxf(most, row_most(qraw[nt][j]));
+    most = fmaxf(most, __shfl_xor(most, 16, kWave));
+    most = fmaxf(most, __shfl_xor(most, 32, kWave));
+    const int k = row_shift(most);
+    const float f = exp2_int(-k);
+    qc[nt] = a.scale * kLog2e * exp2_int(k);
+#pragma unroll
+    for (int j = 0; j < 2 * KJ; ++j) qf[nt][j] = scaled_row(qraw[nt][j], f);
+  }
+
+  f32x4 o[NT][ND];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    m[nt] = -__builtin_inff();
+    l[nt] = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) o[nt][dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  for (int from = first;;) {
+    while (todo) {
+      todo &= todo - 1;
+      const int next = todo ? __builtin_ctzll(todo) : -1;
+      const int at = (from + wave + 4 * i) * kPage;           // the page's first token
+      const float kscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), i));
+      const int ev = exp_of(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), i)));
+
+      f32x4 s[NT][4];
+#pragma unroll
+      for (int mt = 0; mt < 4; ++mt) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) s[nt][mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < KJ; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const f16x8 k8 = widen8<E4M3>(kraw[mt][j][2 * e], kraw[mt][j][2 * e + 1]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              s[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k8, qf[nt][2 * j + e], s[nt][mt], 0, 0, 0);
+          }
+      }
+      if (next >= 0) load_k(next);
+
+      f16x8 w[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        if (at + kPage - 1 > lim_lo) {
+#pragma unroll
+          for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (at + 16 * g + 4 * mt + e > lim[nt]) s[nt][mt][e] = -__builtin_inff();
+        }
+        float mx = -__builtin_inff();
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) mx = fmaxf(mx, fmaxf(s[nt][mt][e], s[nt][mt][e + 1]));
+        mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        const float c = kscale * qc[nt], u = mx * c + (float)ev;
+        if (__ballot(u > m[nt] + kSlack)) {
+          const float to = fmaxf(m[nt], u), f = to == m[nt] ? 1.0f : exp2_fast(m[nt] - to);
+          m[nt] = to;
+          l[nt] *= f;
+#pragma unroll
+          for (int dt = 0; dt < ND; ++dt) o[nt][dt] *= f;
+        }
+        const float b = (float)ev + kLift - (m[nt] == -__builtin_inff() ? 0.0f : m[nt]);
+        float sum = 0.0f;
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[nt][mt][e] = exp2_fast(__builtin_fmaf(s[nt][mt][e], c, b));
+            sum += s[nt][mt][e];
+          }
+        l[nt] += sum * exp2_int(-ev);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          w[nt][h] = __builtin_bit_cast(f16x8, i32x4{(int)pack_f16x2(s[nt][2 * h][0], s[nt][2 * h][1]),
+                                                     (int)pack_f16x2(s[nt][2 * h][2], s[nt][2 * h][3]),
+                                                     (int)pack_f16x2(s[nt][2 * h + 1][0], s[nt][2 * h + 1][1]),
+                                                     (int)pack_f16x2(s[nt][2 * h + 1][2], s[nt][2 * h + 1][3])});
+      }
+      if (at + kPage > t.q.lk) {                               // what lies behind the last token is not read
+        const int have = t.q.lk - at - 16 * g;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vraw[dt][e] &= (int)keep_bytes(have, e);
+      }
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f16x8 v8 = widen8<E4M3>(vraw[dt][2 * h], vraw[dt][2 * h + 1]);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v8, w[nt][h], o[nt][dt], 0, 0, 0);
+        }
+      if (next >= 0) load_v(next);
+      i = next;
+    }
+    from += 4 * kWave;
+    if (from >= end) break;
+    begin(from);
+  }
+
+  // the four waves' sums on a common M
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    l[nt] += __shfl_xor(l[nt], 16, kWave);
+    l[nt] += __shfl_xor(l[nt], 32, kWave);
+    if (g == 0) {
+      part_m[wave][16 * nt + n] = m[nt];
+      part_l[wave][16 * nt + n] = l[nt];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = 16 * nt + n;
+    const float all = fmaxf(fmaxf(part_m[0][r], part_m[1][r]), fmaxf(part_m[2][r], part_m[3][r]));
+    const float f = m[nt] == all ? 1.0f : exp2_fast(m[nt] - all);
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) *reinterpret_cast<f32x4*>(&part_o[wave][r][16 * dt + 4 * g]) = o[nt][dt] * f;
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < ROWS * (D / 4); x += 256) {
+    const int r = x / (D / 4), d = 4 * (x % (D / 4));
+    if (t.r0 + r >= t.rows) break;
+    float all = part_m[0][r], sum = 0.0f;
+#pragma unroll
+    for (int v = 1; v < 4; ++v) all = fmaxf(all, part_m[v][r]);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) sum += part_m[v][r] == all ? part_l[v][r] : part_l[v][r] * exp2_fast(part_m[v][r] - all);
+    f32x4 y = *reinterpret_cast<const f32x4*>(&part_o[0][r][d]);
+#pragma unroll
+    for (int v = 1; v < 4; ++v) y += *reinterpret_cast<const f32x4*>(&part_o[v][r][d]);
+    y *= all == -__builtin_inff() ? 0.0f : 1.0f / sum;
+    const float lse = all == -__builtin_inff() ? all : all - kLift + log2f(sum);
+    const int tk = row_token(a, t.r0 + r), hd = kvh * a.c.group + (t.r0 + r - tk * a.c.group);
+    const int64_t row = t.q.q0 + tk;
+    if (a.splits == 1) {
+      *reinterpret_cast<uint2*>(a.O + row * a.o_tok + hd * a.o_head + 2 * d) = uint2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+      if (d == 0 && a.lse != nullptr) a.lse[(int64_t)hd * a.c.tq + row] = lse * kLn2;
+    } else {
+      const int64_t at = ((int64_t)split * a.c.tq + row) * a.c.heads + hd;
+      *reinterpret_cast<f32x4*>(a.part + at * D + d) = y;
+      if (d == 0) a.part_lse[at] = lse;
+    }
+  }
+}
+
+// Joins the splits of one row (a wave each): o = sum_p 2^(L_p - L) o_p / sum_p 2^(L_p - L).
+template <int D>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (at >= (int64_t)a.c.tq * a.c.heads) return;
+  const int row = (int)(at / a.c.heads), hd = (int)(at - (int64_t)row * a.c.heads);
+  int tok = 0;
+  const KvSeq q = a.c.q_start == nullptr ? kv_seq(a.c, row) : kv_find(a.c, row, 1, 1, 0, tok);
+  if (tok < 0 || tok >= q.lq) return;                // a token outside every sequence
+  const int r = tok * a.c.group + hd % a.c.group;
+  const Tile t = tile_at(a, q, r / a.tile_rows);
+  const int parts = (t.nblk + a.chunk - 1) / a.chunk;
+  const int64_t step = (int64_t)a.c.tq * a.c.heads;
+  float all = -__builtin_inff();
+  for (int p = lane; p < parts; p += kWave) all = fmaxf(all, a.part_lse[p * step + at]);
+  all = wave_max(all);
+  float y[D / 64], sum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < D / 64; ++e) y[e] = 0.0f;
+  if (all > -__builtin_inff()) {
+    for (int p = 0; p < parts; ++p) {
+      const float w = exp2_fast(a.part_lse[p * step + at] - all);
+      const float* x = a.part + (p * step + at) * D + lane * (D / 64);
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e) y[e] += w * x[e];
+      sum += w;
+    }
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) y[e] /= sum;
+  }
+  uint8_t* o = a.O + row * a.o_tok + hd * a.o_head + lane * (D / 32);
+  if constexpr (D == 128) *reinterpret_cast<uint32_t*>(o) = pack_bf16x2(y[0], y[1]);
+  else *reinterpret_cast<uint16_t*>(o) = (uint16_t)(pack_bf16x2(y[0], y[0]) & 0xFFFFu);
+  if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)hd * a.c.tq + row] = all == -__builtin_inff() ? all : (all + log2f(sum)) * kLn2;
+}
+
+}  // namespace
+
+void kv_attn_plan(KvAttnArgs* a) {
+  const int64_t rows = (int64_t)a->c.tq * a->c.group, blocks = ((int64_t)a->c.max_len + kPage - 1) / kPage;
+  a->tile_rows = rows <= 16 * (int64_t)a->c.n_seq ? 16 : 32;
+  a->tiles = (int)(a->c.q_start == nullptr && a->c.group <= a->tile_rows ? a->c.n_seq : rows / a->tile_rows + a->c.n_seq);
+  const int64_t base = (int64_t)a->tiles * a->c.kv_heads;
+  int64_t chunk = (blocks * base + 2047) / 2048;
+  chunk = (chunk + 3) / 4 * 4;
+  a->chunk = (int)(chunk < 8 ? 8 : chunk);
+  a->splits = (int)((blocks + a->chunk - 1) / a->chunk);
+  if (a->splits < 1) a->splits = 1;
+}
+
+hipError_t launch_kv_attn(bool e4m3, const KvAttnArgs& a, hipStream_t s) {
+  const dim3 grid((uint32_t)((int64_t)a.tiles * a.c.kv_heads * a.splits));
+  LaunchStatus st;
+  auto go = [&](auto k) { st << launch_kernel(k, grid, dim3(256), s, a); };
+  if (a.c.d == 128) {
+    if (a.tile_rows == 16) e4m3 ? go(kv_attn_kernel<128, true, 1>) : go(kv_attn_kernel<128, false, 1>);
+    else e4m3 ? go(kv_attn_kernel<128, true, 2>) : go(kv_attn_kernel<128, false, 2>);
+  } else {
+    if (a.tile_rows == 16) e4m3 ? go(kv_attn_kernel<64, true, 1>) : go(kv_attn_kernel<64, false, 1>);
+    else e4m3 ? go(kv_attn_kernel<64, true, 2>) : go(kv_attn_kernel<64, false, 2>);
+  }
+  if (a.splits > 1) {
+    const dim3 join((uint32_t)(((int64_t)a.c.tq * a.c.heads + 3) / 4));
+    auto j = [&](auto k) { st << launch_kernel(k, join, dim3(256), s, a); };
+    a.c.d == 128 ? j(kv_join_kernel<128>) : j(kv_join_kernel<64>);
+  }
+  return st.e;
+}
+
+}  // namespace dqt

@@ -34,7 +34,9 @@ EXPORTS = (
     "dqt_unpack_ternary", "dqt_pack_int4", "dqt_unpack_int4", "dqt_pack_int3", "dqt_unpack_int3", "dqt_launch_timer_start", "dqt_launch_timer_stop", "dqt_read_stream",
     "dqt_swiglu_act_quant", "dqt_swiglu_backward", "dqt_logprob_workspace", "dqt_logprob_fwd",
     "dqt_logprob_bwd", "dqt_attn_fwd_workspace", "dqt_attn_fwd", "dqt_attn_bwd_workspace",
-    "dqt_attn_bwd", "dqt_status_string", "dqt_version",
+    "dqt_attn_bwd", "dqt_rope_freqs", "dqt_rope_fwd", "dqt_rope_bwd", "dqt_kv_append", "dqt_kv_attn_workspace",
+    "dqt_kv_attn", "dqt_kv_copy", "dqt_kv_pool_init", "dqt_kv_pool_extend", "dqt_kv_pool_fork", "dqt_kv_pool_trim",
+    "dqt_kv_pool_compact", "dqt_status_string", "dqt_version",
 )
 
 
@@ -79,6 +81,32 @@ class DqtRows(ctypes.Structure):
     _fields_ = [("p", ctypes.c_void_p), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
 
 
+class DqtRope(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("d", ctypes.c_int32), ("rot", ctypes.c_int32), ("pairs", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("amp", ctypes.c_double)]
+
+
+class DqtRopeIO(ctypes.Structure):
+    _fields_ = [("X", DqtRows), ("Y", DqtRows), ("heads", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class DqtKvCache(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("pages", ctypes.c_int64),
+                ("kv_heads", ctypes.c_int32), ("d", ctypes.c_int32), ("fmt", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class DqtKvBatch(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("q_start", ctypes.c_void_p),
+                ("q_tokens", ctypes.c_int64), ("max_len", ctypes.c_int64), ("n_seq", ctypes.c_int32),
+                ("table_stride", ctypes.c_int32), ("heads", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class DqtKvPool(ctypes.Structure):
+    _fields_ = [("refs", ctypes.c_void_p), ("free_pages", ctypes.c_void_p), ("pages", ctypes.c_int32),
+                ("n_free", ctypes.c_int32)]
+
+
 def weight(d_out: int, d_in: int, wfmt: int, qmin: int, qmax: int, alpha: float,
            tensor_id: int = 0) -> DqtWeight:
     return DqtWeight(d_out, d_in, wfmt, qmin, qmax, float(alpha), tensor_id, 0)
@@ -111,6 +139,18 @@ _SIGS = {
     "dqt_attn_fwd": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
     "dqt_attn_bwd_workspace": (ctypes.c_size_t, [_vp]),
     "dqt_attn_bwd": (_i32, [_vp] * 11 + [ctypes.c_size_t, _vp]),
+    "dqt_rope_freqs": (_i32, [_i32] + [ctypes.c_double] * 5 + [_vp]),
+    "dqt_rope_fwd": (_i32, [_vp, _i32, _vp, _i32, _i64, _vp, _vp]),
+    "dqt_rope_bwd": (_i32, [_vp, _i32, _vp, _i32, _i64, _vp, _vp]),
+    "dqt_kv_append": (_i32, [_vp] * 8),
+    "dqt_kv_attn_workspace": (ctypes.c_size_t, [_vp, _vp]),
+    "dqt_kv_attn": (_i32, [_vp] * 6 + [ctypes.c_size_t, _vp]),
+    "dqt_kv_copy": (_i32, [_i32, _vp, _i32, _vp, _vp, _vp]),
+    "dqt_kv_pool_init": (_i32, [_vp, _i32, _vp, _vp]),
+    "dqt_kv_pool_extend": (_i32, [_vp, _vp, _i32, _i64, _i64, _vp, _vp]),
+    "dqt_kv_pool_fork": (_i32, [_vp, _vp, _i32, _i64, _vp]),
+    "dqt_kv_pool_trim": (_i32, [_vp, _vp, _i32, _i64, _i64]),
+    "dqt_kv_pool_compact": (_i32, [_vp, _vp, _i32, _i32, _vp, _vp, _vp]),
     "dqt_linear_fwd_workspace": (ctypes.c_size_t, [_wp]),
     "dqt_linear_fwd": (_i32, [_wp, _vp, _vp, _i32, _i64, _i32, _vp, _vp, _vp, _i32, _vp,
                               ctypes.c_size_t, _vp]),
@@ -486,6 +526,245 @@ def dqt_attn_bwd(a: DqtAttn, Q, K, V, O, lse, dO, dQ, dK, dV, ws, stream=None):
     dev, r = _rows(a, (Q, K, V, O, dO, dQ, dK, dV), "qkkqqqkk", lse)
     _check("dqt_attn_bwd", load().dqt_attn_bwd(ctypes.byref(a), *r[:4], _addr(lse), *r[4:], _addr(ws), _ws_bytes(dev, ws),
                                                _stream(stream)))
+
+
+# ----------------------------------------------------------------- rotary positions and the 8-bit cache
+
+def _row(t, shape, dtype):
+    """The dqt_rows (as bytes) of a tensor [tokens, heads, d] with any token and head strides."""
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"expected a {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    st, sh, sd = t.stride()
+    n, h, d = shape
+    if sd != 1 and t.numel() > 0:
+        raise ValueError(f"expected unit last stride, got strides {t.stride()}")
+    # (strides of a dimension of one do not matter)
+    return _pack_rows(t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d)
+
+
+def dqt_rope_freqs(rot: int, base: float = 10000.0, factor: float = 1.0, context: float = 0.0, slow: float = 1.0,
+                   fast: float = 32.0) -> np.ndarray:
+    """Turns per position of each pair, as 64-bit fractions of a turn (host uint64 [rot / 2])."""
+    freq = np.empty((max(rot, 0) // 2,), dtype=np.uint64)
+    _check("dqt_rope_freqs", load().dqt_rope_freqs(rot, base, factor, context, slow, fast, freq.ctypes.data))
+    return freq
+
+
+class Rope:
+    """Descriptor of a model's rotary positions.  freq: device int64 [rot / 2] (the bits of
+    dqt_rope_freqs); pairs: the values 2 i and 2 i + 1 turn together, else i and i + rot / 2."""
+
+    def __init__(self, freq, d: int, pairs: bool = False, amp: float = 1.0):
+        _bufs(_here(freq), (freq, 8, _torch().int64))
+        if freq.dim() != 1:
+            raise ValueError("expected freq of shape [rot / 2]")
+        self.freq, self.d = freq, d
+        self.desc = DqtRope(freq.data_ptr(), d, 2 * freq.shape[0], int(pairs), 0, amp)
+        self.ref = ctypes.byref(self.desc)
+
+
+def rope(d: int, rot: int | None = None, pairs: bool = False, amp: float = 1.0, device="cuda:0", **freqs) -> Rope:
+    """A Rope of dqt_rope_freqs(rot, **freqs); rot: the whole head by default."""
+    f = dqt_rope_freqs(d if rot is None else rot, **freqs)
+    return Rope(_torch().from_numpy(f.view(np.int64)).to(device), d, pairs, amp)
+
+
+def _rope(fn, rope: Rope, pairs, pos, stream):
+    if not pairs:
+        raise ValueError("expected at least one tensor")
+    x0 = pairs[0][0]
+    dev = _here(x0, rope.freq, *(t for xy in pairs for t in xy))
+    tokens, _, d = x0.shape
+    if d != rope.d:
+        raise ValueError(f"expected heads of {rope.d} values, got {d}")
+    if pos is not None:
+        _bufs(dev, (pos, 4 * tokens, _torch().int32))
+        if pos.numel() != tokens:
+            raise ValueError(f"expected {tokens} positions, got {pos.numel()}")
+    io = b"".join([_row(x, (tokens, x.shape[1], d), x0.dtype) + _row(y, x.shape, x0.dtype) +
+                   _pack_heads(x.shape[1], 0) for x, y in pairs])
+    _check(fn, getattr(load(), fn)(rope.ref, len(pairs), io, dtype_code(x0), tokens, _addr(pos), _stream(stream)))
+
+
+_pack_heads = struct.Struct("2i").pack
+
+
+def dqt_rope_fwd(rope: Rope, pairs, pos=None, stream=None):
+    """pairs: up to 4 (X, Y) of one dtype (bf16 or fp32), each [tokens, heads, d] with any
+    token and head strides; Y may be X.  pos: int32 [tokens], or None for 0, 1, 2 ..."""
+    _rope("dqt_rope_fwd", rope, pairs, pos, stream)
+
+
+def dqt_rope_bwd(rope: Rope, pairs, pos=None, stream=None):
+    """pairs: (gradient of the rotated values, gradient of the values)."""
+    _rope("dqt_rope_bwd", rope, pairs, pos, stream)
+
+
+KV_PAGE = 64
+
+
+class KvCache:
+    """A layer's cache: codes K [pages, kv_heads, 64, d] and V [pages, kv_heads, d, 64]
+    (torch.float8_e4m3fn or torch.int8), scales [pages, kv_heads, 2] (fp32)."""
+
+    def __init__(self, K, V, scales):
+        torch = _torch()
+        if len(_same(K)) != 4 or K.shape[2] != KV_PAGE or K.dtype not in (torch.float8_e4m3fn, torch.int8):
+            raise ValueError(f"expected contiguous 8-bit codes [pages, kv_heads, {KV_PAGE}, d], got {K.dtype} {tuple(K.shape)}")
+        pages, kvh, _, d = K.shape
+        if V.shape != (pages, kvh, d, KV_PAGE) or V.dtype is not K.dtype or not V.is_contiguous():
+            raise ValueError(f"expected contiguous {K.dtype} values [pages, kv_heads, d, {KV_PAGE}], got {V.dtype} {tuple(V.shape)}")
+        if scales.shape != (pages, kvh, 2) or scales.dtype is not torch.float32 or not scales.is_contiguous():
+            raise ValueError(f"expected contiguous fp32 scales [pages, kv_heads, 2], got {scales.dtype} {tuple(scales.shape)}")
+        self.dev = _here(K, V, scales)
+        self.K, self.V, self.scales = K, V, scales
+        self.kv_heads, self.d = kvh, d
+        self.desc = DqtKvCache(K.data_ptr(), V.data_ptr(), scales.data_ptr(), pages, kvh, d, dtype_code(K), 0)
+        self.ref = ctypes.byref(self.desc)
+
+
+def kv_cache(pages: int, kv_heads: int, d: int, fmt: int = DQT_FP8E4M3, device="cuda:0") -> KvCache:
+    """An empty cache (its contents do not matter)."""
+    torch = _torch()
+    dt = {DQT_FP8E4M3: torch.float8_e4m3fn, DQT_I8: torch.int8}[fmt]
+    return KvCache(torch.empty((pages, kv_heads, KV_PAGE, d), dtype=dt, device=device),
+                   torch.empty((pages, kv_heads, d, KV_PAGE), dtype=dt, device=device),
+                   torch.empty((pages, kv_heads, 2), dtype=torch.float32, device=device))
+
+
+class KvBatch:
+    """The new tokens of a batch of sequences (see kv_batch)."""
+
+    def __init__(self, desc, keep, scale):
+        self.desc, self._keep, self.scale = desc, keep, scale
+        self.ref = ctypes.byref(desc)
+        self.dev = keep[0].get_device()
+        self.q_tokens, self.heads = desc.q_tokens, desc.heads
+
+
+def kv_batch(table, kv_len, q_tokens: int, heads: int, q_start=None, max_len: int | None = None,
+             scale: float | None = None, causal: bool = True) -> KvBatch:
+    """table: device int32 [n_seq, pages of the longest]; kv_len: int32 [n_seq], the new tokens included;
+    q_start: int32 [n_seq + 1], or None for one new token each; max_len: the longest that kv_len may
+    hold (64 times the table's width by default); scale: 1 / sqrt(d) by default.  All tensors are kept
+    alive on the descriptor; their values may change between calls."""
+    torch = _torch()
+    _here(table, kv_len)
+    if table.dim() != 2 or table.dtype is not torch.int32 or not table.is_contiguous():
+        raise ValueError("expected a contiguous int32 table [n_seq, pages]")
+    n, width = table.shape
+    _bufs(table.get_device(), (kv_len, 4 * n, torch.int32), (q_start, 4 * (n + 1), torch.int32))
+    if kv_len.numel() != n or (q_start is not None and q_start.numel() != n + 1):
+        raise ValueError(f"expected {n} lengths and {n + 1} starts")
+    desc = DqtKvBatch(table.data_ptr(), kv_len.data_ptr(), _addr(q_start), q_tokens,
+                      KV_PAGE * width if max_len is None else max_len, n, width, heads, int(causal),
+                      1.0 if scale is None else scale, 0)
+    return KvBatch(desc, (table, kv_len, q_start), scale)
+
+
+def _kv(cache: KvCache, batch: KvBatch, *tensors):
+    """Their device; the batch's scale is that of the cache's heads unless it was given."""
+    dev = _here(cache.K, *tensors)
+    if batch.dev != dev:
+        raise ValueError(f"batch on device {batch.dev}, cache on device {dev}")
+    if batch.scale is None:
+        batch.desc.scale = cache.d ** -0.5
+    return dev
+
+
+def dqt_kv_append(cache: KvCache, batch: KvBatch, K, V, rope: Rope | None = None, Q=None, Qr=None, stream=None):
+    """K, V: [q_tokens, kv_heads, d], Q and Qr (with rope): [q_tokens, heads, d], bf16 with any token
+    and head strides.  Qr may be Q."""
+    bf16 = _torch().bfloat16
+    if (Q is None) != (Qr is None):
+        raise ValueError("Q and Qr go together")
+    _kv(cache, batch, K, V, *(() if rope is None else (rope.freq,)), *(() if Q is None else (Q, Qr)))
+    kv, q = (batch.q_tokens, cache.kv_heads, cache.d), (batch.q_tokens, batch.heads, cache.d)
+    _check("dqt_kv_append",
+           load().dqt_kv_append(cache.ref, batch.ref, _row(K, kv, bf16), _row(V, kv, bf16),
+                                None if rope is None else rope.ref, None if Q is None else _row(Q, q, bf16),
+                                None if Q is None else _row(Qr, q, bf16), _stream(stream)))
+
+
+def dqt_kv_attn_workspace(cache: KvCache, batch: KvBatch) -> int:
+    _kv(cache, batch)
+    return int(load().dqt_kv_attn_workspace(cache.ref, batch.ref))
+
+
+def dqt_kv_attn(cache: KvCache, batch: KvBatch, Q, O, lse=None, ws=None, stream=None):
+    """Q, O: [q_tokens, heads, d], bf16 with any token and head strides; lse: contiguous fp32
+    [heads, q_tokens] or None."""
+    torch = _torch()
+    dev = _kv(cache, batch, Q, O)
+    shape = (batch.q_tokens, batch.heads, cache.d)
+    _bufs(dev, (lse, 4 * batch.heads * batch.q_tokens, torch.float32))
+    _check("dqt_kv_attn",
+           load().dqt_kv_attn(cache.ref, batch.ref, _row(Q, shape, torch.bfloat16), _row(O, shape, torch.bfloat16),
+                              _addr(lse), _addr(ws), _ws_bytes(dev, ws), _stream(stream)))
+
+
+def _pages(x) -> np.ndarray:
+    return np.ascontiguousarray(x, dtype=np.int32)
+
+
+def dqt_kv_copy(caches, src, dst, stream=None):
+    """caches: a list of KvCache of one shape (a model's layers); src, dst: page numbers (host)."""
+    src, dst = _pages(src), _pages(dst)
+    if src.shape != dst.shape or src.ndim != 1:
+        raise ValueError("expected as many sources as destinations")
+    if caches:
+        _here(*(c.K for c in caches))
+    arr = (DqtKvCache * len(caches))(*[c.desc for c in caches])
+    _check("dqt_kv_copy", load().dqt_kv_copy(len(caches), arr, src.size, src.ctypes.data, dst.ctypes.data, _stream(stream)))
+
+
+class KvPool:
+    """Which sequence holds which page (host): table int32 [n_seq, row_pages] with -1 for none, the
+    sequences' lengths, and the pages' holders.  extend, fork, trim and compact call the entry
+    points of the same names; extend and compact return the copies (src, dst) that have to be made
+    (dqt_kv_copy) before the cache is used."""
+
+    def __init__(self, pages: int, n_seq: int, row_pages: int):
+        self.refs, self.free_pages = np.zeros(pages, np.int32), np.zeros(pages, np.int32)
+        self.table = np.full((n_seq, row_pages), -1, np.int32)
+        self.len = np.zeros(n_seq, np.int64)
+        self.desc = DqtKvPool()
+        _check("dqt_kv_pool_init", load().dqt_kv_pool_init(ctypes.byref(self.desc), pages, self.refs.ctypes.data,
+                                                           self.free_pages.ctypes.data))
+
+    @property
+    def n_free(self) -> int:
+        return self.desc.n_free
+
+    def _at(self, s: int):
+        if not 0 <= s < len(self.len):
+            raise ValueError(f"sequence {s} of {len(self.len)}")
+        return self.table[s].ctypes.data, self.table.shape[1], int(self.len[s])
+
+    def extend(self, s: int, new_len: int):
+        src, dst = ctypes.c_int32(-1), ctypes.c_int32(-1)
+        _check("dqt_kv_pool_extend", load().dqt_kv_pool_extend(ctypes.byref(self.desc), *self._at(s), new_len,
+                                                               ctypes.byref(src), ctypes.byref(dst)))
+        self.len[s] = new_len
+        return ([src.value], [dst.value]) if src.value >= 0 else ([], [])
+
+    def fork(self, s: int, to: int):
+        """Sequence `to`, which holds nothing, holds s's pages too."""
+        if self._at(to)[2] != 0:
+            raise ValueError(f"sequence {to} holds {self.len[to]} tokens")
+        _check("dqt_kv_pool_fork", load().dqt_kv_pool_fork(ctypes.byref(self.desc), *self._at(s), self._at(to)[0]))
+        self.len[to] = self.len[s]
+
+    def trim(self, s: int, new_len: int = 0):
+        _check("dqt_kv_pool_trim", load().dqt_kv_pool_trim(ctypes.byref(self.desc), *self._at(s), new_len))
+        self.len[s] = new_len
+
+    def compact(self):
+        src, dst, n = np.empty_like(self.refs), np.empty_like(self.refs), ctypes.c_int32(0)
+        _check("dqt_kv_pool_compact",
+               load().dqt_kv_pool_compact(ctypes.byref(self.desc), self.table.ctypes.data, *self.table.shape,
+                                          src.ctypes.data, dst.ctypes.data, ctypes.byref(n)))
+        return src[:n.value].copy(), dst[:n.value].copy()
 
 
 def dqt_linear_fwd_workspace(w: DqtWeight) -> int:
