@@ -396,7 +396,7 @@ dqt_status dqt_rope_freqs(int32_t rot, double base, double factor, double contex
 /* Rotates n (1 .. DQT_MAX_ROPE) tensors of x_t = DQT_F32 or DQT_BF16, as a rule
  * queries and keys, in one launch.
  *   pos: device int32 [tokens], the position of each, or NULL: 0, 1, 2 ...
- *   tokens < 2^31, tokens times d below 2^36.
+ *   tokens < 2^26.
  * dqt_rope_bwd turns back (the transposed rotation): X holds the gradient of the
  * rotated values, Y receives that of the values. */
 #define DQT_MAX_ROPE 4

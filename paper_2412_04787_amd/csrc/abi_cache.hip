@@ -27,7 +27,7 @@ dqt_status rope(const dqt_rope* r, int32_t n, const dqt_rope_io* io, int32_t x_t
   if (n < 1 || n > DQT_MAX_ROPE) return DQT_ERR_SHAPE;
   if (io == nullptr) return DQT_ERR_NULL;
   if (!is_float_type(x_t)) return DQT_ERR_DTYPE;
-  if (tokens < 0 || tokens > kMaxTokens || tokens * r->d >= (int64_t(1) << 36)) return DQT_ERR_SHAPE;
+  if (tokens < 0 || tokens > kMaxTokens || tokens >= 4 * kMaxBlocks) return DQT_ERR_SHAPE;
   if (!aligned4(pos)) return DQT_ERR_ALIGN;
   dqt::RopeArgs a{};
   const int64_t size = x_t == DQT_BF16 ? 2 : 4;

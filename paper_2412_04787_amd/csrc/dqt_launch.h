@@ -341,7 +341,8 @@ struct RopeArgs {
   double amp;
   int n, d, rot, pairs, back;
   int all_heads;               // of all tensors
-  int items;                   // of a token: runs of 16 values
+  int items;                   // of a head: runs of 16 values
+  int block_tokens;            // tokens of a block
 };
 hipError_t launch_rope(bool bf16, const RopeArgs& a, hipStream_t stream);
 

@@ -8,12 +8,12 @@
 // divisions are by powers of two, so a code is rounded once from the fp32 value.
 //
 // A block takes the new tokens of one page and key head, and the queries of the heads
-// that share it: waves 0 and 1 the keys, 2 and 3 the values, 16 values per thread
-// and step, held in registers between the page's maximum and its codes.  Rotations
-// come from a table of the page's cosines and sines in LDS, which keys and queries
-// share.  Values go through LDS to lie as the cache has them (a channel's tokens
-// together).  Bound by HBM for prompts, by the chain of dependent loads (length,
-// page, scale) for single tokens.
+// that share it: waves 0 and 1 the keys, 16 values of a token per thread and step, waves
+// 2 and 3 the values, 8 channels of 4 tokens, held in registers between the page's
+// maximum and its codes.  Rotations come from a table of the page's cosines and sines
+// in LDS, which keys and queries share.  Values go through LDS to lie as the cache has
+// them (a channel's tokens together).  Bound by HBM for prompts, by the chain of
+// dependent loads (length, page, scale) for single tokens.
 #include "kv_common.h"
 #include "rope.h"
 
@@ -21,14 +21,15 @@ namespace dqt {
 
 namespace {
 
-__device__ __forceinline__ void load16(const uint8_t* p, float (&v)[8]) {
-  const i32x4 x = *reinterpret_cast<const i32x4*>(p);
+// 8 bf16 values as fp32
+__device__ __forceinline__ void widen8(i32x4 x, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    v[2 * i] = bf16_bits_to_f32((uint32_t)x[i] & 0xFFFFu);
+    v[2 * i] = __uint_as_float((uint32_t)x[i] << 16);
     v[2 * i + 1] = __uint_as_float((uint32_t)x[i] & 0xFFFF0000u);
   }
 }
+__device__ __forceinline__ void load16(const uint8_t* p, float (&v)[8]) { widen8(*reinterpret_cast<const i32x4*>(p), v); }
 
 // values on their scale (not NaN) -> four codes
 template <bool E4M3>
@@ -53,42 +54,31 @@ __device__ __forceinline__ float finite_abs(float x) {
 
 // A token's run of 16 values: rotated pairs 8 item .. + 7, or 16 values as they are.
 struct Run {
-  int i0, i1, cs;        // first of its two runs of 8 values, second; its cosines (-1: none)
+  int i0, i1;            // first of its two runs of 8 values, second
+  bool turns;
   __device__ __forceinline__ Run(const KvAppendArgs& a, int item) {
-    const bool turns = a.freq != nullptr && item < a.rot / 16;
-    cs = turns ? 8 * item : -1;
+    turns = a.freq != nullptr && 16 * item < a.rot;
     i0 = turns && !a.pairs ? 8 * item : 16 * item;
     i1 = turns && !a.pairs ? a.rot / 2 + 8 * item : i0 + 8;
   }
-  // cs_row: the token's cosines and sines
-  __device__ __forceinline__ void rotate(const KvAppendArgs& a, const float2* cs_row, float (&u)[8], float (&v)[8]) const {
-    if (cs < 0) return;
-    if (a.pairs) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 f = cs_row[cs + i], g = cs_row[cs + 4 + i];
-        const float p = u[2 * i], q = u[2 * i + 1], r = v[2 * i], w = v[2 * i + 1];
-        u[2 * i] = p * f.x - q * f.y;
-        u[2 * i + 1] = p * f.y + q * f.x;
-        v[2 * i] = r * g.x - w * g.y;
-        v[2 * i + 1] = r * g.y + w * g.x;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float2 f = cs_row[cs + i];
-        const float p = u[i], q = v[i];
-        u[i] = p * f.x - q * f.y;
-        v[i] = p * f.y + q * f.x;
-      }
-    }
-  }
 };
+
+// 4 tokens' codes of 4 channels (byte = channel) -> 4 channels' codes of 4 tokens
+__device__ __forceinline__ void transpose4(const uint32_t (&a)[4], uint32_t (&b)[4]) {
+  const uint32_t t0 = __builtin_amdgcn_perm(a[1], a[0], 0x05010400u), t1 = __builtin_amdgcn_perm(a[1], a[0], 0x07030602u);
+  const uint32_t t2 = __builtin_amdgcn_perm(a[3], a[2], 0x05010400u), t3 = __builtin_amdgcn_perm(a[3], a[2], 0x07030602u);
+  b[0] = __builtin_amdgcn_perm(t2, t0, 0x05040100u);
+  b[1] = __builtin_amdgcn_perm(t2, t0, 0x07060302u);
+  b[2] = __builtin_amdgcn_perm(t3, t1, 0x05040100u);
+  b[3] = __builtin_amdgcn_perm(t3, t1, 0x07060302u);
+}
 
 template <int D, bool E4M3>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
-  constexpr int ITEMS = D / 16, STEPS = kPage * ITEMS / 128, VROW = kPage + 4;
-  __shared__ float2 cs[kPage][D / 2];
+  constexpr int ITEMS = D / 16, STEPS = kPage * ITEMS / 128, UNITS = STEPS / 2, QSTEPS = 4;
+  constexpr int CROW = D / 2 + 16;                   // (two tokens' rows fall on different halves of the banks)
+  constexpr int VROW = kPage + 4;
+  __shared__ __attribute__((aligned(16))) float2 cs[kPage * CROW];
   __shared__ uint32_t vt[D * VROW / 4];              // the values' codes, [channel][token]
   __shared__ float red[4];
   __shared__ int stood[2];
@@ -104,52 +94,78 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
   const int64_t row0 = (int64_t)sq.q0 + (base + lo - pos0);        // the first of these tokens in the batch
   const int64_t page = a.c.table[(int64_t)sq.s * a.c.table_stride + page_at];
   const bool there = page >= 0 && page < a.c.pages;
+  float* sc = a.c.scales + 2 * (page * a.c.kv_heads + kvh);
 
-  // 16 values per item: waves 0, 1 of the keys, waves 2, 3 of the values
   const bool keys = tid < 128;
   const int first = tid & 127;
-  const uint8_t* src = keys ? a.k + row0 * a.k_tok + (int64_t)kvh * a.k_head : a.v + row0 * a.v_tok + (int64_t)kvh * a.v_head;
-  const int64_t tok = keys ? a.k_tok : a.v_tok;
-  float x[STEPS][2][8];
+  float x[2 * STEPS][8];
+  if (keys) {
+    const uint8_t* src = a.k + row0 * a.k_tok + (int64_t)kvh * a.k_head;
 #pragma unroll
-  for (int st = 0; st < STEPS; ++st) {
-    const int i = first + 128 * st, t = i / ITEMS, item = i % ITEMS;
-    if (there && t < n) {
-      int i0 = 16 * item, i1 = i0 + 8;
-      if (keys) {
-        const Run r(a, item);
-        i0 = r.i0;
-        i1 = r.i1;
+    for (int st = 0; st < STEPS; ++st) {
+      const int i = first + 128 * st, t = i / ITEMS;
+      const Run r(a, i % ITEMS);
+      if (t < n) {
+        load16(src + t * a.k_tok + 2 * r.i0, x[2 * st]);
+        load16(src + t * a.k_tok + 2 * r.i1, x[2 * st + 1]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[2 * st][e] = x[2 * st + 1][e] = 0.0f;
       }
-      load16(src + t * tok + 2 * i0, x[st][0]);
-      load16(src + t * tok + 2 * i1, x[st][1]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[st][0][e] = x[st][1][e] = 0.0f;
     }
+  } else {
+    const uint8_t* src = a.v + row0 * a.v_tok + (int64_t)kvh * a.v_head;
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int i = first + 128 * u, t = 4 * (i / (D / 8)) + b;         // (of the page)
+        if (t >= lo && t < hi) {
+          load16(src + (t - lo) * a.v_tok + 16 * (i % (D / 8)), x[4 * u + b]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[4 * u + b][e] = 0.0f;
+        }
+      }
   }
-  float* sc = a.c.scales + 2 * (page * a.c.kv_heads + kvh);
   // (read by the thread that will write it, before the others know the new one)
   if (there && first == 0) stood[keys ? 0 : 1] = lo > 0 ? exp_of(sc[keys ? 0 : 1]) : kMinExp;
   if (a.freq != nullptr) {
-    const int half = a.rot / 2;
-    for (int i = tid; i < n * half; i += 256) {
-      const int t = i / half, f = i - t * half;
-      float2 w;
-      turn((uint64_t)(base + lo + t) * a.freq[f], a.amp, w.x, w.y);
-      cs[t][f] = w;
+    // a thread takes one pair through a run of tokens: the first one's turn, then
+    // products with that of one position (each adds 2^-52 to what is rounded to fp32)
+    const int half = a.rot / 2, runs = 256 / half, p = tid % half, len = (n + runs - 1) / runs, t0 = tid / half * len;
+    if (tid < runs * half && t0 < n) {
+      const uint64_t f = a.freq[p];
+      double c, s, c1 = 1.0, s1 = 0.0;
+      turn((uint64_t)(base + lo + t0) * f, c, s);
+      if (len > 1) turn(f, c1, s1);
+      const int place = turn_place(p, half), end = min(t0 + len, n);
+      for (int t = t0; t < end; ++t) {
+        cs[t * CROW + place] = float2{(float)(a.amp * c), (float)(a.amp * s)};
+        const double d = __builtin_fma(c, c1, -(s * s1));
+        s = __builtin_fma(s, c1, c * s1);
+        c = d;
+      }
     }
     __syncthreads();
   }
   if (there) {
+    if (keys && a.freq != nullptr) {
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
+        const int i = first + 128 * st, t = i / ITEMS, item = i % ITEMS;
+        if (t < n && 16 * item < a.rot) {
+          Turns w;
+          w.read(cs + t * CROW, item, a.rot / 2);
+          w.apply(a.pairs, x[2 * st], x[2 * st + 1]);
+        }
+      }
+    }
     float most = 0.0f;
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) {
-      const int i = first + 128 * st, t = i / ITEMS, item = i % ITEMS;
-      if (keys && t < n) Run(a, item).rotate(a, cs[t], x[st][0], x[st][1]);
+    for (int st = 0; st < 2 * STEPS; ++st)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) most = fmaxf(most, fmaxf(finite_abs(x[st][0][e]), finite_abs(x[st][1][e])));
-    }
+      for (int e = 0; e < 8; ++e) most = fmaxf(most, finite_abs(x[st][e]));
     most = wave_max(most);
     if ((tid & 63) == 0) red[tid >> 6] = most;
     __syncthreads();
@@ -159,30 +175,36 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
     const float inv = exp2_int(-e), f = exp2_int(max(was - e, -126));
     if (first == 0) sc[keys ? 0 : 1] = exp2_int(e);
     uint8_t* dst = (keys ? a.c.K : a.c.V) + (page * a.c.kv_heads + kvh) * (int64_t)(kPage * D);
+    auto codes = [&](const float (&y)[8], int from) {
+      float z[4];
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) {
-      const int i = first + 128 * st, t = i / ITEMS, item = i % ITEMS;
-      if (t >= n) continue;
-      uint32_t w[4];
+      for (int b = 0; b < 4; ++b) z[b] = y[from + b] == y[from + b] ? y[from + b] * inv : 0.0f;
+      return codes4<E4M3>(z[0], z[1], z[2], z[3]);
+    };
+    if (keys) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float y[4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const float z = x[st][j / 2][4 * (j & 1) + b];
-          y[b] = z == z ? z * inv : 0.0f;
-        }
-        w[j] = codes4<E4M3>(y[0], y[1], y[2], y[3]);
-      }
-      if (keys) {
-        const Run r(a, item);
+      for (int st = 0; st < STEPS; ++st) {
+        const int i = first + 128 * st, t = i / ITEMS;
+        if (t >= n) continue;
+        const Run r(a, i % ITEMS);
         uint8_t* p = dst + (lo + t) * D;
-        *reinterpret_cast<uint2*>(p + r.i0) = uint2{w[0], w[1]};
-        *reinterpret_cast<uint2*>(p + r.i1) = uint2{w[2], w[3]};
-      } else {
-        uint8_t* p = reinterpret_cast<uint8_t*>(vt) + (16 * item) * VROW + lo + t;
+        *reinterpret_cast<uint2*>(p + r.i0) = uint2{codes(x[2 * st], 0), codes(x[2 * st], 4)};
+        *reinterpret_cast<uint2*>(p + r.i1) = uint2{codes(x[2 * st + 1], 0), codes(x[2 * st + 1], 4)};
+      }
+    } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) p[j * VROW] = (uint8_t)(w[j / 4] >> (8 * (j & 3)));
+      for (int u = 0; u < UNITS; ++u) {
+        const int i = first + 128 * u, grp = i / (D / 8);
+        if (4 * grp + 3 < lo || 4 * grp >= hi) continue;
+        uint32_t* p = vt + 8 * (i % (D / 8)) * (VROW / 4) + grp;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t w[4] = {codes(x[4 * u], 4 * h), codes(x[4 * u + 1], 4 * h), codes(x[4 * u + 2], 4 * h), codes(x[4 * u + 3], 4 * h)};
+          uint32_t y[4];
+          transpose4(w, y);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) p[(4 * h + j) * (VROW / 4)] = y[j];
+        }
       }
     }
     __syncthreads();
@@ -229,21 +251,43 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
   }
   // the queries of the heads that share this key head
   if (a.q != nullptr) {
-    const int G = a.c.group;
-    for (int i = tid; i < n * G * ITEMS; i += 256) {
-      const int item = i % ITEMS, tg = i / ITEMS, t = tg / G, g = tg - t * G;
-      const Run r(a, item);
-      const int64_t head = (int64_t)kvh * G + g;
-      float u[8], v[8];
-      const uint8_t* p = a.q + (row0 + t) * a.q_tok + head * a.q_head;
-      load16(p + 2 * r.i0, u);
-      load16(p + 2 * r.i1, v);
-      r.rotate(a, cs[t], u, v);
-      uint8_t* o = a.qr + (row0 + t) * a.qr_tok + head * a.qr_head;
-      *reinterpret_cast<i32x4*>(o + 2 * r.i0) = i32x4{(int)pack_bf16x2(u[0], u[1]), (int)pack_bf16x2(u[2], u[3]),
-                                                     (int)pack_bf16x2(u[4], u[5]), (int)pack_bf16x2(u[6], u[7])};
-      *reinterpret_cast<i32x4*>(o + 2 * r.i1) = i32x4{(int)pack_bf16x2(v[0], v[1]), (int)pack_bf16x2(v[2], v[3]),
-                                                     (int)pack_bf16x2(v[4], v[5]), (int)pack_bf16x2(v[6], v[7])};
+    const uint32_t G = (uint32_t)a.c.group, all = n * G * ITEMS;
+    const uint8_t* q = a.q + row0 * a.q_tok + (int64_t)kvh * G * a.q_head;
+    uint8_t* qr = a.qr + row0 * a.qr_tok + (int64_t)kvh * G * a.qr_head;
+    for (uint32_t i0 = tid; i0 < all; i0 += 256 * QSTEPS) {
+      i32x4 ru[QSTEPS], rv[QSTEPS];
+      int t[QSTEPS], g[QSTEPS];
+#pragma unroll
+      for (int e = 0; e < QSTEPS; ++e) {
+        const uint32_t i = i0 + 256 * e, tg = i / ITEMS;
+        t[e] = (int)(tg / G);
+        g[e] = (int)(tg - t[e] * G);
+        if (i >= all) continue;
+        const Run r(a, i % ITEMS);
+        const uint8_t* p = q + t[e] * a.q_tok + g[e] * a.q_head;
+        ru[e] = *reinterpret_cast<const i32x4*>(p + 2 * r.i0);
+        rv[e] = *reinterpret_cast<const i32x4*>(p + 2 * r.i1);
+      }
+#pragma unroll
+      for (int e = 0; e < QSTEPS; ++e) {
+        const uint32_t i = i0 + 256 * e;
+        if (i >= all) continue;
+        const int item = i % ITEMS;
+        const Run r(a, item);
+        float u[8], v[8];
+        widen8(ru[e], u);
+        widen8(rv[e], v);
+        if (r.turns) {
+          Turns w;
+          w.read(cs + t[e] * CROW, item, a.rot / 2);
+          w.apply(a.pairs, u, v);
+        }
+        uint8_t* o = qr + t[e] * a.qr_tok + g[e] * a.qr_head;
+        *reinterpret_cast<i32x4*>(o + 2 * r.i0) = i32x4{(int)pack_bf16x2(u[0], u[1]), (int)pack_bf16x2(u[2], u[3]),
+                                                       (int)pack_bf16x2(u[4], u[5]), (int)pack_bf16x2(u[6], u[7])};
+        *reinterpret_cast<i32x4*>(o + 2 * r.i1) = i32x4{(int)pack_bf16x2(v[0], v[1]), (int)pack_bf16x2(v[2], v[3]),
+                                                       (int)pack_bf16x2(v[4], v[5]), (int)pack_bf16x2(v[6], v[7])};
+      }
     }
   }
 }

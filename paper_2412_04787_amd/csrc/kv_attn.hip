@@ -129,7 +129,7 @@ __global__ __launch_bounds__(256, 2) void kv_attn_kernel(KvAttnArgs a) {
   if (item < 0 || t.r0 >= t.rows) return;
   const int first = split * a.chunk, end = min(first + a.chunk, t.nblk);
   if (split > 0 && first >= t.nblk) return;
-  if (a.splits > 1 && t.nblk == 0) return;          // (the join writes the empty rows)
+  const bool whole = t.nblk <= a.chunk;             // no other block works on these rows
 
   // the rows
   i32x4 qraw[NT][2 * KJ];
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(256, 2) void kv_attn_kernel(KvAttnArgs a) {
     const float lse = all == -__builtin_inff() ? all : all - kLift + log2f(sum);
     const int tk = row_token(a, t.r0 + r), hd = kvh * a.c.group + (t.r0 + r - tk * a.c.group);
     const int64_t row = t.q.q0 + tk;
-    if (a.splits == 1) {
+    if (whole) {
       *reinterpret_cast<uint2*>(a.O + row * a.o_tok + hd * a.o_head + 2 * d) = uint2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
       if (d == 0 && a.lse != nullptr) a.lse[(int64_t)hd * a.c.tq + row] = lse * kLn2;
     } else {
@@ -359,11 +359,16 @@ __global__ __launch_bounds__(256, 2) void kv_attn_kernel(KvAttnArgs a) {
   }
 }
 
-// Joins the splits of one row (a wave each): o = sum_p 2^(L_p - L) o_p / sum_p 2^(L_p - L).
-template <int D>
+// Joins the parts of the rows that have several: o = sum_p 2^(L_p - L) o_p / sum_p
+// 2^(L_p - L).  WIDE: a block for a row, else a wave.  A wave reads GR parts at a time,
+// 16 bytes per lane.  (A wave for each of 128 rows of 64 parts took 20 us.)
+template <int D, bool WIDE>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int GR = 256 / D, STEP = WIDE ? 4 * GR : GR;
+  __shared__ f32x4 part[4][D / 4];
+  __shared__ float part_sum[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t at = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   if (at >= (int64_t)a.c.tq * a.c.heads) return;
   const int row = (int)(at / a.c.heads), hd = (int)(at - (int64_t)row * a.c.heads);
   int tok = 0;
@@ -371,28 +376,44 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
   if (tok < 0 || tok >= q.lq) return;                // a token outside every sequence
   const int r = tok * a.c.group + hd % a.c.group;
   const Tile t = tile_at(a, q, r / a.tile_rows);
+  if (t.nblk <= a.chunk) return;                     // (written already)
   const int parts = (t.nblk + a.chunk - 1) / a.chunk;
   const int64_t step = (int64_t)a.c.tq * a.c.heads;
   float all = -__builtin_inff();
   for (int p = lane; p < parts; p += kWave) all = fmaxf(all, a.part_lse[p * step + at]);
   all = wave_max(all);
-  float y[D / 64], sum = 0.0f;
-#pragma unroll
-  for (int e = 0; e < D / 64; ++e) y[e] = 0.0f;
-  if (all > -__builtin_inff()) {
-    for (int p = 0; p < parts; ++p) {
-      const float w = exp2_fast(a.part_lse[p * step + at] - all);
-      const float* x = a.part + (p * step + at) * D + lane * (D / 64);
-#pragma unroll
-      for (int e = 0; e < D / 64; ++e) y[e] += w * x[e];
-      sum += w;
-    }
-#pragma unroll
-    for (int e = 0; e < D / 64; ++e) y[e] /= sum;
+  const float base = all == -__builtin_inff() ? 0.0f : all;
+  const int d = 4 * (lane % (D / 4));
+  f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+  float sum = 0.0f;
+#pragma unroll 4
+  for (int p = (WIDE ? GR * wave : 0) + lane / (D / 4); p < parts; p += STEP) {
+    const float w = exp2_fast(a.part_lse[p * step + at] - base);
+    y += w * *reinterpret_cast<const f32x4*>(a.part + (p * step + at) * D + d);
+    sum += w;
   }
-  uint8_t* o = a.O + row * a.o_tok + hd * a.o_head + lane * (D / 32);
-  if constexpr (D == 128) *reinterpret_cast<uint32_t*>(o) = pack_bf16x2(y[0], y[1]);
-  else *reinterpret_cast<uint16_t*>(o) = (uint16_t)(pack_bf16x2(y[0], y[0]) & 0xFFFFu);
+#pragma unroll
+  for (int x = D / 4; x < kWave; x *= 2) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], x, kWave);
+    sum += __shfl_xor(sum, x, kWave);
+  }
+  if constexpr (WIDE) {
+    if (lane < D / 4) part[wave][lane] = y;
+    if (lane == 0) part_sum[wave] = sum;
+    __syncthreads();
+    if (wave != 0) return;
+    y = part[0][lane % (D / 4)];
+    sum = part_sum[0];
+#pragma unroll
+    for (int v = 1; v < 4; ++v) {
+      y += part[v][lane % (D / 4)];
+      sum += part_sum[v];
+    }
+  }
+  if (lane >= D / 4) return;
+  const float f = all == -__builtin_inff() ? 0.0f : 1.0f / sum;
+  *reinterpret_cast<uint2*>(a.O + row * a.o_tok + hd * a.o_head + 2 * d) = uint2{pack_bf16x2(y[0] * f, y[1] * f), pack_bf16x2(y[2] * f, y[3] * f)};
   if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)hd * a.c.tq + row] = all == -__builtin_inff() ? all : (all + log2f(sum)) * kLn2;
 }
 
@@ -422,9 +443,12 @@ hipError_t launch_kv_attn(bool e4m3, const KvAttnArgs& a, hipStream_t s) {
     else e4m3 ? go(kv_attn_kernel<64, true, 2>) : go(kv_attn_kernel<64, false, 2>);
   }
   if (a.splits > 1) {
-    const dim3 join((uint32_t)(((int64_t)a.c.tq * a.c.heads + 3) / 4));
+    const int64_t rows = (int64_t)a.c.tq * a.c.heads;
+    const bool wide = a.splits > 4 && rows <= 4096;
+    const dim3 join((uint32_t)(wide ? rows : (rows + 3) / 4));
     auto j = [&](auto k) { st << launch_kernel(k, join, dim3(256), s, a); };
-    a.c.d == 128 ? j(kv_join_kernel<128>) : j(kv_join_kernel<64>);
+    if (a.c.d == 128) wide ? j(kv_join_kernel<128, true>) : j(kv_join_kernel<128, false>);
+    else wide ? j(kv_join_kernel<64, true>) : j(kv_join_kernel<64, false>);
   }
   return st.e;
 }

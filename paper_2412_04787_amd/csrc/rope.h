@@ -5,11 +5,11 @@
 
 namespace dqt {
 
-// cos and sin (times amp) of 2 pi t 2^-64.  t is cut into the nearest quarter turn
-// and a rest of an eighth at most, whose sine and cosine are Taylor sums: the terms
-// left out are below 2^-45, so the rounding to fp32 is the one of the exact value in
-// all but one case in 2^20.  In double, which runs at the rate of fp32 here.
-__device__ __forceinline__ void turn(uint64_t t, double amp, float& c, float& s) {
+// cos and sin of 2 pi t 2^-64 in double.  t is cut into the nearest quarter turn and a
+// rest of an eighth at most, whose sine and cosine are Taylor sums: the terms left out
+// are below 2^-45, so the rounding to fp32 is the one of the exact value in all but one
+// case in 2^20.  (Double runs at the rate of fp32 here.)
+__device__ __forceinline__ void turn(uint64_t t, double& c, double& s) {
   const uint32_t quarter = (uint32_t)((t + (1ull << 61)) >> 62);
   const int64_t r = (int64_t)(t - ((uint64_t)quarter << 62));
   const double hi = (double)(int32_t)(r >> 32), lo = (double)(uint32_t)r;
@@ -31,8 +31,48 @@ __device__ __forceinline__ void turn(uint64_t t, double amp, float& c, float& s)
   q = __builtin_fma(q, y, -0.5);
   q = __builtin_fma(q, y, 1.0);
   const double a = (quarter & 1) ? p : q, b = (quarter & 1) ? q : p;
-  c = (float)(((quarter + 1) & 2) ? -amp * a : amp * a);
-  s = (float)((quarter & 2) ? -amp * b : amp * b);
+  c = ((quarter + 1) & 2) ? -a : a;
+  s = (quarter & 2) ? -b : b;
 }
+
+// Cosines and sines of a token's rot / 2 = half pairs, times amp and in fp32, lie in a
+// row of LDS.  Pairs 8 j, 8 j + 1 of all j lie side by side, then 8 j + 2, 8 j + 3 and so
+// on: lanes of consecutive j read consecutive 16-byte words.
+__device__ __forceinline__ int turn_place(int p, int half) { return ((p & 7) >> 1) * (half / 4) + 2 * (p >> 3) + (p & 1); }
+
+// those of pairs 8 j .. 8 j + 7
+struct Turns {
+  float c[8], s[8];
+  __device__ __forceinline__ void read(const float2* row, int j, int half) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(row + i * (half / 4) + 2 * j);
+      c[2 * i] = v[0];
+      s[2 * i] = v[1];
+      c[2 * i + 1] = v[2];
+      s[2 * i + 1] = v[3];
+    }
+  }
+  // u, v: the two runs of 8 values; pairs are neighbours, or (u[i], v[i])
+  __device__ __forceinline__ void apply(bool neighbours, float (&u)[8], float (&v)[8]) const {
+    if (neighbours) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = u[2 * i], q = u[2 * i + 1], r = v[2 * i], w = v[2 * i + 1];
+        u[2 * i] = p * c[i] - q * s[i];
+        u[2 * i + 1] = p * s[i] + q * c[i];
+        v[2 * i] = r * c[4 + i] - w * s[4 + i];
+        v[2 * i + 1] = r * s[4 + i] + w * c[4 + i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float p = u[i], q = v[i];
+        u[i] = p * c[i] - q * s[i];
+        v[i] = p * s[i] + q * c[i];
+      }
+    }
+  }
+};
 
 }  // namespace dqt

@@ -2,10 +2,10 @@
 // are in the header): pair (a, b) of a head at position p turns by t = p f,
 //   a' = a cos t - b sin t,  b' = a sin t + b cos t,  backward by -t.
 //
-// Bound by HBM: every value is read and written once.  A thread takes 8 pairs of a
-// token (16 values, or 16 of those that are copied) through several heads, so that
-// the angles' sines and cosines (8 sums in double, about 300 instructions) are formed
-// once for them; a token's threads lie side by side and read whole lines.
+// Bound by HBM: every value is read and written once.  A block takes a few tokens and
+// a range of the heads of all tensors: it forms the tokens' cosines and sines in LDS
+// (once for all heads), then walks the values in the order of memory, 16 of a head per
+// thread and step (8 pairs, or 16 values that are copied), four steps in flight.
 #include "dqt_launch.h"
 #include "rope.h"
 
@@ -13,25 +13,22 @@ namespace dqt {
 
 namespace {
 
-// 8 consecutive values of X as fp32, and back
+// 8 consecutive values as they lie in memory, as fp32, and back
 template <class T>
-__device__ __forceinline__ void load8(const uint8_t* p, float (&v)[8]) {
-  if constexpr (sizeof(T) == 2) {
-    const i32x4 x = *reinterpret_cast<const i32x4*>(p);
+struct Raw8 {
+  i32x4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const uint8_t* p) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = bf16_bits_to_f32((uint32_t)x[i] & 0xFFFFu);
-      v[2 * i + 1] = __uint_as_float((uint32_t)x[i] & 0xFFFF0000u);
-    }
-  } else {
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const i32x4*>(p)[i];
+  }
+  __device__ __forceinline__ void widen(float (&v)[8]) const {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const f32x4 x = reinterpret_cast<const f32x4*>(p)[i];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[4 * i + e] = x[e];
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(T) == 4) v[i] = __uint_as_float((uint32_t)w[i / 4][i & 3]);
+      else v[i] = __uint_as_float(i & 1 ? (uint32_t)w[0][i / 2] & 0xFFFF0000u : (uint32_t)w[0][i / 2] << 16);
     }
   }
-}
+};
 template <class T>
 __device__ __forceinline__ void store8(uint8_t* p, const float (&v)[8]) {
   if constexpr (sizeof(T) == 2) {
@@ -43,58 +40,69 @@ __device__ __forceinline__ void store8(uint8_t* p, const float (&v)[8]) {
   }
 }
 
+constexpr int kRopeTokens = 8;       // of a block at most
+constexpr int kRopeSteps = 4;
+
 template <class T, bool PAIRS>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t tok = at / a.items;
-  if (tok >= a.tokens) return;
-  const int item = (int)(at - tok * a.items), turned = a.rot / 16;
-  // first of the item's two runs of 8 values, and the second
-  const bool turns = item < turned;
-  const int i0 = PAIRS || !turns ? 16 * item : 8 * item, i1 = PAIRS || !turns ? i0 + 8 : a.rot / 2 + 8 * item;
-  float c[8], s[8];
-  if (turns) {
-    const int64_t p = a.pos == nullptr ? tok : a.pos[tok];
-    const uint64_t dir = a.back ? 0 - (uint64_t)p : (uint64_t)p;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) turn(dir * a.freq[8 * item + i], a.amp, c[i], s[i]);
+  extern __shared__ __attribute__((aligned(16))) float2 cs[];        // [block_tokens][rot / 2]
+  const int tid = threadIdx.x, half = a.rot / 2;
+  const int64_t t0 = (int64_t)blockIdx.x * a.block_tokens;
+  const int nt = (int)min((int64_t)a.block_tokens, a.tokens - t0);
+  for (int i = tid; i < nt * half; i += 256) {
+    const int t = i / half, p = i - t * half;
+    const int64_t pos = a.pos == nullptr ? t0 + t : a.pos[t0 + t];
+    double c, s;
+    turn((a.back ? 0 - (uint64_t)pos : (uint64_t)pos) * a.freq[p], c, s);
+    cs[t * half + turn_place(p, half)] = float2{(float)(a.amp * c), (float)(a.amp * s)};
   }
+  __syncthreads();
   const int first = (int)((int64_t)a.all_heads * blockIdx.y / gridDim.y);
   const int last = (int)((int64_t)a.all_heads * (blockIdx.y + 1) / gridDim.y);
   int h0 = 0;                                       // the tensor's first head among all
-  for (int t = 0; t < a.n; ++t) {
-    const RopeIO& io = a.io[t];
-    const int from = max(first, h0) - h0, to = min(last, h0 + io.heads) - h0;
+  for (int k = 0; k < a.n; ++k) {
+    const RopeIO& io = a.io[k];
+    const int from = max(first, h0) - h0, heads = min(last, h0 + io.heads) - h0 - from;
     h0 += io.heads;
-    if (!turns && io.X == io.Y) continue;           // (in place: what is copied is there)
-    const uint8_t* x = io.X + tok * io.x_tok + (int64_t)from * io.x_head;
-    uint8_t* y = io.Y + tok * io.y_tok + (int64_t)from * io.y_head;
-#pragma unroll 2
-    for (int h = from; h < to; ++h, x += io.x_head, y += io.y_head) {
-      float u[8], v[8];
-      load8<T>(x + i0 * sizeof(T), u);
-      load8<T>(x + i1 * sizeof(T), v);
-      if (turns) {
-        if constexpr (PAIRS) {
+    if (heads <= 0) continue;
+    const bool copies = io.X != io.Y;               // (in place: what is copied is there)
+    const uint32_t per = (uint32_t)heads * a.items, all = nt * per;
+    for (uint32_t at = tid; at < all; at += 256 * kRopeSteps) {
+      Raw8<T> ru[kRopeSteps], rv[kRopeSteps];
+      uint8_t* y[kRopeSteps];
+      int tok[kRopeSteps], item[kRopeSteps];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p = u[2 * i], q = u[2 * i + 1], r = v[2 * i], w = v[2 * i + 1];
-            u[2 * i] = p * c[i] - q * s[i];
-            u[2 * i + 1] = p * s[i] + q * c[i];
-            v[2 * i] = r * c[4 + i] - w * s[4 + i];
-            v[2 * i + 1] = r * s[4 + i] + w * c[4 + i];
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float p = u[i], q = v[i];
-            u[i] = p * c[i] - q * s[i];
-            v[i] = p * s[i] + q * c[i];
-          }
-        }
+      for (int e = 0; e < kRopeSteps; ++e) {
+        const uint32_t i = at + 256 * e;
+        y[e] = nullptr;
+        if (i >= all) continue;
+        tok[e] = (int)(i / per);
+        const uint32_t r = i - tok[e] * per, h = r / a.items;
+        item[e] = (int)(r - h * a.items);
+        const bool turns = 16 * item[e] < a.rot;
+        if (!turns && !copies) continue;
+        const int i0 = PAIRS || !turns ? 16 * item[e] : 8 * item[e], i1 = PAIRS || !turns ? i0 + 8 : half + i0;
+        const uint8_t* x = io.X + (t0 + tok[e]) * io.x_tok + (int64_t)(from + h) * io.x_head;
+        ru[e].load(x + i0 * sizeof(T));
+        rv[e].load(x + i1 * sizeof(T));
+        y[e] = io.Y + (t0 + tok[e]) * io.y_tok + (int64_t)(from + h) * io.y_head;
       }
-      store8<T>(y + i0 * sizeof(T), u);
-      store8<T>(y + i1 * sizeof(T), v);
+#pragma unroll
+      for (int e = 0; e < kRopeSteps; ++e) {
+        if (y[e] == nullptr) continue;
+        const bool turns = 16 * item[e] < a.rot;
+        const int i0 = PAIRS || !turns ? 16 * item[e] : 8 * item[e], i1 = PAIRS || !turns ? i0 + 8 : half + i0;
+        float u[8], v[8];
+        ru[e].widen(u);
+        rv[e].widen(v);
+        if (turns) {
+          Turns w;
+          w.read(cs + tok[e] * half, item[e], half);
+          w.apply(PAIRS, u, v);
+        }
+        store8<T>(y[e] + i0 * sizeof(T), u);
+        store8<T>(y[e] + i1 * sizeof(T), v);
+      }
     }
   }
 }
@@ -104,11 +112,17 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 hipError_t launch_rope(bool bf16, const RopeArgs& in, hipStream_t s) {
   RopeArgs a = in;
   a.items = a.d / 16;
-  const int64_t blocks = (a.tokens * a.items + 255) / 256;
-  // few tokens: the heads are spread over blocks as well, up to about four a unit
-  const int64_t split = (1024 + blocks - 1) / blocks;
-  const dim3 grid((uint32_t)blocks, (uint32_t)(split < a.all_heads ? split : a.all_heads));
-  auto go = [&](auto k) { return launch_kernel(k, grid, dim3(256), s, a); };
+  // as many tokens to a block as leave two blocks to each compute unit; few tokens: the
+  // heads are spread over blocks too, no fewer than 256 runs of 16 values to each
+  a.block_tokens = 1;
+  while (a.block_tokens < kRopeTokens && a.tokens >= 1024 * a.block_tokens) a.block_tokens *= 2;
+  const int64_t blocks = (a.tokens + a.block_tokens - 1) / a.block_tokens;
+  int64_t split = (1024 + blocks - 1) / blocks, most = ((int64_t)a.all_heads * a.items * a.block_tokens + 255) / 256;
+  if (split > most) split = most;
+  if (split > a.all_heads) split = a.all_heads;
+  const dim3 grid((uint32_t)blocks, (uint32_t)split);
+  const size_t lds = (size_t)a.block_tokens * (a.rot / 2) * sizeof(float2);
+  auto go = [&](auto k) { return launch_kernel_lds(k, grid, dim3(256), lds, s, a); };
   if (bf16) return a.pairs ? go(rope_kernel<uint16_t, true>) : go(rope_kernel<uint16_t, false>);
   return a.pairs ? go(rope_kernel<float, true>) : go(rope_kernel<float, false>);
 }
