@@ -21,6 +21,7 @@ namespace {
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 using lds_f32 = __attribute__((address_space(3))) float;
+using lds_i32x4 = __attribute__((address_space(3))) i32x4;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLift = 8.0f;        // w = 2^(u - M + kLift)
@@ -79,6 +80,12 @@ __device__ __forceinline__ float row_most(i32x4 x) {
     m = fmaxf(m, fmaxf(finite_abs((uint32_t)x[i] << 16), finite_abs((uint32_t)x[i] & 0xFFFF0000u)));
   return m;
 }
+__device__ __forceinline__ f32x16 splat(float x) {
+  f32x16 v;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = x;
+  return v;
+}
 // bytes 4 i .. 4 i + 3 of 16, of which the first n count: a mask
 __device__ __forceinline__ uint32_t keep_bytes(int n, int i) {
   const int k = n - 4 * i;
@@ -114,8 +121,14 @@ __device__ __forceinline__ Tile tile_at(const KvAttnArgs& a, const KvSeq& q, int
 // token 16 (m / 4) + 4 t + m % 4 of a page is row m of token tile t, so that a lane's
 // results of four tiles are tokens 16 (l / 16) + 0..15: those of the 16 bytes that
 // it loads of a value channel, and, as they are, the second product's B operand.
-template <int D, bool E4M3, int NT>
-__global__ __launch_bounds__(256, 2) void kv_attn_kernel(KvAttnArgs a) {
+template <bool ONCE>
+__device__ __forceinline__ i32x4 load_codes(const uint8_t* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(p));
+  return *reinterpret_cast<const i32x4*>(p);
+}
+
+template <int D, bool E4M3, int NT, bool ONCE>
+__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attn_kernel(KvAttnArgs a) {
   constexpr int KJ = D / 64, ND = D / 16, ROWS = 16 * NT, OROW = D + 4;
   __shared__ float part_o[4][ROWS][OROW];
   __shared__ float part_m[4][ROWS], part_l[4][ROWS];
@@ -178,12 +191,12 @@ __global__ __launch_bounds__(256, 2) void kv_attn_kernel(KvAttnArgs a) {
 #pragma unroll
     for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
-      for (int j = 0; j < KJ; ++j) kraw[mt][j] = *reinterpret_cast<const i32x4*>(p + koff + 4 * D * mt + 64 * j);
+      for (int j = 0; j < KJ; ++j) kraw[mt][j] = load_codes<ONCE>(p + koff + 4 * D * mt + 64 * j);
   };
   auto load_v = [&](int i) {
     const uint8_t* p = a.c.V + block_at(i);
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt) vraw[dt] = *reinterpret_cast<const i32x4*>(p + voff + 16 * kPage * dt);
+    for (int dt = 0; dt < ND; ++dt) vraw[dt] = load_codes<ONCE>(p + voff + 16 * kPage * dt);
   };
 
   unsigned long long todo;
@@ -359,6 +372,304 @@ __global__ __launch_bounds__(256, 2) void kv_attn_kernel(KvAttnArgs a) {
   }
 }
 
+// ------------------------------------------------------------------ many rows
+// 128 rows of a sequence and key head, 32 per wave, by two groups of four waves, which
+// take every second page each and join at the end (a block is done in half the time,
+// which counts where contexts differ: the longest block ends the kernel).  A group
+// loads a page's codes to registers while the page before is worked on, widens them
+// once for its 128 rows and passes them through LDS as fp16, two stages.
+//
+// v_mfma_f32_32x32x16_f16: A lane l holds row l % 32, 8 values of the reduction from
+// 8 (l / 32); B the same of columns; result register i is row 8 (i / 4) + 4 (l / 32) +
+// i % 4 of column l % 32.  Scores are formed transposed (A = keys); key 8 h + 4 x + y of
+// 16 is row 8 x + 4 h + y of the tile, so that registers 8 k .. 8 k + 7 are keys
+// 16 k + 8 (l / 32) + 0..7: the second product's B operand as they are, beside 16 bytes
+// of a value channel, whose tokens the cache keeps together.
+constexpr int kTileRows = 128;
+
+// The tile of rank p, those of the longest sequences first: a block's time goes by the
+// pages that its sequence has, and the long ones that began last ended the kernel (8
+// chunks over 460 to 7870 tokens: 19 % of it).  Up to 64 sequences, one per lane; more:
+// in their order.
+__device__ __forceinline__ KvSeq find_longest(const KvAttnArgs& a, int p, int& item) {
+  if (a.c.n_seq > kWave) return kv_find(a.c, p, a.c.group, kTileRows, 1, item);
+  const int lane = threadIdx.x & (kWave - 1);
+  KvSeq q{0, 0, 0, -1};
+  if (lane < a.c.n_seq) q = kv_seq(a.c, lane);
+  const int n = (int)(((int64_t)q.lq * a.c.group + kTileRows - 1) / kTileRows);
+  int before = 0;
+  for (int s = 0; s < a.c.n_seq; ++s) {
+    const int lk = __builtin_amdgcn_readlane(q.lk, s), tiles = __builtin_amdgcn_readlane(n, s);
+    before += lk > q.lk || (lk == q.lk && s < lane) ? tiles : 0;
+  }
+  const unsigned long long here = __ballot(before <= p && p < before + n);
+  if (here == 0) {
+    item = -1;
+    return KvSeq{0, 0, 0, 0};
+  }
+  const int s = __builtin_ctzll(here);
+  item = p - __builtin_amdgcn_readlane(before, s);
+  return KvSeq{s, __builtin_amdgcn_readlane(q.q0, s), __builtin_amdgcn_readlane(q.lq, s), __builtin_amdgcn_readlane(q.lk, s)};
+}
+
+template <int D, bool E4M3, int GR>
+__global__ __launch_bounds__(256 * GR, 2) void kv_tile_kernel(KvAttnArgs a) {
+  // rows of a staged tile end in 16 bytes that nothing uses: the 16 rows that as many
+  // lanes read at one place then fall on all banks, at offsets that are constants
+  constexpr int NK = D / 16, ND = D / 32, CH = kPage * D / 16 / 256;
+  constexpr int KROW = 2 * D + 16, VROW = 2 * kPage + 16, KB = kPage * KROW, VB = D * VROW, GB = 2 * (KB + VB);
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[GR * GB];         // of each group: keys, values; two stages
+  __shared__ float row_m[GR][kTileRows], row_l[GR][kTileRows];
+  const int lane = threadIdx.x & 63, h = lane >> 5, n = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 3, grp = wave >> 2;
+  const int tid = threadIdx.x & 255;
+  int id = blockIdx.x, item;
+  const int kvh = id % a.c.kv_heads;
+  id /= a.c.kv_heads;
+  const int split = id / a.tiles;
+  const Tile t = tile_at(a, find_longest(a, id - split * a.tiles, item), item);
+  if (item < 0 || t.r0 >= t.rows) return;
+  const int first = split * a.chunk, end = min(first + a.chunk, t.nblk);
+  if (split > 0 && first >= t.nblk) return;
+  const bool whole = t.nblk <= a.chunk;             // no other block works on these rows
+
+  // this lane's row
+  const int r = min(t.r0 + 32 * w + n, t.rows - 1);
+  const int tok = row_token(a, r), head = kvh * a.c.group + (r - tok * a.c.group);
+  const int lim = a.causal ? tok + t.q.lk - t.q.lq : t.q.lk - 1;
+  const int lim_lo = __builtin_amdgcn_readlane(lim, 0);
+  const int lim_hi = t.r0 + 32 * w < t.rows ? __builtin_amdgcn_readlane(lim, 31) : -1;
+  i32x4 qraw[NK];
+  const uint8_t* qp = a.Q + (int64_t)(t.q.q0 + tok) * a.q_tok + head * a.q_head;
+#pragma unroll
+  for (int ks = 0; ks < NK; ++ks) qraw[ks] = *reinterpret_cast<const i32x4*>(qp + 32 * ks + 16 * h);
+
+  // pages of this group (up to 128 of the block's at a time), one per lane
+  int page;
+  float ks_, vs_;
+  auto find_pages = [&](int from) {
+    const int blk = from + grp + GR * lane;
+    page = -1;
+    ks_ = vs_ = 1.0f;
+    if (blk < end) page = a.c.table[(int64_t)t.q.s * a.c.table_stride + blk];
+    if (page < 0 || page >= a.c.pages) page = -1;
+    if (page >= 0) {
+      const float2 s = *reinterpret_cast<const float2*>(a.c.scales + 2 * ((int64_t)page * a.c.kv_heads + kvh));
+      ks_ = s.x;
+      vs_ = s.y;
+    }
+  };
+  auto kscale = [&](int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_), i)); };
+  auto vexp = [&](int i) { return exp_of(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_), i))); };
+  // codes of page i (zeros of one that is not there, or behind the last)
+  i32x4 kraw[CH], vraw[CH];
+  // (of a page's keys a thread takes every 256th run of 16 bytes; of its values those of
+  // one row for 16 lanes of a quarter each, whose stores fall on all banks)
+  const int vrow = 16 * w + (lane & 15), vat = 4 * vrow + (lane >> 4);
+  auto load = [&](const uint8_t* base, int first, int i, i32x4 (&raw)[CH]) {
+    const int p = i < kWave ? __builtin_amdgcn_readlane(page, i) : -1;
+    if (p < 0) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) raw[c] = i32x4{0, 0, 0, 0};
+    } else {
+      const i32x4* x = reinterpret_cast<const i32x4*>(base + ((int64_t)p * a.c.kv_heads + kvh) * (int64_t)(kPage * D));
+#pragma unroll
+      for (int c = 0; c < CH; ++c) raw[c] = x[first + 256 * c];
+    }
+  };
+  auto load_k = [&](int i) { load(a.c.K, tid, i, kraw); };
+  auto load_v = [&](int i) { load(a.c.V, vat, i, vraw); };
+  lds_u8* lds = (lds_u8*)&smem[0] + grp * GB;
+  // codes -> fp16 in stage st; of the values, tokens behind the sequence's end as 0
+  auto stage_k = [&](int st) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int p = tid + 256 * c, row = p / (D / 16), col = 2 * (p % (D / 16));
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        *(lds_i32x4*)(lds + st * KB + row * KROW + 16 * (col + e)) = __builtin_bit_cast(i32x4, widen8<E4M3>(kraw[c][2 * e], kraw[c][2 * e + 1]));
+    }
+  };
+  auto stage_v = [&](int st, int at) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int row = vrow + 64 * c, col = 2 * (lane >> 4);
+      if (at + kPage > t.q.lk) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vraw[c][e] &= (int)keep_bytes(t.q.lk - at - 8 * col, e);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        *(lds_i32x4*)(lds + 2 * KB + st * VB + row * VROW + 16 * (col + e)) = __builtin_bit_cast(i32x4, widen8<E4M3>(vraw[c][2 * e], vraw[c][2 * e + 1]));
+    }
+  };
+
+  f16x8 qf[NK];
+  float qc;
+  {
+    float most = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < NK; ++ks) most = fmaxf(most, row_most(qraw[ks]));
+    most = fmaxf(most, __shfl_xor(most, 32, kWave));
+    const int k = row_shift(most);
+    const float f = exp2_int(-k);
+    qc = a.scale * kLog2e * exp2_int(k);
+#pragma unroll
+    for (int ks = 0; ks < NK; ++ks) qf[ks] = scaled_row(qraw[ks], f);
+  }
+  // row n of a key tile's 32 is this key
+  const int key = (n & 16) + ((n & 4) << 1) + ((n & 8) >> 1) + (n & 3);
+  const lds_u8 *kread = lds + key * KROW + 16 * h, *vread = lds + 2 * KB + n * VROW + 16 * h;
+
+  f32x16 o[ND];
+#pragma unroll
+  for (int db = 0; db < ND; ++db) o[db] = splat(0.0f);
+  float m = -__builtin_inff(), l = 0.0f;
+
+  // groups of up to 128 pages; both groups of waves go round as often, for the barriers
+  for (int from = first; from < end; from += GR * kWave) {
+    find_pages(from);
+    const int rounds = (min(end - from, GR * kWave) + GR - 1) / GR;
+    auto at_of = [&](int i) { return (from + grp + GR * i) * kPage; };       // page i's first token
+    f32x16 s[2];
+    load_k(0);
+    load_v(0);
+    stage_k(0);
+    stage_v(0, at_of(0));
+    load_k(1);
+    load_v(1);
+    __syncthreads();
+    auto round = [&](int i, auto stage) {
+      constexpr int S = decltype(stage)::value;
+      const int at = at_of(i);
+      const bool there = __builtin_amdgcn_readlane(page, i) >= 0 && at <= lim_hi;
+      if (there) {
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) s[nb] = splat(0.0f);
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+          for (int ks = 0; ks < NK; ++ks)
+            s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                __builtin_bit_cast(f16x8, *(const lds_i32x4*)(kread + S * KB + nb * 32 * KROW + 32 * ks)), qf[ks], s[nb], 0, 0, 0);
+      }
+      if (i + 1 < rounds) {
+        stage_k(1 - S);
+        stage_v(1 - S, at + GR * kPage);
+        load_k(i + 2);
+        load_v(i + 2);
+      }
+      if (there) {
+        if (at + kPage - 1 > lim_lo) {
+          const int left = lim - at - 8 * h;       // the last key seen, from this lane's first
+#pragma unroll
+          for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (32 * nb + 16 * (e / 8) + e % 8 > left) s[nb][e] = -__builtin_inff();
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int e = 1; e < 32; ++e) mx = fmaxf(mx, s[e / 16][e % 16]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        const int ev = vexp(i);
+        const float c = kscale(i) * qc, u = mx * c + (float)ev;
+        if (__ballot(u > m + kSlack)) {
+          const float to = fmaxf(m, u), f = to == m ? 1.0f : exp2_fast(m - to);
+          m = to;
+          l *= f;
+#pragma unroll
+          for (int db = 0; db < ND; ++db) o[db] *= f;
+        }
+        const float b = (float)ev + kLift - (m == -__builtin_inff() ? 0.0f : m);
+        float sum = 0.0f;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          float w[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            w[e] = exp2_fast(__builtin_fmaf(s[kk / 2][8 * (kk & 1) + e], c, b));
+            sum += w[e];
+          }
+          const f16x8 p = __builtin_bit_cast(f16x8, i32x4{(int)pack_f16x2(w[0], w[1]), (int)pack_f16x2(w[2], w[3]),
+                                                          (int)pack_f16x2(w[4], w[5]), (int)pack_f16x2(w[6], w[7])});
+#pragma unroll
+          for (int db = 0; db < ND; ++db)
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                __builtin_bit_cast(f16x8, *(const lds_i32x4*)(vread + S * VB + db * 32 * VROW + 32 * kk)), p, o[db], 0, 0, 0);
+        }
+        l += sum * exp2_int(-ev);
+      }
+      __syncthreads();
+    };
+    for (int i = 0; i < rounds; i += 2) {
+      round(i, std::integral_constant<int, 0>{});
+      if (i + 1 < rounds) round(i + 1, std::integral_constant<int, 1>{});
+    }
+  }
+
+  // the groups' sums on a common M: group g finishes the ND / GR blocks of 32 channels from
+  // g ND / GR on
+  l += __shfl_xor(l, 32, kWave);
+  const int rr = 32 * w + n;
+  float both = m, total = l, f0 = 1.0f, f1 = 0.0f;
+  if constexpr (GR == 2) {
+    if (h == 0) {
+      row_m[grp][rr] = m;
+      row_l[grp][rr] = l;
+    }
+    __syncthreads();
+    const float m1 = row_m[1 - grp][rr];
+    both = fmaxf(m, m1);
+    f0 = m == both ? 1.0f : exp2_fast(m - both);
+    f1 = m1 == both ? 1.0f : exp2_fast(m1 - both);
+    total = l * f0 + row_l[1 - grp][rr] * f1;
+  }
+  const bool none = both == -__builtin_inff();
+  const float inv = none ? 0.0f : 1.0f / total, lse = none ? both : both - kLift + log2f(total);
+  lds_f32* give = (lds_f32*)&smem[0];
+  if constexpr (GR == 2) {
+#pragma unroll
+    for (int d = 0; d < ND / 2; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        give[(((grp * 4 + w) * (ND / 2) + d) * 16 + e) * 64 + lane] = grp == 0 ? o[ND / 2 + d][e] : o[d][e];
+    __syncthreads();
+  }
+  const bool mine = t.r0 + rr < t.rows;
+  const int64_t row = t.q.q0 + tok;
+#pragma unroll
+  for (int d = 0; d < ND / GR; ++d) {
+    f32x16 y;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      if constexpr (GR == 2) {
+        const float own = grp == 0 ? o[d][e] : o[ND / 2 + d][e];
+        y[e] = (own * f0 + give[((((1 - grp) * 4 + w) * (ND / 2) + d) * 16 + e) * 64 + lane] * f1) * inv;
+      } else {
+        y[e] = o[d][e] * inv;
+      }
+    }
+    const int d0 = 32 * (grp * (ND / GR) + d) + 4 * h;
+    if (mine) {
+      if (whole) {
+        uint8_t* p = a.O + row * a.o_tok + head * a.o_head + 2 * d0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<uint2*>(p + 16 * e) = uint2{pack_bf16x2(y[4 * e], y[4 * e + 1]), pack_bf16x2(y[4 * e + 2], y[4 * e + 3])};
+      } else {
+        float* p = a.part + (((int64_t)split * a.c.tq + row) * a.c.heads + head) * D + d0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *reinterpret_cast<f32x4*>(p + 8 * e) = f32x4{y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]};
+      }
+    }
+  }
+  if (mine && grp == 0 && h == 0) {
+    if (!whole) a.part_lse[((int64_t)split * a.c.tq + row) * a.c.heads + head] = lse;
+    else if (a.lse != nullptr) a.lse[(int64_t)head * a.c.tq + row] = lse * kLn2;
+  }
+}
+
 // Joins the parts of the rows that have several: o = sum_p 2^(L_p - L) o_p / sum_p
 // 2^(L_p - L).  WIDE: a block for a row, else a wave.  A wave reads GR parts at a time,
 // 16 bytes per lane.  (A wave for each of 128 rows of 64 parts took 20 us.)
@@ -420,28 +731,59 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
 }  // namespace
 
 void kv_attn_plan(KvAttnArgs* a) {
-  const int64_t rows = (int64_t)a->c.tq * a->c.group, blocks = ((int64_t)a->c.max_len + kPage - 1) / kPage;
-  a->tile_rows = rows <= 16 * (int64_t)a->c.n_seq ? 16 : 32;
+  const int64_t rows = (int64_t)a->c.tq * a->c.group, seqs = a->c.n_seq > 0 ? a->c.n_seq : 1;
+  const int64_t pages = a->c.max_len > 0 ? ((int64_t)a->c.max_len + kPage - 1) / kPage : 1;
+  a->tile_rows = rows <= 16 * seqs ? 16 : rows <= 48 * seqs ? 32 : kTileRows;
   a->tiles = (int)(a->c.q_start == nullptr && a->c.group <= a->tile_rows ? a->c.n_seq : rows / a->tile_rows + a->c.n_seq);
-  const int64_t base = (int64_t)a->tiles * a->c.kv_heads;
-  int64_t chunk = (blocks * base + 2047) / 2048;
-  chunk = (chunk + 3) / 4 * 4;
-  a->chunk = (int)(chunk < 8 ? 8 : chunk);
-  a->splits = (int)((blocks + a->chunk - 1) / a->chunk);
-  if (a->splits < 1) a->splits = 1;
+  int64_t splits = 1;
+  if (a->tile_rows == kTileRows) {
+    // one block to a compute unit: as many rounds of blocks as it takes, of half the
+    // pages each and about 4 more to begin and end
+    const int64_t blocks = seqs * ((rows + seqs * kTileRows - 1) / (seqs * kTileRows)) * a->c.kv_heads;
+    int64_t best = INT64_MAX;
+    for (int64_t s = 1; s <= 32 && s * 4 <= pages + 3; ++s) {
+      const int64_t cost = (blocks * s + 255) / 256 * ((pages + s - 1) / s + 8) + (s > 1 ? 4 + rows * a->c.kv_heads * s / 20000 : 0);
+      if (cost < best) {
+        best = cost;
+        splits = s;
+      }
+    }
+  } else {
+    // about 8 blocks to a unit (a part of them beyond the ends of shorter sequences), no
+    // fewer than 8 pages to a block, 2 to a wave
+    const int64_t blocks = (int64_t)a->tiles * a->c.kv_heads;
+    splits = (2048 + blocks - 1) / blocks;
+    if (splits > pages / 8) splits = pages / 8;
+  }
+  if (splits < 1) splits = 1;
+  a->chunk = (int)(((pages + splits - 1) / splits + 3) / 4 * 4);
+  a->splits = (int)((pages + a->chunk - 1) / a->chunk);
 }
 
 hipError_t launch_kv_attn(bool e4m3, const KvAttnArgs& a, hipStream_t s) {
   const dim3 grid((uint32_t)((int64_t)a.tiles * a.c.kv_heads * a.splits));
   LaunchStatus st;
-  auto go = [&](auto k) { st << launch_kernel(k, grid, dim3(256), s, a); };
-  if (a.c.d == 128) {
-    if (a.tile_rows == 16) e4m3 ? go(kv_attn_kernel<128, true, 1>) : go(kv_attn_kernel<128, false, 1>);
-    else e4m3 ? go(kv_attn_kernel<128, true, 2>) : go(kv_attn_kernel<128, false, 2>);
-  } else {
-    if (a.tile_rows == 16) e4m3 ? go(kv_attn_kernel<64, true, 1>) : go(kv_attn_kernel<64, false, 1>);
-    else e4m3 ? go(kv_attn_kernel<64, true, 2>) : go(kv_attn_kernel<64, false, 2>);
-  }
+  auto go = [&](auto k) { st << launch_kernel(k, grid, dim3(a.tile_rows == kTileRows ? 512 : 256), s, a); };
+  // each code is read by one block, and there are more than the last-level cache (256 MB)
+  // holds from one call to the next: past it (32 tokens over 1 to 8192, 270 MB: 60.2 ->
+  // 55.6 us; 79 MB that it may still hold: 28.0 -> 31.4)
+  const bool once = a.tiles == a.c.n_seq && (int64_t)a.c.n_seq * a.c.max_len * a.c.kv_heads * a.c.d * 2 > (int64_t)256 << 20;
+  auto few = [&](auto d, auto fmt, auto nt) {
+    constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
+    constexpr bool F = decltype(fmt)::value;
+    once ? go(kv_attn_kernel<D, F, NT, true>) : go(kv_attn_kernel<D, F, NT, false>);
+  };
+  auto pick = [&](auto d, auto fmt) {
+    constexpr int D = decltype(d)::value;
+    constexpr bool F = decltype(fmt)::value;
+    if (a.tile_rows == kTileRows) go(kv_tile_kernel<D, F, 2>);
+    else if (a.tile_rows == 16) few(d, fmt, std::integral_constant<int, 1>{});
+    else few(d, fmt, std::integral_constant<int, 2>{});
+  };
+  auto width = [&](auto fmt) {
+    a.c.d == 128 ? pick(std::integral_constant<int, 128>{}, fmt) : pick(std::integral_constant<int, 64>{}, fmt);
+  };
+  e4m3 ? width(std::true_type{}) : width(std::false_type{});
   if (a.splits > 1) {
     const int64_t rows = (int64_t)a.c.tq * a.c.heads;
     const bool wide = a.splits > 4 && rows <= 4096;

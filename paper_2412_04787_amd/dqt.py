@@ -569,35 +569,52 @@ def rope(d: int, rot: int | None = None, pairs: bool = False, amp: float = 1.0, 
     return Rope(_torch().from_numpy(f.view(np.int64)).to(device), d, pairs, amp)
 
 
-def _rope(fn, rope: Rope, pairs, pos, stream):
+_pack_rope_io = struct.Struct("6q2i").pack
+
+
+def _rope(fn, call, rope: Rope, pairs, pos, stream):
     if not pairs:
         raise ValueError("expected at least one tensor")
     x0 = pairs[0][0]
-    dev = _here(x0, rope.freq, *(t for xy in pairs for t in xy))
-    tokens, _, d = x0.shape
-    if d != rope.d:
-        raise ValueError(f"expected heads of {rope.d} values, got {d}")
-    if pos is not None:
-        _bufs(dev, (pos, 4 * tokens, _torch().int32))
-        if pos.numel() != tokens:
-            raise ValueError(f"expected {tokens} positions, got {pos.numel()}")
-    io = b"".join([_row(x, (tokens, x.shape[1], d), x0.dtype) + _row(y, x.shape, x0.dtype) +
-                   _pack_heads(x.shape[1], 0) for x, y in pairs])
-    _check(fn, getattr(load(), fn)(rope.ref, len(pairs), io, dtype_code(x0), tokens, _addr(pos), _stream(stream)))
-
-
-_pack_heads = struct.Struct("2i").pack
+    dev, dt, tokens, width = _here(x0, rope.freq), x0.dtype, x0.shape[0], rope.d
+    io = b""
+    for x, y in pairs:
+        shape = x.shape
+        if x.get_device() != dev or y.get_device() != dev:
+            _here(x0, x, y)
+        if x.dtype is not dt or y.dtype is not dt or y.shape != shape or len(shape) != 3:
+            raise ValueError(f"expected {dt} tensors of one shape [tokens, heads, d], got {x.dtype} {tuple(shape)} and "
+                             f"{y.dtype} {tuple(y.shape)}")
+        n, h, d = shape
+        if n != tokens or d != width:
+            raise ValueError(f"expected {tokens} tokens and heads of {width} values, got {tuple(shape)}")
+        (xt, xh, xd), (yt, yh, yd) = x.stride(), y.stride()
+        if (xd != 1 or yd != 1) and n * h > 0:
+            raise ValueError(f"expected unit last stride, got strides {x.stride()} and {y.stride()}")
+        # (strides of a dimension of one do not matter)
+        if n <= 1:
+            xt = yt = h * d
+        if h <= 1:
+            xh = yh = d
+        io += _pack_rope_io(x.data_ptr(), xt, xh, y.data_ptr(), yt, yh, h, 0)
+    if pos is not None and (pos.get_device() != dev or pos.dtype is not _torch().int32 or pos.numel() != tokens or
+                            not pos.is_contiguous()):
+        raise ValueError(f"expected {tokens} contiguous int32 positions on device {dev}, got {pos.dtype} {tuple(pos.shape)} "
+                         f"with strides {pos.stride()} on {pos.device}")
+    st = call(rope.ref, len(pairs), io, dtype_code(x0), tokens, _addr(pos), _stream(stream))
+    if st != DQT_OK:
+        raise DqtError(fn, st)
 
 
 def dqt_rope_fwd(rope: Rope, pairs, pos=None, stream=None):
     """pairs: up to 4 (X, Y) of one dtype (bf16 or fp32), each [tokens, heads, d] with any
     token and head strides; Y may be X.  pos: int32 [tokens], or None for 0, 1, 2 ..."""
-    _rope("dqt_rope_fwd", rope, pairs, pos, stream)
+    _rope("dqt_rope_fwd", load().dqt_rope_fwd, rope, pairs, pos, stream)
 
 
 def dqt_rope_bwd(rope: Rope, pairs, pos=None, stream=None):
     """pairs: (gradient of the rotated values, gradient of the values)."""
-    _rope("dqt_rope_bwd", rope, pairs, pos, stream)
+    _rope("dqt_rope_bwd", load().dqt_rope_bwd, rope, pairs, pos, stream)
 
 
 KV_PAGE = 64
