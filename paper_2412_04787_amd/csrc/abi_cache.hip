@@ -105,7 +105,7 @@ dqt_status check_batch(const dqt_kv_cache* c, const dqt_kv_batch* b, dqt::KvArgs
   a->d = c->d;
   // the pages that tokens are written to, and the tiles of 16 rows, at most
   const int64_t pages = a->tq / dqt::kPage + 2 * (int64_t)a->n_seq, tiles = (int64_t)a->tq * a->group / 16 + a->n_seq;
-  if (pages * a->kv_heads >= kMaxBlocks || tiles * a->kv_heads >= kMaxBlocks) return DQT_ERR_SHAPE;
+  if (4 * pages * a->kv_heads >= kMaxBlocks || tiles * a->kv_heads >= kMaxBlocks) return DQT_ERR_SHAPE;
   return DQT_OK;
 }
 
