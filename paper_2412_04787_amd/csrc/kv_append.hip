@@ -100,7 +100,7 @@ __device__ __forceinline__ void turn_table(const KvAppendArgs& a, float2* cs, in
 // The queries of the G heads that share a key head: n tokens from row0 on.
 template <int D, int CROW>
 __device__ __forceinline__ void turn_queries(const KvAppendArgs& a, const float2* cs, int64_t row0, int kvh, int n) {
-  constexpr int ITEMS = D / 16, QSTEPS = 4;
+  constexpr int ITEMS = D / 16, QSTEPS = 2;
   const int tid = threadIdx.x;
   const uint32_t G = (uint32_t)a.c.group, all = n * G * ITEMS;
   const uint8_t* q = a.q + row0 * a.q_tok + (int64_t)kvh * G * a.q_head;

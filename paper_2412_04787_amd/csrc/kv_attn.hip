@@ -751,7 +751,7 @@ void kv_attn_plan(KvAttnArgs* a) {
   } else {
     // about 8 blocks to a unit (a part of them beyond the ends of shorter sequences), no
     // fewer than 8 pages to a block, 2 to a wave
-    const int64_t blocks = (int64_t)a->tiles * a->c.kv_heads;
+    const int64_t blocks = (int64_t)(a->tiles > 0 ? a->tiles : 1) * a->c.kv_heads;
     splits = (2048 + blocks - 1) / blocks;
     if (splits > pages / 8) splits = pages / 8;
   }

@@ -530,12 +530,13 @@ def dqt_attn_bwd(a: DqtAttn, Q, K, V, O, lse, dO, dQ, dK, dV, ws, stream=None):
 
 # ----------------------------------------------------------------- rotary positions and the 8-bit cache
 
-def _row(t, shape, dtype):
-    """The dqt_rows (as bytes) of a tensor [tokens, heads, d] with any token and head strides."""
-    if t.dtype is not dtype or t.shape != shape:
-        raise ValueError(f"expected a {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+def _row(t, n, h, d, dev):
+    """The dqt_rows (as bytes) of a bf16 tensor [n, h, d] on device dev with any token and head strides."""
+    if t.get_device() != dev:
+        raise ValueError(f"tensor on {t.device}, others on device {dev}")
+    if t.dtype is not _torch().bfloat16 or t.shape != (n, h, d):
+        raise ValueError(f"expected a bfloat16 tensor of shape {(n, h, d)}, got {t.dtype} {tuple(t.shape)}")
     st, sh, sd = t.stride()
-    n, h, d = shape
     if sd != 1 and t.numel() > 0:
         raise ValueError(f"expected unit last stride, got strides {t.stride()}")
     # (strides of a dimension of one do not matter)
@@ -679,9 +680,9 @@ def kv_batch(table, kv_len, q_tokens: int, heads: int, q_start=None, max_len: in
     return KvBatch(desc, (table, kv_len, q_start), scale)
 
 
-def _kv(cache: KvCache, batch: KvBatch, *tensors):
+def _kv(cache: KvCache, batch: KvBatch) -> int:
     """Their device; the batch's scale is that of the cache's heads unless it was given."""
-    dev = _here(cache.K, *tensors)
+    dev = _here(cache.K)
     if batch.dev != dev:
         raise ValueError(f"batch on device {batch.dev}, cache on device {dev}")
     if batch.scale is None:
@@ -692,15 +693,17 @@ def _kv(cache: KvCache, batch: KvBatch, *tensors):
 def dqt_kv_append(cache: KvCache, batch: KvBatch, K, V, rope: Rope | None = None, Q=None, Qr=None, stream=None):
     """K, V: [q_tokens, kv_heads, d], Q and Qr (with rope): [q_tokens, heads, d], bf16 with any token
     and head strides.  Qr may be Q."""
-    bf16 = _torch().bfloat16
+    dev, n, kvh, d = _kv(cache, batch), batch.q_tokens, cache.kv_heads, cache.d
     if (Q is None) != (Qr is None):
         raise ValueError("Q and Qr go together")
-    _kv(cache, batch, K, V, *(() if rope is None else (rope.freq,)), *(() if Q is None else (Q, Qr)))
-    kv, q = (batch.q_tokens, cache.kv_heads, cache.d), (batch.q_tokens, batch.heads, cache.d)
+    if rope is not None and rope.freq.get_device() != dev:
+        raise ValueError(f"frequencies on {rope.freq.device}, cache on device {dev}")
+    q = qr = None
+    if Q is not None:
+        q, qr = _row(Q, n, batch.heads, d, dev), _row(Qr, n, batch.heads, d, dev)
     _check("dqt_kv_append",
-           load().dqt_kv_append(cache.ref, batch.ref, _row(K, kv, bf16), _row(V, kv, bf16),
-                                None if rope is None else rope.ref, None if Q is None else _row(Q, q, bf16),
-                                None if Q is None else _row(Qr, q, bf16), _stream(stream)))
+           load().dqt_kv_append(cache.ref, batch.ref, _row(K, n, kvh, d, dev), _row(V, n, kvh, d, dev),
+                                None if rope is None else rope.ref, q, qr, _stream(stream)))
 
 
 def dqt_kv_attn_workspace(cache: KvCache, batch: KvBatch) -> int:
@@ -711,13 +714,12 @@ def dqt_kv_attn_workspace(cache: KvCache, batch: KvBatch) -> int:
 def dqt_kv_attn(cache: KvCache, batch: KvBatch, Q, O, lse=None, ws=None, stream=None):
     """Q, O: [q_tokens, heads, d], bf16 with any token and head strides; lse: contiguous fp32
     [heads, q_tokens] or None."""
-    torch = _torch()
-    dev = _kv(cache, batch, Q, O)
-    shape = (batch.q_tokens, batch.heads, cache.d)
-    _bufs(dev, (lse, 4 * batch.heads * batch.q_tokens, torch.float32))
+    dev, n, h, d = _kv(cache, batch), batch.q_tokens, batch.heads, cache.d
+    if lse is not None:
+        _bufs(dev, (lse, 4 * h * n, _torch().float32))
     _check("dqt_kv_attn",
-           load().dqt_kv_attn(cache.ref, batch.ref, _row(Q, shape, torch.bfloat16), _row(O, shape, torch.bfloat16),
-                              _addr(lse), _addr(ws), _ws_bytes(dev, ws), _stream(stream)))
+           load().dqt_kv_attn(cache.ref, batch.ref, _row(Q, n, h, d, dev), _row(O, n, h, d, dev), _addr(lse), _addr(ws),
+                              _ws_bytes(dev, ws), _stream(stream)))
 
 
 def _pages(x) -> np.ndarray:
