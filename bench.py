@@ -402,6 +402,7 @@ def run_model(args):
                         f"{cfg.heads} heads, FFN {cfg.ffn}, vocab {cfg.vocab}, RMSNorm, RoPE; "
                         + ("attention, SwiGLU and loss in this library's kernels, gate and up held in "
                            f"{'8 bits' if cfg.ckpt8 else 'bf16'} for the backward; " if cfg.own_ops else "")
+                        + ("rotary positions too; " if cfg.own_rope else "")
                         + f"all {7 * cfg.layers} block linears DQT ternary (int8 activations, "
                         f"bf16 environment); batch {cfg.batch} x seq {cfg.seq}; lr {cfg.lr}",
             "tokens": cfg.tokens, "dqt_weights": cfg.dqt_weights,

@@ -5,7 +5,7 @@
 // Bound by HBM: every value is read and written once.  A block takes a few tokens and
 // a range of the heads of all tensors: it forms the tokens' cosines and sines in LDS
 // (once for all heads), then walks the values in the order of memory, 16 of a head per
-// thread and step (8 pairs, or 16 values that are copied), four steps in flight.
+// thread and step (8 pairs, or 16 values that are copied), two steps in flight.
 #include "dqt_launch.h"
 #include "rope.h"
 
@@ -41,7 +41,7 @@ __device__ __forceinline__ void store8(uint8_t* p, const float (&v)[8]) {
 }
 
 constexpr int kRopeTokens = 8;       // of a block at most
-constexpr int kRopeSteps = 4;
+constexpr int kRopeSteps = 2;
 
 template <class T, bool PAIRS>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {

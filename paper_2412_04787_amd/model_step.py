@@ -30,6 +30,9 @@ What runs where:
     feed-forward held for the backward, 6 in PyTorch; with ckpt8 = False gate and
     up themselves, 4 bytes); dqt_logprob_fwd / _bwd give the loss and the logits'
     gradient.
+  * With own_rope as well, queries and keys are rotated by dqt_rope_fwd / _bwd:
+    angles as exact fractions of a turn and cosines in fp32, where PyTorch's form
+    has angles in fp32 and rounds cosines to bf16.
 
 Initialisation (untimed): codes by Eq. 2-4 for the ternary grid from
 W0 ~ N(0, 0.02) (alpha = mean |W0|, q = Clip(Round(W0 / alpha), -1, 1));
@@ -64,8 +67,11 @@ class ModelConfig:
     # elements (the forward is the same; gradients through the product are off by
     # 0.7 % rms for normal values); False: as they are, in bf16
     ckpt8: bool = True
+    own_rope: bool = False     # (with own_ops) rotary positions in this library's kernel too
 
     def __post_init__(self):
+        if self.own_rope and not self.own_ops:
+            raise ValueError("own_rope needs own_ops")
         if self.kv_heads and (self.heads % self.kv_heads or (self.kv_heads != self.heads and not self.own_ops)):
             raise ValueError("kv_heads must divide heads, and grouped heads need own_ops")
 
@@ -114,6 +120,11 @@ MODELS = {
                                      ffn=5632, vocab=32000, batch=8, seq=2048, lr=3e-4, own_ops=True),
     "tiny_ops": ModelConfig(name="tiny_ops", layers=2, hidden=256, heads=4, kv_heads=2, ffn=512,
                             vocab=1000, batch=2, seq=128, lr=3e-4, own_ops=True),
+    # and with the rotary positions too
+    "llama24_h2048_rope": ModelConfig(name="llama24_h2048_rope", layers=24, hidden=2048, heads=16, ffn=5632,
+                                      vocab=32000, batch=8, seq=2048, lr=3e-4, own_ops=True, own_rope=True),
+    "tiny_rope": ModelConfig(name="tiny_rope", layers=2, hidden=256, heads=4, kv_heads=2, ffn=512,
+                             vocab=1000, batch=2, seq=128, lr=3e-4, own_ops=True, own_rope=True),
 }
 
 
@@ -256,6 +267,23 @@ class _OwnFns:
             return cls._cls
         torch = dqt._torch()
 
+        class Rotate(torch.autograd.Function):
+            """Queries and keys [T, heads, d] turned by their positions (int32 [T])."""
+
+            @staticmethod
+            def forward(ctx, q, k, pos, rope):
+                ctx.rope = rope
+                ctx.save_for_backward(pos)
+                out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k)]
+                dqt.dqt_rope_fwd(rope, [(q, out[0]), (k, out[1])], pos)
+                return tuple(out)
+
+            @staticmethod
+            def backward(ctx, dq, dk):
+                out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (dq, dk)]
+                dqt.dqt_rope_bwd(ctx.rope, [(dq.contiguous(), out[0]), (dk.contiguous(), out[1])], ctx.saved_tensors[0])
+                return out[0], out[1], None, None
+
         class Attn(torch.autograd.Function):
             """softmax(q k^T / sqrt(d)) v, causal, per packed sequence; q
             [T, heads, d], k and v [T, kv heads, d]."""
@@ -335,7 +363,7 @@ class _OwnFns:
                 dqt.dqt_logprob_bwd(logits, targets, stat, dlogp, dx)
                 return dx, None, None
 
-        cls._cls = (Attn, SwigluGroup, TokenLoss)
+        cls._cls = (Attn, SwigluGroup, TokenLoss, Rotate)
         return cls._cls
 
 
@@ -367,6 +395,7 @@ class DQTModel:
         dense = [self.emb, self.head, self.final_norm] + [p for n in self.norms for p in n]
         self.opt = torch.optim.AdamW(dense, lr=cfg.lr, betas=(0.9, 0.95), weight_decay=0.1)
         hd = H // cfg.heads
+        self.rope = dqt.rope(hd, base=cfg.rope_base, device=device) if cfg.own_rope else None
         inv = 1.0 / (cfg.rope_base ** (torch.arange(0, hd, 2, device=device, dtype=torch.float32) / hd))
         # (packed documents may be as long as the batch)
         rows = cfg.tokens if cfg.own_ops else cfg.seq
@@ -418,14 +447,16 @@ class DQTModel:
         hd = H // nh
         fn = _DQTGroupFn.get()
         if cfg.own_ops:
-            attn_fn, swiglu_fn, _ = _OwnFns.get()
+            attn_fn, swiglu_fn, _, rotate_fn = _OwnFns.get()
             if starts is None:
                 starts = self.starts
             else:      # (padding forms sequences of its own, mostly empty: every row is written)
                 starts = torch.cat((self.starts[:1], starts, self.starts[-1:]))
             tok = torch.arange(B * S, dtype=torch.int32, device=self.dev)
-            pos = (tok - starts[torch.searchsorted(starts[1:], tok, right=True)]).long()
-            cos, sin = self.cos[0, 0, pos][:, None], self.sin[0, 0, pos][:, None]
+            pos = tok - starts[torch.searchsorted(starts[1:], tok, right=True)]
+            if not cfg.own_rope:
+                pos = pos.long()
+                cos, sin = self.cos[0, 0, pos][:, None], self.sin[0, 0, pos][:, None]
         elif starts is not None:
             raise ValueError("packed documents need own_ops")
         h = F.embedding(tokens.reshape(-1), self.emb.to(torch.bfloat16))     # [T, H] bf16
@@ -435,7 +466,11 @@ class DQTModel:
             q, k, v = fn.apply(h, n_attn, grp["attn_in"])
             if cfg.own_ops:
                 q, k, v = (t.view(B * S, -1, hd) for t in (q, k, v))
-                a = attn_fn.apply(self._rope(q, cos, sin), self._rope(k, cos, sin), v, starts, self)
+                if cfg.own_rope:
+                    q, k = rotate_fn.apply(q, k, pos, self.rope)
+                else:
+                    q, k = self._rope(q, cos, sin), self._rope(k, cos, sin)
+                a = attn_fn.apply(q, k, v, starts, self)
                 a = a.view(B * S, H)
             else:
                 q, k, v = (t.view(B, S, nh, hd).transpose(1, 2) for t in (q, k, v))
