@@ -386,6 +386,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attn_kernel(KvAttnArg
 // 16 k + 8 (l / 32) + 0..7: the second product's B operand as they are, beside 16 bytes
 // of a value channel, whose tokens the cache keeps together.
 constexpr int kTileRows = 128;
+constexpr int kAhead = 6;
 
 // The tile of rank p, those of the longest sequences first: a block's time goes by the
 // pages that its sequence has, and the long ones that began last ended the kernel (8
@@ -547,11 +548,19 @@ __global__ __launch_bounds__(256 * GR, 2) void kv_tile_kernel(KvAttnArgs a) {
 #pragma unroll
         for (int nb = 0; nb < 2; ++nb) s[nb] = splat(0.0f);
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb)
+        for (int ks = 0; ks < NK; ++ks)
 #pragma unroll
-          for (int ks = 0; ks < NK; ++ks)
+          for (int nb = 0; nb < 2; ++nb)
             s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
                 __builtin_bit_cast(f16x8, *(const lds_i32x4*)(kread + S * KB + nb * 32 * KROW + 32 * ks)), qf[ks], s[nb], 0, 0, 0);
+        // (reads run six ahead of the products: one behind each was waited for)
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+        for (int e = 0; e < 2 * NK - kAhead; ++e) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
       }
       if (i + 1 < rounds) {
         stage_k(1 - S);
@@ -598,6 +607,17 @@ __global__ __launch_bounds__(256 * GR, 2) void kv_tile_kernel(KvAttnArgs a) {
             o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
                 __builtin_bit_cast(f16x8, *(const lds_i32x4*)(vread + S * VB + db * 32 * VROW + 32 * kk)), p, o[db], 0, 0, 0);
         }
+        // the first values' reads, then the powers of 16 keys beside the product of the
+        // 16 before, whose reads are ND ahead
+        __builtin_amdgcn_sched_group_barrier(0x100, ND, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 28, 0);
+#pragma unroll
+        for (int e = 0; e < 3 * ND; ++e) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x402, 28 / ND, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, ND, 0);
         l += sum * exp2_int(-ev);
       }
       __syncthreads();
@@ -741,7 +761,7 @@ void kv_attn_plan(KvAttnArgs* a) {
     // pages each and about 4 more to begin and end
     const int64_t blocks = seqs * ((rows + seqs * kTileRows - 1) / (seqs * kTileRows)) * a->c.kv_heads;
     int64_t best = INT64_MAX;
-    for (int64_t s = 1; s <= 32 && s * 4 <= pages + 3; ++s) {
+    for (int64_t s = 1; s <= (blocks < 2048 ? 32 : 1) && s * 4 <= pages + 3; ++s) {
       const int64_t cost = (blocks * s + 255) / 256 * ((pages + s - 1) / s + 8) + (s > 1 ? 4 + rows * a->c.kv_heads * s / 20000 : 0);
       if (cost < best) {
         best = cost;

@@ -723,6 +723,9 @@ def dqt_kv_attn(cache: KvCache, batch: KvBatch, Q, O, lse=None, ws=None, stream=
 
 
 def _pages(x) -> np.ndarray:
+    x = np.asarray(x)
+    if x.size and (x.dtype.kind not in "iu" or x.min() < -2 ** 31 or x.max() >= 2 ** 31):
+        raise ValueError(f"expected page numbers, got {x.dtype}")
     return np.ascontiguousarray(x, dtype=np.int32)
 
 

@@ -221,6 +221,14 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         dqt.kv_batch(torch.zeros((2, 3), dtype=torch.int32), torch.zeros(2, dtype=torch.int32), 2, 4)
 
 
+def test_binding_refuses_what_is_no_page():
+    for bad in ([1 << 32], [-(1 << 40)], [1.0], np.array([1 << 35])):
+        with pytest.raises(ValueError):
+            dqt.dqt_kv_copy([], bad, [1])
+    with pytest.raises(ValueError):
+        dqt.dqt_kv_copy([], [1, 2], [3])
+
+
 # ------------------------------------------------------------------ pages
 
 def consistent(p, tables):
