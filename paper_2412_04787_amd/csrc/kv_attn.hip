@@ -491,14 +491,18 @@ __global__ __launch_bounds__(256 * GR, 2) void kv_tile_kernel(KvAttnArgs a) {
         *(lds_i32x4*)(lds + st * KB + row * KROW + 16 * (col + e)) = __builtin_bit_cast(i32x4, widen8<E4M3>(kraw[c][2 * e], kraw[c][2 * e + 1]));
     }
   };
-  auto stage_v = [&](int st, int at) {
+  auto cut_v = [&](int at) {
+    if (at + kPage > t.q.lk) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vraw[c][e] &= (int)keep_bytes(t.q.lk - at - 16 * (lane >> 4), e);
+    }
+  };
+  auto stage_v = [&](int st) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int row = vrow + 64 * c, col = 2 * (lane >> 4);
-      if (at + kPage > t.q.lk) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) vraw[c][e] &= (int)keep_bytes(t.q.lk - at - 8 * col, e);
-      }
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         *(lds_i32x4*)(lds + 2 * KB + st * VB + row * VROW + 16 * (col + e)) = __builtin_bit_cast(i32x4, widen8<E4M3>(vraw[c][2 * e], vraw[c][2 * e + 1]));
@@ -536,7 +540,8 @@ __global__ __launch_bounds__(256 * GR, 2) void kv_tile_kernel(KvAttnArgs a) {
     load_k(0);
     load_v(0);
     stage_k(0);
-    stage_v(0, at_of(0));
+    cut_v(at_of(0));
+    stage_v(0);
     load_k(1);
     load_v(1);
     __syncthreads();
@@ -544,30 +549,29 @@ __global__ __launch_bounds__(256 * GR, 2) void kv_tile_kernel(KvAttnArgs a) {
       constexpr int S = decltype(stage)::value;
       const int at = at_of(i);
       const bool there = __builtin_amdgcn_readlane(page, i) >= 0 && at <= lim_hi;
-      if (there) {
+      // the scores, beside them the staging of what comes (behind the last page: zeros)
+      cut_v(at + GR * kPage);
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb) s[nb] = splat(0.0f);
+      for (int nb = 0; nb < 2; ++nb) s[nb] = splat(0.0f);
 #pragma unroll
-        for (int ks = 0; ks < NK; ++ks)
+      for (int ks = 0; ks < NK; ++ks)
 #pragma unroll
-          for (int nb = 0; nb < 2; ++nb)
-            s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                __builtin_bit_cast(f16x8, *(const lds_i32x4*)(kread + S * KB + nb * 32 * KROW + 32 * ks)), qf[ks], s[nb], 0, 0, 0);
-        // (reads run six ahead of the products: one behind each was waited for)
-        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+        for (int nb = 0; nb < 2; ++nb)
+          s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+              __builtin_bit_cast(f16x8, *(const lds_i32x4*)(kread + S * KB + nb * 32 * KROW + 32 * ks)), qf[ks], s[nb], 0, 0, 0);
+      stage_k(1 - S);
+      stage_v(1 - S);
+      // (reads run six ahead of the products: one behind each was waited for)
+      __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
 #pragma unroll
-        for (int e = 0; e < 2 * NK - kAhead; ++e) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+      for (int e = 0; e < 2 * NK; ++e) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (e < 2 * NK - kAhead) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, E4M3 ? 2 : 5, 0);
+        if (e >= 2 * NK - kAhead) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
       }
-      if (i + 1 < rounds) {
-        stage_k(1 - S);
-        stage_v(1 - S, at + GR * kPage);
-        load_k(i + 2);
-        load_v(i + 2);
-      }
+      load_k(i + 2);
+      load_v(i + 2);
       if (there) {
         if (at + kPage - 1 > lim_lo) {
           const int left = lim - at - 8 * h;       // the last key seen, from this lane's first
