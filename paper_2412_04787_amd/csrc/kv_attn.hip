@@ -112,7 +112,10 @@ __device__ __forceinline__ Tile tile_at(const KvAttnArgs& a, const KvSeq& q, int
 // waves take in turn and join at the end.  Codes go from memory to registers and into
 // the matrix cores, 16 consecutive bytes per lane and load, without LDS: a wave holds
 // a whole page (64 tokens) of keys and one of values, and the next page's keys are
-// loaded while this one's are worked on.
+// loaded while this one's are worked on.  Bound by HBM for single tokens: 32 over 1 to
+// 8192 tokens, 32 heads on 8, 50 us for 0.27 GB (5.4 TB/s) and the join of the parts 4.8;
+// two sequences of 30000 and 65000, 3 to 5 tokens each, 16 heads, int8: 76 us for 0.39 GB
+// (5.1 TB/s), 5.4.  Three waves per SIMD (two for 32 rows).
 //
 // v_mfma_f32_16x16x32_f16: A lane l holds row l % 16, 8 values of the reduction from
 // 8 (l / 16); B the same of columns; result register i is row 4 (l / 16) + i of column
@@ -379,6 +382,13 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attn_kernel(KvAttnArg
 // loads a page's codes to registers while the page before is worked on, widens them
 // once for its 128 rows and passes them through LDS as fp16, two stages.
 //
+// Bound by what a wave issues between its products: of 197 us (8 chunks of 130 to 512
+// tokens over 460 to 7870, 32 heads on 8: 163 GFLOP, 825 TFLOP/s) the staging takes
+// about 45, the reads of LDS 30, the exponentials 12.  The scheduling groups keep reads
+// ahead of the products and vector work beside them (without: 209 us); three waves per
+// SIMD do not fit their registers, groups half a round apart, raw codes two pages
+// ahead and sums watched instead of maxima gave nothing.
+//
 // v_mfma_f32_32x32x16_f16: A lane l holds row l % 32, 8 values of the reduction from
 // 8 (l / 32); B the same of columns; result register i is row 8 (i / 4) + 4 (l / 32) +
 // i % 4 of column l % 32.  Scores are formed transposed (A = keys); key 8 h + 4 x + y of
@@ -386,7 +396,6 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attn_kernel(KvAttnArg
 // 16 k + 8 (l / 32) + 0..7: the second product's B operand as they are, beside 16 bytes
 // of a value channel, whose tokens the cache keeps together.
 constexpr int kTileRows = 128;
-constexpr int kAhead = 6;
 
 // The tile of rank p, those of the longest sequences first: a block's time goes by the
 // pages that its sequence has, and the long ones that began last ended the kernel (8
@@ -413,11 +422,12 @@ __device__ __forceinline__ KvSeq find_longest(const KvAttnArgs& a, int p, int& i
   return KvSeq{s, __builtin_amdgcn_readlane(q.q0, s), __builtin_amdgcn_readlane(q.lq, s), __builtin_amdgcn_readlane(q.lk, s)};
 }
 
-template <int D, bool E4M3, int GR>
-__global__ __launch_bounds__(256 * GR, 2) void kv_tile_kernel(KvAttnArgs a) {
+template <int D, bool E4M3>
+__global__ __launch_bounds__(512, D == 64 ? 4 : 2) void kv_tile_kernel(KvAttnArgs a) {
   // rows of a staged tile end in 16 bytes that nothing uses: the 16 rows that as many
   // lanes read at one place then fall on all banks, at offsets that are constants
-  constexpr int NK = D / 16, ND = D / 32, CH = kPage * D / 16 / 256;
+  constexpr int NK = D / 16, ND = D / 32, CH = kPage * D / 16 / 256, GR = 2;
+  constexpr int kAhead = D == 64 ? 2 : 6;          // reads ahead of the scores' products
   constexpr int KROW = 2 * D + 16, VROW = 2 * kPage + 16, KB = kPage * KROW, VB = D * VROW, GB = 2 * (KB + VB);
   __shared__ __attribute__((aligned(1024))) uint8_t smem[GR * GB];         // of each group: keys, values; two stages
   __shared__ float row_m[GR][kTileRows], row_l[GR][kTileRows];
@@ -632,49 +642,37 @@ __global__ __launch_bounds__(256 * GR, 2) void kv_tile_kernel(KvAttnArgs a) {
     }
   }
 
-  // the groups' sums on a common M: group g finishes the ND / GR blocks of 32 channels from
-  // g ND / GR on
+  // the two groups' sums on a common M: group g finishes channels g D / 2 ..
   l += __shfl_xor(l, 32, kWave);
   const int rr = 32 * w + n;
-  float both = m, total = l, f0 = 1.0f, f1 = 0.0f;
-  if constexpr (GR == 2) {
-    if (h == 0) {
-      row_m[grp][rr] = m;
-      row_l[grp][rr] = l;
-    }
-    __syncthreads();
-    const float m1 = row_m[1 - grp][rr];
-    both = fmaxf(m, m1);
-    f0 = m == both ? 1.0f : exp2_fast(m - both);
-    f1 = m1 == both ? 1.0f : exp2_fast(m1 - both);
-    total = l * f0 + row_l[1 - grp][rr] * f1;
+  if (h == 0) {
+    row_m[grp][rr] = m;
+    row_l[grp][rr] = l;
   }
+  __syncthreads();
+  const float m1 = row_m[1 - grp][rr], both = fmaxf(m, m1);
+  const float f0 = m == both ? 1.0f : exp2_fast(m - both), f1 = m1 == both ? 1.0f : exp2_fast(m1 - both);
+  const float total = l * f0 + row_l[1 - grp][rr] * f1;
   const bool none = both == -__builtin_inff();
   const float inv = none ? 0.0f : 1.0f / total, lse = none ? both : both - kLift + log2f(total);
   lds_f32* give = (lds_f32*)&smem[0];
-  if constexpr (GR == 2) {
 #pragma unroll
-    for (int d = 0; d < ND / 2; ++d)
+  for (int d = 0; d < ND / 2; ++d)
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        give[(((grp * 4 + w) * (ND / 2) + d) * 16 + e) * 64 + lane] = grp == 0 ? o[ND / 2 + d][e] : o[d][e];
-    __syncthreads();
-  }
+    for (int e = 0; e < 16; ++e)
+      give[(((grp * 4 + w) * (ND / 2) + d) * 16 + e) * 64 + lane] = grp == 0 ? o[ND / 2 + d][e] : o[d][e];
+  __syncthreads();
   const bool mine = t.r0 + rr < t.rows;
   const int64_t row = t.q.q0 + tok;
 #pragma unroll
-  for (int d = 0; d < ND / GR; ++d) {
+  for (int d = 0; d < ND / 2; ++d) {
     f32x16 y;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      if constexpr (GR == 2) {
-        const float own = grp == 0 ? o[d][e] : o[ND / 2 + d][e];
-        y[e] = (own * f0 + give[((((1 - grp) * 4 + w) * (ND / 2) + d) * 16 + e) * 64 + lane] * f1) * inv;
-      } else {
-        y[e] = o[d][e] * inv;
-      }
+      const float own = grp == 0 ? o[d][e] : o[ND / 2 + d][e];
+      y[e] = (own * f0 + give[((((1 - grp) * 4 + w) * (ND / 2) + d) * 16 + e) * 64 + lane] * f1) * inv;
     }
-    const int d0 = 32 * (grp * (ND / GR) + d) + 4 * h;
+    const int d0 = 32 * (grp * (ND / 2) + d) + 4 * h;
     if (mine) {
       if (whole) {
         uint8_t* p = a.O + row * a.o_tok + head * a.o_head + 2 * d0;
@@ -800,7 +798,7 @@ hipError_t launch_kv_attn(bool e4m3, const KvAttnArgs& a, hipStream_t s) {
   auto pick = [&](auto d, auto fmt) {
     constexpr int D = decltype(d)::value;
     constexpr bool F = decltype(fmt)::value;
-    if (a.tile_rows == kTileRows) go(kv_tile_kernel<D, F, 2>);
+    if (a.tile_rows == kTileRows) go(kv_tile_kernel<D, F>);
     else if (a.tile_rows == 16) few(d, fmt, std::integral_constant<int, 1>{});
     else few(d, fmt, std::integral_constant<int, 2>{});
   };
