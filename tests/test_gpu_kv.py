@@ -335,6 +335,71 @@ def test_attention_many_sequences(lib):
     run_attn("int8", 128, 2, 2, [1] * 130, rng.integers(1, 140, 130).tolist(), seed=25, none=True)
 
 
+def test_attention_many_sequences_of_many_rows(lib):
+    """More sequences than lanes, each with more rows than a tile of few rows: chunks,
+    and single tokens of large groups without starts."""
+    rng = np.random.default_rng(4)
+    lq = rng.integers(0, 70, 90).tolist()
+    lk = [x + int(c) for x, c in zip(lq, rng.integers(0, 150, 90))]
+    log("cache attention: 90 sequences of chunks, 70 of groups of 200")
+    run_attn("int8", 64, 2, 1, lq, lk, seed=42)
+    run_attn("e4m3", 64, 200, 1, [1] * 70, rng.integers(0, 140, 70).tolist(), seed=43, none=True)
+    run_attn("e4m3", 128, 260, 2, [1, 1], [300, 70], seed=44, none=True)
+
+
+def test_thousands_of_sequences(lib):
+    """3000 sequences of one new token: every page is the plain implementation's, every
+    row that of its sequence."""
+    log("append and attention: 3000 sequences")
+    rng, gen = np.random.default_rng(6), torch.Generator().manual_seed(6)
+    n = 3000
+    lens = rng.integers(0, 70, n)
+    table, pages = page_table(rng, lens.tolist())
+    c = random_cache(gen, pages, 1, 64, "e4m3")
+    h = device_cache(c)
+    K, V, Q = (torch.randn((n, x, 64), generator=gen).to(torch.bfloat16) for x in (1, 1, 2))
+    b = dqt.kv_batch(dev32(table), dev32(lens), n, 2)
+    O = torch.full((n, 2, 64), SENT, dtype=torch.bfloat16, device=DEV)
+    dqt.dqt_kv_append(h, b, K.to(DEV), V.to(DEV))
+    dqt.dqt_kv_attn(h, b, Q.to(DEV), O, None, dqt.workspace(dqt.dqt_kv_attn_workspace(h, b)))
+    torch.cuda.synchronize()
+    for i in range(n):
+        if lens[i]:
+            c.write(table[i], lens[i] - 1, K[i:i + 1].float(), V[i:i + 1].float())
+    same_cache(h, c)
+    got = O.double().cpu()
+    for i in range(0, n, 7):
+        k, v, there = c.values(table[i], int(lens[i]), pages)
+        r = R.attention(Q[i:i + 1], k, v, there, 0.125, True)
+        assert ((got[i:i + 1] - r["O"]).abs() <= r["t_O"]).all(), (i, int(lens[i]))
+
+
+def test_starts_and_lengths_out_of_range(lib):
+    """Values that break the rules are clamped: sequences that follow them are right, and
+    tokens outside every sequence stay as they are."""
+    log("append and attention: starts and lengths out of range")
+    gen = torch.Generator().manual_seed(9)
+    c = random_cache(gen, 6, 1, 64, "int8")
+    table = np.arange(6, dtype=np.int32).reshape(3, 2)
+    for heads in (1, 64):                             # tiles of few rows, and of many
+        for qs, lk, good in (([-7, 3, 5, 9], [50, 90, 1 << 30], {0: (0, 3, 50), 1: (3, 5, 90), 2: (5, 9, 128)}),
+                             ([0, 1 << 30, 4, 6], [-5, 100, 64], {2: (4, 6, 64)}),
+                             ([9, 9, 2, 2 ** 31 - 1], [3, 100, 128], {2: (2, 9, 128)})):
+            h = device_cache(c)
+            Q = torch.randn((9, heads, 64), generator=gen).to(torch.bfloat16)
+            O = torch.full((9, heads, 64), SENT, dtype=torch.bfloat16, device=DEV)
+            b = dqt.kv_batch(dev32(table), dev32(lk), 9, heads, dev32(qs))
+            dqt.dqt_kv_attn(h, b, Q.to(DEV), O, None, dqt.workspace(dqt.dqt_kv_attn_workspace(h, b)))
+            torch.cuda.synchronize()
+            for s, (x, y, n) in good.items():
+                k, v, there = c.values(table[s], n, 6)
+                r = R.attention(Q[x:y], k, v, there, 0.125, True)
+                assert ((O[x:y].double().cpu() - r["O"]).abs() <= r["t_O"]).all(), (heads, qs, s)
+            kv = torch.randn((9, 1, 64), generator=gen).to(torch.bfloat16).to(DEV)
+            dqt.dqt_kv_append(h, dqt.kv_batch(dev32(table), dev32(lk), 9, 1, dev32(qs)), kv, kv)
+            torch.cuda.synchronize()
+
+
 def test_attention_long(lib):
     log("cache attention: one token over 20001, five over 9000, a chunk over 5000; room for more than there is")
     run_attn("e4m3", 128, 4, 1, [1], [20001], seed=27)
