@@ -530,6 +530,16 @@ def dqt_attn_bwd(a: DqtAttn, Q, K, V, O, lse, dO, dQ, dK, dV, ws, stream=None):
 
 # ----------------------------------------------------------------- rotary positions and the 8-bit cache
 
+def _current(t):
+    """The current device, which has to be t's, and the handle of torch's current stream there
+    (_here and _stream in one, without their second looks: half a microsecond of a call)."""
+    c = _torch()._C
+    dev = t.get_device()
+    if dev < 0 or dev != c._cuda_getDevice():
+        _here(t)
+    return dev, c._cuda_getCurrentRawStream(dev)
+
+
 def _row(t, n, h, d, dev):
     """The dqt_rows (as bytes) of a bf16 tensor [n, h, d] on device dev with any token and head strides."""
     if t.get_device() != dev:
@@ -556,7 +566,8 @@ class Rope:
     dqt_rope_freqs); pairs: the values 2 i and 2 i + 1 turn together, else i and i + rot / 2."""
 
     def __init__(self, freq, d: int, pairs: bool = False, amp: float = 1.0):
-        _bufs(_here(freq), (freq, 8, _torch().int64))
+        self.dev = _here(freq)
+        _bufs(self.dev, (freq, 8, _torch().int64))
         if freq.dim() != 1:
             raise ValueError("expected freq of shape [rot / 2]")
         self.freq, self.d = freq, d
@@ -577,7 +588,10 @@ def _rope(fn, call, rope: Rope, pairs, pos, stream):
     if not pairs:
         raise ValueError("expected at least one tensor")
     x0 = pairs[0][0]
-    dev, dt, tokens, width = _here(x0, rope.freq), x0.dtype, x0.shape[0], rope.d
+    dev, handle = _current(x0)
+    dt, tokens, width = x0.dtype, x0.shape[0], rope.d
+    if rope.dev != dev:
+        raise ValueError(f"frequencies on device {rope.dev}, tensors on device {dev}")
     io = b""
     for x, y in pairs:
         shape = x.shape
@@ -602,7 +616,8 @@ def _rope(fn, call, rope: Rope, pairs, pos, stream):
                             not pos.is_contiguous()):
         raise ValueError(f"expected {tokens} contiguous int32 positions on device {dev}, got {pos.dtype} {tuple(pos.shape)} "
                          f"with strides {pos.stride()} on {pos.device}")
-    st = call(rope.ref, len(pairs), io, dtype_code(x0), tokens, _addr(pos), _stream(stream))
+    st = call(rope.ref, len(pairs), io, dtype_code(x0), tokens, None if pos is None else pos.data_ptr(),
+              handle if stream is None else stream.cuda_stream)
     if st != DQT_OK:
         raise DqtError(fn, st)
 
@@ -680,30 +695,33 @@ def kv_batch(table, kv_len, q_tokens: int, heads: int, q_start=None, max_len: in
     return KvBatch(desc, (table, kv_len, q_start), scale)
 
 
-def _kv(cache: KvCache, batch: KvBatch) -> int:
-    """Their device; the batch's scale is that of the cache's heads unless it was given."""
-    dev = _here(cache.K)
-    if batch.dev != dev:
-        raise ValueError(f"batch on device {batch.dev}, cache on device {dev}")
+def _kv(cache: KvCache, batch: KvBatch):
+    """Their device and the stream's handle; the batch's scale is that of the cache's heads
+    unless it was given."""
+    now = _current(cache.K)
+    if batch.dev != now[0]:
+        raise ValueError(f"batch on device {batch.dev}, cache on device {now[0]}")
     if batch.scale is None:
         batch.desc.scale = cache.d ** -0.5
-    return dev
+    return now
 
 
 def dqt_kv_append(cache: KvCache, batch: KvBatch, K, V, rope: Rope | None = None, Q=None, Qr=None, stream=None):
     """K, V: [q_tokens, kv_heads, d], Q and Qr (with rope): [q_tokens, heads, d], bf16 with any token
     and head strides.  Qr may be Q."""
-    dev, n, kvh, d = _kv(cache, batch), batch.q_tokens, cache.kv_heads, cache.d
+    dev, handle = _kv(cache, batch)
+    n, kvh, d = batch.q_tokens, cache.kv_heads, cache.d
     if (Q is None) != (Qr is None):
         raise ValueError("Q and Qr go together")
-    if rope is not None and rope.freq.get_device() != dev:
-        raise ValueError(f"frequencies on {rope.freq.device}, cache on device {dev}")
+    if rope is not None and rope.dev != dev:
+        raise ValueError(f"frequencies on device {rope.dev}, cache on device {dev}")
     q = qr = None
     if Q is not None:
         q, qr = _row(Q, n, batch.heads, d, dev), _row(Qr, n, batch.heads, d, dev)
-    _check("dqt_kv_append",
-           load().dqt_kv_append(cache.ref, batch.ref, _row(K, n, kvh, d, dev), _row(V, n, kvh, d, dev),
-                                None if rope is None else rope.ref, q, qr, _stream(stream)))
+    st = load().dqt_kv_append(cache.ref, batch.ref, _row(K, n, kvh, d, dev), _row(V, n, kvh, d, dev),
+                              None if rope is None else rope.ref, q, qr, handle if stream is None else stream.cuda_stream)
+    if st != DQT_OK:
+        raise DqtError("dqt_kv_append", st)
 
 
 def dqt_kv_attn_workspace(cache: KvCache, batch: KvBatch) -> int:
@@ -714,12 +732,15 @@ def dqt_kv_attn_workspace(cache: KvCache, batch: KvBatch) -> int:
 def dqt_kv_attn(cache: KvCache, batch: KvBatch, Q, O, lse=None, ws=None, stream=None):
     """Q, O: [q_tokens, heads, d], bf16 with any token and head strides; lse: contiguous fp32
     [heads, q_tokens] or None."""
-    dev, n, h, d = _kv(cache, batch), batch.q_tokens, batch.heads, cache.d
+    dev, handle = _kv(cache, batch)
+    n, h, d = batch.q_tokens, batch.heads, cache.d
     if lse is not None:
         _bufs(dev, (lse, 4 * h * n, _torch().float32))
-    _check("dqt_kv_attn",
-           load().dqt_kv_attn(cache.ref, batch.ref, _row(Q, n, h, d, dev), _row(O, n, h, d, dev), _addr(lse), _addr(ws),
-                              _ws_bytes(dev, ws), _stream(stream)))
+    st = load().dqt_kv_attn(cache.ref, batch.ref, _row(Q, n, h, d, dev), _row(O, n, h, d, dev),
+                            None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(),
+                            _ws_bytes(dev, ws), handle if stream is None else stream.cuda_stream)
+    if st != DQT_OK:
+        raise DqtError("dqt_kv_attn", st)
 
 
 def _pages(x) -> np.ndarray:
