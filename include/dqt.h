@@ -447,7 +447,7 @@ typedef struct {
  *      max_len, pages outside the cache (-1 for instance) hold no tokens (what
  *      is written to them is lost), new tokens that come before position 0 see
  *      nothing, and neither they nor their rotated queries are written.
- *   max_len: no kv_len is larger; at most 64 table_stride and 2^31 - 64.  The work
+ *   max_len: no kv_len is larger; at most 64 table_stride and 2^31 - 1024.  The work
  *      is laid out for it (which a captured graph keeps), so close is better.
  *   heads: query heads, a multiple of the cache's kv_heads, at most 1024; query
  *      head h reads key head h / (heads / kv_heads).  q_tokens * heads < 2^31.

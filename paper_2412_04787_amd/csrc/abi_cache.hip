@@ -81,7 +81,7 @@ dqt_status check_batch(const dqt_kv_cache* c, const dqt_kv_batch* b, dqt::KvArgs
   if (b->n_seq < 0 || b->table_stride < 0 || b->q_tokens < 0 || b->q_tokens > kMaxTokens) return DQT_ERR_SHAPE;
   if (b->heads < 1 || b->heads > 1024 || b->heads % c->kv_heads != 0) return DQT_ERR_SHAPE;
   if (b->q_tokens * b->heads > kMaxTokens) return DQT_ERR_SHAPE;
-  if (b->max_len < 0 || b->max_len > kMaxTokens - 63 || b->max_len > (int64_t)DQT_KV_PAGE * b->table_stride) return DQT_ERR_SHAPE;
+  if (b->max_len < 0 || b->max_len > kMaxTokens - 1023 || b->max_len > (int64_t)DQT_KV_PAGE * b->table_stride) return DQT_ERR_SHAPE;
   if (b->q_start == nullptr && b->q_tokens != b->n_seq) return DQT_ERR_SHAPE;
   if (b->q_tokens > 0 && b->n_seq == 0) return DQT_ERR_SHAPE;
   if (b->n_seq > 0 && (b->kv_len == nullptr || (b->max_len > 0 && b->table == nullptr))) return DQT_ERR_NULL;

