@@ -37,9 +37,15 @@ __device__ __forceinline__ void load16(const uint8_t* p, float (&v)[8]) { widen8
 // values on their scale (not NaN) -> four codes
 template <bool E4M3>
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
-  if constexpr (E4M3) return f32x4_to_e4m3x4(a, b, c, d);
-  auto lim = [](float x) { return fminf(fmaxf(x, -127.0f), 127.0f); };
-  return f32x4_to_i8x4(lim(a), lim(b), lim(c), lim(d));
+  if constexpr (E4M3) {
+    auto q = [](float v) { return __builtin_amdgcn_fmed3f(v, -448.0f, 448.0f); };
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(q(a), q(b), 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(q(c), q(d), w, true);
+    return (uint32_t)w;
+  }
+  // (1.5 2^23 + v ends in v, rounded to nearest even)
+  auto q = [](float v) { return __float_as_uint(__builtin_amdgcn_fmed3f(v, -127.0f, 127.0f) + 12582912.0f); };
+  return __builtin_amdgcn_perm(q(b), q(a), 0x0C0C0400u) | (__builtin_amdgcn_perm(q(d), q(c), 0x0C0C0400u) << 16);
 }
 // four codes that stand for x -> those of x / 2^n
 template <bool E4M3>
@@ -50,9 +56,12 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
     v[i] = (E4M3 ? e4m3_to_f32((w >> (8 * i)) & 0xFFu) : (float)(int8_t)(w >> (8 * i))) * f;
   return codes4<E4M3>(v[0], v[1], v[2], v[3]);
 }
-__device__ __forceinline__ float finite_abs(float x) {
-  const float a = fabsf(x);
-  return a <= 3.402823466e38f ? a : 0.0f;
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+constexpr uint32_t kInfBits = 0x7F800000u;
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, off, kWave));
+  return v;
 }
 
 // A token's run of 16 values: rotated pairs 8 item .. + 7, or 16 values as they are.
@@ -150,7 +159,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
   constexpr int VROW = kPage + 4;
   __shared__ __attribute__((aligned(16))) float2 cs[kTurnTokens * CROW];
   __shared__ uint32_t vt[D * VROW / 4];              // the values' codes, [channel][token]
-  __shared__ float red[4];
+  __shared__ uint32_t red[4];
   __shared__ int stood;
   // blocks of keys, of values, of the queries of each half of the page
   const int tid = threadIdx.x, part = (int)blockIdx.y / a.c.kv_heads, kvh = (int)blockIdx.y - part * a.c.kv_heads;
@@ -226,24 +235,44 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
       }
     }
   }
-  float most = 0.0f;
+  // the block's largest |x|, as bits
+  auto largest = [&] {
+    uint32_t m = 0;
 #pragma unroll
-  for (int st = 0; st < 4; ++st)
+    for (int st = 0; st < 4; ++st)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) most = fmaxf(most, finite_abs(x[st][e]));
-  most = wave_max(most);
-  if ((tid & 63) == 0) red[tid >> 6] = most;
-  __syncthreads();
-  const int was = stood, e = max(scale_exp<E4M3>(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]))), was);
+      for (int e = 0; e < 8; ++e) m = max(m, abs_bits(x[st][e]));
+    m = wave_max_u32(m);
+    if ((tid & 63) == 0) red[tid >> 6] = m;
+    __syncthreads();
+    return max(max(red[0], red[1]), max(red[2], red[3]));
+  };
+  uint32_t most = largest();
+  if (most >= kInfBits) {
+    // (rare: what is not finite does not count; then it is held as the largest code, NaN as 0)
+    float keep[4][8];
+#pragma unroll
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = x[st][e];
+        keep[st][e] = v != v ? 0.0f : __builtin_amdgcn_fmed3f(v, -3.402823466e38f, 3.402823466e38f);
+        if (abs_bits(v) >= kInfBits) x[st][e] = 0.0f;
+      }
+    __syncthreads();
+    most = largest();
+#pragma unroll
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[st][e] = keep[st][e];
+  }
+  const int was = stood, e = max(scale_exp<E4M3>(__uint_as_float(most)), was);
   const bool grows = lo > 0 && e > was;
   const float inv = exp2_int(-e), f = exp2_int(max(was - e, -126));
   if (tid == 0) *sc = exp2_int(e);
   uint8_t* dst = (keys ? a.c.K : a.c.V) + (page * a.c.kv_heads + kvh) * (int64_t)(kPage * D);
   auto codes = [&](const float (&y)[8], int from) {
-    float z[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) z[b] = y[from + b] == y[from + b] ? y[from + b] * inv : 0.0f;
-    return codes4<E4M3>(z[0], z[1], z[2], z[3]);
+    return codes4<E4M3>(y[from] * inv, y[from + 1] * inv, y[from + 2] * inv, y[from + 3] * inv);
   };
   if (keys) {
 #pragma unroll
