@@ -493,7 +493,7 @@ dqt_status dqt_kv_append(const dqt_kv_cache* c, const dqt_kv_batch* b, const dqt
  * strides and lse as for dqt_attn_fwd.  Q and O are bf16.  Codes enter the matrix
  * products as they are, in 16-bit floating point which holds them exactly; the
  * queries on a power of two of their largest value (exactly, but for values below
- * 2^-31 of it), the probabilities times the values' scale relative to the largest such
+ * 2^-31 of it or 2^-57), the probabilities times the values' scale relative to the largest such
  * product so far (each off by 2^-11 of itself at most, those below 2^-22 of the
  * largest by 2^-33 of it); sums are fp32.
  * The values' scales of one sequence and head lie within 2^100 of each other.

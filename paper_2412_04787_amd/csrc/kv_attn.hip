@@ -9,8 +9,8 @@
 //
 // Both products run on the matrix cores in 16-bit floating point (fp16), which holds
 // every code exactly; the row of Q is brought to 2^14 .. 2^15 by a power of two (bf16
-// values fit, those below 2^-31 of the row's largest lose bits), and w, at most 2^14,
-// is off by 2^-11 of itself (below 2^-14, which is 2^-22 of the largest, by 2^-25).
+// values fit, those below 2^-31 of the row's largest or 2^-57 lose bits), and w, at most
+// 2^14, is off by 2^-11 of itself (below 2^-14, which is 2^-22 of the largest, by 2^-25).
 // In bf16 it would be off by 2^-8, as much as the result's own rounding.
 #include "kv_common.h"
 
@@ -56,8 +56,9 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   const f32x2_t v = {lo, hi};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
 }
-// the power of two k with 2^14 <= most 2^-k < 2^15 (no less than -40: smaller rows
-// need no more)
+// the power of two k with 2^14 <= most 2^-k < 2^15 (no less than -40: times the smallest
+// scales of a call and of a page, 2^-20 and 2^-64, 2^k is still a normal number, which c
+// has to be where scores are -inf)
 __device__ __forceinline__ int row_shift(float most) {
   return max((int)(__float_as_uint(most) >> 23) - 127 - 14, -40);
 }
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attn_kernel(KvAttnArg
   // 32 over 1 to 8192: 55.6 -> 57.4)
   const bool one = !ONCE && a.tiles == a.c.n_seq;
   int early = -1;
-  if (one && first + wave + 4 * lane < min(first + a.chunk, a.c.table_stride))
+  if (one && first + wave + 4 * lane < min(first + a.chunk, (a.c.max_len + kPage - 1) / kPage))
     early = a.c.table[(int64_t)(id - split * a.tiles) * a.c.table_stride + first + wave + 4 * lane];
   const Tile t = tile_at(a, kv_find(a.c, id - split * a.tiles, a.c.group, ROWS, 1, item), item);
   if (item < 0 || t.r0 >= t.rows) return;

@@ -400,6 +400,27 @@ def test_starts_and_lengths_out_of_range(lib):
             torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("rows", [1, 3, 40])
+def test_no_table(lib, rows):
+    """max_len = 0 needs no table, whatever table_stride says: nothing is seen, nothing is written."""
+    n, heads, kvh, d = 3, 8, 2, 64
+    h = dqt.kv_cache(2, kvh, d, FMT["e4m3"], device=DEV)
+    h.K.view(torch.uint8).fill_(3)
+    h.scales.fill_(1.0)
+    x = torch.randn(n * rows, heads, d, dtype=torch.bfloat16, device=DEV)
+    kv_len, q_start = dev32([0, rows, 9]), dev32(starts([rows] * n))
+    desc = dqt.DqtKvBatch(None, kv_len.data_ptr(), None if rows == 1 else q_start.data_ptr(), n * rows, 0, n, 1 << 20, heads, 1,
+                          0.125, 0)
+    batch = dqt.KvBatch(desc, (kv_len, q_start), 0.125)
+    o, lse = torch.full_like(x, SENT), torch.full((heads, n * rows), SENT, device=DEV)
+    dqt.dqt_kv_append(h, batch, x[:, :kvh], x[:, :kvh])
+    assert dqt.dqt_kv_attn_workspace(h, batch) == 0
+    dqt.dqt_kv_attn(h, batch, x, o, lse)
+    torch.cuda.synchronize()
+    assert (o == 0).all() and (lse == -float("inf")).all()
+    assert (h.K.view(torch.uint8) == 3).all() and (h.scales == 1.0).all()
+
+
 def test_attention_long(lib):
     log("cache attention: one token over 20001, five over 9000, a chunk over 5000; room for more than there is")
     run_attn("e4m3", 128, 4, 1, [1], [20001], seed=27)
