@@ -116,7 +116,7 @@ dqt_status attn_args(const dqt_kv_cache* c, const dqt_kv_batch* b, dqt::KvAttnAr
   group_division(a->c.group, &a->gmul, &a->gone, &a->gshift);
   a->scale = b->scale;
   a->causal = b->causal;
-  dqt::kv_attn_plan(a);
+  dqt::kv_attn_plan(c->fmt == DQT_FP8E4M3, a);
   return DQT_OK;
 }
 

@@ -383,7 +383,7 @@ struct KvAttnArgs {
   float *part, *part_lse;            // [splits, tq, heads, d], [splits, tq, heads]
 };
 // fills tile_rows .. splits from the sizes
-void kv_attn_plan(KvAttnArgs* a);
+void kv_attn_plan(bool e4m3, KvAttnArgs* a);
 hipError_t launch_kv_attn(bool e4m3, const KvAttnArgs& a, hipStream_t stream);
 
 constexpr int kCopyCaches = 32, kCopyPages = 256;    // of one launch

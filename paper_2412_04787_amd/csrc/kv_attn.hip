@@ -404,7 +404,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attn_kernel(KvAttnArg
 // 16 is row 8 x + 4 h + y of the tile, so that registers 8 k .. 8 k + 7 are keys
 // 16 k + 8 (l / 32) + 0..7: the second product's B operand as they are, beside 16 bytes
 // of a value channel, whose tokens the cache keeps together.
-constexpr int kTileRows = 128;
+constexpr int kTileRows = 128, kMaxSplits = 32;
 
 // The tile of rank p, those of the longest sequences first: a block's time goes by the
 // pages that its sequence has, and the long ones that began last ended the kernel (8
@@ -702,16 +702,15 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void kv_tile_kernel(KvAttnArg
 }
 
 // Joins the parts of the rows that have several: o = sum_p 2^(L_p - L) o_p / sum_p
-// 2^(L_p - L).  WIDE: a block for a row, else a wave.  A wave reads GR parts at a time,
-// 16 bytes per lane.  (A wave for each of 128 rows of 64 parts took 20 us.)
-template <int D, bool WIDE>
+// 2^(L_p - L).  A block for a row; a wave reads GR parts at a time, 16 bytes per lane.  (A
+// wave for each of 128 rows of 64 parts took 20 us.)
+template <int D>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
-  constexpr int GR = 256 / D, STEP = WIDE ? 4 * GR : GR;
+  constexpr int GR = 256 / D, STEP = 4 * GR;
   __shared__ f32x4 part[4][D / 4];
   __shared__ float part_sum[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t at = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
-  if (at >= (int64_t)a.c.tq * a.c.heads) return;
+  const int64_t at = blockIdx.x;
   const int row = (int)(at / a.c.heads), hd = (int)(at - (int64_t)row * a.c.heads);
   const int64_t step = (int64_t)a.c.tq * a.c.heads;
   // (of all splits: the ones that were not written are left out when the length is known)
@@ -735,7 +734,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
   for (int g = 0; g < parts; g += kWave) {
     if (g > 0) mine = g + lane < parts ? a.part_lse[(g + lane) * step + at] : -__builtin_inff();
     const float mw = exp2_fast(mine - base);
-    for (int p0 = WIDE ? GR * wave : 0; p0 < kWave && g + p0 < parts; p0 += 4 * STEP) {
+    for (int p0 = GR * wave; p0 < kWave && g + p0 < parts; p0 += 4 * STEP) {
       f32x4 x[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -757,61 +756,160 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
     for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], x, kWave);
     sum += __shfl_xor(sum, x, kWave);
   }
-  if constexpr (WIDE) {
-    if (lane < D / 4) part[wave][lane] = y;
-    if (lane == 0) part_sum[wave] = sum;
-    __syncthreads();
-    if (wave != 0) return;
-    y = part[0][lane % (D / 4)];
-    sum = part_sum[0];
+  if (lane < D / 4) part[wave][lane] = y;
+  if (lane == 0) part_sum[wave] = sum;
+  __syncthreads();
+  if (wave != 0 || lane >= D / 4) return;
+  y = part[0][lane];
+  sum = part_sum[0];
 #pragma unroll
-    for (int v = 1; v < 4; ++v) {
-      y += part[v][lane % (D / 4)];
-      sum += part_sum[v];
-    }
+  for (int v = 1; v < 4; ++v) {
+    y += part[v][lane];
+    sum += part_sum[v];
   }
-  if (lane >= D / 4) return;
   const float f = all == -__builtin_inff() ? 0.0f : 1.0f / sum;
   *reinterpret_cast<uint2*>(a.O + row * a.o_tok + hd * a.o_head + 2 * d) = uint2{pack_bf16x2(y[0] * f, y[1] * f), pack_bf16x2(y[2] * f, y[3] * f)};
   if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)hd * a.c.tq + row] = all == -__builtin_inff() ? all : (all + log2f(sum)) * kLn2;
 }
 
+// The same for many rows of few parts: a wave joins those of 4 heads of a token, four reads
+// in flight; lane l holds the weight of part l / 4 of head l % 4.  (A wave for each row,
+// two parts of 82000: 247 us with the attention, 227.)
+template <int D>
+__global__ __launch_bounds__(256) void kv_join_heads_kernel(KvAttnArgs a) {
+  constexpr int GR = 256 / D, NP = kWave / 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per = (a.c.heads + 3) / 4;
+  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
+  if (id >= (int64_t)a.c.tq * per) return;
+  const int row = (int)(id / per), hd0 = 4 * (int)(id - (int64_t)row * per), nh = min(4, a.c.heads - hd0);
+  const int64_t step = (int64_t)a.c.tq * a.c.heads, at0 = (int64_t)row * a.c.heads + hd0;
+  const int hk = min(lane & 3, nh - 1), pl = lane >> 2;
+  // (of all splits: the ones that were not written are left out when the length is known)
+  float mine = pl < a.splits ? a.part_lse[pl * step + at0 + hk] : 0.0f;
+  int tok = 0;
+  const KvSeq q = a.c.q_start == nullptr ? kv_seq(a.c, row) : kv_find(a.c, row, 1, 1, 0, tok);
+  if (tok < 0 || tok >= q.lq) return;                // a token outside every sequence
+  const int r = tok * a.c.group + (hd0 + hk) % a.c.group, nblk = tile_at(a, q, r / a.tile_rows).nblk;
+  const int parts = nblk <= a.chunk ? 0 : (nblk + a.chunk - 1) / a.chunk;      // (none: written already)
+  const int most = max(max(__builtin_amdgcn_readlane(parts, 0), __builtin_amdgcn_readlane(parts, 1)),
+                       max(__builtin_amdgcn_readlane(parts, 2), __builtin_amdgcn_readlane(parts, 3)));
+  if (most == 0) return;
+  if (pl >= parts) mine = -__builtin_inff();
+  float all = mine;
+  for (int p = pl + NP; p < parts; p += NP) all = fmaxf(all, a.part_lse[p * step + at0 + hk]);
+#pragma unroll
+  for (int x = 4; x < kWave; x *= 2) all = fmaxf(all, __shfl_xor(all, x, kWave));
+  const float base = all == -__builtin_inff() ? 0.0f : all;
+  const int sub = lane / (D / 4), d = 4 * (lane % (D / 4));
+  f32x4 y[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) y[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float sum = 0.0f;
+  for (int g = 0; g < most; g += NP) {
+    if (g > 0) mine = g + pl < parts ? a.part_lse[(g + pl) * step + at0 + hk] : -__builtin_inff();
+    const float mw = exp2_fast(mine - base);
+    sum += mw;
+    for (int p0 = 0; p0 < NP && g + p0 < most; p0 += GR) {
+      f32x4 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int n = __builtin_amdgcn_readlane(parts, k);
+        x[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (k < nh && g + p0 + sub < n) x[k] = *reinterpret_cast<const f32x4*>(a.part + ((g + p0 + sub) * step + at0 + k) * D + d);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] += __shfl(mw, 4 * (p0 + sub) + k, kWave) * x[k];
+    }
+  }
+#pragma unroll
+  for (int x = 4; x < kWave; x *= 2) sum += __shfl_xor(sum, x, kWave);
+#pragma unroll
+  for (int x = D / 4; x < kWave; x *= 2)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[k][e] += __shfl_xor(y[k][e], x, kWave);
+#pragma unroll
+  for (int k0 = 0; k0 < 4; k0 += GR) {
+    const int k = k0 + sub;
+    const float f = __shfl(all == -__builtin_inff() ? 0.0f : 1.0f / sum, k, kWave);
+    const int n = __shfl(parts, k, kWave);
+    f32x4 v = y[k0];
+#pragma unroll
+    for (int e = 1; e < GR; ++e)
+      if (sub == e) v = y[k0 + e];
+    if (k < nh && n > 0)
+      *reinterpret_cast<uint2*>(a.O + row * a.o_tok + (hd0 + k) * a.o_head + 2 * d) =
+          uint2{pack_bf16x2(v[0] * f, v[1] * f), pack_bf16x2(v[2] * f, v[3] * f)};
+  }
+  if (lane < nh && parts > 0 && a.lse != nullptr)
+    a.lse[(int64_t)(hd0 + lane) * a.c.tq + row] = all == -__builtin_inff() ? all : (all + log2f(sum)) * kLn2;
+}
+
 }  // namespace
 
-void kv_attn_plan(KvAttnArgs* a) {
+// The blocks of a tile size that have rows (when sequences have as many each).
+static int64_t kv_blocks(const KvAttnArgs& a, int tile_rows) {
+  const int64_t rows = (int64_t)a.c.tq * a.c.group, seqs = a.c.n_seq > 0 ? a.c.n_seq : 1;
+  return seqs * ((rows + seqs * tile_rows - 1) / (seqs * tile_rows)) * a.c.kv_heads;
+}
+
+// Tile and splits by estimated time in us, fitted to what 120 calls of up to 16 rows a
+// sequence and 105 of more took, over 400 to 65000 tokens, with 1 to 64 parts (beyond 32
+// none gained) and tiles of 32 and 128 rows.  x is the rounds of a block to each of 256
+// units; a page costs a block of few rows what it waits for and a share of each round;
+// blocks of 128 rows have a unit for themselves, and of unequal lengths fill the last
+// round in part; a join costs 6.3 and 1 for 5000 rows of parts.  What is picked takes 3 %
+// (up to 16 rows) and 4 % longer than the best of each call.  (8 blocks to a unit whatever
+// they hold: 9 % for up to 16 rows; 128 rows from 48 on: two sequences of 243 and 468
+// tokens over 484 and 1826, 24 heads of 64, 31 us, 32 rows 18; 32 rows always: 8 chunks of
+// 130 to 512 over 457 to 7865, 32 heads on 8, 286 us, 128 rows 196.)
+void kv_attn_plan(bool e4m3, KvAttnArgs* a) {
   const int64_t rows = (int64_t)a->c.tq * a->c.group, seqs = a->c.n_seq > 0 ? a->c.n_seq : 1;
   const int64_t pages = a->c.max_len > 0 ? ((int64_t)a->c.max_len + kPage - 1) / kPage : 1;
-  a->tile_rows = rows <= 16 * seqs ? 16 : rows <= 48 * seqs ? 32 : kTileRows;
-  a->tiles = (int)(a->c.q_start == nullptr && a->c.group <= a->tile_rows ? a->c.n_seq : rows / a->tile_rows + a->c.n_seq);
-  int64_t splits = 1;
-  if (a->tile_rows == kTileRows) {
-    // one block to a compute unit: as many rounds of blocks as it takes, of half the
-    // pages each and about 4 more to begin and end
-    const int64_t blocks = seqs * ((rows + seqs * kTileRows - 1) / (seqs * kTileRows)) * a->c.kv_heads;
-    int64_t best = INT64_MAX;
-    for (int64_t s = 1; s <= (blocks < 2048 ? 32 : 1) && s * 4 <= pages + 3; ++s) {
-      const int64_t cost = (blocks * s + 255) / 256 * ((pages + s - 1) / s + 8) + (s > 1 ? 4 + rows * a->c.kv_heads * s / 20000 : 0);
-      if (cost < best) {
-        best = cost;
-        splits = s;
+  const double w = a->c.d / 128.0, joined = (double)rows * a->c.kv_heads * (0.3 + 0.7 * w) / 5000;
+  const double wait = 0.15 + 0.85 * w;
+  double best = 1e300;
+  auto look = [&](int tile_rows) {
+    const int64_t blocks = kv_blocks(*a, tile_rows);
+    // (parts of whole groups of 4 pages, one for each wave; grids stay far below their limit)
+    const int64_t fit = (int64_t(1) << 22) / ((rows + seqs) * a->c.kv_heads), most = fit < 1 ? 1 : fit < kMaxSplits ? fit : kMaxSplits;
+    for (int64_t s = 1; s <= most && 4 * (s - 1) < pages; ++s) {
+      const int64_t chunk = ((pages + s - 1) / s + 3) / 4 * 4, parts = (pages + chunk - 1) / chunk;
+      if (parts < s) continue;
+      const double n = (double)(chunk < pages ? chunk : pages), x = blocks * s / 256.0, full = x > 1 ? x : 1;
+      double us = parts > 1 ? 6.3 + joined * s : 0;
+      if (tile_rows == 16) us += 4.6 + 0.33 * full + n * (0.15 * wait + 0.4 * w * full);
+      else if (tile_rows == 32) us += 4.6 + 0.5 * full + n * (e4m3 ? 1 : 1.16) * (0.24 * wait + 0.25 * (0.2 + 0.8 * w) * full);
+      else us += 1.6 + (x > 1 ? 0.8 * x + 0.2 * (double)((blocks * s + 255) / 256) : 1) * (3.4 + (0.57 + 0.32 * w) * n);
+      if (us < best) {
+        best = us;
+        a->tile_rows = tile_rows;
+        a->chunk = (int)chunk;
+        a->splits = (int)parts;
       }
     }
+  };
+  if (rows <= 16 * seqs) {
+    look(16);
   } else {
-    // about 8 blocks to a unit (a part of them beyond the ends of shorter sequences), no
-    // fewer than 8 pages to a block, 2 to a wave
-    const int64_t blocks = (int64_t)(a->tiles > 0 ? a->tiles : 1) * a->c.kv_heads;
-    splits = (2048 + blocks - 1) / blocks;
-    if (splits > pages / 8) splits = pages / 8;
+    look(32);
+    look(kTileRows);
   }
-  if (splits < 1) splits = 1;
-  a->chunk = (int)(((pages + splits - 1) / splits + 3) / 4 * 4);
-  a->splits = (int)((pages + a->chunk - 1) / a->chunk);
+  a->tiles = (int)(a->c.q_start == nullptr && a->c.group <= a->tile_rows ? a->c.n_seq : rows / a->tile_rows + a->c.n_seq);
 }
 
 hipError_t launch_kv_attn(bool e4m3, const KvAttnArgs& a, hipStream_t s) {
   const dim3 grid((uint32_t)((int64_t)a.tiles * a.c.kv_heads * a.splits));
   LaunchStatus st;
-  auto go = [&](auto k) { st << launch_kernel(k, grid, dim3(a.tile_rows == kTileRows ? 512 : 256), s, a); };
+  // Blocks of few sequences are put on one compute unit while others have none: LDS that nothing
+  // uses keeps them apart, as many to a unit as there are for each (256 tiles of 32 rows
+  // over 4512 tokens, 128-wide heads: 55 -> 38 us).
+  const int64_t each = (kv_blocks(a, a.tile_rows) * a.splits + 255) / 256, apart = 160 * 1024 / (each + 1) + 1024;
+  const int64_t own = a.tile_rows == kTileRows ? 4 * (kPage * (2 * a.c.d + 16) + a.c.d * (2 * kPage + 16)) + 16 * kTileRows
+                                               : 16 * a.tile_rows * (a.c.d + 6);
+  const size_t idle = apart > own ? (size_t)(apart - own) : 0;
+  auto go = [&](auto k) { st << launch_kernel_lds(k, grid, dim3(a.tile_rows == kTileRows ? 512 : 256), idle, s, a); };
   // each code is read by one block, and there are more than the last-level cache (256 MB)
   // holds from one call to the next: past it (32 tokens over 1 to 8192, 270 MB: 60.2 ->
   // 55.6 us; 79 MB that it may still hold: 28.0 -> 31.4)
@@ -835,10 +933,10 @@ hipError_t launch_kv_attn(bool e4m3, const KvAttnArgs& a, hipStream_t s) {
   if (a.splits > 1) {
     const int64_t rows = (int64_t)a.c.tq * a.c.heads;
     const bool wide = a.splits > 4 && rows <= 4096;
-    const dim3 join((uint32_t)(wide ? rows : (rows + 3) / 4));
+    const dim3 join((uint32_t)(wide ? rows : ((int64_t)a.c.tq * ((a.c.heads + 3) / 4) + 3) / 4));
     auto j = [&](auto k) { st << launch_kernel(k, join, dim3(256), s, a); };
-    if (a.c.d == 128) wide ? j(kv_join_kernel<128, true>) : j(kv_join_kernel<128, false>);
-    else wide ? j(kv_join_kernel<64, true>) : j(kv_join_kernel<64, false>);
+    if (a.c.d == 128) wide ? j(kv_join_kernel<128>) : j(kv_join_heads_kernel<128>);
+    else wide ? j(kv_join_kernel<64>) : j(kv_join_heads_kernel<64>);
   }
   return st.e;
 }

@@ -41,8 +41,8 @@ __device__ __forceinline__ KvSeq kv_find(const KvArgs& a, int p, int mul, int si
   int lo = 0, hi = a.n_seq;            // the last sequence whose items begin at or before p
   while (hi - lo > 1) {
     const int step = (hi - lo + kWave - 1) / kWave, s = lo + lane * step;
-    const int cnt = __popcll(__ballot(s < hi && start(min(s, hi - 1)) <= p));
-    lo += (max(cnt, 1) - 1) * step;
+    const unsigned long long before = __ballot(s < hi && start(min(s, hi - 1)) <= p);
+    lo += (before ? 63 - __builtin_clzll(before) : 0) * step;
     hi = min(hi, lo + step);
   }
   lo = __builtin_amdgcn_readfirstlane(lo);

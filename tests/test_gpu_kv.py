@@ -429,6 +429,45 @@ def test_attention_long(lib):
     run_attn("int8", 128, 2, 1, [150], [3000], seed=30, max_len=3001)
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_chunks_of_many_heads(lib, fmt, d):
+    """As many tiles of 128 rows as there are compute units, or a few less: one sequence,
+    three of odd lengths with holes and rows that see nothing, strided."""
+    log(f"cache attention: chunks of 85 heads {fmt} d={d}")
+    run_attn(fmt, d, 85, 85, [384], [384], seed=50)
+    run_attn(fmt, d, 85, 85, [127, 100, 128], [127, 60, 301], seed=51, holes=[(2, 1, -1), (2, 4, 1 << 20)], layout="wide")
+    run_attn(fmt, d, 170, 85, [60, 64, 0, 57], [64, 65, 9, 70], causal=False, seed=52, before=5, behind=3)
+
+
+@pytest.mark.parametrize("fmt,d", [("e4m3", 128), ("int8", 128)])
+def test_attention_long_chunk(lib, fmt, d):
+    """Tiles of 128 rows whose pages are split, and those of fewer rows."""
+    log(f"cache attention: a chunk over 5000 tokens {fmt} d={d}")
+    run_attn(fmt, d, 42, 42, [384], [5000], seed=53)
+    run_attn(fmt, d, 8, 4, [200, 90], [5000, 2100], seed=54, holes=[(0, 7, -1)])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,kvh", [(40, 8), (39, 13), (10, 5), (5, 5), (9, 9)])
+def test_attention_joined_rows(lib, d, heads, kvh):
+    """More than 4096 rows of several parts: numbers of heads that are no multiple of 4,
+    rows of one part and of none beside them, tokens of no sequence."""
+    log(f"cache attention: joined rows d={d} heads={heads}/{kvh}")
+    n, far = 4200 // heads + 2, 3000 if d == 128 else 9000
+    run_attn("e4m3", d, heads, kvh, [n - 9, 7, 3], [far, 2, far - 500], seed=55, before=2, behind=6)
+    run_attn("int8", d, heads, kvh, [n], [far - 700], seed=56, causal=False, holes=[(0, i, -1) for i in range(4, 30)])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_joined_single_tokens(lib, d):
+    """Thousands of rows of several parts, one token a sequence."""
+    log(f"cache attention: joined rows of single tokens d={d}")
+    lk = [1, 0, 3000, 1500, 700, 64, 65, 4100 if d == 128 else 9000, 2000]
+    run_attn("e4m3", d, 512, 4, [1] * 9, lk, seed=57, none=True)
+    run_attn("int8", d, 250, 2, [1] * 17, lk + [1000] * 8, seed=58)
+
+
 def test_attention_holes(lib):
     """Pages outside the cache hold no tokens: at the start, the end, all of them."""
     log("cache attention: holes")
@@ -639,15 +678,16 @@ def test_decoding(lib, fmt):
     step({2: 70, 0: 1})
 
 
-def test_decoding_captured(lib):
+@pytest.mark.parametrize("width,split", [(20, False), (150, True)])
+def test_decoding_captured(lib, width, split):
     """Append and attention captured once, replayed while the lengths move on the device;
     eager calls of the same kind between the replays."""
-    log("decoding captured")
+    log(f"decoding captured {width}")
     heads, kvh, d, n = 4, 2, 64, 3
     gen = torch.Generator().manual_seed(12)
-    table = dev32(np.random.default_rng(1).permutation(60).reshape(n, 20))
-    kv_len = dev32([60, 1, 1198])
-    caches = [dqt.kv_cache(60, kvh, d, dqt.DQT_I8) for _ in range(2)]
+    table = dev32(np.random.default_rng(1).permutation(n * width).reshape(n, width))
+    kv_len = dev32([60, 1, 64 * width - 82])
+    caches = [dqt.kv_cache(n * width, kvh, d, dqt.DQT_I8) for _ in range(2)]
     for x in ("K", "V", "scales"):
         getattr(caches[0], x).copy_((torch.rand(getattr(caches[0], x).shape, generator=gen) * 40).to(getattr(caches[0], x).dtype))
         if x == "scales":
@@ -658,7 +698,7 @@ def test_decoding_captured(lib):
     out = [[torch.empty_like(Q), torch.empty_like(Q), torch.empty((heads, n), device=DEV)] for _ in range(2)]
     b = dqt.kv_batch(table, kv_len, n, heads)
     ws = [dqt.workspace(dqt.dqt_kv_attn_workspace(caches[0], b)) for _ in range(2)]
-    assert ws[0] is not None                          # (the keys are split over blocks)
+    assert (ws[0] is not None) == split               # (the keys are split over blocks)
 
     def run(i):
         dqt.dqt_kv_append(caches[i], b, K, V, rope, Q, out[i][0])
