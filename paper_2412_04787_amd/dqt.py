@@ -653,7 +653,7 @@ class KvCache:
         self.K, self.V, self.scales = K, V, scales
         self.kv_heads, self.d = kvh, d
         self.desc = DqtKvCache(K.data_ptr(), V.data_ptr(), scales.data_ptr(), pages, kvh, d, dtype_code(K), 0)
-        self.ref = ctypes.byref(self.desc)
+        self.ref, self.raw = ctypes.byref(self.desc), bytes(self.desc)
 
 
 def kv_cache(pages: int, kv_heads: int, d: int, fmt: int = DQT_FP8E4M3, device="cuda:0") -> KvCache:
@@ -745,9 +745,10 @@ def dqt_kv_attn(cache: KvCache, batch: KvBatch, Q, O, lse=None, ws=None, stream=
 
 def _pages(x) -> np.ndarray:
     x = np.asarray(x)
-    if x.size and (x.dtype.kind not in "iu" or x.min() < -2 ** 31 or x.max() >= 2 ** 31):
+    y = x.astype(np.int32, copy=False) if x.size == 0 or x.dtype.kind in "iu" else None
+    if y is None or (y is not x and not (y == x).all()):
         raise ValueError(f"expected page numbers, got {x.dtype}")
-    return np.ascontiguousarray(x, dtype=np.int32)
+    return y
 
 
 def dqt_kv_copy(caches, src, dst, stream=None):
@@ -756,9 +757,15 @@ def dqt_kv_copy(caches, src, dst, stream=None):
     if src.shape != dst.shape or src.ndim != 1:
         raise ValueError("expected as many sources as destinations")
     if caches:
-        _here(*(c.K for c in caches))
-    arr = (DqtKvCache * len(caches))(*[c.desc for c in caches])
-    _check("dqt_kv_copy", load().dqt_kv_copy(len(caches), arr, src.size, src.ctypes.data, dst.ctypes.data, _stream(stream)))
+        dev, handle = _current(caches[0].K)
+        for c in caches:
+            if c.dev != dev:
+                raise ValueError(f"cache on device {c.dev}, others on device {dev}")
+    # (lists as bytes: a third of a small call's host time was in ctypes' arrays of them)
+    st = load().dqt_kv_copy(len(caches), b"".join([c.raw for c in caches]), src.size, src.tobytes(), dst.tobytes(),
+                            stream.cuda_stream if stream is not None else handle if caches else None)
+    if st != DQT_OK:
+        raise DqtError("dqt_kv_copy", st)
 
 
 class KvPool:
