@@ -14,9 +14,9 @@
 // 16 values of each of two tokens' keys, or 8 channels of 4 tokens' values, between the
 // page's maximum and its codes.  Rotations come from a table of cosines and sines in
 // LDS.  Values go through LDS to lie as the cache has them (a channel's tokens
-// together).  Bound by HBM for prompts (those five 45 us, 4.1 TB/s; the turns are 2 of
-// it), by the chain of dependent loads (length, page, scale) for single tokens (32
-// sequences 5.1 us).
+// together).  Bound by HBM for prompts (those five 44 us, 4.2 TB/s; the turns are 2 of
+// it; the maximum as an integer and clamps in one operation took 1.6 off), by the chain
+// of dependent loads (length, page, scale) for single tokens (32 sequences 4.7 us).
 #include "kv_common.h"
 #include "rope.h"
 

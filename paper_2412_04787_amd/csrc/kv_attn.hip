@@ -114,9 +114,9 @@ __device__ __forceinline__ Tile tile_at(const KvAttnArgs& a, const KvSeq& q, int
 // the matrix cores, 16 consecutive bytes per lane and load, without LDS: a wave holds
 // a whole page (64 tokens) of keys and one of values, and the next page's keys are
 // loaded while this one's are worked on.  Bound by HBM for single tokens: 32 over 1 to
-// 8192 tokens, 32 heads on 8, 50 us for 0.27 GB (5.4 TB/s) and the join of the parts 4.8;
-// two sequences of 30000 and 65000, 3 to 5 tokens each, 16 heads, int8: 76 us for 0.39 GB
-// (5.1 TB/s), 5.4.  Three waves per SIMD (two for 32 rows).
+// 8192 tokens, 32 heads on 8, 50 us for 0.27 GB (5.4 TB/s) and the join of the parts 4.7;
+// two sequences of 30000 and 65000, 3 to 5 tokens each, 16 heads, int8: 74.5 us for 0.39
+// GB (5.3 TB/s), 4.6.  Three waves per SIMD (two for 32 rows).
 //
 // v_mfma_f32_16x16x32_f16: A lane l holds row l % 16, 8 values of the reduction from
 // 8 (l / 16); B the same of columns; result register i is row 4 (l / 16) + i of column
@@ -396,7 +396,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attn_kernel(KvAttnArg
 // about 45, the reads of LDS 30, the exponentials 12.  The scheduling groups keep reads
 // ahead of the products and vector work beside them (without: 209 us); three waves per
 // SIMD do not fit their registers, groups half a round apart, raw codes two pages
-// ahead and sums watched instead of maxima gave nothing.
+// ahead and sums watched instead of maxima gave nothing; 256 rows, eight waves on one
+// page, gain 6 % in rate but end later, their blocks being twice as long (236 us).
 //
 // v_mfma_f32_32x32x16_f16: A lane l holds row l % 32, 8 values of the reduction from
 // 8 (l / 32); B the same of columns; result register i is row 8 (i / 4) + 4 (l / 32) +

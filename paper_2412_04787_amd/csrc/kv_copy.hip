@@ -1,8 +1,8 @@
 // Copies of pages within caches: page src[i] to page dst[i], in each layer's cache.
 // The lists come with the launch (the host checks them: no page is read and
 // written).  Bound by HBM.  A block copies 4 KB, 16 bytes per thread, and its stores go
-// past the caches: 16 pages in 24 layers of 16 heads of 128 (100 MB each way) 33 us, 6.1
-// TB/s, 700 pages in 4 layers of 8 heads 137 us, 5.4 TB/s; 16 KB to a block 43 and 161
+// past the caches: 16 pages in 24 layers of 16 heads of 128 (100 MB each way) 31 us, 6.4
+// TB/s, 700 pages in 4 layers of 8 heads 136 us, 5.4 TB/s; 16 KB to a block 43 and 161
 // us, with such stores 36.7 and 152.
 #include "dqt_launch.h"
 
