@@ -11,7 +11,9 @@ constexpr int kMinExp = -64, kMaxExp = 112;          // of the scales
 __device__ __forceinline__ int clamp_to(int x, int n) { return x < 0 ? 0 : x > n ? n : x; }
 
 // A sequence's new tokens (queries) and length.  Nothing that stands in the arrays
-// leads out of bounds: starts are clamped to the tensors, lengths to max_len.
+// leads out of bounds: starts are clamped to the tensors, lengths to max_len.  An end
+// beyond the following end is cut there, so that a single wrong start makes no two
+// sequences write the same rows, in an order that no one knows.
 struct KvSeq {
   int s, q0, lq, lk;
 };
@@ -19,7 +21,7 @@ __device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, int s) {
   KvSeq q;
   q.s = s;
   q.q0 = a.q_start == nullptr ? s : clamp_to(a.q_start[s], a.tq);
-  const int end = a.q_start == nullptr ? s + 1 : clamp_to(a.q_start[s + 1], a.tq);
+  const int end = a.q_start == nullptr ? s + 1 : clamp_to(min(a.q_start[s + 1], a.q_start[min(s + 2, a.n_seq)]), a.tq);
   q.lq = end > q.q0 ? end - q.q0 : 0;
   q.lk = clamp_to(a.kv_len[s], a.max_len);
   return q;
