@@ -499,7 +499,7 @@ dqt_status dqt_kv_append(const dqt_kv_cache* c, const dqt_kv_batch* b, const dqt
  * The values' scales of one sequence and head lie within 2^100 of each other.
  * A NaN code in the cache (dqt_kv_append writes none) may reach any query of its
  * sequence and head; what lies behind a sequence's last token reaches none.
- *   ws: dqt_kv_attn_workspace() bytes, which depend on sizes alone.
+ *   ws: dqt_kv_attn_workspace() bytes, which depend on sizes and the format alone.
  */
 size_t dqt_kv_attn_workspace(const dqt_kv_cache* c, const dqt_kv_batch* b);
 dqt_status dqt_kv_attn(const dqt_kv_cache* c, const dqt_kv_batch* b, const dqt_rows* Q,
