@@ -414,8 +414,7 @@ constexpr int kTileRows = 128, kMaxSplits = 32;
 __device__ __forceinline__ KvSeq find_longest(const KvAttnArgs& a, int p, int& item) {
   if (a.c.n_seq > kWave) return kv_find(a.c, p, a.c.group, kTileRows, 1, item);
   const int lane = threadIdx.x & (kWave - 1);
-  KvSeq q{0, 0, 0, -1};
-  if (lane < a.c.n_seq) q = kv_seq(a.c, lane);
+  const KvSeq q = kv_seq_of_lane(a.c);
   const int n = (int)(((int64_t)q.lq * a.c.group + kTileRows - 1) / kTileRows);
   int before = 0;
   for (int s = 0; s < a.c.n_seq; ++s) {
@@ -716,8 +715,9 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
   const int64_t step = (int64_t)a.c.tq * a.c.heads;
   // (of all splits: the ones that were not written are left out when the length is known)
   float mine = lane < a.splits ? a.part_lse[lane * step + at] : 0.0f;
-  int tok = 0;
-  const KvSeq q = a.c.q_start == nullptr ? kv_seq(a.c, row) : kv_find(a.c, row, 1, 1, 0, tok);
+  int item;
+  const KvSeq q = a.c.q_start == nullptr ? kv_seq(a.c, row) : kv_find(a.c, row, 1, 1, 0, item);
+  const int tok = row - q.q0;
   if (tok < 0 || tok >= q.lq) return;                // a token outside every sequence
   const int r = tok * a.c.group + hd % a.c.group;
   const Tile t = tile_at(a, q, r / a.tile_rows);
@@ -787,8 +787,9 @@ __global__ __launch_bounds__(256) void kv_join_heads_kernel(KvAttnArgs a) {
   const int hk = min(lane & 3, nh - 1), pl = lane >> 2;
   // (of all splits: the ones that were not written are left out when the length is known)
   float mine = pl < a.splits ? a.part_lse[pl * step + at0 + hk] : 0.0f;
-  int tok = 0;
-  const KvSeq q = a.c.q_start == nullptr ? kv_seq(a.c, row) : kv_find(a.c, row, 1, 1, 0, tok);
+  int item;
+  const KvSeq q = a.c.q_start == nullptr ? kv_seq(a.c, row) : kv_find(a.c, row, 1, 1, 0, item);
+  const int tok = row - q.q0;
   if (tok < 0 || tok >= q.lq) return;                // a token outside every sequence
   const int r = tok * a.c.group + (hd0 + hk) % a.c.group, nblk = tile_at(a, q, r / a.tile_rows).nblk;
   const int parts = nblk <= a.chunk ? 0 : (nblk + a.chunk - 1) / a.chunk;      // (none: written already)

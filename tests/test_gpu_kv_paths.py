@@ -1,0 +1,142 @@
+"""The 8-bit cache of keys and values, further calls: values that break a batch's
+rules, and inputs that are not numbers.  Helpers as in test_gpu_kv.py."""
+import numpy as np
+import pytest
+import torch
+
+import kv_reference as R
+from gpu_util import DEV, log
+from paper_2412_04787_amd import dqt
+from test_gpu_kv import SENT, dev32, device_cache, random_cache, same_cache
+
+pytestmark = pytest.mark.gpu
+
+
+def spans(qs, tq):
+    """Rows of each sequence by their starts: from its own (clamped) to the least of those after it."""
+    c = [min(max(int(x), 0), tq) for x in qs]
+    return [(c[s], max(c[s], min(c[s + 1:]))) for s in range(len(c) - 1)]
+
+
+def searched(qs, tq):
+    """The same for more than 64 sequences: each row's sequence by a search that takes, of 64
+    starts (or fewer) at even distances, the last one at or before the row, and goes on behind it."""
+    n, out = len(qs) - 1, {}
+    for r in range(min(tq, int(qs[-1]))):
+        lo, hi = 0, n
+        while hi - lo > 1:
+            step = (hi - lo + 63) // 64
+            lo = max([i for i in range(lo, hi, step) if qs[i] <= r] + [lo])
+            hi = min(hi, lo + step)
+        if qs[lo] <= r:
+            out.setdefault(lo, []).append(r)
+    assert all(x == list(range(x[0], x[-1] + 1)) for x in out.values())
+    return [(out[s][0], out[s][-1] + 1) if s in out else (0, 0) for s in range(n)]
+
+
+BROKEN = [
+    # (starts, lengths) of 9 rows
+    ([0, 5, 8, 3, 9], [100, 70, 128, 90]),            # one start too low: sequences 0 and 3 meet
+    ([0, 5, 2, 3, 9], [100, 70, 128, 90]),
+    ([0, 9, 9, 0, 9], [100, 70, 128, 90]),
+    ([9, 7, 5, 3, 1], [100, 70, 128, 90]),
+    ([3, 1 << 30, -4, 5, 7], [100, 1 << 30, 128, 90]),
+]
+
+
+@pytest.mark.parametrize("heads", [1, 64])                # tiles of few rows, and of many
+@pytest.mark.parametrize("width", [2, 300])               # whole, and split over blocks
+@pytest.mark.parametrize("qs,lk", BROKEN)
+def test_starts_that_do_not_ascend(lib, heads, width, qs, lk):
+    """A row belongs to the last sequence that starts at or before it, and to no other: attention,
+    rotated queries (in place: turned once) and the cache are those of that division; what no
+    sequence has stays as it is, byte for byte."""
+    log(f"starts that do not ascend: {qs} heads={heads} table of {width}")
+    gen = torch.Generator().manual_seed(19)
+    tq, n, d = 9, 4, 64
+    c = random_cache(gen, 2 * n, 1, d, "int8")
+    table = np.full((n, width), -1, np.int32)
+    table[:, :2] = np.arange(2 * n).reshape(n, 2)
+    lens = [min(x, 64 * width) for x in lk]
+    h = device_cache(c)
+    f = dqt.dqt_rope_freqs(d)
+    Q, K, V = (torch.randn((tq, x, d), generator=gen).to(torch.bfloat16) for x in (heads, 1, 1))
+    b = dqt.kv_batch(dev32(table), dev32(lk), tq, heads, dev32(qs))
+    need = dqt.dqt_kv_attn_workspace(h, b)
+    ws = dqt.workspace(need)
+    if ws is not None:
+        ws.fill_(float("nan"))
+    O, lse = torch.full((tq, heads, d), SENT, dtype=torch.bfloat16, device=DEV), torch.full((heads, tq), SENT, device=DEV)
+    dqt.dqt_kv_attn(h, b, Q.to(DEV), O, lse, ws)
+    Qd = Q.to(DEV)
+    dqt.dqt_kv_append(h, b, K.to(DEV), V.to(DEV), dqt.rope(d), Qd, Qd)
+    torch.cuda.synchronize()
+    got, gl, qr = O.double().cpu(), lse.double().cpu(), Qd.double().cpu()
+    held = [c.values(table[s], min(lens[s], 128), 2 * n) for s in range(n)]
+    own = torch.zeros(tq, dtype=torch.bool)
+    want = R.Cache(2 * n, 1, d, "int8", 0)
+    want.K, want.V, want.scales = c.K.clone(), c.V.clone(), c.scales.clone()
+    for s, (x, y) in enumerate(spans(qs, tq)):
+        if x == y:
+            continue
+        own[x:y] = True
+        # (tokens past 128 lie in pages of -1: nothing is there)
+        k, v, there = held[s]
+        far = lens[s] - k.shape[0]
+        pad = lambda t: torch.cat((t, torch.zeros((far, *t.shape[1:]), dtype=t.dtype)))
+        r = R.attention(Q[x:y], pad(k), pad(v), pad(there), d ** -0.5, True)
+        assert ((got[x:y] - r["O"]).abs() <= r["t_O"]).all(), (s, x, y)
+        assert ((gl[:, x:y] - r["lse"]).abs() <= r["t_lse"]).all(), (s, x, y)
+        pos = np.arange(lens[s] - (y - x), lens[s])
+        t, bound = R.rotate(Q[x:y], pos, f, d, False)
+        assert ((qr[x:y] - t).abs() <= bound + R.BF16 * t.abs() * (1 + R.BF16)).all(), (s, x, y)
+    assert (O.cpu()[~own] == SENT).all() and (gl[:, ~own] == SENT).all()
+    assert torch.equal(Qd.cpu()[~own], Q[~own])
+    # keys and values written without a rotation: the plain implementation's bytes, all others untouched
+    h = device_cache(c)
+    dqt.dqt_kv_append(h, b, K.to(DEV), V.to(DEV))
+    torch.cuda.synchronize()
+    for s, (x, y) in enumerate(spans(qs, tq)):
+        if x < y:
+            want.write(table[s], lens[s] - (y - x), K[x:y].float(), V[x:y].float())
+    same_cache(h, want)
+
+
+@pytest.mark.parametrize("n,at", [(65, 64), (150, 91), (150, 90), (4200, 132)])
+def test_one_start_too_low_among_many(lib, n, at):
+    """Starts that descend once: each row that is written is that of the sequence that a search
+    for it ends at; and two runs give the same bits."""
+    log(f"starts that do not ascend: {n} sequences, {at} too low")
+    rng, gen = np.random.default_rng(20), torch.Generator().manual_seed(20)
+    d, heads = 64, 2
+    qs = np.concatenate([[0], np.cumsum(rng.integers(0, 4, n))])
+    tq = int(qs[-1])
+    qs[at] = qs[30] + 1
+    lk = rng.integers(40, 129, n)
+    c = random_cache(gen, 2 * n, 1, d, "e4m3")
+    table = np.arange(2 * n, dtype=np.int32).reshape(n, 2)
+    h = device_cache(c)
+    Q = torch.randn((tq, heads, d), generator=gen).to(torch.bfloat16)
+    b = dqt.kv_batch(dev32(table), dev32(lk), tq, heads, dev32(qs))
+    out = []
+    for _ in range(2):
+        O = torch.full((tq, heads, d), SENT, dtype=torch.bfloat16, device=DEV)
+        dqt.dqt_kv_attn(h, b, Q.to(DEV), O, None, dqt.workspace(dqt.dqt_kv_attn_workspace(h, b)))
+        torch.cuda.synchronize()
+        out.append(O.cpu())
+    assert torch.equal(out[0], out[1])
+    written = (out[0] != SENT).any(-1).any(-1)
+    own = torch.zeros(tq, dtype=torch.bool)
+    for s, (x, y) in enumerate(searched(qs, tq)):
+        if x == y:
+            continue
+        own[x:y] = True
+        if n > 1000 and abs(s - at) > 200 and s % 16:
+            continue
+        k, v, there = c.values(table[s], int(lk[s]), 2 * n)
+        r = R.attention(Q[x:y], k, v, there, d ** -0.5, True)
+        ok = ((out[0][x:y].double() - r["O"]).abs() <= r["t_O"]).flatten(1).all(1)
+        assert (ok | ~written[x:y]).all(), (s, x, y)
+        if s > at or s < 30:                        # (away from the wrong one all are right)
+            assert ok.all(), (s, x, y)
+    assert not written[~own].any()
