@@ -5,7 +5,9 @@
 // scales a_j, b_j = 2^ev (powers of two) and c = scale log2 e:
 //   u_j = c a_j q.k_j + ev,  M = max u_j so far,  w_j = 2^(u_j - M + 8),
 //   o = sum w_j v_j / l,  l = sum w_j 2^-ev,  lse = ln 2 (M - 8 + log2 l)
-// so that the values' scale rides in the exponent and o is summed from codes.
+// so that the values' scale rides in the exponent and o is summed from codes.  l is 0
+// for a row that sees nothing and no other: where scores are NaN, which no maximum keeps,
+// M may be -inf too, and l is NaN.
 //
 // Both products run on the matrix cores in 16-bit floating point (fp16), which holds
 // every code exactly; the row of Q is brought to 2^14 .. 2^15 by a power of two (bf16
@@ -369,8 +371,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attn_kernel(KvAttnArg
     f32x4 y = *reinterpret_cast<const f32x4*>(&part_o[0][r][d]);
 #pragma unroll
     for (int v = 1; v < 4; ++v) y += *reinterpret_cast<const f32x4*>(&part_o[v][r][d]);
-    y *= all == -__builtin_inff() ? 0.0f : 1.0f / sum;
-    const float lse = all == -__builtin_inff() ? all : all - kLift + log2f(sum);
+    y *= sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float lse = sum == 0.0f ? -__builtin_inff() : all - kLift + log2f(sum);
     const int tk = row_token(a, t.r0 + r), hd = kvh * a.c.group + (t.r0 + r - tk * a.c.group);
     const int64_t row = t.q.q0 + tk;
     if (whole) {
@@ -662,8 +664,8 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void kv_tile_kernel(KvAttnArg
   const float m1 = row_m[1 - grp][rr], both = fmaxf(m, m1);
   const float f0 = m == both ? 1.0f : exp2_fast(m - both), f1 = m1 == both ? 1.0f : exp2_fast(m1 - both);
   const float total = l * f0 + row_l[1 - grp][rr] * f1;
-  const bool none = both == -__builtin_inff();
-  const float inv = none ? 0.0f : 1.0f / total, lse = none ? both : both - kLift + log2f(total);
+  const bool none = total == 0.0f;
+  const float inv = none ? 0.0f : 1.0f / total, lse = none ? -__builtin_inff() : both - kLift + log2f(total);
   lds_f32* give = (lds_f32*)&smem[0];
 #pragma unroll
   for (int d = 0; d < ND / 2; ++d)
@@ -768,9 +770,9 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
     y += part[v][lane];
     sum += part_sum[v];
   }
-  const float f = all == -__builtin_inff() ? 0.0f : 1.0f / sum;
+  const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
   *reinterpret_cast<uint2*>(a.O + row * a.o_tok + hd * a.o_head + 2 * d) = uint2{pack_bf16x2(y[0] * f, y[1] * f), pack_bf16x2(y[2] * f, y[3] * f)};
-  if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)hd * a.c.tq + row] = all == -__builtin_inff() ? all : (all + log2f(sum)) * kLn2;
+  if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)hd * a.c.tq + row] = sum == 0.0f ? -__builtin_inff() : (all + log2f(sum)) * kLn2;
 }
 
 // The same for many rows of few parts: a wave joins those of 4 heads of a token, four reads
@@ -834,7 +836,7 @@ __global__ __launch_bounds__(256) void kv_join_heads_kernel(KvAttnArgs a) {
 #pragma unroll
   for (int k0 = 0; k0 < 4; k0 += GR) {
     const int k = k0 + sub;
-    const float f = __shfl(all == -__builtin_inff() ? 0.0f : 1.0f / sum, k, kWave);
+    const float f = __shfl(sum == 0.0f ? 0.0f : 1.0f / sum, k, kWave);
     const int n = __shfl(parts, k, kWave);
     f32x4 v = y[k0];
 #pragma unroll
@@ -845,7 +847,7 @@ __global__ __launch_bounds__(256) void kv_join_heads_kernel(KvAttnArgs a) {
           uint2{pack_bf16x2(v[0] * f, v[1] * f), pack_bf16x2(v[2] * f, v[3] * f)};
   }
   if (lane < nh && parts > 0 && a.lse != nullptr)
-    a.lse[(int64_t)(hd0 + lane) * a.c.tq + row] = all == -__builtin_inff() ? all : (all + log2f(sum)) * kLn2;
+    a.lse[(int64_t)(hd0 + lane) * a.c.tq + row] = sum == 0.0f ? -__builtin_inff() : (all + log2f(sum)) * kLn2;
 }
 
 }  // namespace

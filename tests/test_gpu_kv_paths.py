@@ -140,3 +140,49 @@ def test_one_start_too_low_among_many(lib, n, at):
         if s > at or s < 30:                        # (away from the wrong one all are right)
             assert ok.all(), (s, x, y)
     assert not written[~own].any()
+
+
+@pytest.mark.parametrize("n,heads,kvh,d,lk", [
+    (4, 2, 1, 64, 500),                                    # one tile of few rows, whole
+    (1, 4, 2, 128, 20001),                                 # few rows, parts
+    (70, 2, 1, 64, 500), (40, 9, 9, 128, 400),             # more rows
+    (150, 42, 42, 64, 300),                                # tiles of 128 rows
+    (150, 42, 42, 128, 3000),                              # and their parts, thousands of rows joined
+    (2, 512, 4, 64, 9000),
+])
+def test_sums_of_nan_queries(lib, n, heads, kvh, d, lk):
+    """A query of NaN has an O and an lse of NaN, in each way that parts are joined; one
+    that sees nothing has 0 and -inf beside it; all others are right."""
+    log(f"lse of a NaN query: {n} tokens of {heads}/{kvh} heads of {d} over {lk}")
+    gen = torch.Generator().manual_seed(21)
+    pages = -(-lk // 64) + 1
+    c = random_cache(gen, pages, kvh, d, "e4m3")
+    h = device_cache(c)
+    # (a second sequence of 3 new tokens, of which the cache has 2)
+    Q = torch.randn((n + 3, heads, d), generator=gen).to(torch.bfloat16)
+    rows = [(0, 0), (n - 1, heads - 1), (n // 2, heads // 2), (n + 2, 1)]
+    for t, x in rows:
+        Q[t, x, 9] = float("nan")
+    table = np.full((2, pages - 1), -1, np.int32)
+    table[0], table[1, 0] = np.arange(pages - 1), pages - 1
+    O = torch.full((n + 3, heads, d), SENT, dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((heads, n + 3), SENT, device=DEV)
+    b = dqt.kv_batch(dev32(table), dev32([lk, 2]), n + 3, heads, dev32([0, n, n + 3]))
+    dqt.dqt_kv_attn(h, b, Q.to(DEV), O, lse, dqt.workspace(dqt.dqt_kv_attn_workspace(h, b)))
+    torch.cuda.synchronize()
+    got, gl = O.double().cpu(), lse.double().cpu()
+    bad = torch.zeros((n + 3, heads), dtype=torch.bool)
+    for t, x in rows:
+        bad[t, x] = True
+    assert torch.equal(torch.isnan(gl.t()), bad)
+    assert torch.equal(torch.isnan(got).all(-1), bad) and torch.equal(torch.isnan(got).any(-1), bad)
+    assert (got[n] == 0).all() and (gl[:, n] == -float("inf")).all()
+    for s, (x, y, m) in enumerate(((0, n, lk), (n, n + 3, 2))):
+        k, v, there = c.values(table[s], m, pages)
+        step = 1 if heads < 100 else 37
+        for j in range(0, heads, step):
+            r = R.attention(torch.nan_to_num(Q[x:y, j:j + 1].float()).double(), k[:, j // (heads // kvh)][:, None],
+                            v[:, j // (heads // kvh)][:, None], there, d ** -0.5, True)
+            ok = ~bad[x:y, j] & (gl[j, x:y] != -float("inf"))
+            assert ((got[x:y, j] - r["O"][:, 0]).abs() <= r["t_O"][:, 0])[ok].all(), (s, j)
+            assert ((gl[j, x:y] - r["lse"][0]).abs() <= r["t_lse"][0])[ok].all(), (s, j)
