@@ -27,6 +27,7 @@ import argparse
 import hashlib
 import json
 import os
+import re
 import sys
 import time
 
@@ -280,23 +281,40 @@ def cpu_baseline(wl, tokens: int, sr_weights: int):
     }
 
 
-def kernel_source_hash() -> str:
-    """Hash of what the kernels are built from: the HIP sources and the build
-    script (its compiler flags)."""
+# What the calls of a linear block's step are built from (the C ABI's file picks their launches).
+LINEAR_SOURCES = ("abi.hip", "act_quant.hip", "adamw_sr.hip", "fwd_small.hip", "gemm_f32.hip", "gemm_f32_small.hip",
+                  "gemm_v3.hip", "sr_update.hip", "update_variants.hip")
+
+
+def kernel_source_hash(sources=LINEAR_SOURCES) -> str:
+    """Hash of what the kernels in these files of csrc are built from: the
+    files, the headers of csrc that they include, directly or through others,
+    and the build script (its compiler flags).  By default those of the linears,
+    so that a profile of theirs stays valid where another operator's file
+    changes or is added; sources = None: every HIP source."""
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2412_04787_amd", "csrc")
-    for f in sorted(os.listdir(csrc)):
-        if f.endswith((".hip", ".h")):
-            h.update(open(os.path.join(csrc, f), "rb").read())
-    h.update(open(os.path.join(ROOT, "paper_2412_04787_amd", "build_lib.py"), "rb").read())
+    if sources is None:
+        sources = [f for f in os.listdir(csrc) if f.endswith((".hip", ".h"))]
+    todo, files = list(sources), {}
+    while todo:
+        f = todo.pop()
+        if f not in files:
+            with open(os.path.join(csrc, f), "rb") as src:
+                files[f] = src.read()
+            todo += re.findall(r'^#include "([^"/]+)"', files[f].decode(), re.M)
+    for f in sorted(files):
+        h.update(files[f])
+    with open(os.path.join(ROOT, "paper_2412_04787_amd", "build_lib.py"), "rb") as src:
+        h.update(src.read())
     return h.hexdigest()[:16]
 
 
 def read_traffic(kernel_class: str, workload: str, kernel_only: bool = False):
     """Bytes per launch that the L2 caches fetched from and wrote to memory
     (FETCH_SIZE + WRITE_SIZE, scaled by a plain copy of known size), from the
-    committed rocprofv3 counter summary, if it was taken on the current
-    kernel sources; else None.  kernel_only: the GEMM kernel's own bytes,
+    committed rocprofv3 counter summary, if it was taken on the linears'
+    current sources; else None.  kernel_only: the GEMM kernel's own bytes,
     without the passes of its call.  The counters see the last-level cache
     (MALL) and HBM alike, so on a block whose data fits the 256 MB MALL this
     is an upper bound of the HBM bytes."""
@@ -417,7 +435,7 @@ def run_model(args):
         "weights_changed_per_step": changed / args.steps,
         "update_fraction_per_step": round(changed / args.steps / cfg.dqt_weights, 6),
         "wall_s_timed_region": round(wall, 3),
-        "kernel_source_hash": kernel_source_hash(),
+        "kernel_source_hash": kernel_source_hash(None),
     }
     if not args.no_cpu_baseline:
         out["cpu_baseline"] = model_cpu_baseline(cfg, args.cpu_tokens, args.cpu_sr_weights // 4)

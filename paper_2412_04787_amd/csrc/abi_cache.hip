@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include "abi_check.h"
+#include "cache_launch.h"
 
 namespace {
 

@@ -2,7 +2,7 @@
 // the pages' scales.
 #pragma once
 
-#include "dqt_launch.h"
+#include "cache_launch.h"
 
 namespace dqt {
 

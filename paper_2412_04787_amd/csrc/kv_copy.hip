@@ -4,7 +4,7 @@
 // past the caches: 16 pages in 24 layers of 16 heads of 128 (100 MB each way) 31 us, 6.4
 // TB/s, 700 pages in 4 layers of 8 heads 136 us, 5.4 TB/s; 16 KB to a block 43 and 161
 // us, with such stores 36.7 and 152.
-#include "dqt_launch.h"
+#include "cache_launch.h"
 
 namespace dqt {
 

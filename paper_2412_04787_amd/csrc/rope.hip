@@ -9,7 +9,7 @@
 // tokens, 16 + 16 heads of 128, bf16, 52 us (5.2 TB/s; 73 us with a thread for 8 pairs of
 // a token through all heads, whose waves asked the same channels at once).  Few tokens:
 // a launch, 4.4 us for 32 tokens of 40 heads.
-#include "dqt_launch.h"
+#include "cache_launch.h"
 #include "rope.h"
 
 namespace dqt {
