@@ -89,7 +89,8 @@ constexpr int kTurnTokens = kPage / 2;               // of the table in LDS
 
 // Cosines and sines of n tokens from position pos on.  A thread takes one pair through
 // a run of tokens: the first one's turn, then products with that of one position (each
-// adds 2^-52 to what is rounded to fp32).
+// adds what the two factors are off by and its own roundings, 2^-51, to what is rounded to
+// fp32; seven at most).
 template <int ROW>
 __device__ __forceinline__ void turn_table(const KvAppendArgs& a, float2* cs, int pos, int n) {
   const int half = a.rot / 2, runs = 256 / half, p = threadIdx.x % half, len = (n + runs - 1) / runs, t0 = threadIdx.x / half * len;
