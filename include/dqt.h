@@ -416,7 +416,7 @@ dqt_status dqt_rope_bwd(const dqt_rope* r, int32_t n, const dqt_rope_io* io, int
  *   fmt = DQT_FP8E4M3 or DQT_I8 (-127 .. 127).
  * A scale is the smallest power of two s in 2^-64 .. 2^112 with |x| <= top s for
  * all finite x that were written to that page and head since its first token was
- * (top = 448 for e4m3, 127 for int8).  A power of two, so that codes that stand in
+ * (top = 448 for e4m3, 127 for int8; 2^112 where none is as large).  A power of two, so that codes that stand in
  * the page when the scale grows move to the new one with hardly a loss: e4m3 codes
  * exactly, unless they fall below its normal range, int8 codes are rounded again,
  * once for each doubling.
@@ -479,7 +479,8 @@ typedef struct {
  * A page whose row 0 is written starts a new scale; otherwise its scale stays or
  * grows over the codes that stand in it.  Rows behind a sequence's last token are
  * left as they are.  An infinite value is held as the largest code of its sign, a
- * NaN as 0; neither counts for the scale, nor do values beyond top 2^112.
+ * NaN as 0; neither counts for the scale.  A finite value beyond top 2^112 is held
+ * as the largest code too and does count: its page goes to the scale 2^112.
  * A page that receives tokens belongs to one sequence of the batch (dqt_kv_pool_
  * extend sees to that).  The scale, batch and attention fields that it does not
  * need (scale, causal) are checked all the same.

@@ -186,3 +186,38 @@ def test_sums_of_nan_queries(lib, n, heads, kvh, d, lk):
             ok = ~bad[x:y, j] & (gl[j, x:y] != -float("inf"))
             assert ((got[x:y, j] - r["O"][:, 0]).abs() <= r["t_O"][:, 0])[ok].all(), (s, j)
             assert ((gl[j, x:y] - r["lse"][0]).abs() <= r["t_lse"][0])[ok].all(), (s, j)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_values_beyond_the_largest_scale(lib, fmt):
+    """Finite values beyond top 2^112 bring their page to the scale 2^112 and are its largest
+    codes; what stands beside them, before them or after them is held on that scale."""
+    log(f"append: values beyond the largest scale {fmt}")
+    top = R.TOP[fmt]
+    x = torch.zeros((6, 1, 64))
+    x[0, 0, :3] = torch.tensor([1.0, -2.0, 2.0 ** 100])
+    x[1, 0, :4] = torch.tensor([3e38, 1.0, -(2.0 ** 110), top * 2.0 ** 112])
+    x[2, 0, :3] = torch.tensor([-3e38, 2.0 ** 116, float("inf")])
+    x[3, 0, :2] = torch.tensor([5.0, 2.0 ** 111])
+    x[4, 0, :3] = torch.tensor([float("nan"), -(2.0 ** 113), 2.0 ** -60])
+    x[5, 0, 0] = 3.0
+    x = x.to(torch.bfloat16)
+    table = np.array([[0], [1]], np.int32)
+    c = R.Cache(2, 1, 64, fmt, 0)
+    h = device_cache(c)
+    at = 0
+    for n in (1, 1, 1, 2, 1):                               # the same tokens in two sequences, one in one call
+        at += n
+        b = dqt.kv_batch(dev32(table[:1]), dev32([at]), n, 1, dev32([0, n]))
+        dqt.dqt_kv_append(h, b, x[at - n:at].to(DEV), x[at - n:at].to(DEV))
+        c.write(table[0], at - n, x[at - n:at].float(), x[at - n:at].float())
+        torch.cuda.synchronize()
+        same_cache(h, c)
+        assert at == 1 or (h.scales[0] == 2.0 ** 112).all()
+    dqt.dqt_kv_append(h, dqt.kv_batch(dev32(table[1:]), dev32([6]), 6, 1, dev32([0, 6])), x.to(DEV), x.to(DEV))
+    c.write(table[1], 0, x.float(), x.float())
+    torch.cuda.synchronize()
+    same_cache(h, c)
+    assert (h.scales == 2.0 ** 112).all()
+    big = h.K[1, 0].float().cpu() * 2.0 ** 112
+    assert big[1, 0] == top * 2.0 ** 112 and big[2, 0] == -top * 2.0 ** 112 and big[0, 0] == 0 and big[5, 0] == 0
