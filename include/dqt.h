@@ -447,8 +447,8 @@ typedef struct {
  *      sequences (of up to 64, it is the last one's that starts at or before it),
  *      lengths are clamped to 0 .. max_len, pages outside the cache (-1 for
  *      instance) hold no tokens (what is written to them is lost), new tokens that
- *      come before position 0 see nothing, and neither they nor their rotated
- *      queries are written.
+ *      come before position 0 see nothing with causal = 1 (and all without it), and
+ *      neither they nor their rotated queries are written.
  *   max_len: no kv_len is larger; at most 64 table_stride and 2^31 - 1024.  The work
  *      is laid out for it (which a captured graph keeps), so close is better.
  *   heads: query heads, a multiple of the cache's kv_heads, at most 1024; query

@@ -221,3 +221,25 @@ def test_values_beyond_the_largest_scale(lib, fmt):
     assert (h.scales == 2.0 ** 112).all()
     big = h.K[1, 0].float().cpu() * 2.0 ** 112
     assert big[1, 0] == top * 2.0 ** 112 and big[2, 0] == -top * 2.0 ** 112 and big[0, 0] == 0 and big[5, 0] == 0
+
+
+@pytest.mark.parametrize("rows", [5, 200])                  # tiles of few rows, and of many
+def test_tokens_before_the_first_position(lib, rows):
+    """More new tokens than a sequence has: those before position 0 see nothing under the mask and
+    every token without it."""
+    log(f"attention: {rows} new tokens of 3")
+    gen = torch.Generator().manual_seed(22)
+    c = random_cache(gen, 1, 16, 64, "int8")
+    h = device_cache(c)
+    Q = torch.randn((rows, 16, 64), generator=gen).to(torch.bfloat16)
+    k, v, there = c.values([0], 3, 1)
+    for causal in (True, False):
+        b = dqt.kv_batch(dev32([[0]]), dev32([3]), rows, 16, dev32([0, rows]), causal=causal)
+        O, lse = torch.empty((rows, 16, 64), dtype=torch.bfloat16, device=DEV), torch.empty((16, rows), device=DEV)
+        dqt.dqt_kv_attn(h, b, Q.to(DEV), O, lse, dqt.workspace(dqt.dqt_kv_attn_workspace(h, b)))
+        torch.cuda.synchronize()
+        r = R.attention(Q, k, v, there, 0.125, causal)
+        assert ((O.double().cpu() - r["O"]).abs() <= r["t_O"]).all()
+        blind = torch.arange(rows) < (rows - 3 if causal else 0)
+        assert (O.cpu()[blind] == 0).all() and (lse.cpu()[:, blind] == -float("inf")).all()
+        assert ((lse.double().cpu() - r["lse"]).abs() <= r["t_lse"])[:, ~blind].all()
