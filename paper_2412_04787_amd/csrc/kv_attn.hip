@@ -704,11 +704,13 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void kv_tile_kernel(KvAttnArg
 }
 
 // Joins the parts of the rows that have several: o = sum_p 2^(L_p - L) o_p / sum_p
-// 2^(L_p - L).  A block for a row; a wave reads GR parts at a time, 16 bytes per lane.  (A
-// wave for each of 128 rows of 64 parts took 20 us.)
+// 2^(L_p - L).  A block for a row, whose waves read GR parts at a time, 16 bytes per lane,
+// four reads in flight; lane l holds the weight of part l for the others.  (A wave for each of
+// 128 rows of 64 parts, when there could be as many, took 20 us.)
 template <int D>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
   constexpr int GR = 256 / D, STEP = 4 * GR;
+  static_assert(kMaxSplits <= 4 * STEP && 4 * STEP <= kWave, "a lane for each part, four reads for all");
   __shared__ f32x4 part[4][D / 4];
   __shared__ float part_sum[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -726,31 +728,22 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
   if (t.nblk <= a.chunk) return;                     // (written already)
   const int parts = (t.nblk + a.chunk - 1) / a.chunk;
   if (lane >= parts) mine = -__builtin_inff();
-  float all = mine;
-  for (int p = lane + kWave; p < parts; p += kWave) all = fmaxf(all, a.part_lse[p * step + at]);
-  all = wave_max(all);
-  const float base = all == -__builtin_inff() ? 0.0f : all;
+  const float all = wave_max(mine), mw = exp2_fast(mine - (all == -__builtin_inff() ? 0.0f : all));
   const int d = 4 * (lane % (D / 4));
   f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
   float sum = 0.0f;
-  // 64 parts at a time, whose weights the lanes hold for each other, four reads in flight
-  for (int g = 0; g < parts; g += kWave) {
-    if (g > 0) mine = g + lane < parts ? a.part_lse[(g + lane) * step + at] : -__builtin_inff();
-    const float mw = exp2_fast(mine - base);
-    for (int p0 = GR * wave; p0 < kWave && g + p0 < parts; p0 += 4 * STEP) {
-      f32x4 x[4];
+  const int p0 = GR * wave + lane / (D / 4);
+  f32x4 x[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        x[e] = *reinterpret_cast<const f32x4*>(a.part + (min(g + p0 + e * STEP + lane / (D / 4), parts - 1) * step + at) * D + d);
+  for (int e = 0; e < 4; ++e)
+    x[e] = *reinterpret_cast<const f32x4*>(a.part + (min(p0 + e * STEP, parts - 1) * step + at) * D + d);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int p = p0 + e * STEP + lane / (D / 4);
-        const float w = __shfl(mw, p & (kWave - 1), kWave);
-        if (p < kWave && g + p < parts) {
-          y += w * x[e];
-          sum += w;
-        }
-      }
+  for (int e = 0; e < 4; ++e) {
+    const int p = p0 + e * STEP;
+    const float w = __shfl(mw, p, kWave);
+    if (p < parts) {
+      y += w * x[e];
+      sum += w;
     }
   }
 #pragma unroll
