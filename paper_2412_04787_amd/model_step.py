@@ -395,13 +395,15 @@ class DQTModel:
         dense = [self.emb, self.head, self.final_norm] + [p for n in self.norms for p in n]
         self.opt = torch.optim.AdamW(dense, lr=cfg.lr, betas=(0.9, 0.95), weight_decay=0.1)
         hd = H // cfg.heads
-        self.rope = dqt.rope(hd, base=cfg.rope_base, device=device) if cfg.own_rope else None
-        inv = 1.0 / (cfg.rope_base ** (torch.arange(0, hd, 2, device=device, dtype=torch.float32) / hd))
-        # (packed documents may be as long as the batch)
-        rows = cfg.tokens if cfg.own_ops else cfg.seq
-        ang = torch.arange(rows, device=device, dtype=torch.float32)[:, None] * inv[None, :]
-        self.cos = torch.cos(ang).to(torch.bfloat16)[None, None]   # [1, 1, rows, hd/2]
-        self.sin = torch.sin(ang).to(torch.bfloat16)[None, None]
+        if cfg.own_rope:
+            self.rope = dqt.rope(hd, base=cfg.rope_base, device=device)
+        else:
+            inv = 1.0 / (cfg.rope_base ** (torch.arange(0, hd, 2, device=device, dtype=torch.float32) / hd))
+            # (packed documents may be as long as the batch)
+            rows = cfg.tokens if cfg.own_ops else cfg.seq
+            ang = torch.arange(rows, device=device, dtype=torch.float32)[:, None] * inv[None, :]
+            self.cos = torch.cos(ang).to(torch.bfloat16)[None, None]   # [1, 1, rows, hd/2]
+            self.sin = torch.sin(ang).to(torch.bfloat16)[None, None]
         # first token of each of the batch's sequences, and behind the last
         self.starts = torch.arange(0, cfg.tokens + 1, cfg.seq, dtype=torch.int32, device=device)
 

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from gpu_util import DEV, log
-from paper_2412_04787_amd import dqt
+from paper_2412_04787_amd import dqt, model_step as MS
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +50,11 @@ def test_turns_round_to_the_nearest(lib, quarter):
             got = np.stack((got[1], -got[0]))
         bad = got[which] != want
         assert not bad.any(), (int(bad.sum()), "sin" if which else "cos")
+
+
+def test_the_model_keeps_one_form_of_its_angles(lib):
+    """Frequencies with own_rope, tables of cosines and sines (2 tokens d bytes) without."""
+    log("model: angles")
+    for name, own in (("tiny_rope", True), ("tiny_ops", False)):
+        m = MS.DQTModel(MS.MODELS[name])
+        assert hasattr(m, "rope") == own and hasattr(m, "cos") != own and hasattr(m, "sin") != own
