@@ -243,3 +243,43 @@ def test_tokens_before_the_first_position(lib, rows):
         blind = torch.arange(rows) < (rows - 3 if causal else 0)
         assert (O.cpu()[blind] == 0).all() and (lse.cpu()[:, blind] == -float("inf")).all()
         assert ((lse.double().cpu() - r["lse"]).abs() <= r["t_lse"])[:, ~blind].all()
+
+
+@pytest.mark.parametrize("heads", [1, 64])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("qs,lk", [([-7, 3, 5, 9], [50, 90, 1 << 30]), ([0, 1 << 30, 4, 6], [-5, 100, 64]),
+                                   ([9, 9, 2, 2 ** 31 - 1], [3, 100, 128]), ([2, 3, 3, 8], [-(1 << 31), 1 << 30, 2])])
+def test_values_out_of_range_touch_nothing_else(lib, heads, fmt, qs, lk):
+    """Starts and lengths out of range are clamped: all rows of O and lse, and every byte of the cache
+    after appending, are those of the clamped values; what no sequence has is left as it was."""
+    log(f"out of range: {qs} {lk} {fmt} heads={heads}")
+    gen = torch.Generator().manual_seed(23)
+    n, tq, d = 3, 9, 64
+    c = random_cache(gen, 2 * n + 1, 1, d, fmt)
+    table = np.arange(2 * n, dtype=np.int32).reshape(n, 2)
+    h = device_cache(c)
+    Q, K, V = (torch.randn((tq, x, d), generator=gen).to(torch.bfloat16) for x in (heads, 1, 1))
+    b = dqt.kv_batch(dev32(table), dev32(lk), tq, heads, dev32(qs))
+    O, lse = torch.full((tq, heads, d), SENT, dtype=torch.bfloat16, device=DEV), torch.full((heads, tq), SENT, device=DEV)
+    dqt.dqt_kv_attn(h, b, Q.to(DEV), O, lse, dqt.workspace(dqt.dqt_kv_attn_workspace(h, b)))
+    torch.cuda.synchronize()
+    same_cache(h, c)
+    own = torch.zeros(tq, dtype=torch.bool)
+    for s, (x, y) in enumerate(spans(qs, tq)):
+        if x == y:
+            continue
+        own[x:y] = True
+        m = min(max(lk[s], 0), 128)
+        k, v, there = c.values(table[s], m, 2 * n + 1)
+        r = R.attention(Q[x:y], k, v, there, 0.125, True)
+        seen = r["lse"] > -float("inf")
+        assert ((O[x:y].double().cpu() - r["O"]).abs() <= r["t_O"]).all(), s
+        assert ((lse[:, x:y].double().cpu() - r["lse"]).abs() <= r["t_lse"])[seen].all(), s
+        assert (lse[:, x:y].cpu()[~seen] == -float("inf")).all(), s
+        first = max(0, (y - x) - m)                        # (tokens before position 0 are left out)
+        if m > 0:
+            c.write(table[s], m - (y - x) + first, K[x + first:y].float(), V[x + first:y].float())
+    assert (O.cpu()[~own] == SENT).all() and (lse.cpu()[:, ~own] == SENT).all()
+    dqt.dqt_kv_append(h, b, K.to(DEV), V.to(DEV))
+    torch.cuda.synchronize()
+    same_cache(h, c)
