@@ -394,7 +394,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attn_kernel(KvAttnArg
 // once for its 128 rows and passes them through LDS as fp16, two stages.
 //
 // Bound by what a wave issues between its products: of 197 us (8 chunks of 130 to 512
-// tokens over 460 to 7870, 32 heads on 8: 163 GFLOP, 825 TFLOP/s) the staging takes
+// tokens over 460 to 7870, 32 heads on 8: 163 GFLOP, 825 TFLOP/s; 240 us for the first
+// launches after a pause, 195 from some 40 ms of them on) the staging takes
 // about 45, the reads of LDS 30, the exponentials 12.  The scheduling groups keep reads
 // ahead of the products and vector work beside them (without: 209 us); three waves per
 // SIMD do not fit their registers, groups half a round apart, raw codes two pages
@@ -852,8 +853,9 @@ static int64_t kv_blocks(const KvAttnArgs& a, int tile_rows) {
 }
 
 // Tile and splits by estimated time in us, fitted to what 120 calls of up to 16 rows a
-// sequence and 105 of more took, over 400 to 65000 tokens, with 1 to 64 parts (beyond 32
-// none gained) and tiles of 32 and 128 rows.  x is the rounds of a block to each of 256
+// sequence and 105 of more took, over 400 to 65000 tokens, with 1 to 64 parts (what up to
+// 48 and 64 would pick is level over these calls, 0.1 % better, and slower for the longest: two
+// sequences of 30000 and 65000, 82.5 us, 79.6 with 32) and tiles of 32 and 128 rows.  x is the rounds of a block to each of 256
 // units; a page costs a block of few rows what it waits for and a share of each round;
 // blocks of 128 rows have a unit for themselves, and of unequal lengths fill the last
 // round in part; a join costs 6.3 and 1 for 5000 rows of parts.  What is picked takes 3 %
@@ -909,7 +911,9 @@ hipError_t launch_kv_attn(bool e4m3, const KvAttnArgs& a, hipStream_t s) {
   auto go = [&](auto k) { st << launch_kernel_lds(k, grid, dim3(a.tile_rows == kTileRows ? 512 : 256), idle, s, a); };
   // each code is read by one block, and there are more than the last-level cache (256 MB)
   // holds from one call to the next: past it (32 tokens over 1 to 8192, 270 MB: 60.2 ->
-  // 55.6 us; 79 MB that it may still hold: 28.0 -> 31.4)
+  // 55.6 us; 79 MB that it may still hold: 28.0 -> 31.4).  Both sides with one cache, read
+  // call after call: where a model's other layers read theirs in between, a smaller one
+  // is as cold, which the call cannot know.
   const bool once = a.tiles == a.c.n_seq && (int64_t)a.c.n_seq * a.c.max_len * a.c.kv_heads * a.c.d * 2 > (int64_t)256 << 20;
   auto few = [&](auto d, auto fmt, auto nt) {
     constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
